@@ -241,8 +241,9 @@ int ec_moe_backward(const ec_problem *p, const void *X, const void *Wg,
 int ec_tc_capacity(int32_t n_groups, const int32_t *group_lengths, int32_t n_experts,
                    int32_t top_k, double cf, int32_t *cap_out);
 
-/* Workspace bytes of ec_tc_route (mode 0) or ec_tc_forward (mode 1); 0 on an
- * invalid problem.                                                            */
+/* Workspace bytes of ec_tc_route (mode 0), ec_tc_forward (mode 1),
+ * ec_tc_balance (mode 2), ec_tc_train_forward (mode 3) or ec_tc_train_backward
+ * (mode 4); 0 on an invalid problem or mode.                                  */
 size_t ec_tc_workspace_size(const ec_problem *p, int32_t top_k, int mode);
 
 /* Token-choice routing: S [N, E] fp32 out; G [N, E] fp32 out, the gate of every
@@ -263,6 +264,86 @@ int ec_tc_forward(const ec_problem *p, int32_t top_k, const void *X, const void 
                   const void *Ws1, const void *Ws3, const void *Ws2, void *Y,
                   int32_t *expert_rows, void *ws, size_t ws_bytes, hipStream_t stream);
 
+/* Balance loss of token choice and the experts' loads, per group: with C_i the
+ * top_k experts of row i of S (equal scores: the lower expert index; a NaN is
+ * never chosen) and L the group's tokens,
+ *   counts_gj = number of the group's tokens i with j in C_i (what the tokens
+ *               ask for, before a capacity drops pairs),
+ *   loss_g = E / (top_k L) sum_j counts_gj P_gj, P_gj = mean of S_ij over the group
+ * (1 under an even load; 0 for an empty group).  A loss over a whole batch is
+ * that of one group.  The sums over tokens are in 64 bits.
+ *   S [N, E] fp32; loss [G] fp32 out; counts [G, E] int32 out.
+ * p gives N, E and the groups (capacities, widths and dtype are checked but not
+ * used).  S may be NULL only when N = 0.  ws: ec_tc_workspace_size(p, top_k, 2).  */
+int ec_tc_balance(const ec_problem *p, int32_t top_k, const float *S, float *loss,
+                  int32_t *counts, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Its gradient in the router's logits, the counts held fixed: with
+ * b_gj = dloss_g E counts_gj / (top_k L^2),
+ *   dZ_ij = inv_temperature S_ij (b_gj - sum_m S_im b_gm).
+ *   counts [G, E] as ec_tc_balance wrote them; dloss [G] fp32 (device);
+ *   dZ [N, E] fp32 out, may be S.  No workspace.                               */
+int ec_tc_balance_backward(const ec_problem *p, int32_t top_k, const float *S,
+                           const int32_t *counts, const float *dloss, float *dZ,
+                           hipStream_t stream);
+
+/* Dropout onto a residual, the mask drawn from a counter-based generator and
+ * never stored: Y = residual + m X with m_e = 0 with probability p and 1/(1 - p)
+ * otherwise.  Element e takes the (e mod 8)-th 16-bit draw (low halves first) of
+ * Philox4x32-10 with counter (e / 8, rng[1]) and key rng[0], 64 bits each, and is
+ * dropped if the draw is below t = rint(65536 p): p acts as the nearest multiple
+ * of 2^-16, t / 65536, and 1/(1 - p) as 65536 / (65536 - t).  A dropped element
+ * contributes exactly 0, whatever it holds.  With the same rng the call draws the
+ * same mask, so the gradient in X is the same call on dY without a residual (the
+ * residual's is dY itself).  rng is read on the device: a captured graph draws
+ * anew when its values change between replays.                                */
+typedef struct {
+  double p;                /* in [0, 1]                                                */
+  const uint64_t *rng;     /* device [2]: seed, offset (one offset per call and step
+                              gives independent masks); may be NULL when t = 0         */
+  const void *residual;    /* dtype, as many elements as X; NULL: none                 */
+} ec_dropout_desc;
+
+/* X, Y [n] dtype.  Y may be X or the residual; other overlaps are refused.
+ * n < 2^40.                                                                    */
+int ec_dropout(int dtype, int64_t n, const ec_dropout_desc *drop, const void *X, void *Y,
+               hipStream_t stream);
+
+/* Bytes of the saved buffer that ec_tc_train_forward fills for
+ * ec_tc_train_backward; 0 on an invalid problem.  R = min(top_k N, E sum_g cap_g)
+ * packed rows; R * 2 * max(d, h) < 2^31.                                       */
+size_t ec_tc_saved_size(const ec_problem *p, int32_t top_k);
+
+/* Token-choice layer forward for training:
+ *   Y = residual + dropout(y),  y_i = sum over kept pairs of g_ij FFN_j(x_i) plus
+ * the shared experts, with the balance loss and loads of ec_tc_balance on its
+ * scores (the element of dropout at [i, c] is i d + c).  Weights as for
+ * ec_tc_forward.
+ *   drop: NULL for neither dropout nor residual; Y [N, d] out (not the residual);
+ *   loss [G] fp32 out; counts [G, E] int32 out; saved: ec_tc_saved_size bytes.
+ * ws: ec_tc_workspace_size(p, top_k, 3).                                       */
+int ec_tc_train_forward(const ec_problem *p, int32_t top_k, const ec_dropout_desc *drop,
+                        const void *X, const void *Wg, const void *W1, const void *W3,
+                        const void *W2, const void *Ws1, const void *Ws3, const void *Ws2,
+                        void *Y, float *loss, int32_t *counts, void *saved, size_t saved_bytes,
+                        void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Its backward: gradients of sum(Y * dY) + sum_g dloss_g loss_g with the choices,
+ * the kept pairs and the counts held fixed.  The gradient reaches the router
+ * through the normalised gates of all top_k choices (a dropped pair still shares
+ * in the normalisation) and through the balance loss.
+ *   drop: as in the forward, rng holding the same values (the residual is not
+ *   read; its gradient is dY); dloss [G] fp32 (device), NULL: no balance term;
+ *   saved: filled by ec_tc_train_forward with the same inputs; outputs as for
+ *   ec_moe_backward.  ws: ec_tc_workspace_size(p, top_k, 4).                   */
+int ec_tc_train_backward(const ec_problem *p, int32_t top_k, const ec_dropout_desc *drop,
+                         const void *X, const void *Wg, const void *W1, const void *W3,
+                         const void *W2, const void *Ws1, const void *Ws3, const void *Ws2,
+                         const void *dY, const float *dloss, const void *saved,
+                         size_t saved_bytes, void *dX, float *dWg, void *dW1, void *dW3,
+                         void *dW2, void *dWs1, void *dWs3, void *dWs2, void *ws,
+                         size_t ws_bytes, hipStream_t stream);
+
 /* Stage timing for profiling.  After this call, every entry point called on
  * the same thread records events[0] on its stream before its first kernel and
  * events[s+1] after stage s, for s < n_events - 1, so that
@@ -277,7 +358,11 @@ int ec_tc_forward(const ec_problem *p, int32_t top_k, const void *X, const void 
  *   gradient partials, 2 dW2, 3 dXe, 4 dW1/dW3, 5 router dZ, 6 router dX,
  *   7 shared dA + SwiGLU backward, 8 shared dW2, 9 shared dX, 10 shared
  *   dW1/dW3 (7-10 empty without shared experts), 11 combine of dXe, 12 dWg.
- * Stages of ec_route: 0 router+softmax, 1 top-k.                              */
+ * Stages of ec_route: 0 router+softmax, 1 top-k.
+ * ec_tc_train_forward and ec_tc_train_backward have the stages of ec_moe_forward and
+ * ec_moe_backward, with the balance loss in the forward's stage 2 and the dropout of
+ * dY in the backward's stage 0.  ec_tc_balance, ec_tc_balance_backward and ec_dropout
+ * record none.                                                                */
 int ec_set_stage_events(hipEvent_t *events /* HOST array */, int n_events);
 
 #ifdef __cplusplus

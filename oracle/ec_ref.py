@@ -368,6 +368,120 @@ def tc_forward_rows_ref(X, Wg, W1, W3, W2, choice, kept, rows, inv_tau: float = 
 # sum without a gate.
 # ---------------------------------------------------------------------------
 
+def tc_balance_ref(S, group_offsets, top_k: int):
+    """Balance loss [G] and loads [G, E] of token choice: each group's
+    E / (top_k L) sum_j counts_j mean_i S_ij over the choices of its rows (ties to the
+    lower expert), 0 for an empty group."""
+    S = np.asarray(S, dtype=np.float64)
+    off = np.asarray(group_offsets, dtype=np.int64)
+    G, E = len(off) - 1, S.shape[1]
+    loss, counts = np.zeros(G), np.zeros((G, E), dtype=np.int64)
+    for g in range(G):
+        rows = S[off[g]:off[g + 1]]
+        if len(rows) == 0:
+            continue
+        for row in rows:
+            counts[g, np.lexsort((np.arange(E), -row))[:top_k]] += 1
+        loss[g] = E / (top_k * len(rows)) * np.sum(counts[g] * rows.mean(axis=0))
+    return loss, counts
+
+
+def tc_balance_backward_ref(S, counts, dloss, group_offsets, top_k: int, inv_tau: float = 1.0):
+    """Gradient of sum(dloss * loss) in the logits Z of S = softmax(Z inv_tau), the counts
+    held fixed: dS_ij = dloss_g E counts_gj / (top_k L^2) through the softmax."""
+    S = np.asarray(S, dtype=np.float64)
+    off = np.asarray(group_offsets, dtype=np.int64)
+    dZ = np.zeros_like(S)
+    for g in range(len(off) - 1):
+        L = int(off[g + 1] - off[g])
+        if L == 0:
+            continue
+        rows = S[off[g]:off[g + 1]]
+        dS = float(dloss[g]) * S.shape[1] * np.asarray(counts[g], np.float64) / (top_k * L * L)
+        dZ[off[g]:off[g + 1]] = rows * (dS - (rows @ dS)[:, None]) * float(inv_tau)
+    return dZ
+
+
+def philox4x32_ref(counter, key, rounds: int = 10):
+    """Philox4x32 (Salmon, Moraes, Dror, Shaw, SC 2011): counter [..., 4] and key [2] of
+    32-bit values, in unsigned 64-bit arithmetic."""
+    m32, sh = np.uint64(0xFFFFFFFF), np.uint64(32)
+    x = [np.asarray(counter[..., i], dtype=np.uint64) for i in range(4)]
+    k0, k1 = int(key[0]), int(key[1])
+    for _ in range(rounds):
+        a, b = x[0] * np.uint64(0xD2511F53), x[2] * np.uint64(0xCD9E8D57)
+        x = [(b >> sh) ^ x[1] ^ np.uint64(k0), b & m32, (a >> sh) ^ x[3] ^ np.uint64(k1), a & m32]
+        k0, k1 = (k0 + 0x9E3779B9) % 2 ** 32, (k1 + 0xBB67AE85) % 2 ** 32
+    return np.stack(x, axis=-1)
+
+
+def dropout_mask_ref(elements, p: float, seed: int, offset: int):
+    """Factor of each of the given elements (0, or the scale of what is kept) in float64."""
+    e = np.asarray(elements, dtype=np.uint64)
+    t = int(np.rint(p * 65536.0))
+    if t == 0:
+        return np.ones(e.shape)
+    block, m32, sh = e >> np.uint64(3), np.uint64(0xFFFFFFFF), np.uint64(32)
+    seed, offset = seed % 2 ** 64, offset % 2 ** 64
+    ctr = np.stack([block & m32, block >> sh, np.full(e.shape, offset % 2 ** 32, np.uint64),
+                    np.full(e.shape, offset >> 32, np.uint64)], axis=-1)
+    words = philox4x32_ref(ctr, (seed % 2 ** 32, seed >> 32))
+    u = (e & np.uint64(7)).astype(np.int64)
+    w = np.take_along_axis(words, (u >> 1)[..., None], -1)[..., 0]
+    draw = (w >> (np.uint64(16) * (u & 1).astype(np.uint64))) & np.uint64(0xFFFF)
+    return np.where(draw >= np.uint64(t), 65536.0 / (65536 - t) if t < 65536 else 0.0, 0.0)
+
+
+def tc_train_ref(X, Wg, W1, W3, W2, dY, group_offsets, top_k: int, capacity,
+                 inv_tau: float = 1.0, shared=None, residual=None, mask=None, dloss=None):
+    """Forward and backward of the token-choice layer in training: Y = residual + mask * y,
+    the balance loss and loads, and the gradients of sum(Y dY) + sum(dloss loss).
+
+    Over the chosen experts C_i the gates are a softmax of the logits (g_ij = S_ij / sum of
+    the chosen), so with q_ij = dL/dg_ij (0 for dropped pairs, whose output is left out)
+      dZ_ij = g_ij (q_ij - sum_m g_im q_im) / tau for j in C_i;
+    the experts' products are those of backward_ref with g in the place of S."""
+    Xf, Wgf, W1f, W3f, W2f, dYf = (widen(a) for a in (X, Wg, W1, W3, W2, dY))
+    fwd = tc_forward_ref(X, Wg, W1, W3, W2, group_offsets, top_k, capacity, inv_tau)
+    S, G = fwd["S"], fwd["G"]
+    N, E = S.shape
+    m = np.ones_like(Xf) if mask is None else np.asarray(mask, np.float64).reshape(Xf.shape)
+    loss, counts = tc_balance_ref(S, group_offsets, top_k)
+    gate = np.zeros((N, E))
+    np.put_along_axis(gate, fwd["choice"], fwd["gate"], 1)
+    y, gy = fwd["Y"], dYf * m
+    dX, q = np.zeros_like(Xf), np.zeros((N, E))
+    dW1, dW3, dW2 = np.zeros_like(W1f), np.zeros_like(W3f), np.zeros_like(W2f)
+    for j in range(E):
+        rows = fwd["rows"][j]
+        if len(rows) == 0:
+            continue
+        x = Xf[rows]
+        h1, h3 = x @ W1f[j].T, x @ W3f[j].T
+        sg = 1.0 / (1.0 + np.exp(-h1))
+        a = h1 * sg * h3
+        q[rows, j] = np.sum(gy[rows] * (a @ W2f[j].T), axis=1)
+        do = G[rows, j][:, None] * gy[rows]
+        da = do @ W2f[j]
+        dW2[j] = do.T @ a
+        dh3 = da * (h1 * sg)
+        dh1 = da * h3 * (sg * (1.0 + h1 * (1.0 - sg)))
+        dX[rows] += dh1 @ W1f[j] + dh3 @ W3f[j]
+        dW1[j], dW3[j] = dh1.T @ x, dh3.T @ x
+    out = {}
+    if shared is not None:
+        y = y + shared_ffn_ref(Xf, shared)
+        dXs, out["dWs1"], out["dWs3"], out["dWs2"] = shared_backward_ref(Xf, shared, gy)
+        dX += dXs
+    Y = y * m + (0.0 if residual is None else widen(residual))
+    dZ = gate * (q - np.sum(gate * q, axis=1, keepdims=True)) * float(inv_tau)
+    if dloss is not None:
+        dZ += tc_balance_backward_ref(S, counts, dloss, group_offsets, top_k, inv_tau)
+    out.update(Y=Y, loss=loss, counts=counts, dX=dX + dZ @ Wgf, dWg=dZ.T @ Xf, dW1=dW1, dW3=dW3,
+               dW2=dW2, fwd=fwd, gate=gate)
+    return out
+
+
 def shared_ffn_ref(X, shared):
     """FFN_shared(x) for every row x of X."""
     Ws1, Ws3, Ws2 = shared

@@ -19,9 +19,15 @@ from .binding import (  # noqa: F401
     tc_capacity,
     tc_route,
     tc_forward,
+    tc_balance,
+    tc_balance_backward,
+    tc_train_forward,
+    tc_train_backward,
+    dropout,
     Layer,
     TcLayer,
 )
 
 __all__ = ["ECError", "Problem", "Layer", "TcLayer", "route", "route_noalloc", "forward", "backward", "capacity",
-           "saved_views", "token_coverage", "tc_capacity", "tc_route", "tc_forward", "lib"]
+           "saved_views", "token_coverage", "tc_capacity", "tc_route", "tc_forward", "tc_balance",
+           "tc_balance_backward", "tc_train_forward", "tc_train_backward", "dropout", "lib"]

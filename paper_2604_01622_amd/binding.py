@@ -23,7 +23,9 @@ SCHEDULERS = {"linear": 0, "linear_rev": 1, "cosine": 2, "cosine_rev": 3, "gauss
 EXPORTS = ("ec_status_string", "ec_last_error", "ec_total_capacity", "ec_workspace_size",
            "ec_saved_size", "ec_saved_layout_of", "ec_capacity", "ec_route", "ec_route_noalloc", "ec_token_coverage", "ec_moe_forward",
            "ec_moe_backward", "ec_tc_capacity", "ec_tc_workspace_size", "ec_tc_route",
-           "ec_tc_forward", "ec_set_stage_events")
+           "ec_tc_forward", "ec_tc_balance", "ec_tc_balance_backward", "ec_dropout",
+           "ec_tc_saved_size", "ec_tc_train_forward", "ec_tc_train_backward",
+           "ec_set_stage_events")
 
 
 class ECError(RuntimeError):
@@ -43,6 +45,10 @@ class _Problem(ctypes.Structure):
 class _SavedLayout(ctypes.Structure):
     _fields_ = [(n, ctypes.c_size_t) for n in ("S", "sel_token", "sel_gate", "slot", "Xe", "H1",
                                                "H3", "A", "O", "Hs1", "Hs3", "As", "total")]
+
+
+class _DropoutDesc(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("rng", ctypes.c_void_p), ("residual", ctypes.c_void_p)]
 
 
 _lib = None
@@ -93,6 +99,20 @@ def lib() -> ctypes.CDLL:
         L.ec_tc_route.argtypes = [pp, ctypes.c_int32] + [vp] * 8 + [sz, vp]
         L.ec_tc_forward.restype = ctypes.c_int
         L.ec_tc_forward.argtypes = [pp, ctypes.c_int32] + [vp] * 11 + [sz, vp]
+        dp = ctypes.POINTER(_DropoutDesc)
+        L.ec_tc_balance.restype = ctypes.c_int
+        L.ec_tc_balance.argtypes = [pp, ctypes.c_int32, vp, vp, vp, vp, sz, vp]
+        L.ec_tc_balance_backward.restype = ctypes.c_int
+        L.ec_tc_balance_backward.argtypes = [pp, ctypes.c_int32, vp, vp, vp, vp, vp]
+        L.ec_dropout.restype = ctypes.c_int
+        L.ec_dropout.argtypes = [ctypes.c_int, ctypes.c_int64, dp, vp, vp, vp]
+        L.ec_tc_saved_size.restype = sz
+        L.ec_tc_saved_size.argtypes = [pp, ctypes.c_int32]
+        L.ec_tc_train_forward.restype = ctypes.c_int
+        L.ec_tc_train_forward.argtypes = [pp, ctypes.c_int32, dp] + [vp] * 12 + [sz, vp, sz, vp]
+        L.ec_tc_train_backward.restype = ctypes.c_int
+        L.ec_tc_train_backward.argtypes = ([pp, ctypes.c_int32, dp] + [vp] * 11 + [sz] + [vp] * 9
+                                           + [sz, vp])
         L.ec_set_stage_events.restype = ctypes.c_int
         L.ec_set_stage_events.argtypes = [ctypes.POINTER(ctypes.c_void_p), ctypes.c_int]
         _lib = L
@@ -297,6 +317,148 @@ def tc_forward(X, Wg, W1, W3, W2, group_offsets, capacity, top_k: int, inv_tempe
     return Y, rows
 
 
+def _operand(name, t, dtype, shape=None, device=None):
+    """Refuses what the library cannot see: another type, shape or device, or gaps."""
+    if not isinstance(t, torch.Tensor):
+        raise ECError(1, f"{name} must be a tensor")
+    if not t.is_cuda:
+        raise ECError(1, f"{name} must be on a GPU")
+    if device is not None and t.device != device:
+        raise ECError(1, f"{name} is on {t.device}, not on {device}")
+    if t.dtype != dtype:
+        raise ECError(4, f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ECError(2, f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ECError(1, f"{name} must be contiguous")
+
+
+def _balance_problem(S, group_offsets, top_k, inv_temperature):
+    if not isinstance(S, torch.Tensor) or S.dim() != 2:
+        raise ECError(2, "S must be [N, E]")
+    _operand("S", S, torch.float32)
+    off = np.asarray(group_offsets, dtype=np.int64)
+    if off.ndim != 1 or len(off) < 2:
+        raise ECError(2, "group_offsets needs n_groups + 1 entries")
+    return Problem(S.shape[0], 64, S.shape[1], 64, off, np.zeros(len(off) - 1), inv_temperature,
+                   torch.float32)
+
+
+def tc_balance(S, group_offsets, top_k: int):
+    """Balance loss of token choice from its scores S [N,E] fp32.  Returns loss [G] fp32 and
+    counts [G,E] int32 (tokens of each group that take each expert, before any capacity)."""
+    P = _balance_problem(S, group_offsets, top_k, 1.0)
+    G, E, dev = P.c.n_groups, P.c.n_experts, S.device
+    with torch.cuda.device(dev):
+        loss = torch.empty((G,), dtype=torch.float32, device=dev)
+        counts = torch.empty((G, E), dtype=torch.int32, device=dev)
+        n = lib().ec_tc_workspace_size(P.ref, int(top_k), 2)
+        ws = _empty(n, dev)
+        _check(lib().ec_tc_balance(P.ref, int(top_k), _ptr(S) if P.c.n_tokens else None,
+                                   _ptr(loss), _ptr(counts), _ptr(ws), ws.numel(), _stream()))
+    return loss, counts
+
+
+def tc_balance_backward(S, counts, dloss, group_offsets, top_k: int, inv_temperature=1.0):
+    """Gradient of sum(dloss * loss) in the router's logits: dZ [N,E] fp32.  counts [G,E] as
+    tc_balance returned them; dloss [G] fp32."""
+    P = _balance_problem(S, group_offsets, top_k, inv_temperature)
+    G, E, dev = P.c.n_groups, P.c.n_experts, S.device
+    _operand("counts", counts, torch.int32, (G, E), dev)
+    _operand("dloss", dloss, torch.float32, (G,), dev)
+    with torch.cuda.device(dev):
+        dZ = torch.empty_like(S)
+        N = P.c.n_tokens
+        _check(lib().ec_tc_balance_backward(P.ref, int(top_k), _ptr(S) if N else None,
+                                            _ptr(counts), _ptr(dloss), _ptr(dZ) if N else None,
+                                            _stream()))
+    return dZ
+
+
+def _dropout_desc(X, p, rng, residual, name="X"):
+    """Checked description (rng: int64 [2] of seed and offset)."""
+    if rng is not None:
+        _operand("rng", rng, torch.int64, (2,), X.device)
+    if residual is not None:
+        _operand("residual", residual, X.dtype, X.shape, X.device)
+    some = X.numel() > 0
+    return _DropoutDesc(float(p), None if rng is None else rng.data_ptr(),
+                        residual.data_ptr() if residual is not None and some else None)
+
+
+def dropout(X, p: float, rng=None, residual=None, out=None):
+    """residual + dropout(X): elements are zero with probability p (the nearest multiple of
+    2^-16), the others scaled to keep the mean, by a mask that rng (int64 [2] on the device:
+    seed, offset) and an element's place alone decide.  The gradient in X is
+    ``dropout(dY, p, rng)`` with the same rng values.  out may be X or the residual."""
+    if not isinstance(X, torch.Tensor):
+        raise ECError(1, "X must be a tensor")
+    code = _dtype_code(X.dtype)
+    _operand("X", X, X.dtype)
+    desc = _dropout_desc(X, p, rng, residual)
+    if out is not None:
+        _operand("out", out, X.dtype, X.shape, X.device)
+    with torch.cuda.device(X.device):
+        Y = torch.empty_like(X) if out is None else out
+        some = X.numel() > 0
+        _check(lib().ec_dropout(code, X.numel(), ctypes.byref(desc), _ptr(X) if some else None,
+                                _ptr(Y) if some else None, _stream()))
+    return Y
+
+
+def _layer_operands(X, Wg, W1, W3, W2, shared):
+    """Types and shapes of the layer's inputs, against X and W1."""
+    for name, t, dims in (("X", X, 2), ("W1", W1, 3), ("Wg", Wg, 2)):
+        if not isinstance(t, torch.Tensor) or t.dim() != dims:
+            raise ECError(2, f"{name} must have {dims} dimensions")
+    _dtype_code(X.dtype)
+    dt, dev, d, E, h = X.dtype, X.device, X.shape[1], Wg.shape[0], W1.shape[1]
+    _operand("X", X, dt)
+    for name, t, shape in (("Wg", Wg, (E, d)), ("W1", W1, (E, h, d)), ("W3", W3, (E, h, d)),
+                           ("W2", W2, (E, d, h))):
+        _operand(name, t, dt, shape, dev)
+    if shared is not None:
+        if len(shared) != 3 or not isinstance(shared[0], torch.Tensor):
+            raise ECError(1, "shared must be (Ws1, Ws3, Ws2)")
+        hs = shared[0].shape[0]
+        for name, t, shape in (("Ws1", shared[0], (hs, d)), ("Ws3", shared[1], (hs, d)),
+                               ("Ws2", shared[2], (d, hs))):
+            _operand(name, t, dt, shape, dev)
+
+
+def _tc_size(n: int) -> int:
+    if n == 0:
+        raise ECError(2, lib().ec_last_error().decode())
+    return int(n)
+
+
+def _tok_ptr(t):
+    """A per-token tensor's address (NULL without tokens)."""
+    return _ptr(t) if t.numel() else None
+
+
+def tc_train_forward(X, Wg, W1, W3, W2, group_offsets, capacity, top_k: int, inv_temperature=1.0,
+                     shared=None, residual=None, dropout: float = 0.0, rng=None):
+    """Token-choice layer forward for training: Y = residual + dropout(layer) (see dropout
+    for rng).  Returns Y [N,d], the balance loss [G] fp32 and loads [G,E] int32 of
+    tc_balance, and the saved-activation buffer for tc_train_backward."""
+    layer = TcLayer(X, Wg, W1, W3, W2, group_offsets, capacity, top_k, inv_temperature, shared,
+                    training=True, residual=residual, dropout=dropout, rng=rng, backward=False)
+    Y = layer.forward()
+    return Y, layer.loss, layer.counts, layer.saved
+
+
+def tc_train_backward(X, Wg, W1, W3, W2, dY, saved, group_offsets, capacity, top_k: int,
+                      inv_temperature=1.0, shared=None, dropout: float = 0.0, rng=None,
+                      dloss=None):
+    """Backward of tc_train_forward: gradients of sum(Y * dY) + sum(dloss * loss) (dloss [G]
+    fp32 or None; the residual's gradient is dY).  Returns dX, dWg (fp32), dW1, dW3, dW2 (and
+    dWs1, dWs3, dWs2 with shared experts)."""
+    layer = TcLayer(X, Wg, W1, W3, W2, group_offsets, capacity, top_k, inv_temperature, shared,
+                    training=True, dropout=dropout, rng=rng, saved=saved)
+    return layer.backward(dY, dloss)
+
+
 def _shared_ptrs(shared):
     return [None, None, None] if shared is None else [_ptr(w) for w in shared]
 
@@ -406,29 +568,89 @@ class Layer:
 
 
 class TcLayer:
-    """Pre-planned token-choice forward (the comparison policy): workspace and outputs
-    allocated once."""
+    """Pre-planned token choice (the comparison policy): workspace and outputs allocated
+    once.  training: forward returns Y = residual + dropout(layer) and leaves the balance
+    loss [G] in ``loss`` and the experts' loads [G,E] in ``counts``; backward returns the
+    gradients (dWg in fp32).  rng (int64 [2] on the device, see dropout) must hold the same
+    values in a step's forward and backward; advance its offset between steps."""
 
     def __init__(self, X, Wg, W1, W3, W2, group_offsets, capacity, top_k: int,
-                 inv_temperature=1.0, shared=None):
+                 inv_temperature=1.0, shared=None, training=False, residual=None,
+                 dropout: float = 0.0, rng=None, saved=None, backward=True):
         self.X, self.Wg, self.W1, self.W3, self.W2 = X, Wg, W1, W3, W2
-        self.shared = shared
+        self.shared, self.training = shared, training
         self.top_k = int(top_k)
+        if not training:
+            if residual is not None or dropout or rng is not None or saved is not None:
+                raise ECError(1, "residual, dropout, rng and saved need training=True")
+            self.P = Problem.of(X, Wg, W1.shape[1], group_offsets, capacity, inv_temperature,
+                                shared)
+            dev = X.device
+            self.Y = torch.empty_like(X)
+            self.rows = torch.empty((Wg.shape[0] + 1,), dtype=torch.int32, device=dev)
+            n = lib().ec_tc_workspace_size(self.P.ref, self.top_k, 1)
+            if n == 0:
+                _check(2)
+            self.ws = _empty(n, dev)
+            return
+        _layer_operands(X, Wg, W1, W3, W2, shared)
+        self.residual, self.rng = residual, rng
+        self.drop = _dropout_desc(X, dropout, rng, residual)
         self.P = Problem.of(X, Wg, W1.shape[1], group_offsets, capacity, inv_temperature, shared)
-        dev = X.device
-        self.Y = torch.empty_like(X)
-        self.rows = torch.empty((Wg.shape[0] + 1,), dtype=torch.int32, device=dev)
-        n = lib().ec_tc_workspace_size(self.P.ref, self.top_k, 1)
-        if n == 0:
-            _check(2)
-        self.ws = _empty(n, dev)
+        if len(self.P.off) != len(self.P.cap) + 1:
+            raise ECError(2, "group_offsets must have one entry more than capacity")
+        L, k, dev = lib(), self.top_k, X.device
+        n_saved = _tc_size(L.ec_tc_saved_size(self.P.ref, k))
+        with torch.cuda.device(dev):
+            if saved is None:
+                self.Y = torch.empty_like(X)
+                self.loss = torch.empty((self.P.c.n_groups,), dtype=torch.float32, device=dev)
+                self.counts = torch.empty((self.P.c.n_groups, Wg.shape[0]), dtype=torch.int32,
+                                          device=dev)
+                self.saved = _empty(n_saved, dev)
+                self.ws_f = _empty(_tc_size(L.ec_tc_workspace_size(self.P.ref, k, 3)), dev)
+            else:
+                _operand("saved", saved, torch.uint8, None, dev)
+                self.saved = saved
+            if backward:
+                self.ws_b = _empty(_tc_size(L.ec_tc_workspace_size(self.P.ref, k, 4)), dev)
+                self.dX = torch.empty_like(X)
+                self.dWg = torch.empty(Wg.shape, dtype=torch.float32, device=dev)
+                self.dW1, self.dW3 = torch.empty_like(W1), torch.empty_like(W3)
+                self.dW2 = torch.empty_like(W2)
+                self.dshared = None if shared is None else [torch.empty_like(w) for w in shared]
 
     def forward(self):
-        _check(lib().ec_tc_forward(self.P.ref, self.top_k, _ptr(self.X), _ptr(self.Wg),
-                                   _ptr(self.W1), _ptr(self.W3), _ptr(self.W2),
-                                   *_shared_ptrs(self.shared), _ptr(self.Y), _ptr(self.rows),
-                                   _ptr(self.ws), self.ws.numel(), _stream()))
+        if not self.training:
+            _check(lib().ec_tc_forward(self.P.ref, self.top_k, _ptr(self.X), _ptr(self.Wg),
+                                       _ptr(self.W1), _ptr(self.W3), _ptr(self.W2),
+                                       *_shared_ptrs(self.shared), _ptr(self.Y), _ptr(self.rows),
+                                       _ptr(self.ws), self.ws.numel(), _stream()))
+            return self.Y
+        with torch.cuda.device(self.X.device):
+            _check(lib().ec_tc_train_forward(
+                self.P.ref, self.top_k, ctypes.byref(self.drop), _tok_ptr(self.X), _ptr(self.Wg),
+                _ptr(self.W1), _ptr(self.W3), _ptr(self.W2), *_shared_ptrs(self.shared),
+                _tok_ptr(self.Y), _ptr(self.loss), _ptr(self.counts), _ptr(self.saved),
+                self.saved.numel(), _ptr(self.ws_f), self.ws_f.numel(), _stream()))
         return self.Y
+
+    def backward(self, dY, dloss=None):
+        """dX, dWg, dW1, dW3, dW2 (and dWs1, dWs3, dWs2) of sum(Y * dY) + sum(dloss * loss)."""
+        if not self.training:
+            raise ECError(1, "backward needs training=True")
+        _operand("dY", dY, self.X.dtype, self.X.shape, self.X.device)
+        if dloss is not None:
+            _operand("dloss", dloss, torch.float32, (self.P.c.n_groups,), self.X.device)
+        with torch.cuda.device(self.X.device):
+            _check(lib().ec_tc_train_backward(
+                self.P.ref, self.top_k, ctypes.byref(self.drop), _tok_ptr(self.X), _ptr(self.Wg),
+                _ptr(self.W1), _ptr(self.W3), _ptr(self.W2), *_shared_ptrs(self.shared),
+                _tok_ptr(dY), _ptr(dloss), _ptr(self.saved), self.saved.numel(),
+                _tok_ptr(self.dX), _ptr(self.dWg), _ptr(self.dW1), _ptr(self.dW3),
+                _ptr(self.dW2), *_shared_ptrs(self.dshared), _ptr(self.ws_b),
+                self.ws_b.numel(), _stream()))
+        return (self.dX, self.dWg, self.dW1, self.dW3, self.dW2) + tuple(self.dshared or ())
 
 
 FORWARD_STAGES = ("router", "topk", "gather", "gemm_w13_swiglu", "gemm_w2", "shared_w13_swiglu",

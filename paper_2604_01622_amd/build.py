@@ -21,7 +21,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libecmoe.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
-SOURCES = ["router.hip", "topk.hip", "tc.hip", "movement.hip", "gemm.hip", "ec_api.cpp"]
+SOURCES = ["router.hip", "topk.hip", "tc.hip", "balance.hip", "dropout.hip", "movement.hip", "gemm.hip", "ec_api.cpp"]
 
 
 def hipcc() -> str:

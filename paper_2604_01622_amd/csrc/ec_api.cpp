@@ -261,7 +261,9 @@ int enqueue_route(const ec_problem* p, const Plan& P, const void* X, const void*
 
 // ---- token choice -------------------------------------------------------------
 
-int tc_validate(const ec_problem* p, int top_k, Plan* P, long* rmax, int* rmax_e) {
+// train: the backward's [rows, 2h] buffer counts too.
+int tc_validate(const ec_problem* p, int top_k, Plan* P, long* rmax, int* rmax_e,
+                bool train = false) {
   EC_TRY(validate(p, P, false));
   if (top_k < 1 || top_k > P->E)
     return fail(EC_ERR_ARG, "top_k must be in [1, n_experts] (got %d)", top_k);
@@ -270,7 +272,7 @@ int tc_validate(const ec_problem* p, int top_k, Plan* P, long* rmax, int* rmax_e
   const long per_e = P->K < P->N ? P->K : P->N;
   if ((long)P->E * per_e < r) r = (long)P->E * per_e;
   const long w = P->d > P->h ? P->d : P->h;
-  if (r * w >= ((long)1 << 31))
+  if (r * w * (train ? 2 : 1) >= ((long)1 << 31))
     return fail(EC_ERR_SHAPE, "too many token-expert pairs for 32-bit element indices");
   *rmax = r;
   *rmax_e = (int)per_e;
@@ -319,10 +321,12 @@ TcFwdWs carve_tc_fwd(Carve& c, const Plan& P, long rmax) {
   return w;
 }
 
-// Router, row top-k, per-(group, expert) counts, offsets and placement.
+// Router, row top-k, per-(group, expert) counts, offsets and placement.  sel_gate and
+// tilesA (training only): the packed rows' gates and the tiles of the dA product.
 int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* X, const void* Wg,
                      float* S, float* G, int32_t* slot, int32_t* rows, int32_t* sel,
-                     const TcRouteWs& w, hipStream_t st) {
+                     const TcRouteWs& w, hipStream_t st, float* sel_gate = nullptr,
+                     int32_t* tilesA = nullptr) {
   EC_HIP(mark(0, st));
   EC_HIP(ec::launch_router_softmax(P.dtype, X, Wg, S, w.ST, P.N, P.d, P.E, p->inv_temperature,
                                    st));
@@ -340,15 +344,161 @@ int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* 
         ++tab.n;
       }
       if (pass == 0) EC_HIP(ec::launch_tc_count(slot, P.N, P.E, tab, g0, w.cnt, st));
-      else EC_HIP(ec::launch_tc_place(slot, G, P.N, P.E, tab, g0, w.seg, sel, st));
+      else EC_HIP(ec::launch_tc_place(slot, G, P.N, P.E, tab, g0, w.seg, sel, sel_gate, st));
     }
     if (pass == 0)
       EC_HIP(ec::launch_tc_offsets(w.cnt, P.G, P.E, ec::TC_BM, ec::tc_col_blocks_w13(P.h),
-                                   ec::tc_col_blocks_w2(P.d), rows, w.seg, w.tiles13, w.tiles2,
-                                   st));
+                                   ec::tc_col_blocks_w2(P.d), ec::tc_col_blocks_dA(P.h), rows,
+                                   w.seg, w.tiles13, w.tiles2, tilesA, st));
   }
   EC_HIP(mark(2, st));
   return EC_OK;
+}
+
+// ---- the balance loss of token choice ------------------------------------------
+
+// The chunk tables of the problem's groups, in passes of TOPK_MAX_GROUPS: body(table, first
+// group, chunks before it) for each.
+template <typename F>
+int for_chunk_tables(const ec_problem* p, const Plan& P, F body) {
+  ec::ChunkTable tab;
+  tab.chunk = ec::balance_chunk(P.N);
+  long before = 0;
+  for (int g0 = 0; g0 < P.G; g0 += ec::TOPK_MAX_GROUPS) {
+    tab.n = 0;
+    tab.seg[0] = 0;
+    for (int g = g0; g < P.G && g < g0 + ec::TOPK_MAX_GROUPS; ++g) {
+      tab.off[tab.n] = p->group_offsets[g];
+      tab.len[tab.n] = p->group_offsets[g + 1] - p->group_offsets[g];
+      tab.seg[tab.n + 1] = tab.seg[tab.n] + (tab.len[tab.n] + tab.chunk - 1) / tab.chunk;
+      ++tab.n;
+    }
+    EC_TRY(body(tab, g0, before));
+    before += tab.seg[tab.n];
+  }
+  return EC_OK;
+}
+
+struct BalanceWs {
+  double* psum;    // [chunks, E]
+  int32_t* pcnt;
+};
+
+BalanceWs carve_balance(Carve& c, const ec_problem* p, const Plan& P) {
+  const int chunk = ec::balance_chunk(P.N);
+  size_t chunks = 0;
+  for (int g = 0; g < P.G; ++g)
+    chunks += (p->group_offsets[g + 1] - p->group_offsets[g] + chunk - 1) / chunk;
+  BalanceWs w;
+  w.psum = (double*)c.take(chunks * P.E * 8);
+  w.pcnt = (int32_t*)c.take(chunks * P.E * 4);
+  return w;
+}
+
+int enqueue_balance(const ec_problem* p, const Plan& P, int top_k, const float* S, float* loss,
+                    int32_t* counts, int32_t* counts2, const BalanceWs& w, hipStream_t st) {
+  return for_chunk_tables(p, P, [&](const ec::ChunkTable& tab, int g0, long before) -> int {
+    double* psum = w.psum + before * P.E;
+    int32_t* pcnt = w.pcnt + before * P.E;
+    const size_t at = (size_t)g0 * P.E;
+    EC_HIP(ec::launch_balance_partial(S, P.E, top_k, tab, psum, pcnt, st));
+    EC_HIP(ec::launch_balance_finish(psum, pcnt, P.E, top_k, tab, loss + g0, counts + at,
+                                     counts2 ? counts2 + at : nullptr, st));
+    return EC_OK;
+  });
+}
+
+// ---- dropout -------------------------------------------------------------------
+
+// The launch form of a description; without one (or with p below 2^-17) nothing is dropped.
+int dropout_of(const ec_dropout_desc* d, ec::Dropout* out) {
+  *out = ec::Dropout{0, 1.f, nullptr};
+  if (!d) return EC_OK;
+  if (!(d->p >= 0.0 && d->p <= 1.0)) return fail(EC_ERR_ARG, "dropout p must be in [0, 1]");
+  const double thr = std::nearbyint(d->p * 65536.0);
+  EC_TRY(check_ptr(d->rng, "rng", thr == 0));
+  EC_TRY(check_ptr(d->residual, "residual", true));
+  out->thr = (uint32_t)thr;
+  out->scale = thr < 65536.0 ? (float)(65536.0 / (65536.0 - thr)) : 0.f;
+  out->rng = d->rng;
+  return EC_OK;
+}
+
+bool overlap(const void* a, const void* b, size_t bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y ? y - x < bytes : x - y < bytes;
+}
+
+// ---- token-choice training ------------------------------------------------------
+
+struct TcSaved {
+  float* S;
+  float* G;          // [N, E] gates of every choice, dropped ones too
+  int32_t* slot;     // [E, N] packed row or -1
+  int32_t* rows;     // [E + 1]
+  int32_t* tiles2;   // [E + 1] tiles of the products of width d
+  int32_t* tilesA;   // [E + 1] tiles of the dA product
+  int32_t* counts;   // [G, E]
+  int32_t* sel;      // [R] token of each packed row
+  float* gate;       // [R] its gate
+  void* H1;          // [R, h]
+  void* H3;
+  void* A;
+  void* Hs1;         // shared experts, [N, hs]
+  void* Hs3;
+  void* As;
+};
+
+TcSaved carve_tc_saved(Carve& c, const Plan& P, long rmax) {
+  TcSaved s;
+  s.S = (float*)c.take((size_t)P.N * P.E * 4);
+  s.G = (float*)c.take((size_t)P.N * P.E * 4);
+  s.slot = (int32_t*)c.take((size_t)P.E * P.N * 4);
+  s.rows = (int32_t*)c.take((size_t)(P.E + 1) * 4);
+  s.tiles2 = (int32_t*)c.take((size_t)(P.E + 1) * 4);
+  s.tilesA = (int32_t*)c.take((size_t)(P.E + 1) * 4);
+  s.counts = (int32_t*)c.take((size_t)P.G * P.E * 4);
+  s.sel = (int32_t*)c.take((size_t)rmax * 4);
+  s.gate = (float*)c.take((size_t)rmax * 4);
+  s.H1 = c.take((size_t)rmax * P.h * P.esz);
+  s.H3 = c.take((size_t)rmax * P.h * P.esz);
+  s.A = c.take((size_t)rmax * P.h * P.esz);
+  const size_t sh = (size_t)P.N * P.hs * P.esz;
+  s.Hs1 = sh ? c.take(sh) : nullptr;
+  s.Hs3 = sh ? c.take(sh) : nullptr;
+  s.As = sh ? c.take(sh) : nullptr;
+  return s;
+}
+
+struct TcTrainFwdWs {
+  TcRouteWs route;
+  BalanceWs balance;
+  void* O;           // [R, d]
+};
+
+TcTrainFwdWs carve_tc_train_fwd(Carve& c, const ec_problem* p, const Plan& P, long rmax) {
+  TcTrainFwdWs w;
+  w.route = carve_tc_route(c, P);
+  w.balance = carve_balance(c, p, P);
+  w.O = c.take((size_t)rmax * P.d * P.esz);
+  return w;
+}
+
+// The buffers of expert choice's backward on packed rows, and the dropped-out dY.
+struct TcTrainBwdWs {
+  BwdWs b;
+  void* dYm;         // [N, d]
+};
+
+TcTrainBwdWs carve_tc_train_bwd(Carve& c, const Plan& P, long rmax) {
+  Plan packed = P;   // one buffer of all experts' rows
+  packed.E = 1;
+  packed.K = rmax;
+  TcTrainBwdWs w;
+  w.b = carve_bwd(c, packed);
+  w.b.part = (float*)c.take((size_t)w.b.splits * P.E * P.d * 4);
+  w.dYm = c.take((size_t)P.N * P.d * P.esz);
+  return w;
 }
 
 // ---- routing without allocation ---------------------------------------------
@@ -746,11 +896,24 @@ size_t ec_tc_workspace_size(const ec_problem* p, int32_t top_k, int mode) {
   Plan P;
   long rmax;
   int rmax_e;
-  if (tc_validate(p, top_k, &P, &rmax, &rmax_e) != EC_OK) return 0;
+  if (tc_validate(p, top_k, &P, &rmax, &rmax_e, mode == 3 || mode == 4) != EC_OK) return 0;
   Carve c(nullptr);
+  if (mode == 2) { carve_balance(c, p, P); return align_up(c.used + 1); }
+  if (mode == 3) { carve_tc_train_fwd(c, p, P, rmax); return c.used; }
+  if (mode == 4) { carve_tc_train_bwd(c, P, rmax); return align_up(c.used + 1); }
   carve_tc_route(c, P);
   if (mode == 1) carve_tc_fwd(c, P, rmax);
   else if (mode != 0) { fail(EC_ERR_ARG, "unknown workspace mode %d", mode); return 0; }
+  return c.used;
+}
+
+size_t ec_tc_saved_size(const ec_problem* p, int32_t top_k) {
+  Plan P;
+  long rmax;
+  int rmax_e;
+  if (tc_validate(p, top_k, &P, &rmax, &rmax_e, true) != EC_OK) return 0;
+  Carve c(nullptr);
+  carve_tc_saved(c, P, rmax);
   return c.used;
 }
 
@@ -810,7 +973,7 @@ int ec_tc_forward(const ec_problem* p, int32_t top_k, const void* X, const void*
   EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, w.S, w.G, w.slot, rows, w.sel, rw, stream));
   // the W1/W3 product reads the kept rows of X itself (empty gather stage)
   EC_HIP(mark(3, stream));
-  EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, w.A, P.E, rows, rw.tiles13, rmax, rmax_e, P.d,
+  EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, w.A, nullptr, nullptr, P.E, rows, rw.tiles13, rmax, rmax_e, P.d,
                                  P.h, stream, w.sel));
   EC_HIP(mark(4, stream));
   EC_HIP(ec::launch_gemm_w2_var(P.dtype, w.A, W2, w.O, P.E, rows, rw.tiles2, rmax, rmax_e, P.d,
@@ -828,6 +991,231 @@ int ec_tc_forward(const ec_problem* p, int32_t top_k, const void* X, const void*
   EC_HIP(ec::launch_combine(P.dtype, w.O, w.G, w.slot, P.hs ? Y : nullptr, Y, P.N, P.E,
                             (int)rmax, P.d, stream, 0));
   EC_HIP(mark(8, stream));
+  return EC_OK;
+}
+
+int ec_tc_balance(const ec_problem* p, int32_t top_k, const float* S, float* loss,
+                  int32_t* counts, void* ws, size_t ws_bytes, hipStream_t stream) {
+  Plan P;
+  long rmax;
+  int rmax_e;
+  EC_TRY(tc_validate(p, top_k, &P, &rmax, &rmax_e));
+  EC_TRY(check_ptr(S, "S", P.N == 0));
+  EC_TRY(check_ptr(loss, "loss"));
+  EC_TRY(check_ptr(counts, "counts"));
+  const size_t need = ec_tc_workspace_size(p, top_k, 2);
+  EC_TRY(check_ptr(ws, "workspace"));
+  if (ws_bytes < need)
+    return fail(EC_ERR_WORKSPACE, "workspace %zu bytes < %zu required", ws_bytes, need);
+  Carve c(ws);
+  return enqueue_balance(p, P, top_k, S, loss, counts, nullptr, carve_balance(c, p, P), stream);
+}
+
+int ec_tc_balance_backward(const ec_problem* p, int32_t top_k, const float* S,
+                           const int32_t* counts, const float* dloss, float* dZ,
+                           hipStream_t stream) {
+  Plan P;
+  long rmax;
+  int rmax_e;
+  EC_TRY(tc_validate(p, top_k, &P, &rmax, &rmax_e));
+  EC_TRY(check_ptr(S, "S", P.N == 0));
+  EC_TRY(check_ptr(counts, "counts"));
+  EC_TRY(check_ptr(dloss, "dloss"));
+  EC_TRY(check_ptr(dZ, "dZ", P.N == 0));
+  return for_chunk_tables(p, P, [&](const ec::ChunkTable& tab, int g0, long) -> int {
+    EC_HIP(ec::launch_balance_backward(S, counts + (size_t)g0 * P.E, dloss + g0, P.E, top_k,
+                                       p->inv_temperature, tab, dZ, stream));
+    return EC_OK;
+  });
+}
+
+int ec_dropout(int dtype, int64_t n, const ec_dropout_desc* drop, const void* X, void* Y,
+               hipStream_t stream) {
+  g_last_error[0] = '\0';
+  if (dtype != EC_F32 && dtype != EC_BF16) return fail(EC_ERR_DTYPE, "unknown dtype %d", dtype);
+  if (n < 0 || n >= (int64_t)1 << 40) return fail(EC_ERR_SHAPE, "n must be in [0, 2^40)");
+  if (!drop) return fail(EC_ERR_ARG, "drop is NULL");
+  ec::Dropout d;
+  EC_TRY(dropout_of(drop, &d));
+  EC_TRY(check_ptr(X, "X", n == 0));
+  EC_TRY(check_ptr(Y, "Y", n == 0));
+  const size_t bytes = (size_t)n * (dtype == EC_F32 ? 4 : 2);
+  if (Y != X && overlap(X, Y, bytes)) return fail(EC_ERR_ARG, "X and Y overlap");
+  if (drop->residual && drop->residual != Y && overlap(drop->residual, Y, bytes))
+    return fail(EC_ERR_ARG, "the residual and Y overlap");
+  EC_HIP(ec::launch_dropout(dtype, X, drop->residual, d, Y, n, stream));
+  return EC_OK;
+}
+
+int ec_tc_train_forward(const ec_problem* p, int32_t top_k, const ec_dropout_desc* drop,
+                        const void* X, const void* Wg, const void* W1, const void* W3,
+                        const void* W2, const void* Ws1, const void* Ws3, const void* Ws2,
+                        void* Y, float* loss, int32_t* counts, void* saved,
+                        size_t saved_bytes_in, void* ws, size_t ws_bytes, hipStream_t stream) {
+  Plan P;
+  long rmax;
+  int rmax_e;
+  EC_TRY(tc_validate(p, top_k, &P, &rmax, &rmax_e, true));
+  ec::Dropout d;
+  EC_TRY(dropout_of(drop, &d));
+  const void* residual = drop ? drop->residual : nullptr;
+  EC_TRY(check_ptr(X, "X", P.N == 0));
+  EC_TRY(check_ptr(Wg, "Wg"));
+  EC_TRY(check_ptr(W1, "W1"));
+  EC_TRY(check_ptr(W3, "W3"));
+  EC_TRY(check_ptr(W2, "W2"));
+  EC_TRY(check_ptr(Ws1, "Ws1", P.hs == 0));
+  EC_TRY(check_ptr(Ws3, "Ws3", P.hs == 0));
+  EC_TRY(check_ptr(Ws2, "Ws2", P.hs == 0));
+  EC_TRY(check_ptr(Y, "Y", P.N == 0));
+  // the shared experts' output is held in Y before the residual is read
+  if (residual && overlap(residual, Y, (size_t)P.N * P.d * P.esz))
+    return fail(EC_ERR_ARG, "the residual and Y overlap");
+  EC_TRY(check_ptr(loss, "loss"));
+  EC_TRY(check_ptr(counts, "counts"));
+  EC_TRY(check_ptr(saved, "saved"));
+  const size_t need_saved = ec_tc_saved_size(p, top_k);
+  if (saved_bytes_in < need_saved)
+    return fail(EC_ERR_WORKSPACE, "saved buffer %zu bytes < %zu required", saved_bytes_in,
+                need_saved);
+  const size_t need = ec_tc_workspace_size(p, top_k, 3);
+  EC_TRY(check_ptr(ws, "workspace"));
+  if (ws_bytes < need)
+    return fail(EC_ERR_WORKSPACE, "workspace %zu bytes < %zu required", ws_bytes, need);
+  Carve cs(saved), c(ws);
+  const TcSaved s = carve_tc_saved(cs, P, rmax);
+  const TcTrainFwdWs w = carve_tc_train_fwd(c, p, P, rmax);
+  if (P.N == 0) {   // no tokens: nothing kept, zero losses and loads
+    EC_HIP(ec::launch_zero(s.rows, (size_t)(P.E + 1) * 4, stream));
+    EC_HIP(ec::launch_zero(s.tiles2, (size_t)(P.E + 1) * 4, stream));
+    EC_HIP(ec::launch_zero(s.tilesA, (size_t)(P.E + 1) * 4, stream));
+    return enqueue_balance(p, P, top_k, s.S, loss, counts, s.counts, w.balance, stream);
+  }
+  TcRouteWs rw = w.route;
+  rw.tiles2 = s.tiles2;
+  EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, s.S, s.G, s.slot, s.rows, s.sel, rw, stream, s.gate,
+                          s.tilesA));
+  EC_TRY(enqueue_balance(p, P, top_k, s.S, loss, counts, s.counts, w.balance, stream));
+  EC_HIP(mark(3, stream));
+  // A carries the gate (A = g SiLU(H1) H3), as in expert choice: the output adds rows
+  EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, s.A, s.H1, s.H3, P.E, s.rows, rw.tiles13,
+                                 rmax, rmax_e, P.d, P.h, stream, s.sel, s.gate));
+  EC_HIP(mark(4, stream));
+  EC_HIP(ec::launch_gemm_w2_var(P.dtype, s.A, W2, w.O, P.E, s.rows, s.tiles2, rmax, rmax_e, P.d,
+                                P.h, stream));
+  EC_HIP(mark(5, stream));
+  if (P.hs) {
+    EC_HIP(ec::launch_gemm_w13(P.dtype, X, Ws1, Ws3, s.As, s.Hs1, s.Hs3, 1, P.N, P.d, P.hs,
+                               stream, true));
+    EC_HIP(mark(6, stream));
+    EC_HIP(ec::launch_gemm_w2(P.dtype, s.As, Ws2, Y, 1, P.N, P.d, P.hs, stream, true));
+  } else {
+    EC_HIP(mark(6, stream));
+  }
+  EC_HIP(mark(7, stream));
+  EC_HIP(ec::launch_combine_drop(P.dtype, w.O, s.slot, P.hs ? Y : nullptr, residual, d, Y, P.N,
+                                 P.E, (int)rmax, P.d, stream));
+  EC_HIP(mark(8, stream));
+  return EC_OK;
+}
+
+int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_desc* drop,
+                         const void* X, const void* Wg, const void* W1, const void* W3,
+                         const void* W2, const void* Ws1, const void* Ws3, const void* Ws2,
+                         const void* dY, const float* dloss, const void* saved,
+                         size_t saved_bytes_in, void* dX, float* dWg, void* dW1, void* dW3,
+                         void* dW2, void* dWs1, void* dWs3, void* dWs2, void* ws,
+                         size_t ws_bytes, hipStream_t stream) {
+  Plan P;
+  long rmax;
+  int rmax_e;
+  EC_TRY(tc_validate(p, top_k, &P, &rmax, &rmax_e, true));
+  ec::Dropout dr;
+  EC_TRY(dropout_of(drop, &dr));
+  EC_TRY(check_ptr(X, "X", P.N == 0));
+  EC_TRY(check_ptr(Wg, "Wg"));
+  EC_TRY(check_ptr(W1, "W1"));
+  EC_TRY(check_ptr(W3, "W3"));
+  EC_TRY(check_ptr(W2, "W2"));
+  EC_TRY(check_ptr(Ws1, "Ws1", P.hs == 0));
+  EC_TRY(check_ptr(Ws3, "Ws3", P.hs == 0));
+  EC_TRY(check_ptr(Ws2, "Ws2", P.hs == 0));
+  EC_TRY(check_ptr(dY, "dY", P.N == 0));
+  EC_TRY(check_ptr(dloss, "dloss", true));
+  EC_TRY(check_ptr(saved, "saved"));
+  EC_TRY(check_ptr(dX, "dX", P.N == 0));
+  EC_TRY(check_ptr(dWg, "dWg"));
+  EC_TRY(check_ptr(dW1, "dW1"));
+  EC_TRY(check_ptr(dW3, "dW3"));
+  EC_TRY(check_ptr(dW2, "dW2"));
+  EC_TRY(check_ptr(dWs1, "dWs1", P.hs == 0));
+  EC_TRY(check_ptr(dWs3, "dWs3", P.hs == 0));
+  EC_TRY(check_ptr(dWs2, "dWs2", P.hs == 0));
+  const size_t need_saved = ec_tc_saved_size(p, top_k);
+  if (saved_bytes_in < need_saved)
+    return fail(EC_ERR_WORKSPACE, "saved buffer %zu bytes < %zu required", saved_bytes_in,
+                need_saved);
+  const size_t need = ec_tc_workspace_size(p, top_k, 4);
+  EC_TRY(check_ptr(ws, "workspace"));
+  if (ws_bytes < need)
+    return fail(EC_ERR_WORKSPACE, "workspace %zu bytes < %zu required", ws_bytes, need);
+  Carve cs((void*)saved), c(ws);
+  const TcSaved s = carve_tc_saved(cs, P, rmax);
+  const TcTrainBwdWs w = carve_tc_train_bwd(c, P, rmax);
+  const BwdWs& b = w.b;
+  const int E = P.E, d = P.d, h = P.h, N = P.N, hs = P.hs;
+  EC_HIP(mark(0, stream));
+  // the gradient before the dropout: the mask again, from the same counters
+  const void* dYm = dY;
+  if (dr.thr && N > 0) {
+    EC_HIP(ec::launch_dropout(P.dtype, dY, nullptr, dr, w.dYm, (long)N * d, stream));
+    dYm = w.dYm;
+  }
+  EC_HIP(mark(1, stream));
+  EC_HIP(ec::launch_gemm_dA_var(P.dtype, dYm, W2, s.H1, s.H3, b.dH, b.dsp, E, s.rows, s.tilesA,
+                                rmax, rmax_e, d, h, s.sel, s.gate, stream));
+  EC_HIP(mark(2, stream));
+  EC_HIP(ec::launch_gemm_dW2_var(P.dtype, dYm, s.A, dW2, E, s.rows, rmax_e, d, h, s.sel, stream));
+  EC_HIP(mark(3, stream));
+  EC_HIP(ec::launch_gemm_dXe_var(P.dtype, b.dH, W1, W3, b.dXe, E, s.rows, s.tiles2, rmax, rmax_e,
+                                 d, h, stream));
+  EC_HIP(mark(4, stream));
+  EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.rows, rmax_e, d, h, s.sel,
+                                  stream));
+  EC_HIP(mark(5, stream));
+  EC_TRY(for_chunk_tables(p, P, [&](const ec::ChunkTable& tab, int g0, long) -> int {
+    EC_HIP(ec::launch_tc_router_dz(P.dtype, s.S, s.G, s.slot, b.dsp, ec::dsp_parts(P.dtype, h),
+                                   s.counts + (size_t)g0 * E, dloss ? dloss + g0 : nullptr, b.dZ, N,
+                                   E, P.EP, top_k, (int)rmax, p->inv_temperature, tab, stream));
+    return EC_OK;
+  }));
+  EC_HIP(mark(6, stream));
+  EC_HIP(ec::launch_router_dx(P.dtype, b.dZ, Wg, dX, N, E, P.EP, d, stream));
+  EC_HIP(mark(7, stream));
+  if (hs && N > 0) {
+    EC_HIP(ec::launch_gemm_dA(P.dtype, dYm, Ws2, s.Hs1, s.Hs3, b.dHs, 1, N, d, hs, stream, true));
+    EC_HIP(mark(8, stream));
+    EC_HIP(ec::launch_shared_dW2(P.dtype, dYm, s.As, dWs2, N, d, hs, b.spart, b.s_splits2, stream));
+    EC_HIP(mark(9, stream));
+    EC_HIP(ec::launch_gemm_dXe(P.dtype, b.dHs, Ws1, Ws3, dX, 1, N, d, hs, stream, true));
+    EC_HIP(mark(10, stream));
+    EC_HIP(ec::launch_shared_dW13(P.dtype, b.dHs, X, dWs1, dWs3, N, d, hs, b.spart, b.s_splits13,
+                                  stream));
+  } else {
+    if (hs) {   // no tokens: zero shared weight gradients
+      EC_HIP(ec::launch_zero(dWs1, (size_t)hs * d * P.esz, stream));
+      EC_HIP(ec::launch_zero(dWs3, (size_t)hs * d * P.esz, stream));
+      EC_HIP(ec::launch_zero(dWs2, (size_t)hs * d * P.esz, stream));
+    }
+    EC_HIP(mark(8, stream));
+    EC_HIP(mark(9, stream));
+    EC_HIP(mark(10, stream));
+  }
+  EC_HIP(mark(11, stream));
+  EC_HIP(ec::launch_bwd_combine(P.dtype, b.dXe, s.slot, dX, dX, N, E, (int)rmax, d, stream, 0));
+  EC_HIP(mark(12, stream));
+  EC_HIP(ec::launch_router_dwg(P.dtype, b.dZ, X, dWg, b.part, b.splits, N, E, P.EP, d, stream));
+  EC_HIP(mark(13, stream));
   return EC_OK;
 }
 

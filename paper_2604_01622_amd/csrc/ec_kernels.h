@@ -41,9 +41,29 @@ hipError_t launch_combine(int dtype, const void* O, const float* S, const int32_
                           const void* Xr, void* Y, int N, int E, int K, int d, hipStream_t st,
                           long kstride = -1);
 
+// Dropout of a call: an element whose 16-bit draw is below thr is dropped, the others are
+// scaled (thr 0: none is drawn); rng: device [2], the seed and the offset (see dropout.h).
+struct Dropout {
+  uint32_t thr;
+  float scale;
+  const uint64_t* rng;
+};
+
+// The combine of token-choice training: Y = R + dropout(Xr + sum_j O[slotT[j, i]]) over the
+// packed rows (R and Xr may be null; Xr may alias Y).
+hipError_t launch_combine_drop(int dtype, const void* O, const int32_t* slotT, const void* Xr,
+                               const void* R, const Dropout& drop, void* Y, int N, int E,
+                               int max_rows, int d, hipStream_t st);
+
+// Y = R + dropout(X) over n elements (R may be null; Y may be X or R).
+hipError_t launch_dropout(int dtype, const void* X, const void* R, const Dropout& drop, void* Y,
+                          long n, hipStream_t st);
+
 // Backward combine: dX[i,:] = Xr[i,:] + sum_j dXe[j, slotT[j,i], :]  (Xr may alias dX).
+// kstride as for launch_combine.
 hipError_t launch_bwd_combine(int dtype, const void* dXe, const int32_t* slotT, const void* Xr,
-                              void* dX, int N, int E, int K, int d, hipStream_t st);
+                              void* dX, int N, int E, int K, int d, hipStream_t st,
+                              long kstride = -1);
 
 // Router backward, part 1: dZ = S * (dS - <S, dS>) / tau  [N, EP] in the storage type
 // (columns E..EP-1 zero), from S_ij dS_ij = sum over q of dsp[(j K + slot_ij) nparts + q]
@@ -135,23 +155,84 @@ hipError_t launch_tc_topk(const float* S, int N, int E, int k, float* G, int32_t
 hipError_t launch_tc_count(const int32_t* flagT, int N, int E, const GroupTable& tab, int g0,
                            int32_t* cnt, hipStream_t st);
 // Packed row offsets rows [E+1], per-(group, expert) row offsets seg [G,E] and the
-// tile offsets of the two grouped products (tiles13, tiles2 [E+1]).
-hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13, int nt2,
+// tile offsets of the grouped products (tiles13, tiles2, and tilesA of the dA product
+// unless null; [E+1] each).
+hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13, int nt2, int ntA,
                              int32_t* rows, int32_t* seg, int32_t* tiles13, int32_t* tiles2,
-                             hipStream_t st);
-// slotT: choice flags in, packed rows (-1: not kept) out; sel[row] = token; G zeroed
-// on dropped pairs.
+                             int32_t* tilesA, hipStream_t st);
+// slotT: choice flags in, packed rows (-1: not kept) out; sel[row] = token.  Without
+// sel_gate G is zeroed on dropped pairs; with it (training) sel_gate[row] = G of the pair
+// and G keeps the gates of every choice.
 hipError_t launch_tc_place(int32_t* slotT, float* G, int N, int E, const GroupTable& tab, int g0,
-                           const int32_t* seg, int32_t* sel, hipStream_t st);
+                           const int32_t* seg, int32_t* sel, float* sel_gate, hipStream_t st);
 // The forward products over packed rows: expert e owns rows [rows[e], rows[e+1]).
 // sel (may be null): Xe is then X itself and packed row r reads X[sel[r]].
+// gate (may be null): [max_rows] fp32, packed row r is written as A = gate[r] SiLU(H1) H3.
+// H1, H3 (may be null): [max_rows, h], the projections themselves.
 hipError_t launch_gemm_w13_var(int dtype, const void* Xe, const void* W1, const void* W3, void* A,
-                               int E, const int32_t* rows, const int32_t* tiles, long max_rows,
-                               int max_rows_per_expert, int d, int h, hipStream_t st,
-                               const int32_t* sel = nullptr);
+                               void* H1, void* H3, int E, const int32_t* rows,
+                               const int32_t* tiles, long max_rows, int max_rows_per_expert, int d,
+                               int h, hipStream_t st, const int32_t* sel = nullptr,
+                               const float* gate = nullptr);
 hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O, int E,
                               const int32_t* rows, const int32_t* tiles, long max_rows,
                               int max_rows_per_expert, int d, int h, hipStream_t st);
+int tc_col_blocks_dA(int h);
+// The backward products over packed rows (conventions of launch_gemm_dA, _dXe, _dW2 and
+// _dW13): sel[r] is the token of packed row r, whose rows of dY (dA, dW2) and X (dW13) the
+// products read themselves.  dH [max_rows, 2h], dsp [max_rows, dsp_parts(dtype, h)].  An
+// expert without rows gets zero weight gradients.
+hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
+                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows,
+                              const int32_t* tiles, long max_rows, int max_rows_per_expert, int d,
+                              int h, const int32_t* sel, const float* gate, hipStream_t st);
+hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const void* W3,
+                               void* dXe, int E, const int32_t* rows, const int32_t* tiles,
+                               long max_rows, int max_rows_per_expert, int d, int h,
+                               hipStream_t st);
+hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
+                               const int32_t* rows, int max_rows_per_expert, int d, int h,
+                               const int32_t* sel, hipStream_t st);
+hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* dW1, void* dW3,
+                                int E, const int32_t* rows, int max_rows_per_expert, int d, int h,
+                                const int32_t* sel, hipStream_t st);
+
+// ---- the balance loss of token choice ----
+
+// The tokens of the table's groups go in chunks of `chunk`; tab.seg[g] is the first chunk
+// of group g in the launch and tab.seg[n] their number (balance_table fills it).
+struct ChunkTable {
+  int n;
+  int chunk;
+  int off[TOPK_MAX_GROUPS];
+  int len[TOPK_MAX_GROUPS];
+  int seg[TOPK_MAX_GROUPS + 1];
+};
+// Tokens of a chunk, for a problem of N tokens.
+int balance_chunk(int N);
+// Sums of S and the number of choices among each row's k largest (ties: the lower index),
+// per chunk: psum, pcnt [seg[n], E].
+hipError_t launch_balance_partial(const float* S, int E, int k, const ChunkTable& tab,
+                                  double* psum, int32_t* pcnt, hipStream_t st);
+// counts [n, E] and loss [n] of the table's groups from their chunks' sums (counts2: a
+// second copy of the counts unless null).
+hipError_t launch_balance_finish(const double* psum, const int32_t* pcnt, int E, int k,
+                                 const ChunkTable& tab, float* loss, int32_t* counts,
+                                 int32_t* counts2, hipStream_t st);
+// dZ [N, E] fp32 of the table's groups: the loss's gradient in the logits (counts [n, E] and
+// dloss [n] of these groups).
+hipError_t launch_balance_backward(const float* S, const int32_t* counts, const float* dloss,
+                                   int E, int k, float inv_tau, const ChunkTable& tab, float* dZ,
+                                   hipStream_t st);
+// The router's dZ [N, EP] (storage type, columns E.. zero) of token-choice training for the
+// table's groups: the gates' gradient, u - G sum_j u with u_ij the sum of the partials of
+// packed row slotT[j, i] < max_rows (0 where it is -1), plus the balance loss's with
+// dloss (null: none).
+hipError_t launch_tc_router_dz(int dtype, const float* S, const float* G, const int32_t* slotT,
+                               const float* dsp, int nparts, const int32_t* counts,
+                               const float* dloss, void* dZ, int N, int E, int EP, int k,
+                               int max_rows, float inv_tau, const ChunkTable& tab,
+                               hipStream_t st);
 
 // Fill n int32/fp32/bytes with zero (a kernel, not a memset node).
 hipError_t launch_zero(void* p, size_t bytes, hipStream_t st);

@@ -58,7 +58,8 @@ enum { EPI_STORE = 0, EPI_SWIGLU = 1, EPI_SWIGLU_BWD = 2, EPI_STORE_ADD = 3 };
 // Stage tags: every product gets its own kernel symbol, so that traces and
 // counters attribute each launch to its stage.
 enum { G_W13 = 1, G_W2, G_DA, G_DXE, G_DW2, G_DW13, G_ROUTER_DX, G_ROUTER_DWG,
-       G_SH_W13, G_SH_W2, G_SH_DA, G_SH_DXE, G_SH_DW2, G_SH_DW13, G_TC_W13, G_TC_W2 };
+       G_SH_W13, G_SH_W2, G_SH_DA, G_SH_DXE, G_SH_DW2, G_SH_DW13, G_TC_W13, G_TC_W2,
+       G_TC_DA, G_TC_DXE, G_TC_DW2, G_TC_DW13 };
 
 struct GemmParams {
   // A operand, element (m, k) of batch e:
@@ -103,15 +104,16 @@ struct GemmParams {
   const int32_t* ka_rows;
   const int32_t* kb_rows;
   long k_rows_bs;
-  // SwiGLU forward and backward, uniform batches only (may be null): a factor
-  // per output row, g = gate[e*gate_bs + m] for row m of batch e.  The forward
+  // SwiGLU forward and backward (may be null): a factor
+  // per output row, g = gate[e*M + m] for row m of batch e (gate[r0 + m] with
+  // var_rows, r0 the batch's first packed row).  The forward
   // writes A = g SiLU(H1) H3 (H1, H3 unscaled); the backward takes dA = g (the
   // product) before the SwiGLU backward.
   const float* gate;
-  long gate_bs;
   // SwiGLU backward only (may be null): the gate-gradient partials.  For row m
   // of batch e and each column block q of the output (128 columns in the bf16
-  // kernel, 64 in the fp32 one), dsp[(e M + m) dsp_ld + q] = sum over the block
+  // kernel, 64 in the fp32 one), dsp[(e M + m) dsp_ld + q] (dsp[(r0 + m) dsp_ld
+  // + q] with var_rows) = sum over the block
   // of dA * A with dA as above and A = SiLU(H1) H3 recomputed from the saved
   // H1, H3 (so the sum over all blocks is g times the gate's gradient when the
   // product is dY W2).
@@ -120,7 +122,10 @@ struct GemmParams {
   // Variable rows per batch (token choice): batch e owns rows
   // [var_rows[e], var_rows[e+1]) of A, C and H (row strides lda, ldc, ldh) and
   // tiles [var_tiles[e], var_tiles[e+1]) of the launch; both device arrays of
-  // batches + 1 entries, null for a uniform batch of M rows.
+  // batches + 1 entries, null for a uniform batch of M rows.  With OPT_KVAR the
+  // rows are the contraction's instead (K-major operands: the weight gradients):
+  // batch e contracts over rows [var_rows[e], var_rows[e+1]) of both, and its
+  // outputs and tiles are those of a uniform batch.
   const int* var_rows;
   const int* var_tiles;
 };
@@ -129,7 +134,9 @@ struct GemmParams {
 // and the element offsets of the batch in A, C and H.
 struct TileCoord {
   int e, m0, n0, M, row0;
+  int K;                        // rows of the contraction (OPT_KVAR; else GemmParams holds it)
   size_t a_off, c_off, h_off;
+  size_t row;                   // place of the batch's row 0 in gate and dsp
 };
 
 // ------------------------------------------------------------------ bf16 MFMA, pipelined
@@ -210,7 +217,8 @@ __device__ __forceinline__ int km_swz(int k) { return ((k & 3) << 2) | ((k >> 2)
 // the rows of a K-major A / B through p.ka_rows / p.kb_rows.  OPT_TAILS:
 // the last row block and column block take a smaller tile where one holds them.
 // OPT_TILE_BASE: an ungathered K-contiguous A of any size, addressed tile by tile.
-enum { OPT_GA = 1, OPT_GB = 2, OPT_TAILS = 4, OPT_TILE_BASE = 8 };
+// OPT_KVAR: the batches contract over rows of their own (GemmParams.var_rows).
+enum { OPT_GA = 1, OPT_GB = 2, OPT_TAILS = 4, OPT_TILE_BASE = 8, OPT_KVAR = 16 };
 template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bool B_KC, int EPI,
           bool OUT_F32, int OPT>
 __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoord& tc,
@@ -229,6 +237,9 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
   static_assert(EPI != EPI_SWIGLU || (NB % 2 == 0), "SwiGLU needs W1 and W3 blocks per wave");
   static_assert(EPI != EPI_SWIGLU || B_KC, "SwiGLU forward has K-contiguous weights");
   const int e = tc.e, M = tc.M, m0 = tc.m0, n0 = tc.n0;
+  constexpr bool KVAR = (OPT & OPT_KVAR) != 0;
+  static_assert(!KVAR || (!A_KC && !B_KC), "a contraction over token rows");
+  const int K = KVAR ? tc.K : p.K, kv_a = KVAR ? tc.K : p.kv_a, kv_b = KVAR ? tc.K : p.kv_b;
 
   const int tid = threadIdx.x, lane = tid & 63;
   // the wave index is uniform: read into a scalar register so that the LDS
@@ -246,11 +257,12 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
 #pragma unroll
     for (int t = 0; t < GR; ++t) {
       const int m = m0 + wm * WM + 64 * t + lane;
-      gate_r[t] = (p.gate && m < M) ? p.gate[(size_t)e * p.gate_bs + m] : 1.f;
+      gate_r[t] = (p.gate && m < M) ? p.gate[tc.row + m] : 1.f;
     }
   }
   const bf16_t* Ab = reinterpret_cast<const bf16_t*>(p.A) + tc.a_off;
-  const bf16_t* Bb = reinterpret_cast<const bf16_t*>(p.B) + (size_t)e * p.b_bs;
+  const bf16_t* Bb = reinterpret_cast<const bf16_t*>(p.B) +
+                     (KVAR && (OPT & OPT_GB) == 0 ? (size_t)tc.row0 * p.ldb : (size_t)e * p.b_bs);
   const bf16_t* B2b = p.B2 ? reinterpret_cast<const bf16_t*>(p.B2) + (size_t)e * p.b_bs : nullptr;
 
   // ---- DMA sources.  Load q of a thread fills 1 KiB block (wave*L + q) of
@@ -276,19 +288,19 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
   uint32_t a_off[OA::LOADS], b_off[OB::LOADS];
   // source row of row k (< K) of a gathered operand; rows past kv re-read the last
   auto k_row = [&](const int32_t* rows, int k, int kv) -> int {
-    return rows[(size_t)e * p.k_rows_bs + (k < kv ? k : kv - 1)];
+    return rows[(KVAR ? (size_t)tc.row0 : (size_t)e * p.k_rows_bs) + (k < kv ? k : kv - 1)];
   };
   int a_kidx = 0, a_kidx1 = 0, b_kidx = 0, b_kidx1 = 0;
   if constexpr (GA) {
-    if (p.kv_a > 0) {
-      a_kidx = k_row(p.ka_rows, lane, p.kv_a);
-      a_kidx1 = k_row(p.ka_rows, KSTEP + lane, p.kv_a);
+    if (kv_a > 0) {
+      a_kidx = k_row(p.ka_rows, lane, kv_a);
+      a_kidx1 = k_row(p.ka_rows, KSTEP + lane, kv_a);
     }
   }
   if constexpr (GB) {
-    if (p.kv_b > 0) {
-      b_kidx = k_row(p.kb_rows, lane, p.kv_b);
-      b_kidx1 = k_row(p.kb_rows, KSTEP + lane, p.kv_b);
+    if (kv_b > 0) {
+      b_kidx = k_row(p.kb_rows, lane, kv_b);
+      b_kidx1 = k_row(p.kb_rows, KSTEP + lane, kv_b);
     }
   }
   // the source row of k row 2 j + (lane >= 32) of the step (j uniform)
@@ -361,16 +373,16 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
       else if constexpr (GA)
         dma16_buf(a_rsrc, a_off[q] + (uint32_t)pick_row(a_kidx, wave * OA::LOADS + q) * (uint32_t)p.lda * 2u, 0, lds);
       else
-        km_load(a_rsrc, a_off[q], ((wave * OA::LOADS + q) * 64 + lane) / OA::CPR, kt * KSTEP, p.kv_a, p.lda, lds);
+        km_load(a_rsrc, a_off[q], ((wave * OA::LOADS + q) * 64 + lane) / OA::CPR, kt * KSTEP, kv_a, p.lda, lds);
     }
     // K-major B split at k_split (a multiple of the k-step): steps from there on read B2
     // (selected, not branched to: a branch would split the interleaved group)
     const bool second = !B_KC && !GB && kt * KSTEP >= p.k_split;
-    const int bk0 = kt * KSTEP - (second ? p.k_split : 0), bkv = p.kv_b - (second ? p.k_split : 0);
+    const int bk0 = kt * KSTEP - (second ? p.k_split : 0), bkv = kv_b - (second ? p.k_split : 0);
     const Rsrc bk_rsrc = make_rsrc(second ? B2b : Bb);
     if constexpr (GA) {   // every A load of step kt has gone out: rows of step kt + 1
       if (lo < OA::LOADS && hi >= OA::LOADS)
-        a_kidx = FIRST ? a_kidx1 : k_row(p.ka_rows, (kt + 1) * KSTEP + lane, p.kv_a);
+        a_kidx = FIRST ? a_kidx1 : k_row(p.ka_rows, (kt + 1) * KSTEP + lane, kv_a);
     }
 #pragma unroll
     for (int q = 0; q < OB::LOADS; ++q) {
@@ -387,7 +399,7 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
     }
     if constexpr (GB) {
       if (hi >= OA::LOADS + OB::LOADS)
-        b_kidx = FIRST ? b_kidx1 : k_row(p.kb_rows, (kt + 1) * KSTEP + lane, p.kv_b);
+        b_kidx = FIRST ? b_kidx1 : k_row(p.kb_rows, (kt + 1) * KSTEP + lane, kv_b);
     }
   };
   auto issue = [&](int kt, int stage, auto first) {
@@ -466,7 +478,7 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
     else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   };
   static_assert((STAGES - 1) * LOADS <= 63, "vmcnt range");
-  const int KT = (p.K + KSTEP - 1) / KSTEP;
+  const int KT = (K + KSTEP - 1) / KSTEP;
   if (KT > 0) issue(0, 0, std::true_type{});
 #pragma unroll
   for (int s2 = 1; s2 < STAGES; ++s2)
@@ -586,7 +598,7 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
       // refills of the steps below KT - 1 skip the K-major row check when
       // every such step lies below both kv (the usual case: only the last step
       // is ragged), and so does the second part of such a refill in the next step
-      const bool full_ok = p.kv_a >= (KT - 1) * KSTEP && p.kv_b >= (KT - 1) * KSTEP;
+      const bool full_ok = kv_a >= (KT - 1) * KSTEP && kv_b >= (KT - 1) * KSTEP;
       const int n_full = full_ok ? KT - STAGES - 1 : 0;
       if (KT > STAGES) {
         kstep(0, T_{}, F_{}, F_{});
@@ -605,7 +617,7 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
 #pragma unroll
     for (int t = 0; t < GR; ++t) {
       const int m = m0 + wm * WM + 64 * t + lane;
-      gate_r[t] = (p.gate && m < M) ? p.gate[(size_t)e * p.gate_bs + m] : 1.f;
+      gate_r[t] = (p.gate && m < M) ? p.gate[tc.row + m] : 1.f;
     }
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -759,7 +771,7 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
             const int n = n0 + wn * WN + (c % CPR) * 8;
             const float t = row16_sum(n < p.N ? dots[e] : 0.f);
             if ((lane & 15) == 0 && m < M && n < p.N)
-              p.dsp[((size_t)tc.e * p.M + m) * p.dsp_ld + (n >> 7)] = t;
+              p.dsp[(tc.row + m) * p.dsp_ld + (n >> 7)] = t;
           }
         }
         if (mi + 1 < WM / 32) {
@@ -790,7 +802,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
   char smem[dma_smem_bytes<BM, BN, WGM, WGN, KSTEP, STAGES, A_KC, B_KC>()];
   TileCoord tc;
   int rem, MT;
-  if (p.var_rows) {
+  constexpr bool KVAR = (OPT & OPT_KVAR) != 0;
+  if (!KVAR && p.var_rows) {
     // the tile count is known only on the device: the grid is an upper bound,
     // and the XCD-contiguous numbering uses the actual count
     const int total = p.var_tiles[p.batches];
@@ -813,6 +826,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
     tc.a_off = (size_t)row0 * p.lda;
     tc.c_off = (size_t)row0 * p.ldc;
     tc.h_off = (size_t)row0 * p.ldh;
+    tc.row = row0;
   } else {
     const int t = xcd_tile_id(blockIdx.x, gridDim.x);
     if (t >= p.batches * p.MT * p.NT) return;
@@ -820,11 +834,17 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
     tc.e = t / per_b;
     tc.row0 = 0;
     tc.M = p.M;
+    tc.row = (size_t)tc.e * p.M;
     MT = p.MT;
     rem = t - tc.e * per_b;
     tc.a_off = (size_t)tc.e * p.a_bs;
     tc.c_off = (size_t)tc.e * p.c_bs;
     tc.h_off = (size_t)tc.e * p.h_bs;
+    if constexpr (KVAR) {
+      tc.row0 = p.var_rows[tc.e];
+      tc.K = p.var_rows[tc.e + 1] - tc.row0;
+      tc.a_off = (size_t)tc.row0 * p.lda;
+    }
   }
   // Tiles go in groups of GROUP_M row blocks, row block fastest inside a
   // group: the workgroups resident on one XCD then share few A row blocks and
@@ -893,7 +913,8 @@ template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bo
           bool OUT_F32, int TAG, int OPT = 0>
 hipError_t run_dma(GemmParams p, hipStream_t st) {
   if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr) ||
-      ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr))
+      ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) ||
+      ((OPT & OPT_KVAR) != 0) != (p.var_rows != nullptr))
     return hipErrorInvalidValue;
   if (!operands_in_reach<A_KC, B_KC, OPT>(p)) return hipErrorInvalidValue;
   p.MT = (p.M + BM - 1) / BM;
@@ -1036,8 +1057,10 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
   static_assert(BM * 8 % NT == 0 && BN * 8 % NT == 0, "whole chunks per thread");
   static_assert(EPI != EPI_SWIGLU || (B_KC && NB == 2), "a W1 and a W3 block per wave");
   static_assert(EPI != EPI_SWIGLU_BWD || WN == 64, "a wave covers one 64-column partial");
-  constexpr bool GA = (OPT & OPT_GA) != 0;
-  static_assert(!(GA && A_KC) && (OPT & ~OPT_GA) == 0, "a K-major A may be gathered");
+  constexpr bool GA = (OPT & OPT_GA) != 0, GB = (OPT & OPT_GB) != 0, KVAR = (OPT & OPT_KVAR) != 0;
+  static_assert(!(GA && A_KC) && !(GB && B_KC) && !(GA && GB) && (!KVAR || (!A_KC && !B_KC)) &&
+                    (OPT & ~(OPT_GA | OPT_GB | OPT_KVAR)) == 0,
+                "a K-major operand may be gathered");
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE_BYTES];
 
   const int t = xcd_tile_id(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
@@ -1047,10 +1070,18 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
   const int m0 = rem % p.MT * BM;
   const int n0 = rem / p.MT * (EPI == EPI_SWIGLU ? BN / 2 : BN);
   // rows of this batch: uniform (M), or [var_rows[e], var_rows[e+1]) of packed buffers
-  int M = p.M, row0 = 0;
+  int M = p.M, row0 = 0, K = p.K, kv_a = p.kv_a, kv_b = p.kv_b;
   size_t a_off = (size_t)e * p.a_bs, c_off = (size_t)e * p.c_bs, h_off = (size_t)e * p.h_bs;
-  if (p.var_rows) {
+  size_t b_off = (size_t)e * p.b_bs, row = (size_t)e * p.M, k_rows = (size_t)e * p.k_rows_bs;
+  if constexpr (KVAR) {
     row0 = p.var_rows[e];
+    K = kv_a = kv_b = p.var_rows[e + 1] - row0;
+    a_off = (size_t)row0 * p.lda;
+    b_off = (size_t)row0 * p.ldb;
+    k_rows = row0;
+  } else if (p.var_rows) {
+    row0 = p.var_rows[e];
+    row = row0;
     M = p.var_rows[e + 1] - row0;
     a_off = (size_t)row0 * p.lda;
     c_off = (size_t)row0 * p.ldc;
@@ -1058,7 +1089,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
   }
   if (m0 >= M) return;
   const float* A = (const float*)p.A + a_off;
-  const float* B = (const float*)p.B + (size_t)e * p.b_bs;
+  const float* B = (const float*)p.B + b_off;
   const float* B2 = p.B2 ? (const float*)p.B2 + (size_t)e * p.b_bs : nullptr;
   const float* zero = reinterpret_cast<const float*>(g_zero_block);
 
@@ -1072,9 +1103,9 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
   // step ahead); rows past the valid K and columns past the width read zeros.
   const float* a_src[AL];
   const float* b_src[BL];
-  int a_idx[AL];
-  auto km_idx = [&](int k) -> int {
-    return p.ka_rows[(size_t)e * p.k_rows_bs + (k < p.kv_a ? k : p.kv_a - 1)];
+  int a_idx[AL], b_idx[BL];
+  auto km_idx = [&](const int32_t* rows, int k, int kv) -> int {
+    return rows[k_rows + (k < kv ? k : kv - 1)];
   };
 #pragma unroll
   for (int q = 0; q < AL; ++q) {
@@ -1089,7 +1120,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
     } else {
       const int col = m0 + id % (BM / 4) * 4;
       a_src[q] = col < M ? (GA ? (const float*)p.A : A) + col : nullptr;
-      if constexpr (GA) a_idx[q] = p.kv_a > 0 ? km_idx(id / (BM / 4)) : 0;
+      if constexpr (GA) a_idx[q] = kv_a > 0 ? km_idx(p.ka_rows, id / (BM / 4), kv_a) : 0;
     }
   }
 #pragma unroll
@@ -1108,7 +1139,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
       }
     } else {
       const int col = n0 + id % (BN / 4) * 4;
-      b_src[q] = col < p.N ? B + col : nullptr;
+      b_src[q] = col < p.N ? (GB ? (const float*)p.B : B) + col : nullptr;
+      if constexpr (GB) b_idx[q] = kv_b > 0 ? km_idx(p.kb_rows, id / (BN / 4), kv_b) : 0;
     }
   }
   const long b2_off = B2 ? B2 - B : 0;
@@ -1121,8 +1153,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
         g = a_src[q] + kt * FK;
       } else {
         const int k = kt * FK + ((wave * AL + q) * 64 + lane) / (BM / 4);
-        g = (k < p.kv_a && a_src[q]) ? a_src[q] + (size_t)(GA ? a_idx[q] : k) * p.lda : zero;
-        if constexpr (GA) a_idx[q] = km_idx(k + FK);
+        g = (k < kv_a && a_src[q]) ? a_src[q] + (size_t)(GA ? a_idx[q] : k) * p.lda : zero;
+        if constexpr (GA) a_idx[q] = km_idx(p.ka_rows, k + FK, kv_a);
       }
       dma16(g, base + (wave * AL + q) * 1024);
     }
@@ -1134,8 +1166,9 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
       } else {
         const int k = kt * FK + ((wave * BL + q) * 64 + lane) / (BN / 4);
         const float* s = b_src[q] + (k < p.k_split ? 0 : b2_off);
-        const int kr = k < p.k_split ? k : k - p.k_split;
-        g = (k < p.kv_b && b_src[q]) ? s + (size_t)kr * p.ldb : zero;
+        const int kr = GB ? b_idx[q] : k < p.k_split ? k : k - p.k_split;
+        g = (k < kv_b && b_src[q]) ? s + (size_t)kr * p.ldb : zero;
+        if constexpr (GB) b_idx[q] = km_idx(p.kb_rows, k + FK, kv_b);
       }
       dma16(g, base + A_BYTES + (wave * BL + q) * 1024);
     }
@@ -1163,7 +1196,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[mi][ni][r] = 0.f;
 
-  const int KT = (p.K + FK - 1) / FK;
+  const int KT = (K + FK - 1) / FK;
   if (KT > 0) issue(0, 0);
   for (int kt = 0; kt < KT; ++kt) {
     // step kt has landed for every wave, and every wave has read step kt - 1
@@ -1207,7 +1240,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
     const bool row_ok = m < M;
     const float gate =
         ((EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_BWD) && p.gate && row_ok)
-            ? p.gate[(size_t)e * p.gate_bs + m] : 1.f;
+            ? p.gate[row + m] : 1.f;
     float dsum = 0.f;   // SwiGLU backward: the row's gate-gradient partial
 #pragma unroll
     for (int ni = 0; ni < (EPI == EPI_SWIGLU ? 1 : NB); ++ni) {
@@ -1266,7 +1299,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
       const float tsum = dsum + __shfl_xor(dsum, 32, 64);
       const int nb = n0 + wn * WN;
       if (p.dsp && half == 0 && row_ok && nb < p.N)
-        p.dsp[((size_t)e * p.M + m) * p.dsp_ld + (nb >> 6)] = tsum;
+        p.dsp[(row + m) * p.dsp_ld + (nb >> 6)] = tsum;
     }
   }
 }
@@ -1291,7 +1324,10 @@ hipError_t launch_f32_tile(GemmParams p, hipStream_t st) {
 // OPT: as in run_dma.
 template <bool A_KC, bool B_KC, int EPI, int OPT = 0>
 hipError_t run_f32(const GemmParams& p, hipStream_t st) {
-  if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr)) return hipErrorInvalidValue;
+  if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr) ||
+      ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) ||
+      ((OPT & OPT_KVAR) != 0 && p.var_rows == nullptr))
+    return hipErrorInvalidValue;
   const int nw = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
   const long big = (long)p.batches * ((p.M + 127) / 128) * ((nw + 127) / 128);
   if (big >= F32_BIG_TILES) return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, st);
@@ -1348,7 +1384,7 @@ hipError_t launch_gemm_w13(int dtype, const void* Xe, const void* W1, const void
                            void* H1, void* H3, int E, int M, int d, int h, hipStream_t st,
                            bool shared, const int32_t* rows, const float* gate) {
   GemmParams p = base_params();
-  p.gate = gate; p.gate_bs = M;
+  p.gate = gate;
   p.A = Xe; p.a_bs = (long)M * d; p.lda = d;
   if (rows) {   // Xe is X itself, row m of expert e is X[rows[e M + m]]
     p.a_bs = 0; p.a_rows = rows; p.a_rows_bs = M;
@@ -1400,7 +1436,7 @@ hipError_t launch_gemm_dA(int dtype, const void* dO, const void* W2, const void*
   if (rows) {   // dO is dY itself, row m of expert e is dY[rows[e M + m]]
     p.a_bs = 0; p.a_rows = rows; p.a_rows_bs = M;
   }
-  p.gate = gate; p.gate_bs = M;
+  p.gate = gate;
   p.B = W2; p.b_bs = (long)d * h; p.ldb = h;
   p.M = M; p.N = h; p.K = d; p.kv_a = d; p.kv_b = d; p.batches = E;
   const size_t esz = dtype == DT_F32 ? 4 : 2;
@@ -1569,10 +1605,11 @@ int tc_col_blocks_w13(int h) { return (h + 127) / 128; }
 int tc_col_blocks_w2(int d) { return (d + 255) / 256; }
 
 hipError_t launch_gemm_w13_var(int dtype, const void* Xe, const void* W1, const void* W3, void* A,
-                               int E, const int32_t* rows, const int32_t* tiles, long max_rows,
-                               int max_rows_per_expert, int d, int h, hipStream_t st,
-                               const int32_t* sel) {
+                               void* H1, void* H3, int E, const int32_t* rows,
+                               const int32_t* tiles, long max_rows, int max_rows_per_expert, int d,
+                               int h, hipStream_t st, const int32_t* sel, const float* gate) {
   GemmParams p = base_params();
+  p.gate = gate; p.H1 = H1; p.H3 = H3;
   p.A = Xe; p.lda = d;
   if (sel) {   // Xe is X itself, packed row r is X[sel[r]]
     p.a_rows = sel; p.a_rows_bs = 0;
@@ -1598,6 +1635,74 @@ hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O,
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, true, EPI_STORE>(p, st);
   return run_fwd<256, EPI_STORE, G_TC_W2, OPT_TAILS, true>(p, st, max_rows);
+}
+
+int tc_col_blocks_dA(int h) { return (h + 255) / 256; }
+
+hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
+                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows,
+                              const int32_t* tiles, long max_rows, int max_rows_per_expert, int d,
+                              int h, const int32_t* sel, const float* gate, hipStream_t st) {
+  GemmParams p = base_params();
+  p.A = dY; p.lda = d; p.a_rows = sel;
+  p.gate = gate;
+  p.B = W2; p.b_bs = (long)d * h; p.ldb = h;
+  p.M = max_rows_per_expert; p.N = h; p.K = d; p.kv_a = d; p.kv_b = d; p.batches = E;
+  const size_t esz = dtype == DT_F32 ? 4 : 2;
+  p.C = dH; p.C2 = (char*)dH + (size_t)h * esz; p.ldc = 2 * h;
+  p.H1 = (void*)H1; p.H3 = (void*)H3; p.ldh = h;
+  p.dsp = dsp; p.dsp_ld = dsp_parts(dtype, h);
+  p.var_rows = rows; p.var_tiles = tiles;
+  if (max_rows == 0) return hipSuccess;
+  if (dtype == DT_F32) return run_f32<true, false, EPI_SWIGLU_BWD>(p, st);
+  return run_dma_var<256, 256, 4, 2, 64, 2, true, false, EPI_SWIGLU_BWD, false, G_TC_DA, OPT_TAILS>(
+      p, max_rows, st);
+}
+
+hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const void* W3,
+                               void* dXe, int E, const int32_t* rows, const int32_t* tiles,
+                               long max_rows, int max_rows_per_expert, int d, int h,
+                               hipStream_t st) {
+  GemmParams p = base_params();
+  p.A = dH; p.lda = 2 * h;
+  p.B = W1; p.B2 = W3; p.b_bs = (long)h * d; p.ldb = d; p.k_split = h;
+  p.M = max_rows_per_expert; p.N = d; p.K = 2 * h; p.kv_a = 2 * h; p.kv_b = 2 * h; p.batches = E;
+  p.C = dXe; p.ldc = d;
+  p.var_rows = rows; p.var_tiles = tiles;
+  if (max_rows == 0) return hipSuccess;
+  if (dtype == DT_F32) return run_f32<true, false, EPI_STORE>(p, st);
+  return run_dma_var<256, 256, 4, 2, 64, 2, true, false, EPI_STORE, false, G_TC_DXE, OPT_TAILS>(
+      p, max_rows, st);
+}
+
+hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
+                               const int32_t* rows, int max_rows_per_expert, int d, int h,
+                               const int32_t* sel, hipStream_t st) {
+  GemmParams p = base_params();
+  const int K = max_rows_per_expert;
+  p.A = dY; p.lda = d; p.ka_rows = sel;
+  p.B = A; p.ldb = h;
+  p.M = d; p.N = h; p.K = K; p.kv_a = K; p.kv_b = K; p.batches = E;
+  p.C = dW2; p.c_bs = (long)d * h; p.ldc = h;
+  p.var_rows = rows;
+  if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GA | OPT_KVAR>(p, st);
+  return run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW2,
+                 OPT_GA | OPT_TAILS | OPT_KVAR>(p, st);
+}
+
+hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* dW1, void* dW3,
+                                int E, const int32_t* rows, int max_rows_per_expert, int d, int h,
+                                const int32_t* sel, hipStream_t st) {
+  GemmParams p = base_params();
+  const int K = max_rows_per_expert;
+  p.A = dH; p.lda = 2 * h;
+  p.B = X; p.ldb = d; p.kb_rows = sel;
+  p.M = 2 * h; p.N = d; p.K = K; p.kv_a = K; p.kv_b = K; p.batches = E;
+  p.C = dW1; p.C2 = dW3; p.c_split = h; p.c_bs = (long)h * d; p.ldc = d;
+  p.var_rows = rows;
+  if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GB | OPT_KVAR>(p, st);
+  return run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW13,
+                 OPT_GB | OPT_TAILS | OPT_KVAR>(p, st);
 }
 
 }  // namespace ec

@@ -3,6 +3,7 @@
 // y_i = sum_j g_ij FFN_j(x_i) with g_ij = S_ij), and their backward
 // counterparts.  No floating-point atomics: every output row is produced by
 // one wave that sums its expert contributions in ascending expert order.
+#include "dropout.h"
 #include "ec_common.h"
 #include "ec_kernels.h"
 
@@ -79,14 +80,14 @@ __device__ __forceinline__ int token_expert_list(const int32_t* sslot, const flo
 // loads per lane in flight) with no branch between the loads and their FMAs:
 // entries past the token's last expert read the zero row with gate 0, and lanes
 // past the row's end read its last chunk and store nothing.
-// BWD: the backward combine of dXe (its own kernel symbol, so that traces and
-// counters tell the two stages apart).
-template <typename T, int MAXE, bool BWD>
-__global__ __launch_bounds__(256) void combine_kernel(const T* __restrict__ Src,
-                                                      const float* __restrict__ S,
-                                                      const int32_t* __restrict__ slotT,
-                                                      const T* Xr, T* Y, int N, int E, int K,
-                                                      int d, long kstride) {
+// DROP (token-choice training): Y[i] = (R[i] if R) + dropout of that sum, before its
+// rounding to the storage type; a lane's eight columns are one block of draws.
+template <typename T, int MAXE, bool DROP>
+__device__ __forceinline__ void combine_rows(const T* __restrict__ Src,
+                                             const float* __restrict__ S,
+                                             const int32_t* __restrict__ slotT, const T* Xr, T* Y,
+                                             int N, int E, int K, int d, long kstride,
+                                             const T* R, Dropout drop) {
   constexpr int U = sizeof(T) == 2 ? 4 : 2;   // expert rows per step
   __shared__ int32_t sslot[MAXE * CB_TOK];
   __shared__ float sgate[CB_TOK * MAXE];
@@ -149,11 +150,58 @@ __global__ __launch_bounds__(256) void combine_kernel(const T* __restrict__ Src,
 #pragma unroll
       for (int q = 0; q < CB_Q; ++q) {
         const int c = c0 + q * 64 + lane;
+        if constexpr (DROP) {
+          const size_t at = (size_t)i * d + cc[q] * 8;
+          if (drop.thr)
+            dropout_apply(acc[q], dropout_block(at >> 3, drop.rng[0], drop.rng[1]), drop.thr,
+                          drop.scale);
+          if (R) {
+            float r[8];
+            Elem<T>::load8(R + at, r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[q][e] += r[e];
+          }
+        }
         if (c < nch) Elem<T>::store8(Y + (size_t)i * d + c * 8, acc[q]);
       }
     }
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+// BWD: the backward combine of dXe (its own kernel symbol, so that traces and
+// counters tell the two stages apart).
+template <typename T, int MAXE, bool BWD>
+__global__ __launch_bounds__(256) void combine_kernel(const T* __restrict__ Src,
+                                                      const float* __restrict__ S,
+                                                      const int32_t* __restrict__ slotT,
+                                                      const T* Xr, T* Y, int N, int E, int K,
+                                                      int d, long kstride) {
+  combine_rows<T, MAXE, false>(Src, S, slotT, Xr, Y, N, E, K, d, kstride, nullptr, Dropout{});
+}
+
+// The output of token-choice training.
+template <typename T, int MAXE>
+__global__ __launch_bounds__(256) void tc_output_kernel(const T* __restrict__ Src,
+                                                        const int32_t* __restrict__ slotT,
+                                                        const T* Xr, T* Y, int N, int E,
+                                                        int max_rows, int d, const T* R,
+                                                        Dropout drop) {
+  combine_rows<T, MAXE, true>(Src, nullptr, slotT, Xr, Y, N, E, max_rows, d, 0, R, drop);
+}
+
+template <typename T>
+hipError_t run_combine_drop(const T* Src, const int32_t* slotT, const T* Xr, const T* R,
+                            const Dropout& drop, T* Y, int N, int E, int max_rows, int d,
+                            hipStream_t st) {
+  const int grid = (N + CB_TOK - 1) / CB_TOK;
+  if (E <= 64)
+    tc_output_kernel<T, 64><<<grid, 256, 0, st>>>(Src, slotT, Xr, Y, N, E, max_rows, d, R, drop);
+  else if (E <= 128)
+    tc_output_kernel<T, 128><<<grid, 256, 0, st>>>(Src, slotT, Xr, Y, N, E, max_rows, d, R, drop);
+  else
+    tc_output_kernel<T, 256><<<grid, 256, 0, st>>>(Src, slotT, Xr, Y, N, E, max_rows, d, R, drop);
+  return hipGetLastError();
 }
 
 template <typename T, bool BWD>
@@ -361,14 +409,27 @@ hipError_t launch_combine(int dtype, const void* O, const float* S, const int32_
                                     E, K, d, st, kstride);
 }
 
-hipError_t launch_bwd_combine(int dtype, const void* dXe, const int32_t* slotT, const void* Xr,
-                              void* dX, int N, int E, int K, int d, hipStream_t st) {
+hipError_t launch_combine_drop(int dtype, const void* O, const int32_t* slotT, const void* Xr,
+                               const void* R, const Dropout& drop, void* Y, int N, int E,
+                               int max_rows, int d, hipStream_t st) {
   if (N == 0) return hipSuccess;
   if (dtype == DT_F32)
+    return run_combine_drop<float>((const float*)O, slotT, (const float*)Xr, (const float*)R, drop,
+                                   (float*)Y, N, E, max_rows, d, st);
+  return run_combine_drop<bf16_t>((const bf16_t*)O, slotT, (const bf16_t*)Xr, (const bf16_t*)R,
+                                  drop, (bf16_t*)Y, N, E, max_rows, d, st);
+}
+
+hipError_t launch_bwd_combine(int dtype, const void* dXe, const int32_t* slotT, const void* Xr,
+                              void* dX, int N, int E, int K, int d, hipStream_t st,
+                              long kstride) {
+  if (N == 0) return hipSuccess;
+  if (kstride < 0) kstride = K;
+  if (dtype == DT_F32)
     return run_combine<float, true>((const float*)dXe, nullptr, slotT, (const float*)Xr,
-                                    (float*)dX, N, E, K, d, st, K);
+                                    (float*)dX, N, E, K, d, st, kstride);
   return run_combine<bf16_t, true>((const bf16_t*)dXe, nullptr, slotT, (const bf16_t*)Xr,
-                                   (bf16_t*)dX, N, E, K, d, st, K);
+                                   (bf16_t*)dX, N, E, K, d, st, kstride);
 }
 
 namespace {

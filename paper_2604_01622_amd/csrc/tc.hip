@@ -123,13 +123,15 @@ __global__ __launch_bounds__(256) void tc_count_kernel(const int32_t* __restrict
 // Offsets, one workgroup (thread j for expert j, E <= 256): expert j's packed
 // rows start at rows[j] (rows[E] = all kept pairs); group g's tokens in expert
 // j start at seg[g E + j]; the tiles of the two grouped products start at
-// tiles13[j] and tiles2[j] (ceil(M_j / bm) row blocks times nt13 / nt2).
+// tiles13[j] and tiles2[j] (ceil(M_j / bm) row blocks times nt13 / nt2), those of the
+// training backward's dA product at tilesA[j] (unless null).
 __global__ __launch_bounds__(256) void tc_offsets_kernel(const int32_t* __restrict__ cnt, int G,
-                                                         int E, int bm, int nt13, int nt2,
+                                                         int E, int bm, int nt13, int nt2, int ntA,
                                                          int32_t* __restrict__ rows,
                                                          int32_t* __restrict__ seg,
                                                          int32_t* __restrict__ tiles13,
-                                                         int32_t* __restrict__ tiles2) {
+                                                         int32_t* __restrict__ tiles2,
+                                                         int32_t* __restrict__ tilesA) {
   __shared__ int sm[256], st[256];
   const int j = threadIdx.x;
   int m = 0;
@@ -150,12 +152,14 @@ __global__ __launch_bounds__(256) void tc_offsets_kernel(const int32_t* __restri
     rows[E] = r;
     tiles13[E] = tt * nt13;
     tiles2[E] = tt * nt2;
+    if (tilesA) tilesA[E] = tt * ntA;
   }
   __syncthreads();
   if (j < E) {
     rows[j] = sm[j];
     tiles13[j] = st[j] * nt13;
     tiles2[j] = st[j] * nt2;
+    if (tilesA) tilesA[j] = st[j] * ntA;
     int r = sm[j];
     for (int g = 0; g < G; ++g) {
       seg[(size_t)g * E + j] = r;
@@ -168,12 +172,15 @@ __global__ __launch_bounds__(256) void tc_offsets_kernel(const int32_t* __restri
 // tokens that chose expert j, in ascending order; the first cap_g take rows
 // seg + 0, 1, ... of the packed buffer (slotT[j, i] = row, sel[row] = i), the
 // others are dropped (slotT = -1, G[i, j] = 0); tokens that did not choose j get
-// slotT = -1.  slotT holds the choice flags on entry.
+// slotT = -1.  slotT holds the choice flags on entry.  Training (sel_gate): the rows' gates
+// go to sel_gate, and G keeps those of dropped pairs, which the normalisation's gradient
+// needs.
 __global__ __launch_bounds__(256) void tc_place_kernel(int32_t* __restrict__ slotT,
                                                        float* __restrict__ G, int N, int E,
                                                        GroupTable tab, int g0,
                                                        const int32_t* __restrict__ seg,
-                                                       int32_t* __restrict__ sel) {
+                                                       int32_t* __restrict__ sel,
+                                                       float* __restrict__ sel_gate) {
   __shared__ int wsum[4];
   const int g = blockIdx.x / E, j = blockIdx.x % E;
   const int off = tab.off[g], len = tab.len[g], cap = tab.k[g];
@@ -199,9 +206,10 @@ __global__ __launch_bounds__(256) void tc_place_kernel(int32_t* __restrict__ slo
         const int row = base_row + pos;
         f[i] = row;
         sel[row] = off + i;
+        if (sel_gate) sel_gate[row] = G[(size_t)(off + i) * E + j];
       } else {
         f[i] = -1;
-        if (flag) G[(size_t)(off + i) * E + j] = 0.f;
+        if (flag && !sel_gate) G[(size_t)(off + i) * E + j] = 0.f;
       }
     }
     base += total;
@@ -228,17 +236,18 @@ hipError_t launch_tc_count(const int32_t* flagT, int N, int E, const GroupTable&
   return hipGetLastError();
 }
 
-hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13, int nt2,
+hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13, int nt2, int ntA,
                              int32_t* rows, int32_t* seg, int32_t* tiles13, int32_t* tiles2,
-                             hipStream_t st) {
-  tc_offsets_kernel<<<1, 256, 0, st>>>(cnt, G, E, bm, nt13, nt2, rows, seg, tiles13, tiles2);
+                             int32_t* tilesA, hipStream_t st) {
+  tc_offsets_kernel<<<1, 256, 0, st>>>(cnt, G, E, bm, nt13, nt2, ntA, rows, seg, tiles13, tiles2,
+                                       tilesA);
   return hipGetLastError();
 }
 
 hipError_t launch_tc_place(int32_t* slotT, float* G, int N, int E, const GroupTable& tab, int g0,
-                           const int32_t* seg, int32_t* sel, hipStream_t st) {
+                           const int32_t* seg, int32_t* sel, float* sel_gate, hipStream_t st) {
   if (tab.n == 0) return hipSuccess;
-  tc_place_kernel<<<tab.n * E, 256, 0, st>>>(slotT, G, N, E, tab, g0, seg, sel);
+  tc_place_kernel<<<tab.n * E, 256, 0, st>>>(slotT, G, N, E, tab, g0, seg, sel, sel_gate);
   return hipGetLastError();
 }
 
