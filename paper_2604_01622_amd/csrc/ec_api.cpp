@@ -287,9 +287,9 @@ struct TcRouteWs {
   int32_t* tiles2;
 };
 
-TcRouteWs carve_tc_route(Carve& c, const Plan& P) {
+TcRouteWs carve_tc_route(Carve& c, const Plan& P, bool with_ST = true) {
   TcRouteWs w;
-  w.ST = (float*)c.take((size_t)P.E * P.N * 4);
+  w.ST = with_ST ? (float*)c.take((size_t)P.E * P.N * 4) : nullptr;
   w.cnt = (int32_t*)c.take((size_t)P.G * P.E * 4);
   w.seg = (int32_t*)c.take((size_t)P.G * P.E * 4);
   w.tiles13 = (int32_t*)c.take((size_t)(P.E + 1) * 4);
@@ -322,14 +322,15 @@ TcFwdWs carve_tc_fwd(Carve& c, const Plan& P, long rmax) {
 }
 
 // Router, row top-k, per-(group, expert) counts, offsets and placement.  sel_gate and
-// tilesA (training only): the packed rows' gates and the tiles of the dA product.
+// tilesA (training only, which needs no transposed scores): the packed rows' gates times
+// gate_scale and the tiles of the dA product.
 int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* X, const void* Wg,
                      float* S, float* G, int32_t* slot, int32_t* rows, int32_t* sel,
                      const TcRouteWs& w, hipStream_t st, float* sel_gate = nullptr,
-                     int32_t* tilesA = nullptr) {
+                     float gate_scale = 1.f, int32_t* tilesA = nullptr) {
   EC_HIP(mark(0, st));
-  EC_HIP(ec::launch_router_softmax(P.dtype, X, Wg, S, w.ST, P.N, P.d, P.E, p->inv_temperature,
-                                   st));
+  EC_HIP(ec::launch_router_softmax(P.dtype, X, Wg, S, sel_gate ? nullptr : w.ST, P.N, P.d, P.E,
+                                   p->inv_temperature, st));
   EC_HIP(mark(1, st));
   EC_HIP(ec::launch_tc_topk(S, P.N, P.E, top_k, G, slot, st));
   ec::GroupTable tab;
@@ -344,7 +345,8 @@ int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* 
         ++tab.n;
       }
       if (pass == 0) EC_HIP(ec::launch_tc_count(slot, P.N, P.E, tab, g0, w.cnt, st));
-      else EC_HIP(ec::launch_tc_place(slot, G, P.N, P.E, tab, g0, w.seg, sel, sel_gate, st));
+      else EC_HIP(ec::launch_tc_place(slot, G, P.N, P.E, tab, g0, w.seg, sel, sel_gate, gate_scale,
+                                      st));
     }
     if (pass == 0)
       EC_HIP(ec::launch_tc_offsets(w.cnt, P.G, P.E, ec::TC_BM, ec::tc_col_blocks_w13(P.h),
@@ -424,6 +426,15 @@ int dropout_of(const ec_dropout_desc* d, ec::Dropout* out) {
   return EC_OK;
 }
 
+// Takes the scale out of a dropout: the layer folds it into the gates, in fp32, so that
+// masking rounds nothing (dY times the scale would be rounded to the storage type).  Where
+// everything is dropped there is nothing to scale.
+float take_scale(ec::Dropout* d) {
+  const float s = d->thr < 65536 ? d->scale : 1.f;
+  d->scale = 1.f;
+  return s;
+}
+
 bool overlap(const void* a, const void* b, size_t bytes) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return x < y ? y - x < bytes : x - y < bytes;
@@ -478,7 +489,7 @@ struct TcTrainFwdWs {
 
 TcTrainFwdWs carve_tc_train_fwd(Carve& c, const ec_problem* p, const Plan& P, long rmax) {
   TcTrainFwdWs w;
-  w.route = carve_tc_route(c, P);
+  w.route = carve_tc_route(c, P, false);
   w.balance = carve_balance(c, p, P);
   w.O = c.take((size_t)rmax * P.d * P.esz);
   return w;
@@ -1085,6 +1096,7 @@ int ec_tc_train_forward(const ec_problem* p, int32_t top_k, const ec_dropout_des
   Carve cs(saved), c(ws);
   const TcSaved s = carve_tc_saved(cs, P, rmax);
   const TcTrainFwdWs w = carve_tc_train_fwd(c, p, P, rmax);
+  const float scale = take_scale(&d);
   if (P.N == 0) {   // no tokens: nothing kept, zero losses and loads
     EC_HIP(ec::launch_zero(s.rows, (size_t)(P.E + 1) * 4, stream));
     EC_HIP(ec::launch_zero(s.tiles2, (size_t)(P.E + 1) * 4, stream));
@@ -1094,10 +1106,11 @@ int ec_tc_train_forward(const ec_problem* p, int32_t top_k, const ec_dropout_des
   TcRouteWs rw = w.route;
   rw.tiles2 = s.tiles2;
   EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, s.S, s.G, s.slot, s.rows, s.sel, rw, stream, s.gate,
-                          s.tilesA));
+                          scale, s.tilesA));
   EC_TRY(enqueue_balance(p, P, top_k, s.S, loss, counts, s.counts, w.balance, stream));
   EC_HIP(mark(3, stream));
-  // A carries the gate (A = g SiLU(H1) H3), as in expert choice: the output adds rows
+  // A carries the gate (A = g SiLU(H1) H3), as in expert choice, and the scale of what the
+  // dropout keeps: the output adds rows and masks their sum
   EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, s.A, s.H1, s.H3, P.E, s.rows, rw.tiles13,
                                  rmax, rmax_e, P.d, P.h, stream, s.sel, s.gate));
   EC_HIP(mark(4, stream));
@@ -1106,7 +1119,7 @@ int ec_tc_train_forward(const ec_problem* p, int32_t top_k, const ec_dropout_des
   EC_HIP(mark(5, stream));
   if (P.hs) {
     EC_HIP(ec::launch_gemm_w13(P.dtype, X, Ws1, Ws3, s.As, s.Hs1, s.Hs3, 1, P.N, P.d, P.hs,
-                               stream, true));
+                               stream, true, nullptr, nullptr, scale));
     EC_HIP(mark(6, stream));
     EC_HIP(ec::launch_gemm_w2(P.dtype, s.As, Ws2, Y, 1, P.N, P.d, P.hs, stream, true));
   } else {
@@ -1165,7 +1178,9 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
   const BwdWs& b = w.b;
   const int E = P.E, d = P.d, h = P.h, N = P.N, hs = P.hs;
   EC_HIP(mark(0, stream));
-  // the gradient before the dropout: the mask again, from the same counters
+  // the gradient before the dropout: the mask again, from the same counters; its scale sits
+  // in the gates and in the saved A
+  const float scale = take_scale(&dr);
   const void* dYm = dY;
   if (dr.thr && N > 0) {
     EC_HIP(ec::launch_dropout(P.dtype, dY, nullptr, dr, w.dYm, (long)N * d, stream));
@@ -1193,7 +1208,8 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
   EC_HIP(ec::launch_router_dx(P.dtype, b.dZ, Wg, dX, N, E, P.EP, d, stream));
   EC_HIP(mark(7, stream));
   if (hs && N > 0) {
-    EC_HIP(ec::launch_gemm_dA(P.dtype, dYm, Ws2, s.Hs1, s.Hs3, b.dHs, 1, N, d, hs, stream, true));
+    EC_HIP(ec::launch_gemm_dA(P.dtype, dYm, Ws2, s.Hs1, s.Hs3, b.dHs, 1, N, d, hs, stream, true,
+                              nullptr, nullptr, nullptr, scale));
     EC_HIP(mark(8, stream));
     EC_HIP(ec::launch_shared_dW2(P.dtype, dYm, s.As, dWs2, N, d, hs, b.spart, b.s_splits2, stream));
     EC_HIP(mark(9, stream));

@@ -116,6 +116,19 @@ __device__ __forceinline__ float row16_sum(float t) {
   return dpp_add(dpp_add(dpp_add(dpp_add(t, 0), 1), 2), 3);
 }
 
+// The same total with the same bits in every lane: mirrors of half rows and rows pair each
+// lane with one that adds the same two sums, where the rotations of row16_sum add the quads
+// in another order in each of them.
+template <int CTRL>
+__device__ __forceinline__ float dpp_plus(float t) {
+  return t + __builtin_bit_cast(
+                 float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, t), CTRL, 0xF, 0xF,
+                                                    false));
+}
+__device__ __forceinline__ float row16_sum_even(float t) {
+  return dpp_plus<0x140>(dpp_plus<0x141>(dpp_plus<0x4E>(dpp_plus<0xB1>(t))));
+}
+
 // DPP move of a 32-bit value within rows of 16 lanes; lanes whose source is
 // outside the row read 0 (bound_ctrl).  Controls used here: quad_perm
 // [1,0,3,2] = 0xB1 and [2,3,0,1] = 0x4E, row_shl:n = 0x100 + n, row_ror:n = 0x120 + n.

@@ -22,7 +22,8 @@ struct GroupTable {
   int seg[TOPK_MAX_GROUPS];         // first row of the group's segment in an expert buffer
 };
 
-// S [N,E] and ST [E,N] fp32 from X [N,d] and Wg [E,d].
+// S [N,E] and ST [E,N] fp32 from X [N,d] and Wg [E,d].  ST null (token-choice training): no
+// transposed copy, and experts of equal logits get equal scores to the bit.
 hipError_t launch_router_softmax(int dtype, const void* X, const void* Wg, float* S, float* ST,
                                  int N, int d, int E, float inv_tau, hipStream_t st);
 
@@ -88,16 +89,17 @@ hipError_t launch_router_dwg(int dtype, const void* dZ, const void* X, float* dW
 // rows (routed experts, may be null): Xe is then X itself and row m of
 // expert e reads X[rows[e M + m]] (the gather happens in the operand load).
 // gate (may be null): [E, M] fp32, row m of expert e is written as
-// A = gate[e M + m] SiLU(H1) H3 (H1, H3 themselves unscaled).
+// A = gate[e M + m] SiLU(H1) H3 (H1, H3 themselves unscaled); scale: every row's factor
+// without gate.
 hipError_t launch_gemm_w13(int dtype, const void* Xe, const void* W1, const void* W3, void* A,
                            void* H1, void* H3, int E, int M, int d, int h, hipStream_t st,
                            bool shared = false, const int32_t* rows = nullptr,
-                           const float* gate = nullptr);
+                           const float* gate = nullptr, float scale = 1.f);
 // O = A W2^T.
 hipError_t launch_gemm_w2(int dtype, const void* A, const void* W2, void* O, int E, int M, int d,
                           int h, hipStream_t st, bool shared = false);
 // dA = g dO W2 and the SwiGLU backward: dH[:, 0:h] = dH1, dH[:, h:2h] = dH3
-// ([E,M,2h]), g = gate[e M + m] per row (1 when gate is null); W2 is read
+// ([E,M,2h]), g = gate[e M + m] per row (scale when gate is null); W2 is read
 // K-major.  dsp (may be null):
 // [E M, dsp_parts(dtype, h)] fp32, per row and column block the sum of dA * A
 // (A = SiLU(H1) H3), whose row sum is the gate's gradient times the gate when
@@ -106,7 +108,7 @@ hipError_t launch_gemm_w2(int dtype, const void* A, const void* W2, void* O, int
 hipError_t launch_gemm_dA(int dtype, const void* dO, const void* W2, const void* H1,
                           const void* H3, void* dH, int E, int M, int d, int h, hipStream_t st,
                           bool shared = false, float* dsp = nullptr, const int32_t* rows = nullptr,
-                          const float* gate = nullptr);
+                          const float* gate = nullptr, float scale = 1.f);
 // gate-gradient partials per row of the dA product (blocks of 128 columns of
 // d_ff in bf16, 64 in fp32)
 int dsp_parts(int dtype, int h);
@@ -161,10 +163,11 @@ hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13,
                              int32_t* rows, int32_t* seg, int32_t* tiles13, int32_t* tiles2,
                              int32_t* tilesA, hipStream_t st);
 // slotT: choice flags in, packed rows (-1: not kept) out; sel[row] = token.  Without
-// sel_gate G is zeroed on dropped pairs; with it (training) sel_gate[row] = G of the pair
-// and G keeps the gates of every choice.
+// sel_gate G is zeroed on dropped pairs; with it (training) sel_gate[row] = scale G of the
+// pair and G keeps the gates of every choice.
 hipError_t launch_tc_place(int32_t* slotT, float* G, int N, int E, const GroupTable& tab, int g0,
-                           const int32_t* seg, int32_t* sel, float* sel_gate, hipStream_t st);
+                           const int32_t* seg, int32_t* sel, float* sel_gate, float scale,
+                           hipStream_t st);
 // The forward products over packed rows: expert e owns rows [rows[e], rows[e+1]).
 // sel (may be null): Xe is then X itself and packed row r reads X[sel[r]].
 // gate (may be null): [max_rows] fp32, packed row r is written as A = gate[r] SiLU(H1) H3.

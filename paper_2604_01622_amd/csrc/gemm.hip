@@ -108,8 +108,9 @@ struct GemmParams {
   // per output row, g = gate[e*M + m] for row m of batch e (gate[r0 + m] with
   // var_rows, r0 the batch's first packed row).  The forward
   // writes A = g SiLU(H1) H3 (H1, H3 unscaled); the backward takes dA = g (the
-  // product) before the SwiGLU backward.
+  // product) before the SwiGLU backward.  Without gate g = scale for every row.
   const float* gate;
+  float scale;
   // SwiGLU backward only (may be null): the gate-gradient partials.  For row m
   // of batch e and each column block q of the output (128 columns in the bf16
   // kernel, 64 in the fp32 one), dsp[(e M + m) dsp_ld + q] (dsp[(r0 + m) dsp_ld
@@ -257,7 +258,7 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
 #pragma unroll
     for (int t = 0; t < GR; ++t) {
       const int m = m0 + wm * WM + 64 * t + lane;
-      gate_r[t] = (p.gate && m < M) ? p.gate[tc.row + m] : 1.f;
+      gate_r[t] = (p.gate && m < M) ? p.gate[tc.row + m] : p.scale;
     }
   }
   const bf16_t* Ab = reinterpret_cast<const bf16_t*>(p.A) + tc.a_off;
@@ -617,7 +618,7 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
 #pragma unroll
     for (int t = 0; t < GR; ++t) {
       const int m = m0 + wm * WM + 64 * t + lane;
-      gate_r[t] = (p.gate && m < M) ? p.gate[tc.row + m] : 1.f;
+      gate_r[t] = (p.gate && m < M) ? p.gate[tc.row + m] : p.scale;
     }
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -1240,7 +1241,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
     const bool row_ok = m < M;
     const float gate =
         ((EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_BWD) && p.gate && row_ok)
-            ? p.gate[row + m] : 1.f;
+            ? p.gate[row + m] : p.scale;
     float dsum = 0.f;   // SwiGLU backward: the row's gate-gradient partial
 #pragma unroll
     for (int ni = 0; ni < (EPI == EPI_SWIGLU ? 1 : NB); ++ni) {
@@ -1338,6 +1339,7 @@ GemmParams base_params() {
   GemmParams p = {};
   p.k_split = 1 << 30;
   p.c_split = 1 << 30;
+  p.scale = 1.f;
   return p;
 }
 
@@ -1382,9 +1384,9 @@ int dsp_parts(int dtype, int h) { return dtype == DT_F32 ? (h + 63) / 64 : (h + 
 
 hipError_t launch_gemm_w13(int dtype, const void* Xe, const void* W1, const void* W3, void* A,
                            void* H1, void* H3, int E, int M, int d, int h, hipStream_t st,
-                           bool shared, const int32_t* rows, const float* gate) {
+                           bool shared, const int32_t* rows, const float* gate, float scale) {
   GemmParams p = base_params();
-  p.gate = gate;
+  p.gate = gate; p.scale = scale;
   p.A = Xe; p.a_bs = (long)M * d; p.lda = d;
   if (rows) {   // Xe is X itself, row m of expert e is X[rows[e M + m]]
     p.a_bs = 0; p.a_rows = rows; p.a_rows_bs = M;
@@ -1429,14 +1431,15 @@ hipError_t launch_gemm_w2(int dtype, const void* A, const void* W2, void* O, int
 
 hipError_t launch_gemm_dA(int dtype, const void* dO, const void* W2, const void* H1,
                           const void* H3, void* dH, int E, int M, int d, int h, hipStream_t st,
-                          bool shared, float* dsp, const int32_t* rows, const float* gate) {
+                          bool shared, float* dsp, const int32_t* rows, const float* gate,
+                          float scale) {
   // dA[m, n] = g_m sum_k dO[m, k] W2[k, n]  (k over d, n over h); epilogue -> dH1, dH3
   GemmParams p = base_params();
   p.A = dO; p.a_bs = (long)M * d; p.lda = d;
   if (rows) {   // dO is dY itself, row m of expert e is dY[rows[e M + m]]
     p.a_bs = 0; p.a_rows = rows; p.a_rows_bs = M;
   }
-  p.gate = gate;
+  p.gate = gate; p.scale = scale;
   p.B = W2; p.b_bs = (long)d * h; p.ldb = h;
   p.M = M; p.N = h; p.K = d; p.kv_a = d; p.kv_b = d; p.batches = E;
   const size_t esz = dtype == DT_F32 ? 4 : 2;

@@ -179,7 +179,9 @@ __global__ __launch_bounds__(64 * TG * RouterCfg<ET>::KS) void router_softmax_bf
         v[t] = (t * 16 + col < E) ? expf(v[t] - m) : 0.f;
         s += v[t];
       }
-      s = row16_sum(s);
+      // without ST a token's scores are compared with each other (token choice): one sum for
+      // all its lanes, so that equal logits have equal scores
+      s = ST ? row16_sum(s) : row16_sum_even(s);
 #pragma unroll
       for (int t = 0; t < ET; ++t) {
         const int e = t * 16 + col;
@@ -191,6 +193,7 @@ __global__ __launch_bounds__(64 * TG * RouterCfg<ET>::KS) void router_softmax_bf
       }
     }
   }
+  if (!ST) return;
   __syncthreads();
   // transposed, coalesced write of ST[e][row0 .. row0+64)
   for (int c = tid; c < E * RT_ROWS; c += NT) {
@@ -317,6 +320,7 @@ __global__ __launch_bounds__(256) void router_softmax_f32_kernel(
       z[e] = p;
     }
   }
+  if (!ST) return;
   __syncthreads();
   for (int c = tid; c < nout; c += 256) {         // ST: TR consecutive tokens of an expert
     const int e = c / TR, r = c % TR;

@@ -173,14 +173,15 @@ __global__ __launch_bounds__(256) void tc_offsets_kernel(const int32_t* __restri
 // seg + 0, 1, ... of the packed buffer (slotT[j, i] = row, sel[row] = i), the
 // others are dropped (slotT = -1, G[i, j] = 0); tokens that did not choose j get
 // slotT = -1.  slotT holds the choice flags on entry.  Training (sel_gate): the rows' gates
-// go to sel_gate, and G keeps those of dropped pairs, which the normalisation's gradient
-// needs.
+// times `scale` go to sel_gate, and G keeps those of dropped pairs, which the
+// normalisation's gradient needs.
 __global__ __launch_bounds__(256) void tc_place_kernel(int32_t* __restrict__ slotT,
                                                        float* __restrict__ G, int N, int E,
                                                        GroupTable tab, int g0,
                                                        const int32_t* __restrict__ seg,
                                                        int32_t* __restrict__ sel,
-                                                       float* __restrict__ sel_gate) {
+                                                       float* __restrict__ sel_gate,
+                                                       float scale) {
   __shared__ int wsum[4];
   const int g = blockIdx.x / E, j = blockIdx.x % E;
   const int off = tab.off[g], len = tab.len[g], cap = tab.k[g];
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(256) void tc_place_kernel(int32_t* __restrict__ slo
         const int row = base_row + pos;
         f[i] = row;
         sel[row] = off + i;
-        if (sel_gate) sel_gate[row] = G[(size_t)(off + i) * E + j];
+        if (sel_gate) sel_gate[row] = scale * G[(size_t)(off + i) * E + j];
       } else {
         f[i] = -1;
         if (flag && !sel_gate) G[(size_t)(off + i) * E + j] = 0.f;
@@ -245,9 +246,10 @@ hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13,
 }
 
 hipError_t launch_tc_place(int32_t* slotT, float* G, int N, int E, const GroupTable& tab, int g0,
-                           const int32_t* seg, int32_t* sel, float* sel_gate, hipStream_t st) {
+                           const int32_t* seg, int32_t* sel, float* sel_gate, float scale,
+                           hipStream_t st) {
   if (tab.n == 0) return hipSuccess;
-  tc_place_kernel<<<tab.n * E, 256, 0, st>>>(slotT, G, N, E, tab, g0, seg, sel, sel_gate);
+  tc_place_kernel<<<tab.n * E, 256, 0, st>>>(slotT, G, N, E, tab, g0, seg, sel, sel_gate, scale);
   return hipGetLastError();
 }
 
