@@ -360,7 +360,7 @@ int ec_tc_train_backward(const ec_problem *p, int32_t top_k, const ec_dropout_de
  *   dW1/dW3 (7-10 empty without shared experts), 11 combine of dXe, 12 dWg.
  * Stages of ec_route: 0 router+softmax, 1 top-k.
  * ec_tc_train_forward and ec_tc_train_backward have the stages of ec_moe_forward and
- * ec_moe_backward, with the balance loss in the forward's stage 2 and the dropout of
+ * ec_moe_backward, with the balance loss in the forward's stage 1 and the dropout of
  * dY in the backward's stage 0.  ec_tc_balance, ec_tc_balance_backward and ec_dropout
  * record none.                                                                */
 int ec_set_stage_events(hipEvent_t *events /* HOST array */, int n_events);

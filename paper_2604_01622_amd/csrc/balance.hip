@@ -7,10 +7,12 @@
 // the counts being constants of the gradient: with b_j = dloss_g E c_j / (k L^2),
 //   dZ_ij = S_ij (b_j - sum_m S_im b_m) / tau.
 //
-// Every kernel takes the tokens in chunks that do not cross groups, sixteen lanes a token:
-// lane r holds experts 4 r + 64 q + {0, 1, 2, 3}.  Chunks' sums are added in a fixed order,
-// no atomics.  Sums of S, the dot product and the difference are in 64 bits (under an even
-// load the difference is far below its terms).
+// Every kernel takes the tokens in chunks that do not cross groups, sixteen lanes (a DPP row)
+// a token: lane r holds experts 4 r + 64 q + {0, 1, 2, 3}, one 16-byte load a quarter row.
+// Chunks' sums are added in a fixed order, no atomics.  Sums of S, the dot product and the
+// difference are in 64 bits (under an even load the difference is far below its terms).
+#include <type_traits>
+
 #include "ec_common.h"
 #include "ec_kernels.h"
 
@@ -39,26 +41,130 @@ template <int Q>
 __device__ __forceinline__ void load_row(const float* row, int E, int r, float fill,
                                          float v[Q][4]) {
 #pragma unroll
-  for (int q = 0; q < Q; ++q)
+  for (int q = 0; q < Q; ++q) {
+    const int j0 = 64 * q + 4 * r;
+    if (E % 4 == 0) {   // rows start at a multiple of 16 bytes
+      const float4 x = *reinterpret_cast<const float4*>(row + (j0 < E ? j0 : 0));
+      const bool in = j0 < E;
+      v[q][0] = in ? x.x : fill;
+      v[q][1] = in ? x.y : fill;
+      v[q][2] = in ? x.z : fill;
+      v[q][3] = in ? x.w : fill;
+    } else {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int j = 64 * q + 4 * r + c;
-      v[q][c] = j < E ? row[j] : fill;
+      for (int c = 0; c < 4; ++c) {
+        const float x = row[j0 + c < E ? j0 + c : 0];
+        v[q][c] = j0 + c < E ? x : fill;
+      }
     }
+  }
 }
 
-// Sums of S and choices per expert over one chunk of tokens.
 template <int Q>
-__global__ __launch_bounds__(256) void balance_partial_kernel(const float* __restrict__ S, int E,
-                                                              int k, ChunkTable tab,
-                                                              double* __restrict__ psum,
-                                                              int32_t* __restrict__ pcnt) {
-  __shared__ double ssum[16][64 * Q];
-  __shared__ int scnt[16][64 * Q];
-  const int g = chunk_group(tab, blockIdx.x);
-  const int t0 = (blockIdx.x - tab.seg[g]) * tab.chunk;
+__device__ __forceinline__ void store_row(float* row, int E, int r, const float v[Q][4]) {
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const int j0 = 64 * q + 4 * r;
+    if (E % 4 == 0) {
+      if (j0 < E)
+        *reinterpret_cast<float4*>(row + j0) = make_float4(v[q][0], v[q][1], v[q][2], v[q][3]);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (j0 + c < E) row[j0 + c] = v[q][c];
+    }
+  }
+}
+
+// Takes the k largest entries out of the four rows that a wave holds (ties: the lower
+// expert; NaN, also in the entries past E, is never taken): a taken entry becomes NaN, and
+// the taken values' sum is returned.  A round is a maximum over the row, a compare and a
+// select per entry; only where some row holds its maximum more than once (the four rows'
+// equal entries are then not four) or nothing but NaN is the lowest expert looked for.
+// Every lane takes part.
+template <int Q>
+__device__ __forceinline__ float take_largest(float w[Q][4], int r, int k) {
+  const float nan = __builtin_nanf("");
+  float sum = 0.f;
+  for (int n = 0; n < k; ++n) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) m = fmaxf(m, w[q][c]);
+    m = row16_max(m);
+    int equal = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) equal += __popcll(__ballot(w[q][c] == m));
+    int first = 1 << 30;
+    if (equal != 4 || __any(m == -INFINITY)) {   // uniform
+#pragma unroll
+      for (int q = Q - 1; q >= 0; --q)
+#pragma unroll
+        for (int c = 3; c >= 0; --c) first = w[q][c] == m ? 64 * q + 4 * r + c : first;
+      first = row16_min_i32(first);
+      if (first < (1 << 30)) sum += m;
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[q][c] = 64 * q + 4 * r + c == first ? nan : w[q][c];
+    } else {
+      sum += m;
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[q][c] = w[q][c] == m ? nan : w[q][c];
+    }
+  }
+  return sum;
+}
+
+// Threads of a workgroup that sums: 1024, 512 where a row takes four quarters (more than 192
+// experts), whose sums need more registers than a lane of 16 waves has.
+template <int Q> constexpr int BL_THREADS = Q == 4 ? 512 : 1024;
+
+// The group's loss and counts from its sums: thread j < E holds expert j's.
+__device__ __forceinline__ void finish_group(double sum, int count, int E, int k, int len, int cap,
+                                             size_t g, double* red, float* loss, int32_t* counts,
+                                             int32_t* counts2, int32_t* kept) {
+  const int j = threadIdx.x;
+  double x = 0.0;
+  if (j < E) {
+    counts[g * E + j] = count;
+    if (counts2) counts2[g * E + j] = count;
+    if (kept) kept[g * E + j] = count < cap ? count : cap;
+    x = sum * (double)count;
+  }
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
+  if ((j & 63) == 0 && j < 256) red[j >> 6] = x;   // E <= 256
+  __syncthreads();
+  if (j == 0) {
+    const double L = len, all = red[0] + red[1] + red[2] + red[3];
+    loss[g] = len > 0 ? (float)(all * E / (L * L * k)) : 0.f;
+  }
+}
+
+// Sums of S and choices per expert over one chunk of tokens.  WHOLE: every group is one
+// chunk, whose workgroup also finishes it.  TRAIN (chunks of TC_CHOOSE_CHUNK): also writes the
+// gates of each token's choices (G [N, E], 0 elsewhere) and the choice flags flagT [E, N],
+// transposed through LDS.
+template <int Q, bool WHOLE, bool TRAIN>
+__global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
+    const float* __restrict__ S, int E, int k, ChunkTable tab, double* __restrict__ psum,
+    int32_t* __restrict__ pcnt, float* __restrict__ loss, int32_t* __restrict__ counts,
+    float* __restrict__ G, int32_t* __restrict__ flagT, int N) {
+  constexpr int WAVES = BL_THREADS<Q> / 64;
+  __shared__ double ssum[WAVES][64 * Q];
+  __shared__ int scnt[WAVES][64 * Q];
+  __shared__ double red[4];
+  __shared__ uint8_t sflag[TRAIN ? TC_CHOOSE_CHUNK : 1][64 * Q + 4];
+  const int g = WHOLE ? blockIdx.x : chunk_group(tab, blockIdx.x);
+  const int t0 = WHOLE ? 0 : (blockIdx.x - tab.seg[g]) * tab.chunk;
   const int t1 = t0 + tab.chunk < tab.len[g] ? t0 + tab.chunk : tab.len[g];
-  const int r = threadIdx.x & 15, grp = threadIdx.x >> 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15;
   double sum[Q][4];
   int cnt[Q][4];
 #pragma unroll
@@ -68,106 +174,121 @@ __global__ __launch_bounds__(256) void balance_partial_kernel(const float* __res
       sum[q][c] = 0.0;
       cnt[q][c] = 0;
     }
-  for (int t = t0 + grp; t < t1; t += 16) {   // uniform over the sixteen lanes
-    float v[Q][4];
-    load_row<Q>(S + (size_t)(tab.off[g] + t) * E, E, r, -INFINITY, v);
+  for (int tw = t0 + wave * 4; tw < t1; tw += 4 * WAVES) {   // a wave's four tokens
+    const int t = tw + (lane >> 4), i = tab.off[g] + (t < t1 ? t : t1 - 1);
+    float v[Q][4], w[Q][4];
+    load_row<Q>(S + (size_t)i * E, E, r, __builtin_nanf(""), v);
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (64 * q + 4 * r + c < E) sum[q][c] += (double)v[q][c];
-    uint32_t taken = 0;   // bit 4 q + c
-    for (int n = 0; n < k; ++n) {
-      float bv = -INFINITY;
-      int bj = 1 << 30;
+      for (int c = 0; c < 4; ++c) w[q][c] = v[q][c];
+    const float chosen = take_largest<Q>(w, r, k);
+    const float inv = 1.0f / chosen;
 #pragma unroll
-      for (int q = 0; q < Q; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int j = 64 * q + 4 * r + c;
-          if (j < E && !((taken >> (4 * q + c)) & 1u) &&
-              (v[q][c] > bv || (v[q][c] == bv && j < bj))) {
-            bv = v[q][c];
-            bj = j;
-          }
+      for (int c = 0; c < 4; ++c) {
+        const bool taken = w[q][c] != w[q][c] && v[q][c] == v[q][c];
+        if (t < t1) {
+          sum[q][c] += (double)v[q][c];
+          cnt[q][c] += taken;
         }
-#pragma unroll
-      for (int m = 8; m >= 1; m >>= 1) {
-        const float ov = __shfl_xor(bv, m, 16);
-        const int oj = __shfl_xor(bj, m, 16);
-        if (ov > bv || (ov == bv && oj < bj)) {
-          bv = ov;
-          bj = oj;
+        if constexpr (TRAIN) {
+          sflag[t - t0][64 * q + 4 * r + c] = taken;   // t - t0 < TC_CHOOSE_CHUNK
+          v[q][c] = taken ? v[q][c] * inv : 0.f;
         }
       }
-      // none left but NaN, which nothing chooses: bj >= E
-      if (bj < E && ((bj >> 2) & 15) == r) taken |= 1u << ((bj >> 6) * 4 + (bj & 3));
+    if constexpr (TRAIN) {
+      if (t < t1) store_row<Q>(G + (size_t)i * E, E, r, v);
     }
-#pragma unroll
-    for (int q = 0; q < Q; ++q)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) cnt[q][c] += (taken >> (4 * q + c)) & 1u;
   }
+  // the four rows of a wave, then the waves in order
 #pragma unroll
   for (int q = 0; q < Q; ++q)
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      ssum[grp][64 * q + 4 * r + c] = sum[q][c];
-      scnt[grp][64 * q + 4 * r + c] = cnt[q][c];
+      double s = sum[q][c];
+      int n = cnt[q][c];
+      s += __shfl_xor(s, 16, 64);
+      n += __shfl_xor(n, 16, 64);
+      s += __shfl_xor(s, 32, 64);
+      n += __shfl_xor(n, 32, 64);
+      if (lane < 16) {
+        ssum[wave][64 * q + 4 * r + c] = s;
+        scnt[wave][64 * q + 4 * r + c] = n;
+      }
     }
   __syncthreads();
-  for (int j = threadIdx.x; j < E; j += 256) {
-    double s = 0.0;
-    int n = 0;
-    for (int w = 0; w < 16; ++w) {
+  const int j = threadIdx.x;
+  double s = 0.0;
+  int n = 0;
+  if (j < E) {
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
       s += ssum[w][j];
       n += scnt[w][j];
     }
+  }
+  if constexpr (WHOLE) {
+    finish_group(s, n, E, k, tab.len[g], 0, g, red, loss, counts, nullptr, nullptr);
+  } else if (j < E) {
     psum[(size_t)blockIdx.x * E + j] = s;
     pcnt[(size_t)blockIdx.x * E + j] = n;
   }
+  if constexpr (TRAIN) {
+    const int i0 = tab.off[g] + t0, nt = t1 - t0;
+    for (int c = threadIdx.x; c < E * TC_CHOOSE_CHUNK; c += BL_THREADS<Q>) {
+      const int e = c / TC_CHOOSE_CHUNK, t = c % TC_CHOOSE_CHUNK;
+      if (t < nt) flagT[(size_t)e * N + i0 + t] = sflag[t][e];
+    }
+  }
 }
 
-// Counts and loss of a group from its chunks' sums, a workgroup a group.
-__global__ __launch_bounds__(256) void balance_finish_kernel(const double* __restrict__ psum,
-                                                             const int32_t* __restrict__ pcnt,
-                                                             int E, int k, ChunkTable tab,
-                                                             float* __restrict__ loss,
-                                                             int32_t* __restrict__ counts,
-                                                             int32_t* __restrict__ counts2) {
-  __shared__ double part[4];
-  const int g = blockIdx.x, j = threadIdx.x;
-  double x = 0.0;
-  if (j < E) {
-    double s = 0.0;
-    int n = 0;
-    for (int c = tab.seg[g]; c < tab.seg[g + 1]; ++c) {
+// Counts and loss of a group from its chunks' sums, a workgroup a group: threads share the
+// chunks out, 1024 / (64 Q) at a time, eight loads of each in flight.
+template <int Q>
+__global__ __launch_bounds__(1024) void balance_finish_kernel(
+    const double* __restrict__ psum, const int32_t* __restrict__ pcnt, int E, int k,
+    ChunkTable tab, float* __restrict__ loss, int32_t* __restrict__ counts,
+    int32_t* __restrict__ counts2, int32_t* __restrict__ kept) {
+  constexpr int SLICES = 1024 / (64 * Q);
+  __shared__ double ssum[SLICES][64 * Q];
+  __shared__ int scnt[SLICES][64 * Q];
+  __shared__ double red[4];
+  const int g = blockIdx.x, j = threadIdx.x % (64 * Q), sl = threadIdx.x / (64 * Q);
+  double s = 0.0;
+  int n = 0;
+  if (sl < SLICES && j < E) {
+#pragma unroll 8
+    for (int c = tab.seg[g] + sl; c < tab.seg[g + 1]; c += SLICES) {
       s += psum[(size_t)c * E + j];
       n += pcnt[(size_t)c * E + j];
     }
-    counts[(size_t)g * E + j] = n;
-    if (counts2) counts2[(size_t)g * E + j] = n;
-    x = s * (double)n;
   }
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
-  if ((j & 63) == 0) part[j >> 6] = x;
+  if (sl < SLICES) {
+    ssum[sl][j] = s;
+    scnt[sl][j] = n;
+  }
   __syncthreads();
-  if (j == 0) {
-    const double L = tab.len[g];
-    const double all = part[0] + part[1] + part[2] + part[3];
-    loss[g] = tab.len[g] > 0 ? (float)(all * E / (L * L * k)) : 0.f;
+  if (threadIdx.x < 64 * Q) {
+    s = 0.0;
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < SLICES; ++w) {
+      s += ssum[w][threadIdx.x];
+      n += scnt[w][threadIdx.x];
+    }
   }
+  finish_group(s, n, E, k, tab.len[g], tab.cap[g], g, red, loss, counts, counts2, kept);
 }
 
 // dZ of the loss alone, fp32 [N, E].
 template <int Q>
-__global__ __launch_bounds__(256) void balance_backward_kernel(const float* __restrict__ S,
+__global__ __launch_bounds__(256) void balance_backward_kernel(const float* S,
                                                                const int32_t* __restrict__ counts,
                                                                const float* __restrict__ dloss,
                                                                int E, int k, float inv_tau,
-                                                               ChunkTable tab,
-                                                               float* __restrict__ dZ) {
+                                                               ChunkTable tab, float* dZ) {
   const int g = chunk_group(tab, blockIdx.x);
   const int t0 = (blockIdx.x - tab.seg[g]) * tab.chunk;
   const int t1 = t0 + tab.chunk < tab.len[g] ? t0 + tab.chunk : tab.len[g];
@@ -195,10 +316,8 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int j = 64 * q + 4 * r + c;
-        if (j < E) dZ[at + j] = (float)((double)v[q][c] * (b[q][c] - dot));
-      }
+      for (int c = 0; c < 4; ++c) v[q][c] = (float)((double)v[q][c] * (b[q][c] - dot));
+    store_row<Q>(dZ + at, E, r, v);
   }
 }
 
@@ -207,8 +326,11 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* __re
 // partials of a packed row sum to; 0 for a dropped pair)
 //   dZ_ij = (u_ij - g_ij sum_m u_im) / tau,
 // nothing elsewhere and nothing at all for one choice, whose gate is 1; plus the balance
-// loss's term with dloss.
-template <int Q, typename T>
+// loss's term with dloss.  Latency bounds it: a token's loads depend on each other (gate,
+// slot, partials), so a quarter row's four slots and then all their partials are requested
+// together, whether chosen or not (row 0 stands in for what is not).  NP: partials of a row
+// read as 16-byte vectors (4, 8, 16; 0: any count, one by one).
+template <int Q, int NP, typename T>
 __global__ __launch_bounds__(256) void tc_dz_kernel(const float* __restrict__ S,
                                                     const float* __restrict__ G,
                                                     const int32_t* __restrict__ slotT,
@@ -222,82 +344,159 @@ __global__ __launch_bounds__(256) void tc_dz_kernel(const float* __restrict__ S,
   const int t0 = (blockIdx.x - tab.seg[g]) * tab.chunk;
   const int t1 = t0 + tab.chunk < tab.len[g] ? t0 + tab.chunk : tab.len[g];
   const int r = threadIdx.x & 15, grp = threadIdx.x >> 4;
-  const double L = tab.len[g];
-  const double coef = dloss ? (double)dloss[g] * E / (L * L * k) : 0.0;
-  double b[Q][4];
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int j = 64 * q + 4 * r + c;
-      b[q][c] = dloss && j < E ? coef * counts[(size_t)g * E + j] : 0.0;
-    }
+  const bool gates = k > 1 && max_rows > 0;
   for (int t = t0 + grp; t < t1; t += 16) {
     const int i = tab.off[g] + t;
     float v[Q][4], gt[Q][4], u[Q][4];
     load_row<Q>(G + (size_t)i * E, E, r, 0.f, gt);
-    float all = 0.f;
-    double dot = 0.0;
     if (dloss) load_row<Q>(S + (size_t)i * E, E, r, 0.f, v);
+    float all = 0.f;
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
+    for (int q = 0; q < Q; ++q) {
+      int row[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const int j = 64 * q + 4 * r + c;
-        u[q][c] = 0.f;
-        if (k > 1 && gt[q][c] != 0.f) {
-          const int row = slotT[(size_t)j * N + i];
-          if (row >= 0 && row < max_rows)
-            for (int n = 0; n < nparts; ++n) u[q][c] += dsp[(size_t)row * nparts + n];
+        const int at = slotT[(size_t)(gates && j < E ? j : 0) * N + i];
+        row[c] = gates && gt[q][c] != 0.f && at < max_rows ? at : -1;
+      }
+      if constexpr (NP > 0) {
+        float4 x[4][NP / 4];
+        if (gates) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int w = 0; w < NP / 4; ++w)
+              x[c][w] = *reinterpret_cast<const float4*>(
+                  dsp + (size_t)(row[c] >= 0 ? row[c] : 0) * NP + 4 * w);
         }
-        all += u[q][c];
-        if (dloss) dot += (double)v[q][c] * b[q][c];
-      }
-    all = row16_sum(all);
-    if (dloss) dot = row16_sum_f64(dot);
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
+        for (int c = 0; c < 4; ++c) {
+          u[q][c] = 0.f;
+          if (row[c] >= 0) {
+#pragma unroll
+            for (int w = 0; w < NP / 4; ++w) {
+              u[q][c] += x[c][w].x; u[q][c] += x[c][w].y;
+              u[q][c] += x[c][w].z; u[q][c] += x[c][w].w;
+            }
+          }
+          all += u[q][c];
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          u[q][c] = 0.f;
+          if (row[c] >= 0)
+            for (int n = 0; n < nparts; ++n) u[q][c] += dsp[(size_t)row[c] * nparts + n];
+          all += u[q][c];
+        }
+      }
+    }
+    all = row16_sum(all);
+    double b[Q][4], dot = 0.0;
+    if (dloss) {
+      const double L = tab.len[g], coef = (double)dloss[g] * E / (L * L * k);
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int j = 64 * q + 4 * r + c;
+          b[q][c] = j < E ? coef * counts[(size_t)g * E + j] : 0.0;
+          dot += (double)v[q][c] * b[q][c];
+        }
+      dot = row16_sum_f64(dot);
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      float z[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const int j = 64 * q + 4 * r + c;
-        float z = k > 1 ? u[q][c] - gt[q][c] * all : 0.f;
-        if (dloss) z = (float)((double)z + (double)v[q][c] * (b[q][c] - dot));
-        if (j < EP) Elem<T>::store1(dZ + (size_t)i * EP + j, z * inv_tau);
+        z[c] = gates ? u[q][c] - gt[q][c] * all : 0.f;
+        if (dloss) z[c] = (float)((double)z[c] + (double)v[q][c] * (b[q][c] - dot));
+        z[c] *= inv_tau;
       }
+      T* out = dZ + (size_t)i * EP + 64 * q + 4 * r;   // EP = 64 Q
+      if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<float4*>(out) = make_float4(z[0], z[1], z[2], z[3]);
+      else
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
+    }
   }
+}
+
+// The quarters of 64 experts that a row takes, as a constant: f(integral_constant).
+template <typename F>
+void by_width(int E, F f) {
+  if (E <= 64) f(std::integral_constant<int, 1>{});
+  else if (E <= 128) f(std::integral_constant<int, 2>{});
+  else if (E <= 192) f(std::integral_constant<int, 3>{});
+  else f(std::integral_constant<int, 4>{});
+}
+
+template <int Q, int NP>
+void run_tc_dz(int dtype, const float* S, const float* G, const int32_t* slotT, const float* dsp,
+               int nparts, const int32_t* counts, const float* dloss, void* dZ, int N, int E,
+               int EP, int k, int max_rows, float inv_tau, const ChunkTable& tab, hipStream_t st) {
+  const int grid = tab.seg[tab.n];
+  if (dtype == DT_F32)
+    tc_dz_kernel<Q, NP, float><<<grid, 256, 0, st>>>(S, G, slotT, dsp, nparts, counts, dloss,
+                                                     (float*)dZ, N, E, EP, k, max_rows, inv_tau,
+                                                     tab);
+  else
+    tc_dz_kernel<Q, NP, bf16_t><<<grid, 256, 0, st>>>(S, G, slotT, dsp, nparts, counts, dloss,
+                                                      (bf16_t*)dZ, N, E, EP, k, max_rows, inv_tau,
+                                                      tab);
 }
 
 }  // namespace
 
-// 1024 chunks of a large batch; 64 tokens at least.
+// Sums: 64 tokens a chunk, or so many that a batch has at most 256 chunks and its groups.
 int balance_chunk(int N) {
-  const int c = (N + 1023) / 1024;
-  return c <= 64 ? 64 : (c + 63) / 64 * 64;
+  return (N + 256 * 64 - 1) / (256 * 64) * 64;
 }
 
-#define EC_BY_WIDTH(E, CALL)         \
-  do {                               \
-    if ((E) <= 64) CALL(1);          \
-    else if ((E) <= 128) CALL(2);    \
-    else if ((E) <= 192) CALL(3);    \
-    else CALL(4);                    \
-  } while (0)
+// Gradients: 16 tokens (one each) while the workgroups are at most 4096, else 64.
+int balance_backward_chunk(int N) { return N <= 65536 ? 16 : 64; }
 
-hipError_t launch_balance_partial(const float* S, int E, int k, const ChunkTable& tab,
-                                  double* psum, int32_t* pcnt, hipStream_t st) {
+hipError_t launch_balance_partial(const float* S, int E, int k, const ChunkTable& tab, bool whole,
+                                  double* psum, int32_t* pcnt, float* loss, int32_t* counts,
+                                  hipStream_t st) {
+  const int grid = whole ? tab.n : tab.seg[tab.n];
+  if (grid == 0) return hipSuccess;
+  by_width(E, [&](auto w) {
+    constexpr int Q = decltype(w)::value;
+    if (whole)
+      balance_partial_kernel<Q, true, false><<<grid, BL_THREADS<Q>, 0, st>>>(
+          S, E, k, tab, psum, pcnt, loss, counts, nullptr, nullptr, 0);
+    else
+      balance_partial_kernel<Q, false, false><<<grid, BL_THREADS<Q>, 0, st>>>(
+          S, E, k, tab, psum, pcnt, loss, counts, nullptr, nullptr, 0);
+  });
+  return hipGetLastError();
+}
+
+hipError_t launch_tc_choose(const float* S, int N, int E, int k, const ChunkTable& tab,
+                            double* psum, int32_t* pcnt, float* G, int32_t* flagT,
+                            hipStream_t st) {
   const int grid = tab.seg[tab.n];
   if (grid == 0) return hipSuccess;
-#define EC_CALL(Q) balance_partial_kernel<Q><<<grid, 256, 0, st>>>(S, E, k, tab, psum, pcnt)
-  EC_BY_WIDTH(E, EC_CALL);
-#undef EC_CALL
+  if (tab.chunk != TC_CHOOSE_CHUNK) return hipErrorInvalidValue;
+  by_width(E, [&](auto w) {
+    constexpr int Q = decltype(w)::value;
+    balance_partial_kernel<Q, false, true><<<grid, BL_THREADS<Q>, 0, st>>>(
+        S, E, k, tab, psum, pcnt, nullptr, nullptr, G, flagT, N);
+  });
   return hipGetLastError();
 }
 
 hipError_t launch_balance_finish(const double* psum, const int32_t* pcnt, int E, int k,
                                  const ChunkTable& tab, float* loss, int32_t* counts,
-                                 int32_t* counts2, hipStream_t st) {
+                                 int32_t* counts2, int32_t* kept, hipStream_t st) {
   if (tab.n == 0) return hipSuccess;
-  balance_finish_kernel<<<tab.n, 256, 0, st>>>(psum, pcnt, E, k, tab, loss, counts, counts2);
+  by_width(E, [&](auto w) {
+    balance_finish_kernel<decltype(w)::value><<<tab.n, 1024, 0, st>>>(
+        psum, pcnt, E, k, tab, loss, counts, counts2, kept);
+  });
   return hipGetLastError();
 }
 
@@ -306,10 +505,10 @@ hipError_t launch_balance_backward(const float* S, const int32_t* counts, const 
                                    hipStream_t st) {
   const int grid = tab.seg[tab.n];
   if (grid == 0) return hipSuccess;
-#define EC_CALL(Q) \
-  balance_backward_kernel<Q><<<grid, 256, 0, st>>>(S, counts, dloss, E, k, inv_tau, tab, dZ)
-  EC_BY_WIDTH(E, EC_CALL);
-#undef EC_CALL
+  by_width(E, [&](auto w) {
+    balance_backward_kernel<decltype(w)::value><<<grid, 256, 0, st>>>(S, counts, dloss, E, k,
+                                                                      inv_tau, tab, dZ);
+  });
   return hipGetLastError();
 }
 
@@ -318,21 +517,20 @@ hipError_t launch_tc_router_dz(int dtype, const float* S, const float* G, const 
                                const float* dloss, void* dZ, int N, int E, int EP, int k,
                                int max_rows, float inv_tau, const ChunkTable& tab,
                                hipStream_t st) {
-  const int grid = tab.seg[tab.n];
-  if (grid == 0) return hipSuccess;
-#define EC_CALL(Q)                                                                              \
-  do {                                                                                          \
-    if (dtype == DT_F32)                                                                        \
-      tc_dz_kernel<Q, float><<<grid, 256, 0, st>>>(S, G, slotT, dsp, nparts, counts, dloss,     \
-                                                   (float*)dZ, N, E, EP, k, max_rows, inv_tau,  \
-                                                   tab);                                        \
-    else                                                                                        \
-      tc_dz_kernel<Q, bf16_t><<<grid, 256, 0, st>>>(S, G, slotT, dsp, nparts, counts, dloss,    \
-                                                    (bf16_t*)dZ, N, E, EP, k, max_rows,         \
-                                                    inv_tau, tab);                              \
-  } while (0)
-  EC_BY_WIDTH(E, EC_CALL);
-#undef EC_CALL
+  if (tab.seg[tab.n] == 0) return hipSuccess;
+  by_width(E, [&](auto w) {
+    constexpr int Q = decltype(w)::value;
+    auto run = [&](auto np) {
+      run_tc_dz<Q, decltype(np)::value>(dtype, S, G, slotT, dsp, nparts, counts, dloss, dZ, N, E,
+                                        EP, k, max_rows, inv_tau, tab, st);
+    };
+    switch (nparts) {
+      case 4: run(std::integral_constant<int, 4>{}); break;
+      case 8: run(std::integral_constant<int, 8>{}); break;
+      case 16: run(std::integral_constant<int, 16>{}); break;
+      default: run(std::integral_constant<int, 0>{});
+    }
+  });
   return hipGetLastError();
 }
 

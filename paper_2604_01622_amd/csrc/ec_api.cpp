@@ -259,6 +259,73 @@ int enqueue_route(const ec_problem* p, const Plan& P, const void* X, const void*
   return EC_OK;
 }
 
+// ---- the balance loss of token choice ------------------------------------------
+
+// The chunk tables of the problem's groups, in passes of TOPK_MAX_GROUPS: body(table, first
+// group, chunks before it) for each.
+template <typename F>
+int for_chunk_tables(const ec_problem* p, const Plan& P, int chunk, F body) {
+  ec::ChunkTable tab;
+  tab.chunk = chunk;
+  long before = 0;
+  for (int g0 = 0; g0 < P.G; g0 += ec::TOPK_MAX_GROUPS) {
+    tab.n = 0;
+    tab.seg[0] = 0;
+    for (int g = g0; g < P.G && g < g0 + ec::TOPK_MAX_GROUPS; ++g) {
+      tab.off[tab.n] = p->group_offsets[g];
+      tab.len[tab.n] = p->group_offsets[g + 1] - p->group_offsets[g];
+      tab.cap[tab.n] = p->capacity[g];
+      tab.seg[tab.n + 1] = tab.seg[tab.n] + (tab.len[tab.n] + tab.chunk - 1) / tab.chunk;
+      ++tab.n;
+    }
+    EC_TRY(body(tab, g0, before));
+    before += tab.seg[tab.n];
+  }
+  return EC_OK;
+}
+
+struct BalanceWs {
+  double* psum;    // [chunks, E]
+  int32_t* pcnt;
+};
+
+BalanceWs carve_balance(Carve& c, const ec_problem* p, const Plan& P, int chunk) {
+  size_t chunks = 0;
+  for (int g = 0; g < P.G; ++g)
+    chunks += (p->group_offsets[g + 1] - p->group_offsets[g] + chunk - 1) / chunk;
+  BalanceWs w;
+  w.psum = (double*)c.take(chunks * P.E * 8);
+  w.pcnt = (int32_t*)c.take(chunks * P.E * 4);
+  return w;
+}
+
+// Every group is one chunk (BALANCE_WHOLE tokens at most).
+bool balance_whole(const ec_problem* p, const Plan& P) {
+  for (int g = 0; g < P.G; ++g)
+    if (p->group_offsets[g + 1] - p->group_offsets[g] > ec::BALANCE_WHOLE) return false;
+  return true;
+}
+
+int balance_chunk_of(const ec_problem* p, const Plan& P) {
+  return balance_whole(p, P) ? ec::BALANCE_WHOLE : ec::balance_chunk(P.N);
+}
+
+int enqueue_balance(const ec_problem* p, const Plan& P, int top_k, const float* S, float* loss,
+                    int32_t* counts, int chunk, const BalanceWs& w, hipStream_t st) {
+  const bool whole = balance_whole(p, P);
+  return for_chunk_tables(p, P, chunk, [&](const ec::ChunkTable& tab, int g0, long before) -> int {
+    double* psum = w.psum + before * P.E;
+    int32_t* pcnt = w.pcnt + before * P.E;
+    const size_t at = (size_t)g0 * P.E;
+    EC_HIP(ec::launch_balance_partial(S, P.E, top_k, tab, whole, psum, pcnt, loss + g0,
+                                      counts + at, st));
+    if (!whole)
+      EC_HIP(ec::launch_balance_finish(psum, pcnt, P.E, top_k, tab, loss + g0, counts + at,
+                                       nullptr, nullptr, st));
+    return EC_OK;
+  });
+}
+
 // ---- token choice -------------------------------------------------------------
 
 // train: the backward's [rows, 2h] buffer counts too.
@@ -321,18 +388,42 @@ TcFwdWs carve_tc_fwd(Carve& c, const Plan& P, long rmax) {
   return w;
 }
 
-// Router, row top-k, per-(group, expert) counts, offsets and placement.  sel_gate and
-// tilesA (training only, which needs no transposed scores): the packed rows' gates times
-// gate_scale and the tiles of the dA product.
+// What training's routing adds: the loads and the balance loss from the pass that chooses, the
+// packed rows' gates times gate_scale, and the tiles of the dA product.
+struct TcTrainRoute {
+  BalanceWs sums;
+  float* loss;
+  int32_t* counts;
+  int32_t* saved_counts;
+  float* sel_gate;
+  float gate_scale;
+  int32_t* tilesA;
+};
+
+// Router, row top-k, per-(group, expert) counts, offsets and placement; with `train` (null in
+// inference) no transposed scores.
 int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* X, const void* Wg,
                      float* S, float* G, int32_t* slot, int32_t* rows, int32_t* sel,
-                     const TcRouteWs& w, hipStream_t st, float* sel_gate = nullptr,
-                     float gate_scale = 1.f, int32_t* tilesA = nullptr) {
+                     const TcRouteWs& w, hipStream_t st, const TcTrainRoute* train = nullptr) {
   EC_HIP(mark(0, st));
-  EC_HIP(ec::launch_router_softmax(P.dtype, X, Wg, S, sel_gate ? nullptr : w.ST, P.N, P.d, P.E,
+  EC_HIP(ec::launch_router_softmax(P.dtype, X, Wg, S, train ? nullptr : w.ST, P.N, P.d, P.E,
                                    p->inv_temperature, st));
   EC_HIP(mark(1, st));
-  EC_HIP(ec::launch_tc_topk(S, P.N, P.E, top_k, G, slot, st));
+  if (train) {
+    EC_TRY(for_chunk_tables(
+        p, P, ec::TC_CHOOSE_CHUNK, [&](const ec::ChunkTable& tab, int g0, long before) -> int {
+          double* psum = train->sums.psum + before * P.E;
+          int32_t* pcnt = train->sums.pcnt + before * P.E;
+          const size_t at = (size_t)g0 * P.E;
+          EC_HIP(ec::launch_tc_choose(S, P.N, P.E, top_k, tab, psum, pcnt, G, slot, st));
+          EC_HIP(ec::launch_balance_finish(psum, pcnt, P.E, top_k, tab, train->loss + g0,
+                                           train->counts + at, train->saved_counts + at,
+                                           w.cnt + at, st));
+          return EC_OK;
+        }));
+  } else {
+    EC_HIP(ec::launch_tc_topk(S, P.N, P.E, top_k, G, slot, st));
+  }
   ec::GroupTable tab;
   for (int pass = 0; pass < 2; ++pass) {
     for (int g0 = 0; g0 < P.G; g0 += ec::TOPK_MAX_GROUPS) {
@@ -344,70 +435,20 @@ int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* 
         tab.seg[tab.n] = 0;
         ++tab.n;
       }
-      if (pass == 0) EC_HIP(ec::launch_tc_count(slot, P.N, P.E, tab, g0, w.cnt, st));
-      else EC_HIP(ec::launch_tc_place(slot, G, P.N, P.E, tab, g0, w.seg, sel, sel_gate, gate_scale,
-                                      st));
+      if (pass == 0 && !train) EC_HIP(ec::launch_tc_count(slot, P.N, P.E, tab, g0, w.cnt, st));
+      if (pass == 1)
+        EC_HIP(ec::launch_tc_place(slot, G, P.N, P.E, tab, g0, w.seg, sel,
+                                   train ? train->sel_gate : nullptr,
+                                   train ? train->gate_scale : 1.f, st));
     }
     if (pass == 0)
       EC_HIP(ec::launch_tc_offsets(w.cnt, P.G, P.E, ec::TC_BM, ec::tc_col_blocks_w13(P.h),
                                    ec::tc_col_blocks_w2(P.d), ec::tc_col_blocks_dA(P.h), rows,
-                                   w.seg, w.tiles13, w.tiles2, tilesA, st));
+                                   w.seg, w.tiles13, w.tiles2, train ? train->tilesA : nullptr,
+                                   st));
   }
   EC_HIP(mark(2, st));
   return EC_OK;
-}
-
-// ---- the balance loss of token choice ------------------------------------------
-
-// The chunk tables of the problem's groups, in passes of TOPK_MAX_GROUPS: body(table, first
-// group, chunks before it) for each.
-template <typename F>
-int for_chunk_tables(const ec_problem* p, const Plan& P, F body) {
-  ec::ChunkTable tab;
-  tab.chunk = ec::balance_chunk(P.N);
-  long before = 0;
-  for (int g0 = 0; g0 < P.G; g0 += ec::TOPK_MAX_GROUPS) {
-    tab.n = 0;
-    tab.seg[0] = 0;
-    for (int g = g0; g < P.G && g < g0 + ec::TOPK_MAX_GROUPS; ++g) {
-      tab.off[tab.n] = p->group_offsets[g];
-      tab.len[tab.n] = p->group_offsets[g + 1] - p->group_offsets[g];
-      tab.seg[tab.n + 1] = tab.seg[tab.n] + (tab.len[tab.n] + tab.chunk - 1) / tab.chunk;
-      ++tab.n;
-    }
-    EC_TRY(body(tab, g0, before));
-    before += tab.seg[tab.n];
-  }
-  return EC_OK;
-}
-
-struct BalanceWs {
-  double* psum;    // [chunks, E]
-  int32_t* pcnt;
-};
-
-BalanceWs carve_balance(Carve& c, const ec_problem* p, const Plan& P) {
-  const int chunk = ec::balance_chunk(P.N);
-  size_t chunks = 0;
-  for (int g = 0; g < P.G; ++g)
-    chunks += (p->group_offsets[g + 1] - p->group_offsets[g] + chunk - 1) / chunk;
-  BalanceWs w;
-  w.psum = (double*)c.take(chunks * P.E * 8);
-  w.pcnt = (int32_t*)c.take(chunks * P.E * 4);
-  return w;
-}
-
-int enqueue_balance(const ec_problem* p, const Plan& P, int top_k, const float* S, float* loss,
-                    int32_t* counts, int32_t* counts2, const BalanceWs& w, hipStream_t st) {
-  return for_chunk_tables(p, P, [&](const ec::ChunkTable& tab, int g0, long before) -> int {
-    double* psum = w.psum + before * P.E;
-    int32_t* pcnt = w.pcnt + before * P.E;
-    const size_t at = (size_t)g0 * P.E;
-    EC_HIP(ec::launch_balance_partial(S, P.E, top_k, tab, psum, pcnt, st));
-    EC_HIP(ec::launch_balance_finish(psum, pcnt, P.E, top_k, tab, loss + g0, counts + at,
-                                     counts2 ? counts2 + at : nullptr, st));
-    return EC_OK;
-  });
 }
 
 // ---- dropout -------------------------------------------------------------------
@@ -490,7 +531,7 @@ struct TcTrainFwdWs {
 TcTrainFwdWs carve_tc_train_fwd(Carve& c, const ec_problem* p, const Plan& P, long rmax) {
   TcTrainFwdWs w;
   w.route = carve_tc_route(c, P, false);
-  w.balance = carve_balance(c, p, P);
+  w.balance = carve_balance(c, p, P, ec::TC_CHOOSE_CHUNK);
   w.O = c.take((size_t)rmax * P.d * P.esz);
   return w;
 }
@@ -909,7 +950,7 @@ size_t ec_tc_workspace_size(const ec_problem* p, int32_t top_k, int mode) {
   int rmax_e;
   if (tc_validate(p, top_k, &P, &rmax, &rmax_e, mode == 3 || mode == 4) != EC_OK) return 0;
   Carve c(nullptr);
-  if (mode == 2) { carve_balance(c, p, P); return align_up(c.used + 1); }
+  if (mode == 2) { carve_balance(c, p, P, balance_chunk_of(p, P)); return align_up(c.used + 1); }
   if (mode == 3) { carve_tc_train_fwd(c, p, P, rmax); return c.used; }
   if (mode == 4) { carve_tc_train_bwd(c, P, rmax); return align_up(c.used + 1); }
   carve_tc_route(c, P);
@@ -1019,7 +1060,8 @@ int ec_tc_balance(const ec_problem* p, int32_t top_k, const float* S, float* los
   if (ws_bytes < need)
     return fail(EC_ERR_WORKSPACE, "workspace %zu bytes < %zu required", ws_bytes, need);
   Carve c(ws);
-  return enqueue_balance(p, P, top_k, S, loss, counts, nullptr, carve_balance(c, p, P), stream);
+  const int chunk = balance_chunk_of(p, P);
+  return enqueue_balance(p, P, top_k, S, loss, counts, chunk, carve_balance(c, p, P, chunk), stream);
 }
 
 int ec_tc_balance_backward(const ec_problem* p, int32_t top_k, const float* S,
@@ -1033,7 +1075,8 @@ int ec_tc_balance_backward(const ec_problem* p, int32_t top_k, const float* S,
   EC_TRY(check_ptr(counts, "counts"));
   EC_TRY(check_ptr(dloss, "dloss"));
   EC_TRY(check_ptr(dZ, "dZ", P.N == 0));
-  return for_chunk_tables(p, P, [&](const ec::ChunkTable& tab, int g0, long) -> int {
+  const int chunk = ec::balance_backward_chunk(P.N);
+  return for_chunk_tables(p, P, chunk, [&](const ec::ChunkTable& tab, int g0, long) -> int {
     EC_HIP(ec::launch_balance_backward(S, counts + (size_t)g0 * P.E, dloss + g0, P.E, top_k,
                                        p->inv_temperature, tab, dZ, stream));
     return EC_OK;
@@ -1101,13 +1144,15 @@ int ec_tc_train_forward(const ec_problem* p, int32_t top_k, const ec_dropout_des
     EC_HIP(ec::launch_zero(s.rows, (size_t)(P.E + 1) * 4, stream));
     EC_HIP(ec::launch_zero(s.tiles2, (size_t)(P.E + 1) * 4, stream));
     EC_HIP(ec::launch_zero(s.tilesA, (size_t)(P.E + 1) * 4, stream));
-    return enqueue_balance(p, P, top_k, s.S, loss, counts, s.counts, w.balance, stream);
+    EC_HIP(ec::launch_zero(s.counts, (size_t)P.G * P.E * 4, stream));
+    EC_HIP(ec::launch_zero(counts, (size_t)P.G * P.E * 4, stream));
+    EC_HIP(ec::launch_zero(loss, (size_t)P.G * 4, stream));
+    return EC_OK;
   }
   TcRouteWs rw = w.route;
   rw.tiles2 = s.tiles2;
-  EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, s.S, s.G, s.slot, s.rows, s.sel, rw, stream, s.gate,
-                          scale, s.tilesA));
-  EC_TRY(enqueue_balance(p, P, top_k, s.S, loss, counts, s.counts, w.balance, stream));
+  const TcTrainRoute train = {w.balance, loss, counts, s.counts, s.gate, scale, s.tilesA};
+  EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, s.S, s.G, s.slot, s.rows, s.sel, rw, stream, &train));
   EC_HIP(mark(3, stream));
   // A carries the gate (A = g SiLU(H1) H3), as in expert choice, and the scale of what the
   // dropout keeps: the output adds rows and masks their sum
@@ -1198,7 +1243,8 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
   EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.rows, rmax_e, d, h, s.sel,
                                   stream));
   EC_HIP(mark(5, stream));
-  EC_TRY(for_chunk_tables(p, P, [&](const ec::ChunkTable& tab, int g0, long) -> int {
+  const int chunk = ec::balance_backward_chunk(N);
+  EC_TRY(for_chunk_tables(p, P, chunk, [&](const ec::ChunkTable& tab, int g0, long) -> int {
     EC_HIP(ec::launch_tc_router_dz(P.dtype, s.S, s.G, s.slot, b.dsp, ec::dsp_parts(P.dtype, h),
                                    s.counts + (size_t)g0 * E, dloss ? dloss + g0 : nullptr, b.dZ, N,
                                    E, P.EP, top_k, (int)rmax, p->inv_temperature, tab, stream));

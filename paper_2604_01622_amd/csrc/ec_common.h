@@ -141,6 +141,15 @@ __device__ __forceinline__ float dpp_f32(float v) {
   return __builtin_bit_cast(float, dpp_u32<CTRL>(__builtin_bit_cast(uint32_t, v)));
 }
 
+// Minimum over the 16 lanes of a DPP row; every lane of the row ends with it.
+__device__ __forceinline__ int row16_min_i32(int t) {
+  const auto low = [](int a, uint32_t b) { return a < (int)b ? a : (int)b; };
+  t = low(t, dpp_u32<0xB1>((uint32_t)t));
+  t = low(t, dpp_u32<0x4E>((uint32_t)t));
+  t = low(t, dpp_u32<0x124>((uint32_t)t));
+  return low(t, dpp_u32<0x128>((uint32_t)t));
+}
+
 // Maximum over the 16 lanes of a DPP row; every lane of the row ends with it.
 __device__ __forceinline__ float row16_max(float t) {
   t = fmaxf(t, dpp_f32<0xB1>(t));

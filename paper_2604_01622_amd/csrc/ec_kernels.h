@@ -209,19 +209,30 @@ struct ChunkTable {
   int chunk;
   int off[TOPK_MAX_GROUPS];
   int len[TOPK_MAX_GROUPS];
+  int cap[TOPK_MAX_GROUPS];
   int seg[TOPK_MAX_GROUPS + 1];
 };
-// Tokens of a chunk, for a problem of N tokens.
+// Tokens of a chunk, for N tokens; where no group has more than BALANCE_WHOLE, each is one
+// chunk and launch_balance_partial finishes it.
+constexpr int BALANCE_WHOLE = 256;
 int balance_chunk(int N);
+// ... of launch_balance_backward and launch_tc_router_dz, and of launch_tc_choose.
+int balance_backward_chunk(int N);
+constexpr int TC_CHOOSE_CHUNK = 64;
 // Sums of S and the number of choices among each row's k largest (ties: the lower index),
-// per chunk: psum, pcnt [seg[n], E].
-hipError_t launch_balance_partial(const float* S, int E, int k, const ChunkTable& tab,
-                                  double* psum, int32_t* pcnt, hipStream_t st);
+// per chunk: psum, pcnt [seg[n], E]; whole: loss [n] and counts [n, E] instead.
+hipError_t launch_balance_partial(const float* S, int E, int k, const ChunkTable& tab, bool whole,
+                                  double* psum, int32_t* pcnt, float* loss, int32_t* counts,
+                                  hipStream_t st);
+// The same sums in one pass with launch_tc_topk's outputs.
+hipError_t launch_tc_choose(const float* S, int N, int E, int k, const ChunkTable& tab,
+                            double* psum, int32_t* pcnt, float* G, int32_t* flagT,
+                            hipStream_t st);
 // counts [n, E] and loss [n] of the table's groups from their chunks' sums (counts2: a
-// second copy of the counts unless null).
+// second copy of the counts, kept: the counts capped at tab.cap, unless null).
 hipError_t launch_balance_finish(const double* psum, const int32_t* pcnt, int E, int k,
                                  const ChunkTable& tab, float* loss, int32_t* counts,
-                                 int32_t* counts2, hipStream_t st);
+                                 int32_t* counts2, int32_t* kept, hipStream_t st);
 // dZ [N, E] fp32 of the table's groups: the loss's gradient in the logits (counts [n, E] and
 // dloss [n] of these groups).
 hipError_t launch_balance_backward(const float* S, const int32_t* counts, const float* dloss,

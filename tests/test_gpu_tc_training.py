@@ -84,7 +84,8 @@ def test_balance_expert_counts(E, k, ties):
 
 
 @pytest.mark.parametrize("lens", [[1], [0], [0, 0, 5, 0], [15], [16], [17], [63], [64], [65], [128],
-                                  [4097], [20000], [300] * 131, [1, 700, 2, 0, 3]])
+                                  [4097], [20000], [300] * 131, [1, 700, 2, 0, 3], [256, 9],
+                                  [257], [10] * 130, [65536], [65500, 36]])
 def test_balance_group_lengths(lens):
     check_balance(scores(sum(lens), 24, len(lens)), lens, 3)
 
