@@ -7,7 +7,9 @@ stale build raises instead of falling back to anything.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -134,12 +136,24 @@ def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _raw_stream(device):
+    """The device's current stream, as _stream() without building a Stream object."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _dtype_code(dt: torch.dtype) -> int:
     if dt == torch.bfloat16:
         return EC_BF16
     if dt == torch.float32:
         return EC_F32
     raise ECError(4, f"unsupported storage dtype {dt}")
+
+
+def _i32_array(a: np.ndarray):
+    """A contiguous int32 array as a ctypes one over the same memory."""
+    if a.flags.writeable and a.size:
+        return (ctypes.c_int32 * a.size).from_buffer(a)
+    return a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
 
 
 class Problem:
@@ -152,9 +166,7 @@ class Problem:
         self.cap = np.ascontiguousarray(np.asarray(capacity, dtype=np.int32))
         self.dtype = dtype
         self.c = _Problem(int(n_tokens), int(d_model), int(n_experts), int(d_ff),
-                          int(len(self.cap)),
-                          self.off.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)),
-                          self.cap.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)),
+                          int(len(self.cap)), _i32_array(self.off), _i32_array(self.cap),
                           float(inv_temperature), _dtype_code(dtype), int(d_shared))
 
     @property
@@ -317,6 +329,14 @@ def tc_forward(X, Wg, W1, W3, W2, group_offsets, capacity, top_k: int, inv_tempe
     return Y, rows
 
 
+_NO_GUARD = contextlib.nullcontext()
+
+
+def _on(device):
+    """Makes a tensor's device the current one, at no cost where it is."""
+    return _NO_GUARD if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
 def _operand(name, t, dtype, shape=None, device=None):
     """Refuses what the library cannot see: another type, shape or device, or gaps."""
     if not isinstance(t, torch.Tensor):
@@ -333,14 +353,19 @@ def _operand(name, t, dtype, shape=None, device=None):
         raise ECError(1, f"{name} must be contiguous")
 
 
+@functools.lru_cache(maxsize=64)
+def _zeros(n):
+    return np.zeros(n, dtype=np.int32)
+
+
 def _balance_problem(S, group_offsets, top_k, inv_temperature):
     if not isinstance(S, torch.Tensor) or S.dim() != 2:
         raise ECError(2, "S must be [N, E]")
     _operand("S", S, torch.float32)
-    off = np.asarray(group_offsets, dtype=np.int64)
+    off = np.asarray(group_offsets, dtype=np.int32)
     if off.ndim != 1 or len(off) < 2:
         raise ECError(2, "group_offsets needs n_groups + 1 entries")
-    return Problem(S.shape[0], 64, S.shape[1], 64, off, np.zeros(len(off) - 1), inv_temperature,
+    return Problem(S.shape[0], 64, S.shape[1], 64, off, _zeros(len(off) - 1), inv_temperature,
                    torch.float32)
 
 
@@ -349,13 +374,13 @@ def tc_balance(S, group_offsets, top_k: int):
     counts [G,E] int32 (tokens of each group that take each expert, before any capacity)."""
     P = _balance_problem(S, group_offsets, top_k, 1.0)
     G, E, dev = P.c.n_groups, P.c.n_experts, S.device
-    with torch.cuda.device(dev):
+    with _on(dev):
         loss = torch.empty((G,), dtype=torch.float32, device=dev)
         counts = torch.empty((G, E), dtype=torch.int32, device=dev)
         n = lib().ec_tc_workspace_size(P.ref, int(top_k), 2)
         ws = _empty(n, dev)
-        _check(lib().ec_tc_balance(P.ref, int(top_k), _ptr(S) if P.c.n_tokens else None,
-                                   _ptr(loss), _ptr(counts), _ptr(ws), ws.numel(), _stream()))
+        _check(lib().ec_tc_balance(P.ref, int(top_k), S.data_ptr() or None, loss.data_ptr(),
+                                   counts.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(dev)))
     return loss, counts
 
 
@@ -366,12 +391,11 @@ def tc_balance_backward(S, counts, dloss, group_offsets, top_k: int, inv_tempera
     G, E, dev = P.c.n_groups, P.c.n_experts, S.device
     _operand("counts", counts, torch.int32, (G, E), dev)
     _operand("dloss", dloss, torch.float32, (G,), dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         dZ = torch.empty_like(S)
-        N = P.c.n_tokens
-        _check(lib().ec_tc_balance_backward(P.ref, int(top_k), _ptr(S) if N else None,
-                                            _ptr(counts), _ptr(dloss), _ptr(dZ) if N else None,
-                                            _stream()))
+        _check(lib().ec_tc_balance_backward(P.ref, int(top_k), S.data_ptr() or None,
+                                            counts.data_ptr(), dloss.data_ptr(),
+                                            dZ.data_ptr() or None, _raw_stream(dev)))
     return dZ
 
 
@@ -381,9 +405,8 @@ def _dropout_desc(X, p, rng, residual, name="X"):
         _operand("rng", rng, torch.int64, (2,), X.device)
     if residual is not None:
         _operand("residual", residual, X.dtype, X.shape, X.device)
-    some = X.numel() > 0
     return _DropoutDesc(float(p), None if rng is None else rng.data_ptr(),
-                        residual.data_ptr() if residual is not None and some else None)
+                        None if residual is None else residual.data_ptr() or None)
 
 
 def dropout(X, p: float, rng=None, residual=None, out=None):
@@ -398,11 +421,10 @@ def dropout(X, p: float, rng=None, residual=None, out=None):
     desc = _dropout_desc(X, p, rng, residual)
     if out is not None:
         _operand("out", out, X.dtype, X.shape, X.device)
-    with torch.cuda.device(X.device):
+    with _on(X.device):
         Y = torch.empty_like(X) if out is None else out
-        some = X.numel() > 0
-        _check(lib().ec_dropout(code, X.numel(), ctypes.byref(desc), _ptr(X) if some else None,
-                                _ptr(Y) if some else None, _stream()))
+        _check(lib().ec_dropout(code, X.numel(), ctypes.byref(desc), X.data_ptr() or None,
+                                Y.data_ptr() or None, _raw_stream(X.device)))
     return Y
 
 
@@ -601,7 +623,7 @@ class TcLayer:
             raise ECError(2, "group_offsets must have one entry more than capacity")
         L, k, dev = lib(), self.top_k, X.device
         n_saved = _tc_size(L.ec_tc_saved_size(self.P.ref, k))
-        with torch.cuda.device(dev):
+        with _on(dev):
             if saved is None:
                 self.Y = torch.empty_like(X)
                 self.loss = torch.empty((self.P.c.n_groups,), dtype=torch.float32, device=dev)
@@ -627,7 +649,7 @@ class TcLayer:
                                        *_shared_ptrs(self.shared), _ptr(self.Y), _ptr(self.rows),
                                        _ptr(self.ws), self.ws.numel(), _stream()))
             return self.Y
-        with torch.cuda.device(self.X.device):
+        with _on(self.X.device):
             _check(lib().ec_tc_train_forward(
                 self.P.ref, self.top_k, ctypes.byref(self.drop), _tok_ptr(self.X), _ptr(self.Wg),
                 _ptr(self.W1), _ptr(self.W3), _ptr(self.W2), *_shared_ptrs(self.shared),
@@ -642,7 +664,7 @@ class TcLayer:
         _operand("dY", dY, self.X.dtype, self.X.shape, self.X.device)
         if dloss is not None:
             _operand("dloss", dloss, torch.float32, (self.P.c.n_groups,), self.X.device)
-        with torch.cuda.device(self.X.device):
+        with _on(self.X.device):
             _check(lib().ec_tc_train_backward(
                 self.P.ref, self.top_k, ctypes.byref(self.drop), _tok_ptr(self.X), _ptr(self.Wg),
                 _ptr(self.W1), _ptr(self.W3), _ptr(self.W2), *_shared_ptrs(self.shared),

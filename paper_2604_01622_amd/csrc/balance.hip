@@ -77,53 +77,65 @@ __device__ __forceinline__ void store_row(float* row, int E, int r, const float 
 }
 
 // Takes the k largest entries out of the four rows that a wave holds (ties: the lower
-// expert; NaN, also in the entries past E, is never taken): a taken entry becomes NaN, and
-// the taken values' sum is returned.  A round is a maximum over the row, a compare and a
-// select per entry; only where some row holds its maximum more than once (the four rows'
-// equal entries are then not four) or nothing but NaN is the lowest expert looked for.
-// Every lane takes part.
+// expert; NaN, also in the entries past E, is never taken); a taken entry's key ends as 0.
+// Keys are integers in the scores' order (f32_order_key; 0 for NaN), whose maxima take three
+// operands an instruction and no care for NaN.  A round is a maximum over the row, a compare
+// and a select per entry, and takes every entry equal to the maximum; only where some row so
+// loses more or fewer than k (equal scores among its largest, or not k numbers) does the
+// wave start over, one lowest expert at a time.  Every lane takes part.
 template <int Q>
-__device__ __forceinline__ float take_largest(float w[Q][4], int r, int k) {
-  const float nan = __builtin_nanf("");
-  float sum = 0.f;
+__device__ __forceinline__ void take_largest(uint32_t w[Q][4], const float v[Q][4], int r, int k) {
+  auto keys = [&] {
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        w[q][c] = v[q][c] == v[q][c] ? f32_order_key(v[q][c] + 0.f) : 0;   // -0 equals 0
+  };
+  auto row_max = [&]() -> uint32_t {
+    uint32_t m = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      m = max(m, max(w[q][0], w[q][1]));
+      m = max(m, max(w[q][2], w[q][3]));
+    }
+    return row16_max_u32(m);
+  };
+  keys();
   for (int n = 0; n < k; ++n) {
-    float m = -INFINITY;
+    const uint32_t m = row_max();
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) m = fmaxf(m, w[q][c]);
-    m = row16_max(m);
-    int equal = 0;
+      for (int c = 0; c < 4; ++c) w[q][c] = w[q][c] == m ? 0 : w[q][c];
+  }
+  int took = 0;
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
+  for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) equal += __popcll(__ballot(w[q][c] == m));
+    for (int c = 0; c < 4; ++c) took += w[q][c] == 0 && v[q][c] == v[q][c];
+  if (!__any(row16_sum_i32(took) != k)) return;
+  keys();
+  for (int n = 0; n < k; ++n) {
+    const uint32_t m = row_max();
     int first = 1 << 30;
-    if (equal != 4 || __any(m == -INFINITY)) {   // uniform
+    if (m != 0) {
 #pragma unroll
       for (int q = Q - 1; q >= 0; --q)
 #pragma unroll
         for (int c = 3; c >= 0; --c) first = w[q][c] == m ? 64 * q + 4 * r + c : first;
-      first = row16_min_i32(first);
-      if (first < (1 << 30)) sum += m;
-#pragma unroll
-      for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) w[q][c] = 64 * q + 4 * r + c == first ? nan : w[q][c];
-    } else {
-      sum += m;
-#pragma unroll
-      for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) w[q][c] = w[q][c] == m ? nan : w[q][c];
     }
+    first = row16_min_i32(first);
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) w[q][c] = 64 * q + 4 * r + c == first ? 0 : w[q][c];
   }
-  return sum;
 }
 
-// Threads of a workgroup that sums: 1024, 512 where a row takes four quarters (more than 192
+// Threads of a workgroup that sums: 1024, 768 where a row takes four quarters (more than 192
 // experts), whose sums need more registers than a lane of 16 waves has.
-template <int Q> constexpr int BL_THREADS = Q == 4 ? 512 : 1024;
+template <int Q> constexpr int BL_THREADS = Q == 4 ? 768 : 1024;
 
 // The group's loss and counts from its sums: thread j < E holds expert j's.
 __device__ __forceinline__ void finish_group(double sum, int count, int E, int k, int len, int cap,
@@ -166,32 +178,50 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
   const int t1 = t0 + tab.chunk < tab.len[g] ? t0 + tab.chunk : tab.len[g];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15;
   double sum[Q][4];
-  int cnt[Q][4];
+  uint32_t cnt[Q][2];   // two counts a register: a lane's tokens are at most chunk / 4 < 2^16
 #pragma unroll
   for (int q = 0; q < Q; ++q)
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       sum[q][c] = 0.0;
-      cnt[q][c] = 0;
+      cnt[q][c / 2] = 0;
     }
-  for (int tw = t0 + wave * 4; tw < t1; tw += 4 * WAVES) {   // a wave's four tokens
+  // a wave's four tokens at a time, the next four's scores requested before these are chosen
+  float next[Q][4];
+  auto request = [&](int tw) {
+    const int t = tw + (lane >> 4);
+    load_row<Q>(S + (size_t)(tab.off[g] + (t < t1 ? t : t1 - 1)) * E, E, r, __builtin_nanf(""), next);
+  };
+  const int tw0 = t0 + wave * 4;
+  if (tw0 < t1) request(tw0);
+  for (int tw = tw0; tw < t1; tw += 4 * WAVES) {
     const int t = tw + (lane >> 4), i = tab.off[g] + (t < t1 ? t : t1 - 1);
-    float v[Q][4], w[Q][4];
-    load_row<Q>(S + (size_t)i * E, E, r, __builtin_nanf(""), v);
+    float v[Q][4];
+    uint32_t w[Q][4];
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) w[q][c] = v[q][c];
-    const float chosen = take_largest<Q>(w, r, k);
-    const float inv = 1.0f / chosen;
+      for (int c = 0; c < 4; ++c) v[q][c] = next[q][c];
+    if (tw + 4 * WAVES < t1) request(tw + 4 * WAVES);
+    take_largest<Q>(w, v, r, k);
+    float inv = 1.f;
+    if constexpr (TRAIN) {   // the gates' sum, the same in all lanes of the row
+      float chosen = 0.f;
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          chosen += w[q][c] == 0 && v[q][c] == v[q][c] ? v[q][c] : 0.f;
+      inv = 1.0f / row16_sum_even(chosen);
+    }
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const bool taken = w[q][c] != w[q][c] && v[q][c] == v[q][c];
+        const bool taken = w[q][c] == 0 && v[q][c] == v[q][c];
         if (t < t1) {
           sum[q][c] += (double)v[q][c];
-          cnt[q][c] += taken;
+          cnt[q][c / 2] += taken ? 1u << (c % 2 * 16) : 0u;
         }
         if constexpr (TRAIN) {
           sflag[t - t0][64 * q + 4 * r + c] = taken;   // t - t0 < TC_CHOOSE_CHUNK
@@ -208,7 +238,7 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       double s = sum[q][c];
-      int n = cnt[q][c];
+      int n = (int)(c % 2 ? cnt[q][c / 2] >> 16 : cnt[q][c / 2] & 0xffffu);
       s += __shfl_xor(s, 16, 64);
       n += __shfl_xor(n, 16, 64);
       s += __shfl_xor(s, 32, 64);
@@ -245,13 +275,15 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
 }
 
 // Counts and loss of a group from its chunks' sums, a workgroup a group: threads share the
-// chunks out, 1024 / (64 Q) at a time, eight loads of each in flight.
+// chunks out, 1024 / (64 Q) at a time, 4 Q loads of each in flight (256 chunks of a group
+// of 65536 tokens and 256 experts: 12.7 us, with a loop of single loads 272; the 32 chunks
+// of a group of 2048 and 64 experts are four loads).
 template <int Q>
 __global__ __launch_bounds__(1024) void balance_finish_kernel(
     const double* __restrict__ psum, const int32_t* __restrict__ pcnt, int E, int k,
     ChunkTable tab, float* __restrict__ loss, int32_t* __restrict__ counts,
     int32_t* __restrict__ counts2, int32_t* __restrict__ kept) {
-  constexpr int SLICES = 1024 / (64 * Q);
+  constexpr int SLICES = 1024 / (64 * Q), B = 4 * Q;
   __shared__ double ssum[SLICES][64 * Q];
   __shared__ int scnt[SLICES][64 * Q];
   __shared__ double red[4];
@@ -259,10 +291,22 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(
   double s = 0.0;
   int n = 0;
   if (sl < SLICES && j < E) {
-#pragma unroll 8
-    for (int c = tab.seg[g] + sl; c < tab.seg[g + 1]; c += SLICES) {
-      s += psum[(size_t)c * E + j];
-      n += pcnt[(size_t)c * E + j];
+    const int end = tab.seg[g + 1];
+    for (int c0 = tab.seg[g] + sl; c0 < end; c0 += B * SLICES) {
+      double x[B];
+      int y[B];
+#pragma unroll
+      for (int u = 0; u < B; ++u) {   // past the end: the last chunk again, not added
+        const int c = c0 + u * SLICES < end ? c0 + u * SLICES : end - 1;
+        x[u] = psum[(size_t)c * E + j];
+        y[u] = pcnt[(size_t)c * E + j];
+      }
+#pragma unroll
+      for (int u = 0; u < B; ++u) {
+        const bool in = c0 + u * SLICES < end;
+        s += in ? x[u] : 0.0;
+        n += in ? y[u] : 0;
+      }
     }
   }
   if (sl < SLICES) {
@@ -455,8 +499,8 @@ int balance_chunk(int N) {
   return (N + 256 * 64 - 1) / (256 * 64) * 64;
 }
 
-// Gradients: 16 tokens (one each) while the workgroups are at most 4096, else 64.
-int balance_backward_chunk(int N) { return N <= 65536 ? 16 : 64; }
+// Gradients: 16 tokens (one each) while the workgroups are at most 1024, else 64.
+int balance_backward_chunk(int N) { return N <= 16384 ? 16 : 64; }
 
 hipError_t launch_balance_partial(const float* S, int E, int k, const ChunkTable& tab, bool whole,
                                   double* psum, int32_t* pcnt, float* loss, int32_t* counts,

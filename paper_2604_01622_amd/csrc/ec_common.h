@@ -141,6 +141,22 @@ __device__ __forceinline__ float dpp_f32(float v) {
   return __builtin_bit_cast(float, dpp_u32<CTRL>(__builtin_bit_cast(uint32_t, v)));
 }
 
+// Maximum of unsigned integers over the 16 lanes of a DPP row; every lane ends with it.
+__device__ __forceinline__ uint32_t row16_max_u32(uint32_t t) {
+  t = max(t, dpp_u32<0xB1>(t));
+  t = max(t, dpp_u32<0x4E>(t));
+  t = max(t, dpp_u32<0x124>(t));
+  return max(t, dpp_u32<0x128>(t));
+}
+
+// Sum of integers over the 16 lanes of a DPP row; every lane of the row ends with it.
+__device__ __forceinline__ int row16_sum_i32(int t) {
+  t += (int)dpp_u32<0xB1>((uint32_t)t);
+  t += (int)dpp_u32<0x4E>((uint32_t)t);
+  t += (int)dpp_u32<0x124>((uint32_t)t);
+  return t + (int)dpp_u32<0x128>((uint32_t)t);
+}
+
 // Minimum over the 16 lanes of a DPP row; every lane of the row ends with it.
 __device__ __forceinline__ int row16_min_i32(int t) {
   const auto low = [](int a, uint32_t b) { return a < (int)b ? a : (int)b; };
