@@ -398,6 +398,7 @@ struct TcTrainRoute {
   float* sel_gate;
   float gate_scale;
   int32_t* tilesA;
+  int32_t* order;
 };
 
 // Router, row top-k, per-(group, expert) counts, offsets and placement; with `train` (null in
@@ -445,7 +446,7 @@ int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* 
       EC_HIP(ec::launch_tc_offsets(w.cnt, P.G, P.E, ec::TC_BM, ec::tc_col_blocks_w13(P.h),
                                    ec::tc_col_blocks_w2(P.d), ec::tc_col_blocks_dA(P.h), rows,
                                    w.seg, w.tiles13, w.tiles2, train ? train->tilesA : nullptr,
-                                   st));
+                                   train ? train->order : nullptr, st));
   }
   EC_HIP(mark(2, st));
   return EC_OK;
@@ -490,6 +491,7 @@ struct TcSaved {
   int32_t* rows;     // [E + 1]
   int32_t* tiles2;   // [E + 1] tiles of the products of width d
   int32_t* tilesA;   // [E + 1] tiles of the dA product
+  int32_t* order;    // [E] the experts as the weight gradients take them
   int32_t* counts;   // [G, E]
   int32_t* sel;      // [R] token of each packed row
   float* gate;       // [R] its gate
@@ -509,6 +511,7 @@ TcSaved carve_tc_saved(Carve& c, const Plan& P, long rmax) {
   s.rows = (int32_t*)c.take((size_t)(P.E + 1) * 4);
   s.tiles2 = (int32_t*)c.take((size_t)(P.E + 1) * 4);
   s.tilesA = (int32_t*)c.take((size_t)(P.E + 1) * 4);
+  s.order = (int32_t*)c.take((size_t)P.E * 4);
   s.counts = (int32_t*)c.take((size_t)P.G * P.E * 4);
   s.sel = (int32_t*)c.take((size_t)rmax * 4);
   s.gate = (float*)c.take((size_t)rmax * 4);
@@ -1141,17 +1144,16 @@ int ec_tc_train_forward(const ec_problem* p, int32_t top_k, const ec_dropout_des
   const TcTrainFwdWs w = carve_tc_train_fwd(c, p, P, rmax);
   const float scale = take_scale(&d);
   if (P.N == 0) {   // no tokens: nothing kept, zero losses and loads
-    EC_HIP(ec::launch_zero(s.rows, (size_t)(P.E + 1) * 4, stream));
-    EC_HIP(ec::launch_zero(s.tiles2, (size_t)(P.E + 1) * 4, stream));
-    EC_HIP(ec::launch_zero(s.tilesA, (size_t)(P.E + 1) * 4, stream));
     EC_HIP(ec::launch_zero(s.counts, (size_t)P.G * P.E * 4, stream));
+    EC_HIP(ec::launch_tc_offsets(s.counts, P.G, P.E, ec::TC_BM, 1, 1, 1, s.rows, w.route.seg,
+                                 w.route.tiles13, s.tiles2, s.tilesA, s.order, stream));
     EC_HIP(ec::launch_zero(counts, (size_t)P.G * P.E * 4, stream));
     EC_HIP(ec::launch_zero(loss, (size_t)P.G * 4, stream));
     return EC_OK;
   }
   TcRouteWs rw = w.route;
   rw.tiles2 = s.tiles2;
-  const TcTrainRoute train = {w.balance, loss, counts, s.counts, s.gate, scale, s.tilesA};
+  const TcTrainRoute train = {w.balance, loss, counts, s.counts, s.gate, scale, s.tilesA, s.order};
   EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, s.S, s.G, s.slot, s.rows, s.sel, rw, stream, &train));
   EC_HIP(mark(3, stream));
   // A carries the gate (A = g SiLU(H1) H3), as in expert choice, and the scale of what the
@@ -1235,13 +1237,14 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
   EC_HIP(ec::launch_gemm_dA_var(P.dtype, dYm, W2, s.H1, s.H3, b.dH, b.dsp, E, s.rows, s.tilesA,
                                 rmax, rmax_e, d, h, s.sel, s.gate, stream));
   EC_HIP(mark(2, stream));
-  EC_HIP(ec::launch_gemm_dW2_var(P.dtype, dYm, s.A, dW2, E, s.rows, rmax_e, d, h, s.sel, stream));
+  EC_HIP(ec::launch_gemm_dW2_var(P.dtype, dYm, s.A, dW2, E, s.rows, s.order, rmax_e, d, h, s.sel,
+                                 stream));
   EC_HIP(mark(3, stream));
   EC_HIP(ec::launch_gemm_dXe_var(P.dtype, b.dH, W1, W3, b.dXe, E, s.rows, s.tiles2, rmax, rmax_e,
                                  d, h, stream));
   EC_HIP(mark(4, stream));
-  EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.rows, rmax_e, d, h, s.sel,
-                                  stream));
+  EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.rows, s.order, rmax_e, d, h,
+                                  s.sel, stream));
   EC_HIP(mark(5, stream));
   const int chunk = ec::balance_backward_chunk(N);
   EC_TRY(for_chunk_tables(p, P, chunk, [&](const ec::ChunkTable& tab, int g0, long) -> int {

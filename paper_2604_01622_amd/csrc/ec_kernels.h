@@ -157,11 +157,12 @@ hipError_t launch_tc_topk(const float* S, int N, int E, int k, float* G, int32_t
 hipError_t launch_tc_count(const int32_t* flagT, int N, int E, const GroupTable& tab, int g0,
                            int32_t* cnt, hipStream_t st);
 // Packed row offsets rows [E+1], per-(group, expert) row offsets seg [G,E] and the
-// tile offsets of the grouped products (tiles13, tiles2, and tilesA of the dA product
-// unless null; [E+1] each).
+// tile offsets of the grouped products (tiles13, tiles2; [E+1] each).  Training (tilesA not
+// null): also those of the dA product, and order [E], in which the products that contract over
+// an expert's rows take the experts.
 hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13, int nt2, int ntA,
                              int32_t* rows, int32_t* seg, int32_t* tiles13, int32_t* tiles2,
-                             int32_t* tilesA, hipStream_t st);
+                             int32_t* tilesA, int32_t* order, hipStream_t st);
 // slotT: choice flags in, packed rows (-1: not kept) out; sel[row] = token.  Without
 // sel_gate G is zeroed on dropped pairs; with it (training) sel_gate[row] = scale G of the
 // pair and G keeps the gates of every choice.
@@ -184,7 +185,8 @@ int tc_col_blocks_dA(int h);
 // The backward products over packed rows (conventions of launch_gemm_dA, _dXe, _dW2 and
 // _dW13): sel[r] is the token of packed row r, whose rows of dY (dA, dW2) and X (dW13) the
 // products read themselves.  dH [max_rows, 2h], dsp [max_rows, dsp_parts(dtype, h)].  An
-// expert without rows gets zero weight gradients.
+// expert without rows gets zero weight gradients.  order [E]: the experts as the weight
+// gradients take them (launch_tc_offsets).
 hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
                               const void* H3, void* dH, float* dsp, int E, const int32_t* rows,
                               const int32_t* tiles, long max_rows, int max_rows_per_expert, int d,
@@ -194,11 +196,13 @@ hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const 
                                long max_rows, int max_rows_per_expert, int d, int h,
                                hipStream_t st);
 hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
-                               const int32_t* rows, int max_rows_per_expert, int d, int h,
-                               const int32_t* sel, hipStream_t st);
+                               const int32_t* rows, const int32_t* order,
+                               int max_rows_per_expert, int d, int h, const int32_t* sel,
+                               hipStream_t st);
 hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* dW1, void* dW3,
-                                int E, const int32_t* rows, int max_rows_per_expert, int d, int h,
-                                const int32_t* sel, hipStream_t st);
+                                int E, const int32_t* rows, const int32_t* order,
+                                int max_rows_per_expert, int d, int h, const int32_t* sel,
+                                hipStream_t st);
 
 // ---- the balance loss of token choice ----
 

@@ -126,9 +126,11 @@ struct GemmParams {
   // batches + 1 entries, null for a uniform batch of M rows.  With OPT_KVAR the
   // rows are the contraction's instead (K-major operands: the weight gradients):
   // batch e contracts over rows [var_rows[e], var_rows[e+1]) of both, and its
-  // outputs and tiles are those of a uniform batch.
+  // outputs and tiles are those of a uniform batch; the tiles take the batches
+  // in the order var_order [batches] (a device array).
   const int* var_rows;
   const int* var_tiles;
+  const int* var_order;
 };
 
 // Where one output tile sits: batch, first row and column, the batch's rows,
@@ -833,11 +835,12 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
     if (t >= p.batches * p.MT * p.NT) return;
     const int per_b = p.MT * p.NT;
     tc.e = t / per_b;
+    rem = t - tc.e * per_b;
+    if constexpr (KVAR) tc.e = p.var_order[tc.e];
     tc.row0 = 0;
     tc.M = p.M;
     tc.row = (size_t)tc.e * p.M;
     MT = p.MT;
-    rem = t - tc.e * per_b;
     tc.a_off = (size_t)tc.e * p.a_bs;
     tc.c_off = (size_t)tc.e * p.c_bs;
     tc.h_off = (size_t)tc.e * p.h_bs;
@@ -915,7 +918,7 @@ template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bo
 hipError_t run_dma(GemmParams p, hipStream_t st) {
   if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr) ||
       ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) ||
-      ((OPT & OPT_KVAR) != 0) != (p.var_rows != nullptr))
+      ((OPT & OPT_KVAR) != 0) != (p.var_rows != nullptr && p.var_order != nullptr))
     return hipErrorInvalidValue;
   if (!operands_in_reach<A_KC, B_KC, OPT>(p)) return hipErrorInvalidValue;
   p.MT = (p.M + BM - 1) / BM;
@@ -1067,7 +1070,9 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
   const int t = xcd_tile_id(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
   const int per_b = p.MT * p.NT;
   if (t >= p.batches * per_b) return;
-  const int e = t / per_b, rem = t - e * per_b;
+  int e = t / per_b;
+  const int rem = t - e * per_b;
+  if constexpr (KVAR) e = p.var_order[e];
   const int m0 = rem % p.MT * BM;
   const int n0 = rem / p.MT * (EPI == EPI_SWIGLU ? BN / 2 : BN);
   // rows of this batch: uniform (M), or [var_rows[e], var_rows[e+1]) of packed buffers
@@ -1327,7 +1332,7 @@ template <bool A_KC, bool B_KC, int EPI, int OPT = 0>
 hipError_t run_f32(const GemmParams& p, hipStream_t st) {
   if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr) ||
       ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) ||
-      ((OPT & OPT_KVAR) != 0 && p.var_rows == nullptr))
+      ((OPT & OPT_KVAR) != 0 && (p.var_rows == nullptr || p.var_order == nullptr)))
     return hipErrorInvalidValue;
   const int nw = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
   const long big = (long)p.batches * ((p.M + 127) / 128) * ((nw + 127) / 128);
@@ -1679,30 +1684,32 @@ hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const 
 }
 
 hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
-                               const int32_t* rows, int max_rows_per_expert, int d, int h,
-                               const int32_t* sel, hipStream_t st) {
+                               const int32_t* rows, const int32_t* order,
+                               int max_rows_per_expert, int d, int h, const int32_t* sel,
+                               hipStream_t st) {
   GemmParams p = base_params();
   const int K = max_rows_per_expert;
   p.A = dY; p.lda = d; p.ka_rows = sel;
   p.B = A; p.ldb = h;
   p.M = d; p.N = h; p.K = K; p.kv_a = K; p.kv_b = K; p.batches = E;
   p.C = dW2; p.c_bs = (long)d * h; p.ldc = h;
-  p.var_rows = rows;
+  p.var_rows = rows; p.var_order = order;
   if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GA | OPT_KVAR>(p, st);
   return run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW2,
                  OPT_GA | OPT_TAILS | OPT_KVAR>(p, st);
 }
 
 hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* dW1, void* dW3,
-                                int E, const int32_t* rows, int max_rows_per_expert, int d, int h,
-                                const int32_t* sel, hipStream_t st) {
+                                int E, const int32_t* rows, const int32_t* order,
+                                int max_rows_per_expert, int d, int h, const int32_t* sel,
+                                hipStream_t st) {
   GemmParams p = base_params();
   const int K = max_rows_per_expert;
   p.A = dH; p.lda = 2 * h;
   p.B = X; p.ldb = d; p.kb_rows = sel;
   p.M = 2 * h; p.N = d; p.K = K; p.kv_a = K; p.kv_b = K; p.batches = E;
   p.C = dW1; p.C2 = dW3; p.c_split = h; p.c_bs = (long)h * d; p.ldc = d;
-  p.var_rows = rows;
+  p.var_rows = rows; p.var_order = order;
   if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GB | OPT_KVAR>(p, st);
   return run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW13,
                  OPT_GB | OPT_TAILS | OPT_KVAR>(p, st);

@@ -124,14 +124,18 @@ __global__ __launch_bounds__(256) void tc_count_kernel(const int32_t* __restrict
 // rows start at rows[j] (rows[E] = all kept pairs); group g's tokens in expert
 // j start at seg[g E + j]; the tiles of the two grouped products start at
 // tiles13[j] and tiles2[j] (ceil(M_j / bm) row blocks times nt13 / nt2), those of the
-// training backward's dA product at tilesA[j] (unless null).
+// training backward's dA product at tilesA[j] (unless null).  With tilesA also order [E]: a
+// product that contracts over an expert's rows takes as long for the expert's every tile as
+// it has rows, and each XCD takes an eighth of the list, so the experts are dealt to the
+// eighths by falling row counts, there and back.
 __global__ __launch_bounds__(256) void tc_offsets_kernel(const int32_t* __restrict__ cnt, int G,
                                                          int E, int bm, int nt13, int nt2, int ntA,
                                                          int32_t* __restrict__ rows,
                                                          int32_t* __restrict__ seg,
                                                          int32_t* __restrict__ tiles13,
                                                          int32_t* __restrict__ tiles2,
-                                                         int32_t* __restrict__ tilesA) {
+                                                         int32_t* __restrict__ tilesA,
+                                                         int32_t* __restrict__ order) {
   __shared__ int sm[256], st[256];
   const int j = threadIdx.x;
   int m = 0;
@@ -139,6 +143,16 @@ __global__ __launch_bounds__(256) void tc_offsets_kernel(const int32_t* __restri
     for (int g = 0; g < G; ++g) m += cnt[(size_t)g * E + j];
   sm[j] = m;
   st[j] = (m + bm - 1) / bm;
+  __syncthreads();
+  if (order && j < E) {
+    int rank = 0;
+    for (int q = 0; q < E; ++q) rank += sm[q] > m || (sm[q] == m && q < j);
+    const int round = rank >> 3, x = (round & 1) ? 7 - (rank & 7) : rank & 7;
+    // eighths before x: a full round each, and those that the last round reaches
+    const int full = E >> 3, rest = E & 7;
+    const int before = (full & 1) ? (x > 8 - rest ? x - (8 - rest) : 0) : (x < rest ? x : rest);
+    order[x * full + before + round] = j;
+  }
   __syncthreads();
   if (j == 0) {   // E <= 256 sequential prefix sums
     int r = 0, tt = 0;
@@ -239,9 +253,9 @@ hipError_t launch_tc_count(const int32_t* flagT, int N, int E, const GroupTable&
 
 hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13, int nt2, int ntA,
                              int32_t* rows, int32_t* seg, int32_t* tiles13, int32_t* tiles2,
-                             int32_t* tilesA, hipStream_t st) {
+                             int32_t* tilesA, int32_t* order, hipStream_t st) {
   tc_offsets_kernel<<<1, 256, 0, st>>>(cnt, G, E, bm, nt13, nt2, ntA, rows, seg, tiles13, tiles2,
-                                       tilesA);
+                                       tilesA, order);
   return hipGetLastError();
 }
 
