@@ -350,8 +350,6 @@ struct TcRouteWs {
   float* ST;
   int32_t* cnt;
   int32_t* seg;
-  int32_t* tiles13;
-  int32_t* tiles2;
 };
 
 TcRouteWs carve_tc_route(Carve& c, const Plan& P, bool with_ST = true) {
@@ -359,8 +357,6 @@ TcRouteWs carve_tc_route(Carve& c, const Plan& P, bool with_ST = true) {
   w.ST = with_ST ? (float*)c.take((size_t)P.E * P.N * 4) : nullptr;
   w.cnt = (int32_t*)c.take((size_t)P.G * P.E * 4);
   w.seg = (int32_t*)c.take((size_t)P.G * P.E * 4);
-  w.tiles13 = (int32_t*)c.take((size_t)(P.E + 1) * 4);
-  w.tiles2 = (int32_t*)c.take((size_t)(P.E + 1) * 4);
   return w;
 }
 
@@ -389,7 +385,7 @@ TcFwdWs carve_tc_fwd(Carve& c, const Plan& P, long rmax) {
 }
 
 // What training's routing adds: the loads and the balance loss from the pass that chooses, the
-// packed rows' gates times gate_scale, and the tiles of the dA product.
+// packed rows' gates times gate_scale, and the order of the experts in the weight gradients.
 struct TcTrainRoute {
   BalanceWs sums;
   float* loss;
@@ -397,7 +393,6 @@ struct TcTrainRoute {
   int32_t* saved_counts;
   float* sel_gate;
   float gate_scale;
-  int32_t* tilesA;
   int32_t* order;
 };
 
@@ -443,10 +438,8 @@ int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* 
                                    train ? train->gate_scale : 1.f, st));
     }
     if (pass == 0)
-      EC_HIP(ec::launch_tc_offsets(w.cnt, P.G, P.E, ec::TC_BM, ec::tc_col_blocks_w13(P.h),
-                                   ec::tc_col_blocks_w2(P.d), ec::tc_col_blocks_dA(P.h), rows,
-                                   w.seg, w.tiles13, w.tiles2, train ? train->tilesA : nullptr,
-                                   train ? train->order : nullptr, st));
+      EC_HIP(ec::launch_tc_offsets(w.cnt, P.G, P.E, rows, w.seg, train ? train->order : nullptr,
+                                   st));
   }
   EC_HIP(mark(2, st));
   return EC_OK;
@@ -489,8 +482,6 @@ struct TcSaved {
   float* G;          // [N, E] gates of every choice, dropped ones too
   int32_t* slot;     // [E, N] packed row or -1
   int32_t* rows;     // [E + 1]
-  int32_t* tiles2;   // [E + 1] tiles of the products of width d
-  int32_t* tilesA;   // [E + 1] tiles of the dA product
   int32_t* order;    // [E] the experts as the weight gradients take them
   int32_t* counts;   // [G, E]
   int32_t* sel;      // [R] token of each packed row
@@ -509,8 +500,6 @@ TcSaved carve_tc_saved(Carve& c, const Plan& P, long rmax) {
   s.G = (float*)c.take((size_t)P.N * P.E * 4);
   s.slot = (int32_t*)c.take((size_t)P.E * P.N * 4);
   s.rows = (int32_t*)c.take((size_t)(P.E + 1) * 4);
-  s.tiles2 = (int32_t*)c.take((size_t)(P.E + 1) * 4);
-  s.tilesA = (int32_t*)c.take((size_t)(P.E + 1) * 4);
   s.order = (int32_t*)c.take((size_t)P.E * 4);
   s.counts = (int32_t*)c.take((size_t)P.G * P.E * 4);
   s.sel = (int32_t*)c.take((size_t)rmax * 4);
@@ -1028,10 +1017,10 @@ int ec_tc_forward(const ec_problem* p, int32_t top_k, const void* X, const void*
   EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, w.S, w.G, w.slot, rows, w.sel, rw, stream));
   // the W1/W3 product reads the kept rows of X itself (empty gather stage)
   EC_HIP(mark(3, stream));
-  EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, w.A, nullptr, nullptr, P.E, rows, rw.tiles13, rmax, rmax_e, P.d,
+  EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, w.A, nullptr, nullptr, P.E, rows, rmax, rmax_e, P.d,
                                  P.h, stream, w.sel));
   EC_HIP(mark(4, stream));
-  EC_HIP(ec::launch_gemm_w2_var(P.dtype, w.A, W2, w.O, P.E, rows, rw.tiles2, rmax, rmax_e, P.d,
+  EC_HIP(ec::launch_gemm_w2_var(P.dtype, w.A, W2, w.O, P.E, rows, rmax, rmax_e, P.d,
                                 P.h, stream));
   EC_HIP(mark(5, stream));
   if (P.hs) {
@@ -1145,23 +1134,21 @@ int ec_tc_train_forward(const ec_problem* p, int32_t top_k, const ec_dropout_des
   const float scale = take_scale(&d);
   if (P.N == 0) {   // no tokens: nothing kept, zero losses and loads
     EC_HIP(ec::launch_zero(s.counts, (size_t)P.G * P.E * 4, stream));
-    EC_HIP(ec::launch_tc_offsets(s.counts, P.G, P.E, ec::TC_BM, 1, 1, 1, s.rows, w.route.seg,
-                                 w.route.tiles13, s.tiles2, s.tilesA, s.order, stream));
+    EC_HIP(ec::launch_tc_offsets(s.counts, P.G, P.E, s.rows, w.route.seg, s.order, stream));
     EC_HIP(ec::launch_zero(counts, (size_t)P.G * P.E * 4, stream));
     EC_HIP(ec::launch_zero(loss, (size_t)P.G * 4, stream));
     return EC_OK;
   }
-  TcRouteWs rw = w.route;
-  rw.tiles2 = s.tiles2;
-  const TcTrainRoute train = {w.balance, loss, counts, s.counts, s.gate, scale, s.tilesA, s.order};
-  EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, s.S, s.G, s.slot, s.rows, s.sel, rw, stream, &train));
+  const TcTrainRoute train = {w.balance, loss, counts, s.counts, s.gate, scale, s.order};
+  EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, s.S, s.G, s.slot, s.rows, s.sel, w.route, stream,
+                          &train));
   EC_HIP(mark(3, stream));
   // A carries the gate (A = g SiLU(H1) H3), as in expert choice, and the scale of what the
   // dropout keeps: the output adds rows and masks their sum
-  EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, s.A, s.H1, s.H3, P.E, s.rows, rw.tiles13,
+  EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, s.A, s.H1, s.H3, P.E, s.rows,
                                  rmax, rmax_e, P.d, P.h, stream, s.sel, s.gate));
   EC_HIP(mark(4, stream));
-  EC_HIP(ec::launch_gemm_w2_var(P.dtype, s.A, W2, w.O, P.E, s.rows, s.tiles2, rmax, rmax_e, P.d,
+  EC_HIP(ec::launch_gemm_w2_var(P.dtype, s.A, W2, w.O, P.E, s.rows, rmax, rmax_e, P.d,
                                 P.h, stream));
   EC_HIP(mark(5, stream));
   if (P.hs) {
@@ -1234,13 +1221,13 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
     dYm = w.dYm;
   }
   EC_HIP(mark(1, stream));
-  EC_HIP(ec::launch_gemm_dA_var(P.dtype, dYm, W2, s.H1, s.H3, b.dH, b.dsp, E, s.rows, s.tilesA,
+  EC_HIP(ec::launch_gemm_dA_var(P.dtype, dYm, W2, s.H1, s.H3, b.dH, b.dsp, E, s.rows,
                                 rmax, rmax_e, d, h, s.sel, s.gate, stream));
   EC_HIP(mark(2, stream));
   EC_HIP(ec::launch_gemm_dW2_var(P.dtype, dYm, s.A, dW2, E, s.rows, s.order, rmax_e, d, h, s.sel,
                                  stream));
   EC_HIP(mark(3, stream));
-  EC_HIP(ec::launch_gemm_dXe_var(P.dtype, b.dH, W1, W3, b.dXe, E, s.rows, s.tiles2, rmax, rmax_e,
+  EC_HIP(ec::launch_gemm_dXe_var(P.dtype, b.dH, W1, W3, b.dXe, E, s.rows, rmax, rmax_e,
                                  d, h, stream));
   EC_HIP(mark(4, stream));
   EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.rows, s.order, rmax_e, d, h,

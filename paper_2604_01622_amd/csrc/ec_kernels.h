@@ -145,56 +145,46 @@ hipError_t launch_shared_dW13(int dtype, const void* dH, const void* X, void* dW
 
 // ---- token choice (the comparison policy): packed, data-dependent expert loads ----
 
-// Row block of the grouped GEMMs (the tile tables of the packed buffers count
-// ceil(M_e / TC_BM) row blocks per expert) and their column blocks.
-constexpr int TC_BM = 256;
-int tc_col_blocks_w13(int h);
-int tc_col_blocks_w2(int d);
 // G [N,E]: normalised gates of each token's top-k experts; flagT [E,N]: 1 if chosen.
 hipError_t launch_tc_topk(const float* S, int N, int E, int k, float* G, int32_t* flagT,
                           hipStream_t st);
 // cnt[(g0+g) E + j] = min(tokens of group g that chose j, cap_g) for the table's groups.
 hipError_t launch_tc_count(const int32_t* flagT, int N, int E, const GroupTable& tab, int g0,
                            int32_t* cnt, hipStream_t st);
-// Packed row offsets rows [E+1], per-(group, expert) row offsets seg [G,E] and the
-// tile offsets of the grouped products (tiles13, tiles2; [E+1] each).  Training (tilesA not
-// null): also those of the dA product, and order [E], in which the products that contract over
-// an expert's rows take the experts.
-hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13, int nt2, int ntA,
-                             int32_t* rows, int32_t* seg, int32_t* tiles13, int32_t* tiles2,
-                             int32_t* tilesA, int32_t* order, hipStream_t st);
+// Packed row offsets rows [E+1] and per-(group, expert) row offsets seg [G,E]; order [E]
+// (training; may be null): the experts as the products that contract over an expert's rows
+// take them.
+hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int32_t* rows, int32_t* seg,
+                             int32_t* order, hipStream_t st);
 // slotT: choice flags in, packed rows (-1: not kept) out; sel[row] = token.  Without
 // sel_gate G is zeroed on dropped pairs; with it (training) sel_gate[row] = scale G of the
 // pair and G keeps the gates of every choice.
 hipError_t launch_tc_place(int32_t* slotT, float* G, int N, int E, const GroupTable& tab, int g0,
                            const int32_t* seg, int32_t* sel, float* sel_gate, float scale,
                            hipStream_t st);
-// The forward products over packed rows: expert e owns rows [rows[e], rows[e+1]).
+// The forward products over packed rows: expert e owns rows [rows[e], rows[e+1]), max_rows
+// of all experts and max_rows_per_expert of each at most.
 // sel (may be null): Xe is then X itself and packed row r reads X[sel[r]].
 // gate (may be null): [max_rows] fp32, packed row r is written as A = gate[r] SiLU(H1) H3.
 // H1, H3 (may be null): [max_rows, h], the projections themselves.
 hipError_t launch_gemm_w13_var(int dtype, const void* Xe, const void* W1, const void* W3, void* A,
-                               void* H1, void* H3, int E, const int32_t* rows,
-                               const int32_t* tiles, long max_rows, int max_rows_per_expert, int d,
+                               void* H1, void* H3, int E, const int32_t* rows, long max_rows, int max_rows_per_expert, int d,
                                int h, hipStream_t st, const int32_t* sel = nullptr,
                                const float* gate = nullptr);
 hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O, int E,
-                              const int32_t* rows, const int32_t* tiles, long max_rows,
+                              const int32_t* rows, long max_rows,
                               int max_rows_per_expert, int d, int h, hipStream_t st);
-int tc_col_blocks_dA(int h);
 // The backward products over packed rows (conventions of launch_gemm_dA, _dXe, _dW2 and
 // _dW13): sel[r] is the token of packed row r, whose rows of dY (dA, dW2) and X (dW13) the
 // products read themselves.  dH [max_rows, 2h], dsp [max_rows, dsp_parts(dtype, h)].  An
 // expert without rows gets zero weight gradients.  order [E]: the experts as the weight
 // gradients take them (launch_tc_offsets).
 hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
-                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows,
-                              const int32_t* tiles, long max_rows, int max_rows_per_expert, int d,
+                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows, long max_rows, int max_rows_per_expert, int d,
                               int h, const int32_t* sel, const float* gate, hipStream_t st);
 hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const void* W3,
-                               void* dXe, int E, const int32_t* rows, const int32_t* tiles,
-                               long max_rows, int max_rows_per_expert, int d, int h,
-                               hipStream_t st);
+                               void* dXe, int E, const int32_t* rows, long max_rows,
+                               int max_rows_per_expert, int d, int h, hipStream_t st);
 hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
                                const int32_t* rows, const int32_t* order,
                                int max_rows_per_expert, int d, int h, const int32_t* sel,

@@ -121,15 +121,14 @@ struct GemmParams {
   float* dsp;
   int dsp_ld;
   // Variable rows per batch (token choice): batch e owns rows
-  // [var_rows[e], var_rows[e+1]) of A, C and H (row strides lda, ldc, ldh) and
-  // tiles [var_tiles[e], var_tiles[e+1]) of the launch; both device arrays of
-  // batches + 1 entries, null for a uniform batch of M rows.  With OPT_KVAR the
+  // [var_rows[e], var_rows[e+1]) of A, C and H (row strides lda, ldc, ldh), a
+  // device array of batches + 1 entries (batches <= 256), null for a uniform batch of
+  // M rows; the tiles follow from the rows (var_tile).  With OPT_KVAR the
   // rows are the contraction's instead (K-major operands: the weight gradients):
   // batch e contracts over rows [var_rows[e], var_rows[e+1]) of both, and its
   // outputs and tiles are those of a uniform batch; the tiles take the batches
   // in the order var_order [batches] (a device array).
   const int* var_rows;
-  const int* var_tiles;
   const int* var_order;
 };
 
@@ -796,6 +795,59 @@ constexpr int dma_smem_bytes() {
   return STAGES * STAGE_BYTES > STAGE_EPI ? STAGES * STAGE_BYTES : STAGE_EPI;
 }
 
+// A tile of batches of variable rows: batch e, whose rows start at row0 and number M; its
+// rem-th tile.
+struct VarTile {
+  int e, rem, row0, M;
+};
+
+// The tile of workgroup `bid` of batches of variable rows, in tiles of bm rows times nt
+// columns; false past the last one (their number is known only here: the grid is an upper
+// bound).  The tiles are numbered batch after batch, an eighth of them in sequence on each XCD.
+// Every wave works it out for itself in one round trip to memory: lane l counts the tiles of
+// batches 4 l .. 4 l + 3, and a prefix sum over the lanes finds the one that holds the tile.
+__device__ __forceinline__ bool var_tile(const int* __restrict__ rows, int batches, int bm, int nt,
+                                         int bid, VarTile* out) {
+  const int lane = threadIdx.x & 63;
+  int r[5], n[4], s = 0;
+#pragma unroll
+  for (int i = 0; i < 5; ++i) r[i] = rows[4 * lane + i < batches ? 4 * lane + i : batches];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    n[i] = (r[i + 1] - r[i] + bm - 1) / bm * nt;
+    s += n[i];
+  }
+  int incl = s;   // inclusive prefix: within rows of 16 lanes, then the rows before
+  incl += (int)dpp_u32<0x111>((uint32_t)incl);
+  incl += (int)dpp_u32<0x112>((uint32_t)incl);
+  incl += (int)dpp_u32<0x114>((uint32_t)incl);
+  incl += (int)dpp_u32<0x118>((uint32_t)incl);
+  const int s0 = __builtin_amdgcn_readlane(incl, 15), s1 = __builtin_amdgcn_readlane(incl, 31),
+            s2 = __builtin_amdgcn_readlane(incl, 47);
+  const int row = lane >> 4;
+  incl += row == 0 ? 0 : row == 1 ? s0 : row == 2 ? s0 + s1 : s0 + s1 + s2;
+  const int total = __builtin_amdgcn_readlane(incl, 63);
+  const int per_xcd = (total + 7) >> 3, j = bid >> 3;
+  if (j >= per_xcd) return false;
+  const int t = (bid & 7) * per_xcd + j;
+  if (t >= total) return false;
+  const int at = __builtin_ctzll(__ballot(incl > t));   // incl grows with the lane
+  int x = t - (incl - s), i = 0, row0 = r[0], end = r[1];
+#pragma unroll
+  for (int u = 0; u < 3; ++u)
+    if (i == u && x >= n[u]) {
+      x -= n[u];
+      i = u + 1;
+      row0 = r[u + 1];
+      end = r[u + 2];
+    }
+  out->e = __builtin_amdgcn_readlane(4 * lane + i, at);
+  out->rem = __builtin_amdgcn_readlane(x, at);
+  out->row0 = __builtin_amdgcn_readlane(row0, at);
+  out->M = __builtin_amdgcn_readlane(end, at) - out->row0;
+  return true;
+}
+
 // One output tile per workgroup; consecutive tile ids (same expert) are kept
 // on one XCD so that its L2 serves their shared A rows and B columns.
 template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bool B_KC, int EPI,
@@ -807,25 +859,14 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
   int rem, MT;
   constexpr bool KVAR = (OPT & OPT_KVAR) != 0;
   if (!KVAR && p.var_rows) {
-    // the tile count is known only on the device: the grid is an upper bound,
-    // and the XCD-contiguous numbering uses the actual count
-    const int total = p.var_tiles[p.batches];
-    const int per_xcd = (total + 7) >> 3;
-    const int j = blockIdx.x >> 3;
-    if (j >= per_xcd) return;
-    const int t = (blockIdx.x & 7) * per_xcd + j;
-    if (t >= total) return;
-    int lo = 0, hi = p.batches;          // var_tiles[lo] <= t < var_tiles[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (p.var_tiles[mid] <= t) lo = mid; else hi = mid;
-    }
-    const int row0 = p.var_rows[lo];
-    tc.e = lo;
+    VarTile v;
+    if (!var_tile(p.var_rows, p.batches, BM, p.NT, blockIdx.x, &v)) return;
+    const int row0 = v.row0;
+    tc.e = v.e;
     tc.row0 = row0;
-    tc.M = p.var_rows[lo + 1] - row0;
+    tc.M = v.M;
     MT = (tc.M + BM - 1) / BM;
-    rem = t - p.var_tiles[lo];
+    rem = v.rem;
     tc.a_off = (size_t)row0 * p.lda;
     tc.c_off = (size_t)row0 * p.ldc;
     tc.h_off = (size_t)row0 * p.ldh;
@@ -939,7 +980,7 @@ hipError_t run_dma(GemmParams p, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Variable rows per batch (p.var_rows / p.var_tiles on the device): the grid
+// Variable rows per batch (p.var_rows on the device): the grid
 // covers max_rows rows in total plus one partial row block per batch.
 template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bool B_KC, int EPI,
           bool OUT_F32, int TAG, int OPT>
@@ -1067,33 +1108,37 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
                 "a K-major operand may be gathered");
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE_BYTES];
 
-  const int t = xcd_tile_id(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
-  const int per_b = p.MT * p.NT;
-  if (t >= p.batches * per_b) return;
-  int e = t / per_b;
-  const int rem = t - e * per_b;
-  if constexpr (KVAR) e = p.var_order[e];
-  const int m0 = rem % p.MT * BM;
-  const int n0 = rem / p.MT * (EPI == EPI_SWIGLU ? BN / 2 : BN);
-  // rows of this batch: uniform (M), or [var_rows[e], var_rows[e+1]) of packed buffers
-  int M = p.M, row0 = 0, K = p.K, kv_a = p.kv_a, kv_b = p.kv_b;
-  size_t a_off = (size_t)e * p.a_bs, c_off = (size_t)e * p.c_bs, h_off = (size_t)e * p.h_bs;
-  size_t b_off = (size_t)e * p.b_bs, row = (size_t)e * p.M, k_rows = (size_t)e * p.k_rows_bs;
-  if constexpr (KVAR) {
-    row0 = p.var_rows[e];
-    K = kv_a = kv_b = p.var_rows[e + 1] - row0;
-    a_off = (size_t)row0 * p.lda;
-    b_off = (size_t)row0 * p.ldb;
-    k_rows = row0;
-  } else if (p.var_rows) {
-    row0 = p.var_rows[e];
-    row = row0;
-    M = p.var_rows[e + 1] - row0;
-    a_off = (size_t)row0 * p.lda;
-    c_off = (size_t)row0 * p.ldc;
-    h_off = (size_t)row0 * p.ldh;
+  const int bid = blockIdx.y * gridDim.x + blockIdx.x;
+  int e, rem, M = p.M, MT = p.MT, row0 = 0, K = p.K, kv_a = p.kv_a, kv_b = p.kv_b;
+  const bool var_m = !KVAR && p.var_rows;
+  if (var_m) {   // rows of the batch: [var_rows[e], var_rows[e+1]) of packed buffers
+    VarTile v;
+    if (!var_tile(p.var_rows, p.batches, BM, p.NT, bid, &v)) return;
+    e = v.e;
+    rem = v.rem;
+    row0 = v.row0;
+    M = v.M;
+    MT = (M + BM - 1) / BM;
+  } else {
+    const int t = xcd_tile_id(bid, gridDim.x * gridDim.y);
+    const int per_b = p.MT * p.NT;
+    if (t >= p.batches * per_b) return;
+    e = t / per_b;
+    rem = t - e * per_b;
+    if constexpr (KVAR) {
+      e = p.var_order[e];
+      row0 = p.var_rows[e];
+      K = kv_a = kv_b = p.var_rows[e + 1] - row0;
+    }
   }
-  if (m0 >= M) return;
+  const int m0 = rem % MT * BM;
+  const int n0 = rem / MT * (EPI == EPI_SWIGLU ? BN / 2 : BN);
+  const size_t a_off = var_m || KVAR ? (size_t)row0 * p.lda : (size_t)e * p.a_bs;
+  const size_t b_off = KVAR ? (size_t)row0 * p.ldb : (size_t)e * p.b_bs;
+  const size_t c_off = var_m ? (size_t)row0 * p.ldc : (size_t)e * p.c_bs;
+  const size_t h_off = var_m ? (size_t)row0 * p.ldh : (size_t)e * p.h_bs;
+  const size_t row = var_m ? (size_t)row0 : (size_t)e * p.M;       // of gate and dsp
+  const size_t k_rows = KVAR ? (size_t)row0 : (size_t)e * p.k_rows_bs;
   const float* A = (const float*)p.A + a_off;
   const float* B = (const float*)p.B + b_off;
   const float* B2 = p.B2 ? (const float*)p.B2 + (size_t)e * p.b_bs : nullptr;
@@ -1310,15 +1355,18 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
   }
 }
 
+// max_rows: of all batches together, with variable rows (OPT_KVAR aside).
 template <int BM, int BN, int WGM, int WGN, bool A_KC, bool B_KC, int EPI, int OPT>
-hipError_t launch_f32_tile(GemmParams p, hipStream_t st) {
+hipError_t launch_f32_tile(GemmParams p, long max_rows, hipStream_t st) {
   p.MT = (p.M + BM - 1) / BM;
   p.NT = (EPI == EPI_SWIGLU) ? (p.N + BN / 2 - 1) / (BN / 2) : (p.N + BN - 1) / BN;
-  const long ntile = (long)p.batches * p.MT * p.NT;
+  // variable rows: one partial row block per batch at most
+  const bool var_m = (OPT & OPT_KVAR) == 0 && p.var_rows;
+  const long blocks = var_m ? (max_rows + BM - 1) / BM + p.batches : (long)p.batches * p.MT;
+  const long ntile = blocks * p.NT;
   if (ntile == 0) return hipSuccess;
   if (ntile >= (1l << 30)) return hipErrorInvalidValue;   // 2^26 at the size limits
-  // One dimension of a launch ends below 2^32 threads, which token choice passes (its
-  // grid covers every token for every expert): rows of at most 2^23 workgroups, whole
+  // One dimension of a launch ends below 2^32 threads: rows of at most 2^23 workgroups, whole
   // rounds of the XCDs each.
   const long rows = (ntile + (1l << 23) - 1) >> 23;
   const long per_row = ((ntile + rows - 1) / rows + 7) / 8 * 8;
@@ -1327,17 +1375,22 @@ hipError_t launch_f32_tile(GemmParams p, hipStream_t st) {
   return hipGetLastError();
 }
 
-// OPT: as in run_dma.
+// OPT, max_rows: as in run_dma and run_dma_var.
 template <bool A_KC, bool B_KC, int EPI, int OPT = 0>
-hipError_t run_f32(const GemmParams& p, hipStream_t st) {
+hipError_t run_f32(const GemmParams& p, hipStream_t st, long max_rows = 0) {
   if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr) ||
       ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) ||
       ((OPT & OPT_KVAR) != 0 && (p.var_rows == nullptr || p.var_order == nullptr)))
     return hipErrorInvalidValue;
   const int nw = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
-  const long big = (long)p.batches * ((p.M + 127) / 128) * ((nw + 127) / 128);
-  if (big >= F32_BIG_TILES) return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, st);
-  return launch_f32_tile<64, 64, 2, 1, A_KC, B_KC, EPI, OPT>(p, st);
+  // variable rows: the row blocks of max_rows in one and half a block more per batch
+  const bool var_m = (OPT & OPT_KVAR) == 0 && p.var_rows;
+  const long blocks = var_m ? max_rows / 128 + (p.batches + 1) / 2
+                            : (long)p.batches * ((p.M + 127) / 128);
+  const long big = blocks * ((nw + 127) / 128);
+  if (big >= F32_BIG_TILES)
+    return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
+  return launch_f32_tile<64, 64, 2, 1, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
 }
 
 GemmParams base_params() {
@@ -1609,12 +1662,8 @@ hipError_t launch_shared_dW13(int dtype, const void* dH, const void* X, void* dW
                                      st);
 }
 
-int tc_col_blocks_w13(int h) { return (h + 127) / 128; }
-int tc_col_blocks_w2(int d) { return (d + 255) / 256; }
-
 hipError_t launch_gemm_w13_var(int dtype, const void* Xe, const void* W1, const void* W3, void* A,
-                               void* H1, void* H3, int E, const int32_t* rows,
-                               const int32_t* tiles, long max_rows, int max_rows_per_expert, int d,
+                               void* H1, void* H3, int E, const int32_t* rows, long max_rows, int max_rows_per_expert, int d,
                                int h, hipStream_t st, const int32_t* sel, const float* gate) {
   GemmParams p = base_params();
   p.gate = gate; p.H1 = H1; p.H3 = H3;
@@ -1625,31 +1674,28 @@ hipError_t launch_gemm_w13_var(int dtype, const void* Xe, const void* W1, const 
   p.B = W1; p.B2 = W3; p.b_bs = (long)h * d; p.ldb = d;
   p.M = max_rows_per_expert; p.N = h; p.K = d; p.kv_a = d; p.kv_b = d; p.batches = E;
   p.C = A; p.ldc = h; p.ldh = h;
-  p.var_rows = rows; p.var_tiles = tiles;
+  p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
-  if (dtype == DT_F32) return run_f32<true, true, EPI_SWIGLU>(p, st);
+  if (dtype == DT_F32) return run_f32<true, true, EPI_SWIGLU>(p, st, max_rows);
   return run_fwd<256, EPI_SWIGLU, G_TC_W13, OPT_TAILS, true>(p, st, max_rows);
 }
 
 hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O, int E,
-                              const int32_t* rows, const int32_t* tiles, long max_rows,
+                              const int32_t* rows, long max_rows,
                               int max_rows_per_expert, int d, int h, hipStream_t st) {
   GemmParams p = base_params();
   p.A = A; p.lda = h;
   p.B = W2; p.b_bs = (long)d * h; p.ldb = h;
   p.M = max_rows_per_expert; p.N = d; p.K = h; p.kv_a = h; p.kv_b = h; p.batches = E;
   p.C = O; p.ldc = d;
-  p.var_rows = rows; p.var_tiles = tiles;
+  p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
-  if (dtype == DT_F32) return run_f32<true, true, EPI_STORE>(p, st);
+  if (dtype == DT_F32) return run_f32<true, true, EPI_STORE>(p, st, max_rows);
   return run_fwd<256, EPI_STORE, G_TC_W2, OPT_TAILS, true>(p, st, max_rows);
 }
 
-int tc_col_blocks_dA(int h) { return (h + 255) / 256; }
-
 hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
-                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows,
-                              const int32_t* tiles, long max_rows, int max_rows_per_expert, int d,
+                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows, long max_rows, int max_rows_per_expert, int d,
                               int h, const int32_t* sel, const float* gate, hipStream_t st) {
   GemmParams p = base_params();
   p.A = dY; p.lda = d; p.a_rows = sel;
@@ -1660,25 +1706,24 @@ hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const v
   p.C = dH; p.C2 = (char*)dH + (size_t)h * esz; p.ldc = 2 * h;
   p.H1 = (void*)H1; p.H3 = (void*)H3; p.ldh = h;
   p.dsp = dsp; p.dsp_ld = dsp_parts(dtype, h);
-  p.var_rows = rows; p.var_tiles = tiles;
+  p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
-  if (dtype == DT_F32) return run_f32<true, false, EPI_SWIGLU_BWD>(p, st);
+  if (dtype == DT_F32) return run_f32<true, false, EPI_SWIGLU_BWD>(p, st, max_rows);
   return run_dma_var<256, 256, 4, 2, 64, 2, true, false, EPI_SWIGLU_BWD, false, G_TC_DA, OPT_TAILS>(
       p, max_rows, st);
 }
 
 hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const void* W3,
-                               void* dXe, int E, const int32_t* rows, const int32_t* tiles,
-                               long max_rows, int max_rows_per_expert, int d, int h,
-                               hipStream_t st) {
+                               void* dXe, int E, const int32_t* rows, long max_rows,
+                               int max_rows_per_expert, int d, int h, hipStream_t st) {
   GemmParams p = base_params();
   p.A = dH; p.lda = 2 * h;
   p.B = W1; p.B2 = W3; p.b_bs = (long)h * d; p.ldb = d; p.k_split = h;
   p.M = max_rows_per_expert; p.N = d; p.K = 2 * h; p.kv_a = 2 * h; p.kv_b = 2 * h; p.batches = E;
   p.C = dXe; p.ldc = d;
-  p.var_rows = rows; p.var_tiles = tiles;
+  p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
-  if (dtype == DT_F32) return run_f32<true, false, EPI_STORE>(p, st);
+  if (dtype == DT_F32) return run_f32<true, false, EPI_STORE>(p, st, max_rows);
   return run_dma_var<256, 256, 4, 2, 64, 2, true, false, EPI_STORE, false, G_TC_DXE, OPT_TAILS>(
       p, max_rows, st);
 }

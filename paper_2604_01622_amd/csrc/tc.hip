@@ -4,8 +4,8 @@
 // j keeps at most cap_g of the tokens of routing group g that chose it, the
 // lowest token indices first, and drops the others.  Per-expert loads are
 // data dependent, so the kept pairs are packed expert after expert into one
-// buffer and the grouped GEMMs read a per-expert (row, tile) offset table
-// from device memory.
+// buffer and the grouped GEMMs read the experts' row offsets from device
+// memory.
 #include "ec_common.h"
 #include "ec_kernels.h"
 
@@ -122,63 +122,40 @@ __global__ __launch_bounds__(256) void tc_count_kernel(const int32_t* __restrict
 
 // Offsets, one workgroup (thread j for expert j, E <= 256): expert j's packed
 // rows start at rows[j] (rows[E] = all kept pairs); group g's tokens in expert
-// j start at seg[g E + j]; the tiles of the two grouped products start at
-// tiles13[j] and tiles2[j] (ceil(M_j / bm) row blocks times nt13 / nt2), those of the
-// training backward's dA product at tilesA[j] (unless null).  With tilesA also order [E]: a
+// j start at seg[g E + j].  order [E] (may be null): a
 // product that contracts over an expert's rows takes as long for the expert's every tile as
 // it has rows, and each XCD takes an eighth of the list, so the experts are dealt to the
 // eighths by falling row counts, there and back.
 __global__ __launch_bounds__(256) void tc_offsets_kernel(const int32_t* __restrict__ cnt, int G,
-                                                         int E, int bm, int nt13, int nt2, int ntA,
-                                                         int32_t* __restrict__ rows,
+                                                         int E, int32_t* __restrict__ rows,
                                                          int32_t* __restrict__ seg,
-                                                         int32_t* __restrict__ tiles13,
-                                                         int32_t* __restrict__ tiles2,
-                                                         int32_t* __restrict__ tilesA,
                                                          int32_t* __restrict__ order) {
-  __shared__ int sm[256], st[256];
+  __shared__ int sm[256];
   const int j = threadIdx.x;
   int m = 0;
   if (j < E)
     for (int g = 0; g < G; ++g) m += cnt[(size_t)g * E + j];
   sm[j] = m;
-  st[j] = (m + bm - 1) / bm;
   __syncthreads();
-  if (order && j < E) {
-    int rank = 0;
-    for (int q = 0; q < E; ++q) rank += sm[q] > m || (sm[q] == m && q < j);
+  if (j >= E) return;
+  int first = 0, rank = 0;
+  for (int q = 0; q < E; ++q) {
+    const int mq = sm[q];   // the same word for every lane
+    first += q < j ? mq : 0;
+    rank += mq > m || (mq == m && q < j);
+  }
+  rows[j] = first;
+  if (j == E - 1) rows[E] = first + m;
+  if (order) {
     const int round = rank >> 3, x = (round & 1) ? 7 - (rank & 7) : rank & 7;
     // eighths before x: a full round each, and those that the last round reaches
     const int full = E >> 3, rest = E & 7;
     const int before = (full & 1) ? (x > 8 - rest ? x - (8 - rest) : 0) : (x < rest ? x : rest);
     order[x * full + before + round] = j;
   }
-  __syncthreads();
-  if (j == 0) {   // E <= 256 sequential prefix sums
-    int r = 0, tt = 0;
-    for (int q = 0; q < E; ++q) {
-      const int mq = sm[q], tq = st[q];
-      sm[q] = r;
-      st[q] = tt;
-      r += mq;
-      tt += tq;
-    }
-    rows[E] = r;
-    tiles13[E] = tt * nt13;
-    tiles2[E] = tt * nt2;
-    if (tilesA) tilesA[E] = tt * ntA;
-  }
-  __syncthreads();
-  if (j < E) {
-    rows[j] = sm[j];
-    tiles13[j] = st[j] * nt13;
-    tiles2[j] = st[j] * nt2;
-    if (tilesA) tilesA[j] = st[j] * ntA;
-    int r = sm[j];
-    for (int g = 0; g < G; ++g) {
-      seg[(size_t)g * E + j] = r;
-      r += cnt[(size_t)g * E + j];
-    }
+  for (int g = 0; g < G; ++g) {
+    seg[(size_t)g * E + j] = first;
+    first += cnt[(size_t)g * E + j];
   }
 }
 
@@ -251,11 +228,9 @@ hipError_t launch_tc_count(const int32_t* flagT, int N, int E, const GroupTable&
   return hipGetLastError();
 }
 
-hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int bm, int nt13, int nt2, int ntA,
-                             int32_t* rows, int32_t* seg, int32_t* tiles13, int32_t* tiles2,
-                             int32_t* tilesA, int32_t* order, hipStream_t st) {
-  tc_offsets_kernel<<<1, 256, 0, st>>>(cnt, G, E, bm, nt13, nt2, ntA, rows, seg, tiles13, tiles2,
-                                       tilesA, order);
+hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int32_t* rows, int32_t* seg,
+                             int32_t* order, hipStream_t st) {
+  tc_offsets_kernel<<<1, 256, 0, st>>>(cnt, G, E, rows, seg, order);
   return hipGetLastError();
 }
 
