@@ -220,7 +220,8 @@ __device__ __forceinline__ int km_swz(int k) { return ((k & 3) << 2) | ((k >> 2)
 // the last row block and column block take a smaller tile where one holds them.
 // OPT_TILE_BASE: an ungathered K-contiguous A of any size, addressed tile by tile.
 // OPT_KVAR: the batches contract over rows of their own (GemmParams.var_rows).
-enum { OPT_GA = 1, OPT_GB = 2, OPT_TAILS = 4, OPT_TILE_BASE = 8, OPT_KVAR = 16 };
+// OPT_MVAR: the batches have rows of their own.
+enum { OPT_GA = 1, OPT_GB = 2, OPT_TAILS = 4, OPT_TILE_BASE = 8, OPT_KVAR = 16, OPT_MVAR = 32 };
 template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bool B_KC, int EPI,
           bool OUT_F32, int OPT>
 __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoord& tc,
@@ -858,7 +859,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
   TileCoord tc;
   int rem, MT;
   constexpr bool KVAR = (OPT & OPT_KVAR) != 0;
-  if (!KVAR && p.var_rows) {
+  if constexpr ((OPT & OPT_MVAR) != 0) {
     VarTile v;
     if (!var_tile(p.var_rows, p.batches, BM, p.NT, blockIdx.x, &v)) return;
     const int row0 = v.row0;
@@ -985,13 +986,14 @@ hipError_t run_dma(GemmParams p, hipStream_t st) {
 template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bool B_KC, int EPI,
           bool OUT_F32, int TAG, int OPT>
 hipError_t run_dma_var(GemmParams p, long max_rows, hipStream_t st) {
+  if (!p.var_rows || p.batches > 256) return hipErrorInvalidValue;
   if (!operands_in_reach<A_KC, B_KC, OPT>(p)) return hipErrorInvalidValue;
   p.MT = 0;
   p.NT = (EPI == EPI_SWIGLU) ? (p.N + BN / 2 - 1) / (BN / 2) : (p.N + BN - 1) / BN;
   const long ntile = ((max_rows + BM - 1) / BM + p.batches) * p.NT;
   if (ntile == 0 || p.batches == 0) return hipSuccess;
   const long grid = (ntile + 7) / 8 * 8;
-  gemm_dma_kernel<BM, BN, WGM, WGN, KSTEP, STAGES, A_KC, B_KC, EPI, OUT_F32, TAG, OPT>
+  gemm_dma_kernel<BM, BN, WGM, WGN, KSTEP, STAGES, A_KC, B_KC, EPI, OUT_F32, TAG, OPT | OPT_MVAR>
       <<<dim3((unsigned)grid), 64 * WGM * WGN, 0, st>>>(p);
   return hipGetLastError();
 }
@@ -1057,6 +1059,69 @@ hipError_t run_fwd(const GemmParams& p, hipStream_t st, long max_rows = 0) {
                                                              : run(std::integral_constant<int, 2>{});
 }
 
+// Tiles of batches of variable rows, whose counts the host does not know: it expects half a
+// row block more per batch than max_rows fills, one at least.  What counts is how many tiles
+// a CU takes one after the other (`at_once` run together); past the first, half a tile is
+// the expected wait for the last.
+double var_rounds(const GemmParams& p, long max_rows, int bm, int nt, int at_once) {
+  double blocks = (double)max_rows / bm + 0.5 * p.batches;
+  if (blocks < p.batches) blocks = p.batches;
+  const double t = blocks * nt / at_once;
+  return t <= 1.0 ? 1.0 : t + 0.5;
+}
+
+// Few rows an expert in enough tiles only stream the weights: 256-row tiles, whose short
+// last blocks (OPT_TAILS) are then all there is.
+bool var_streams(const GemmParams& p, long max_rows, int nt) {
+  return max_rows <= 96l * p.batches && (long)p.batches * nt > 128;
+}
+
+// A forward product over packed rows: 256-row tiles, or smaller ones where those leave CUs
+// idle or end in a poorly filled round, by var_rounds and the time of a tile relative to a
+// 256 x 256 one (192 rows 0.85; 128 rows, three stages, 0.65; 128 x 128 0.4).  Measured
+// with rows spread by a factor of 1.35, us of W1/W3 in tiles of 256, 192, 128 rows and 128 x
+// 128: 8 experts x 128 rows, d 2048, h 1024 54, 46, 38 and 31; x 600 65, 52, 65 and 77; 16 x
+// 300, d 1024, h 512 38, 28, 23 and 32; 64 x 128, d 2048, h 1024 186, 183, 164 and 197; x 256
+// 193, 222, 208 and 284; x 512 296, 362, 372 and 503; 64 rows (streaming) 144, 143, 159 and
+// 157.  W2 follows (8 x 128 31, 24, 20, 17; 64 x 128 114, 112, 95, 105; x 512 180, 206, 197,
+// 267).
+template <int EPI, int TAG>
+hipError_t run_fwd_var(const GemmParams& p, long max_rows, hipStream_t st) {
+  const int width = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
+  const int nt = (width + 255) / 256, nt128 = (width + 127) / 128;
+  if (!var_streams(p, max_rows, nt)) {
+    const double t256 = var_rounds(p, max_rows, 256, nt, 256);
+    const double t192 = 0.85 * var_rounds(p, max_rows, 192, nt, 256);
+    const double t128 = 0.65 * var_rounds(p, max_rows, 128, nt, 256);
+    const double tsq = 0.4 * var_rounds(p, max_rows, 128, nt128, 256);
+    if (tsq < t128 && tsq < t192 && tsq < t256)
+      return run_dma_var<128, 128, 2, 2, 64, 3, true, true, EPI, false, TAG, 0>(p, max_rows, st);
+    if (t128 < t192 && t128 < t256)
+      return run_dma_var<128, 256, 2, 4, 64, 3, true, true, EPI, false, TAG, 0>(p, max_rows, st);
+    if (t192 < t256)
+      return run_dma_var<192, 256, 2, 2, 64, 2, true, true, EPI, false, TAG, 0>(p, max_rows, st);
+  }
+  return run_fwd<256, EPI, TAG, OPT_TAILS, true>(p, st, max_rows);
+}
+
+// A backward product over packed rows (K-major weights): 256 x 256 tiles, or 128 x 128, two
+// at a time on a CU, by the same estimate; rel: a CU's time for two of these relative to a
+// 256 x 256 one's (dA 0.6, whose epilogues then overlap the other's MFMAs; dX 0.7).
+// Measured as above, 256 x 256 against 128 x 128: dA of 8 experts x 600 rows, d 2048, h 1024
+// 61 and 44, 64 x 160 143 and 119, x 256 148 and 150, x 512 210 and 234, 24 x 400, d 1024, h
+// 1024 47 and 53; dX 8 x 128 63 and 40, 64 x 128 175 and 165, x 256 191 and 219.
+template <int EPI, int TAG>
+hipError_t run_bwd_var(const GemmParams& p, long max_rows, double rel, hipStream_t st) {
+  constexpr int GM = EPI == EPI_SWIGLU_BWD ? 4 : 2;
+  const int nt = (p.N + 255) / 256, nt128 = (p.N + 127) / 128;
+  if (!var_streams(p, max_rows, nt) &&
+      rel * var_rounds(p, max_rows, 128, nt128, 512) < var_rounds(p, max_rows, 256, nt, 256))
+    return run_dma_var<128, 128, GM, 4 / GM, 64, 2, true, false, EPI, false, TAG, 0>(p, max_rows,
+                                                                                     st);
+  return run_dma_var<256, 256, 4, 2, 64, 2, true, false, EPI, false, TAG, OPT_TAILS>(p, max_rows,
+                                                                                     st);
+}
+
 // Buffers of one 128-row block (three stages): 128 x 128 tiles of four waves while there
 // is at most one per CU; 128 x 256 of eight, which read the rows half as often, where
 // those are at most one per CU.  Past that W1/W3 takes the narrow and W2 the wide ones, by
@@ -1092,6 +1157,13 @@ constexpr int FK = 32;   // k-step
 // read a third more LDS per MFMA and meet at twice as many barriers: 1037 against 795 us
 // a training step); below that 64 x 64 tiles keep more CUs busy.
 constexpr long F32_BIG_TILES = 256;
+// Packed rows: 64 x 128 tiles of four waves, three workgroups a CU, which end their rounds
+// more evenly (us, 128 x 128 against 64 x 128: W1/W3 of 16 experts x 250 rows, d 1024, h 512
+// 151 and 117, x 2000 655 and 587; dA 94 and 90, 421 and 354; 64 experts x 300 rows 316 and
+// 258; dX 152 and 128, 632 and 630).  The weight gradients take 128 x 128 tiles from two per
+// CU on (16 x 250 rows, dW2 in 512 tiles 53 and 59, dW1/dW3 in 1024 97 and 106; 8 x 1000, dW2
+// in 256 105 and 100; 17 x 900, d 512, h 512, in 272 145 and 111).
+constexpr long F32_BIG_KVAR_TILES = 512;
 
 template <int BM, int BN, int WGM, int WGN, bool A_KC, bool B_KC, int EPI, int OPT>
 __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) {
@@ -1383,11 +1455,12 @@ hipError_t run_f32(const GemmParams& p, hipStream_t st, long max_rows = 0) {
       ((OPT & OPT_KVAR) != 0 && (p.var_rows == nullptr || p.var_order == nullptr)))
     return hipErrorInvalidValue;
   const int nw = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
-  // variable rows: the row blocks of max_rows in one and half a block more per batch
-  const bool var_m = (OPT & OPT_KVAR) == 0 && p.var_rows;
-  const long blocks = var_m ? max_rows / 128 + (p.batches + 1) / 2
-                            : (long)p.batches * ((p.M + 127) / 128);
-  const long big = blocks * ((nw + 127) / 128);
+  const long big = (long)p.batches * ((p.M + 127) / 128) * ((nw + 127) / 128);
+  if (p.var_rows) {
+    if (!((OPT & OPT_KVAR) != 0 && big >= F32_BIG_KVAR_TILES))
+      return launch_f32_tile<64, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
+    return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
+  }
   if (big >= F32_BIG_TILES)
     return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
   return launch_f32_tile<64, 64, 2, 1, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
@@ -1677,7 +1750,7 @@ hipError_t launch_gemm_w13_var(int dtype, const void* Xe, const void* W1, const 
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, true, EPI_SWIGLU>(p, st, max_rows);
-  return run_fwd<256, EPI_SWIGLU, G_TC_W13, OPT_TAILS, true>(p, st, max_rows);
+  return run_fwd_var<EPI_SWIGLU, G_TC_W13>(p, max_rows, st);
 }
 
 hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O, int E,
@@ -1691,7 +1764,7 @@ hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O,
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, true, EPI_STORE>(p, st, max_rows);
-  return run_fwd<256, EPI_STORE, G_TC_W2, OPT_TAILS, true>(p, st, max_rows);
+  return run_fwd_var<EPI_STORE, G_TC_W2>(p, max_rows, st);
 }
 
 hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
@@ -1709,8 +1782,7 @@ hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const v
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, false, EPI_SWIGLU_BWD>(p, st, max_rows);
-  return run_dma_var<256, 256, 4, 2, 64, 2, true, false, EPI_SWIGLU_BWD, false, G_TC_DA, OPT_TAILS>(
-      p, max_rows, st);
+  return run_bwd_var<EPI_SWIGLU_BWD, G_TC_DA>(p, max_rows, 0.6, st);
 }
 
 hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const void* W3,
@@ -1724,8 +1796,7 @@ hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const 
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, false, EPI_STORE>(p, st, max_rows);
-  return run_dma_var<256, 256, 4, 2, 64, 2, true, false, EPI_STORE, false, G_TC_DXE, OPT_TAILS>(
-      p, max_rows, st);
+  return run_bwd_var<EPI_STORE, G_TC_DXE>(p, max_rows, 0.7, st);
 }
 
 hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
@@ -1740,6 +1811,12 @@ hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* d
   p.C = dW2; p.c_bs = (long)d * h; p.ldc = h;
   p.var_rows = rows; p.var_order = order;
   if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GA | OPT_KVAR>(p, st);
+  // few tiles: half as wide, so that they fill the chip (128 rows, us: 64 experts, d 512, h
+  // 256, 128 tiles of 256 x 256 17 and 13; 32 experts, d 768, h 512, 192 tiles 24 and 21; 8
+  // experts, d 2048, h 1024, 256 tiles 16 and 18)
+  if ((long)E * ((d + 255) / 256) * ((h + 255) / 256) <= 192)
+    return run_dma<256, 128, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW2,
+                   OPT_GA | OPT_KVAR>(p, st);
   return run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW2,
                  OPT_GA | OPT_TAILS | OPT_KVAR>(p, st);
 }
