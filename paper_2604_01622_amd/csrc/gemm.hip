@@ -127,9 +127,11 @@ struct GemmParams {
   // rows are the contraction's instead (K-major operands: the weight gradients):
   // batch e contracts over rows [var_rows[e], var_rows[e+1]) of both, and its
   // outputs and tiles are those of a uniform batch; the tiles take the batches
-  // in the order var_order [batches] (a device array).
+  // in the order var_order [batches] (a device array).  Without var_rows its
+  // batches are a split of k_total rows: K rows each, the last one what is left.
   const int* var_rows;
   const int* var_order;
+  int k_total;
 };
 
 // Where one output tile sits: batch, first row and column, the batch's rows,
@@ -878,7 +880,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
     const int per_b = p.MT * p.NT;
     tc.e = t / per_b;
     rem = t - tc.e * per_b;
-    if constexpr (KVAR) tc.e = p.var_order[tc.e];
+    if constexpr (KVAR)
+      if (p.var_rows) tc.e = p.var_order[tc.e];
     tc.row0 = 0;
     tc.M = p.M;
     tc.row = (size_t)tc.e * p.M;
@@ -887,8 +890,13 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
     tc.c_off = (size_t)tc.e * p.c_bs;
     tc.h_off = (size_t)tc.e * p.h_bs;
     if constexpr (KVAR) {
-      tc.row0 = p.var_rows[tc.e];
-      tc.K = p.var_rows[tc.e + 1] - tc.row0;
+      if (p.var_rows) {
+        tc.row0 = p.var_rows[tc.e];
+        tc.K = p.var_rows[tc.e + 1] - tc.row0;
+      } else {
+        tc.row0 = tc.e * p.K;
+        tc.K = p.k_total - tc.row0 < p.K ? p.k_total - tc.row0 : p.K;
+      }
       tc.a_off = (size_t)tc.row0 * p.lda;
     }
   }
@@ -953,6 +961,13 @@ bool operands_in_reach(const GemmParams& p) {
   return a <= (long)BUF_BYTES && b <= (long)BUF_BYTES;
 }
 
+// The rows that OPT_KVAR's batches contract over: their own, or a split of k_total that
+// leaves every batch some.
+bool kvar_given(const GemmParams& p) {
+  if (p.var_rows) return p.var_order != nullptr;
+  return p.k_total > 0 && (long)(p.batches - 1) * p.K < p.k_total;
+}
+
 // OPT: the options of the instantiation; the pointers of each option must be
 // set exactly when it is.
 template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bool B_KC, int EPI,
@@ -960,7 +975,7 @@ template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bo
 hipError_t run_dma(GemmParams p, hipStream_t st) {
   if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr) ||
       ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) ||
-      ((OPT & OPT_KVAR) != 0) != (p.var_rows != nullptr && p.var_order != nullptr))
+      ((OPT & OPT_KVAR) != 0 ? !kvar_given(p) : p.var_rows != nullptr))
     return hipErrorInvalidValue;
   if (!operands_in_reach<A_KC, B_KC, OPT>(p)) return hipErrorInvalidValue;
   p.MT = (p.M + BM - 1) / BM;
@@ -1198,9 +1213,15 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
     e = t / per_b;
     rem = t - e * per_b;
     if constexpr (KVAR) {
-      e = p.var_order[e];
-      row0 = p.var_rows[e];
-      K = kv_a = kv_b = p.var_rows[e + 1] - row0;
+      if (p.var_rows) {
+        e = p.var_order[e];
+        row0 = p.var_rows[e];
+        K = p.var_rows[e + 1] - row0;
+      } else {
+        row0 = e * p.K;
+        K = p.k_total - row0 < p.K ? p.k_total - row0 : p.K;
+      }
+      kv_a = kv_b = K;
     }
   }
   const int m0 = rem % MT * BM;
@@ -1452,12 +1473,12 @@ template <bool A_KC, bool B_KC, int EPI, int OPT = 0>
 hipError_t run_f32(const GemmParams& p, hipStream_t st, long max_rows = 0) {
   if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr) ||
       ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) ||
-      ((OPT & OPT_KVAR) != 0 && (p.var_rows == nullptr || p.var_order == nullptr)))
+      ((OPT & OPT_KVAR) != 0 && !kvar_given(p)))
     return hipErrorInvalidValue;
   const int nw = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
   const long big = (long)p.batches * ((p.M + 127) / 128) * ((nw + 127) / 128);
   if (p.var_rows) {
-    if (!((OPT & OPT_KVAR) != 0 && big >= F32_BIG_KVAR_TILES))
+    if ((OPT & OPT_KVAR) == 0 || big < F32_BIG_KVAR_TILES)
       return launch_f32_tile<64, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
     return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
   }
@@ -1660,20 +1681,16 @@ hipError_t launch_router_dwg(int dtype, const void* dZ, const void* X, float* dW
   // dWg[j, n] = sum_i dZ[i, j] X[i, n], split over i in at most `splits` chunks
   if (N == 0 || splits < 1) return launch_zero(dWg, (size_t)E * d * sizeof(float), st);
   const RowSplit rs = split_rows(N, splits, 1);
-  const size_t esz = dtype == DT_F32 ? 4 : 2;
-  // `batches` chunks from row `row0` on, of which `rows` rows each are there
-  auto run = [&](int batches, long row0, int rows, float* out) -> hipError_t {
-    GemmParams p = base_params();
-    p.A = (const char*)dZ + row0 * EP * esz; p.a_bs = (long)rs.chunk * EP; p.lda = EP;
-    p.B = (const char*)X + row0 * d * esz; p.b_bs = (long)rs.chunk * d; p.ldb = d;
-    p.M = E; p.N = d; p.K = rs.chunk; p.kv_a = rows; p.kv_b = rows; p.batches = batches;
-    p.C = out; p.c_bs = (long)E * d; p.ldc = d;
-    if (dtype == DT_F32) return run_f32<false, false, EPI_STORE>(p, st);
-    return run_dma<128, 256, 2, 4, 64, 2, false, false, EPI_STORE, true, G_ROUTER_DWG>(p, st);
-  };
-  hipError_t err = rs.full > 0 ? run(rs.full, 0, rs.chunk, part) : hipSuccess;
-  if (err == hipSuccess && rs.last > 0)
-    err = run(1, (long)rs.full * rs.chunk, rs.last, part + (size_t)rs.full * E * d);
+  GemmParams p = base_params();
+  p.A = dZ; p.lda = EP;
+  p.B = X; p.ldb = d;
+  p.M = E; p.N = d; p.K = rs.chunk; p.kv_a = rs.chunk; p.kv_b = rs.chunk; p.batches = rs.parts();
+  p.k_total = N;
+  p.C = part; p.c_bs = (long)E * d; p.ldc = d;
+  const hipError_t err =
+      dtype == DT_F32 ? run_f32<false, false, EPI_STORE, OPT_KVAR>(p, st)
+                      : run_dma<128, 256, 2, 4, 64, 2, false, false, EPI_STORE, true, G_ROUTER_DWG,
+                                OPT_KVAR>(p, st);
   if (err != hipSuccess) return err;
   return run_splitk_store<float>(part, rs.parts(), E, d, E, dWg, dWg, d, st);
 }
@@ -1694,27 +1711,15 @@ hipError_t run_wgrad_splitk(const void* A, int lda, const void* B, int ldb, int 
     return launch_zero(C2, (size_t)(M - c_split) * ldc * 2, st);
   }
   const RowSplit rs = split_rows(K, splits, 64);
-  const int chunk = rs.chunk, full = rs.full, last = rs.last;
   GemmParams p = base_params();
-  p.A = A; p.a_bs = (long)chunk * lda; p.lda = lda;
-  p.B = B; p.b_bs = (long)chunk * ldb; p.ldb = ldb;
-  p.M = M; p.N = N; p.K = chunk; p.kv_a = chunk; p.kv_b = chunk;
+  p.A = A; p.lda = lda;
+  p.B = B; p.ldb = ldb;
+  p.M = M; p.N = N; p.K = rs.chunk; p.kv_a = rs.chunk; p.kv_b = rs.chunk; p.batches = rs.parts();
+  p.k_total = K;
   p.C = part; p.c_bs = (long)M * N; p.ldc = N;
-  hipError_t err = hipSuccess;
-  if (full > 0) {
-    p.batches = full;
-    err = run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, true, TAG>(p, st);
-    if (err != hipSuccess) return err;
-  }
-  if (last > 0) {
-    GemmParams q = p;
-    q.A = (const bf16_t*)A + (size_t)full * chunk * lda;
-    q.B = (const bf16_t*)B + (size_t)full * chunk * ldb;
-    q.C = part + (size_t)full * M * N;
-    q.K = last; q.kv_a = last; q.kv_b = last; q.batches = 1;
-    err = run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, true, TAG>(q, st);
-    if (err != hipSuccess) return err;
-  }
+  const hipError_t err =
+      run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, true, TAG, OPT_KVAR>(p, st);
+  if (err != hipSuccess) return err;
   return run_splitk_store<bf16_t>(part, rs.parts(), M, N, c_split, (bf16_t*)C, (bf16_t*)C2, ldc, st);
 }
 
