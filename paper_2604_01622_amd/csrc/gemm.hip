@@ -1191,14 +1191,14 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
   static_assert(EPI != EPI_SWIGLU_BWD || WN == 64, "a wave covers one 64-column partial");
   constexpr bool GA = (OPT & OPT_GA) != 0, GB = (OPT & OPT_GB) != 0, KVAR = (OPT & OPT_KVAR) != 0;
   static_assert(!(GA && A_KC) && !(GB && B_KC) && !(GA && GB) && (!KVAR || (!A_KC && !B_KC)) &&
-                    (OPT & ~(OPT_GA | OPT_GB | OPT_KVAR)) == 0,
+                    (OPT & ~(OPT_GA | OPT_GB | OPT_KVAR | OPT_MVAR)) == 0,
                 "a K-major operand may be gathered");
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE_BYTES];
 
   const int bid = blockIdx.y * gridDim.x + blockIdx.x;
   int e, rem, M = p.M, MT = p.MT, row0 = 0, K = p.K, kv_a = p.kv_a, kv_b = p.kv_b;
-  const bool var_m = !KVAR && p.var_rows;
-  if (var_m) {   // rows of the batch: [var_rows[e], var_rows[e+1]) of packed buffers
+  constexpr bool var_m = (OPT & OPT_MVAR) != 0;
+  if constexpr (var_m) {   // rows of the batch: [var_rows[e], var_rows[e+1]) of packed buffers
     VarTile v;
     if (!var_tile(p.var_rows, p.batches, BM, p.NT, bid, &v)) return;
     e = v.e;
@@ -1448,13 +1448,14 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
   }
 }
 
-// max_rows: of all batches together, with variable rows (OPT_KVAR aside).
+// max_rows: of all batches together (OPT_MVAR).
 template <int BM, int BN, int WGM, int WGN, bool A_KC, bool B_KC, int EPI, int OPT>
 hipError_t launch_f32_tile(GemmParams p, long max_rows, hipStream_t st) {
   p.MT = (p.M + BM - 1) / BM;
   p.NT = (EPI == EPI_SWIGLU) ? (p.N + BN / 2 - 1) / (BN / 2) : (p.N + BN - 1) / BN;
   // variable rows: one partial row block per batch at most
-  const bool var_m = (OPT & OPT_KVAR) == 0 && p.var_rows;
+  constexpr bool var_m = (OPT & OPT_MVAR) != 0;
+  if (var_m && (!p.var_rows || p.batches > 256)) return hipErrorInvalidValue;
   const long blocks = var_m ? (max_rows + BM - 1) / BM + p.batches : (long)p.batches * p.MT;
   const long ntile = blocks * p.NT;
   if (ntile == 0) return hipSuccess;
@@ -1477,10 +1478,13 @@ hipError_t run_f32(const GemmParams& p, hipStream_t st, long max_rows = 0) {
     return hipErrorInvalidValue;
   const int nw = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
   const long big = (long)p.batches * ((p.M + 127) / 128) * ((nw + 127) / 128);
-  if (p.var_rows) {
-    if ((OPT & OPT_KVAR) == 0 || big < F32_BIG_KVAR_TILES)
+  if constexpr ((OPT & OPT_KVAR) == 0 && A_KC) {
+    if (p.var_rows)
+      return launch_f32_tile<64, 128, 2, 2, A_KC, B_KC, EPI, OPT | OPT_MVAR>(p, max_rows, st);
+  }
+  if constexpr ((OPT & OPT_KVAR) != 0) {
+    if (p.var_rows && big < F32_BIG_KVAR_TILES)
       return launch_f32_tile<64, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
-    return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
   }
   if (big >= F32_BIG_TILES)
     return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
