@@ -163,7 +163,8 @@ def check_dropout(n, p, dtype, residual, seed, offset, shape=None):
     assert np.all(np.abs(dX - want) <= bound)
 
 
-@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 15, 511, 2048, 2055, 917, 65536, 100003])
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 7, 8, 9, 15, 252, 257, 511, 514, 1020, 2048, 2055, 4099, 917,
+                               65536, 100003])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("residual", [False, True])
 def test_dropout_sizes(n, dtype, residual):
