@@ -319,7 +319,8 @@ size_t ec_tc_saved_size(const ec_problem *p, int32_t top_k);
  * the shared experts, with the balance loss and loads of ec_tc_balance on its
  * scores (the element of dropout at [i, c] is i d + c).  Weights as for
  * ec_tc_forward.
- *   drop: NULL for neither dropout nor residual; Y [N, d] out (not the residual);
+ *   drop: NULL for neither dropout nor residual; Y [N, d] out, apart from X and
+ *   the residual (which may be X);
  *   loss [G] fp32 out; counts [G, E] int32 out; saved: ec_tc_saved_size bytes.
  * ws: ec_tc_workspace_size(p, top_k, 3).                                       */
 int ec_tc_train_forward(const ec_problem *p, int32_t top_k, const ec_dropout_desc *drop,
@@ -335,7 +336,7 @@ int ec_tc_train_forward(const ec_problem *p, int32_t top_k, const ec_dropout_des
  *   drop: as in the forward, rng holding the same values (the residual is not
  *   read; its gradient is dY); dloss [G] fp32 (device), NULL: no balance term;
  *   saved: filled by ec_tc_train_forward with the same inputs; outputs as for
- *   ec_moe_backward.  ws: ec_tc_workspace_size(p, top_k, 4).                   */
+ *   ec_moe_backward, dX apart from X and dY.  ws: ec_tc_workspace_size(p, top_k, 4).                   */
 int ec_tc_train_backward(const ec_problem *p, int32_t top_k, const ec_dropout_desc *drop,
                          const void *X, const void *Wg, const void *W1, const void *W3,
                          const void *W2, const void *Ws1, const void *Ws3, const void *Ws2,

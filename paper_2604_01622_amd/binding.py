@@ -379,7 +379,7 @@ def tc_balance(S, group_offsets, top_k: int):
         counts = torch.empty((G, E), dtype=torch.int32, device=dev)
         n = lib().ec_tc_workspace_size(P.ref, int(top_k), 2)
         ws = _empty(n, dev)
-        _check(lib().ec_tc_balance(P.ref, int(top_k), S.data_ptr() or None, loss.data_ptr(),
+        _check(lib().ec_tc_balance(P.ref, int(top_k), _addr(S), loss.data_ptr(),
                                    counts.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(dev)))
     return loss, counts
 
@@ -393,9 +393,8 @@ def tc_balance_backward(S, counts, dloss, group_offsets, top_k: int, inv_tempera
     _operand("dloss", dloss, torch.float32, (G,), dev)
     with _on(dev):
         dZ = torch.empty_like(S)
-        _check(lib().ec_tc_balance_backward(P.ref, int(top_k), S.data_ptr() or None,
-                                            counts.data_ptr(), dloss.data_ptr(),
-                                            dZ.data_ptr() or None, _raw_stream(dev)))
+        _check(lib().ec_tc_balance_backward(P.ref, int(top_k), _addr(S), counts.data_ptr(),
+                                            dloss.data_ptr(), _addr(dZ), _raw_stream(dev)))
     return dZ
 
 
@@ -406,7 +405,7 @@ def _dropout_desc(X, p, rng, residual, name="X"):
     if residual is not None:
         _operand("residual", residual, X.dtype, X.shape, X.device)
     return _DropoutDesc(float(p), None if rng is None else rng.data_ptr(),
-                        None if residual is None else residual.data_ptr() or None)
+                        _addr(residual))
 
 
 def dropout(X, p: float, rng=None, residual=None, out=None):
@@ -423,8 +422,8 @@ def dropout(X, p: float, rng=None, residual=None, out=None):
         _operand("out", out, X.dtype, X.shape, X.device)
     with _on(X.device):
         Y = torch.empty_like(X) if out is None else out
-        _check(lib().ec_dropout(code, X.numel(), ctypes.byref(desc), X.data_ptr() or None,
-                                Y.data_ptr() or None, _raw_stream(X.device)))
+        _check(lib().ec_dropout(code, X.numel(), ctypes.byref(desc), _addr(X), _addr(Y),
+                                _raw_stream(X.device)))
     return Y
 
 
@@ -454,9 +453,9 @@ def _tc_size(n: int) -> int:
     return int(n)
 
 
-def _tok_ptr(t):
-    """A per-token tensor's address (NULL without tokens)."""
-    return _ptr(t) if t.numel() else None
+def _addr(t):
+    """A tensor's address; NULL for None and for a tensor without elements."""
+    return None if t is None else t.data_ptr() or None
 
 
 def tc_train_forward(X, Wg, W1, W3, W2, group_offsets, capacity, top_k: int, inv_temperature=1.0,
@@ -594,7 +593,8 @@ class TcLayer:
     once.  training: forward returns Y = residual + dropout(layer) and leaves the balance
     loss [G] in ``loss`` and the experts' loads [G,E] in ``counts``; backward returns the
     gradients (dWg in fp32).  rng (int64 [2] on the device, see dropout) must hold the same
-    values in a step's forward and backward; advance its offset between steps."""
+    values in a step's forward and backward; advance its offset between steps.  A layer has one
+    set of buffers: order its calls (and the replays of graphs that captured them)."""
 
     def __init__(self, X, Wg, W1, W3, W2, group_offsets, capacity, top_k: int,
                  inv_temperature=1.0, shared=None, training=False, residual=None,
@@ -651,11 +651,15 @@ class TcLayer:
             return self.Y
         with _on(self.X.device):
             _check(lib().ec_tc_train_forward(
-                self.P.ref, self.top_k, ctypes.byref(self.drop), _tok_ptr(self.X), _ptr(self.Wg),
-                _ptr(self.W1), _ptr(self.W3), _ptr(self.W2), *_shared_ptrs(self.shared),
-                _tok_ptr(self.Y), _ptr(self.loss), _ptr(self.counts), _ptr(self.saved),
-                self.saved.numel(), _ptr(self.ws_f), self.ws_f.numel(), _stream()))
+                self.P.ref, self.top_k, ctypes.byref(self.drop), *self._inputs(),
+                _addr(self.Y), self.loss.data_ptr(), self.counts.data_ptr(),
+                self.saved.data_ptr(), self.saved.numel(), self.ws_f.data_ptr(),
+                self.ws_f.numel(), _raw_stream(self.X.device)))
         return self.Y
+
+    def _inputs(self):
+        return [_addr(t) for t in (self.X, self.Wg, self.W1, self.W3, self.W2,
+                                   *(self.shared or (None,) * 3))]
 
     def backward(self, dY, dloss=None):
         """dX, dWg, dW1, dW3, dW2 (and dWs1, dWs3, dWs2) of sum(Y * dY) + sum(dloss * loss)."""
@@ -666,12 +670,11 @@ class TcLayer:
             _operand("dloss", dloss, torch.float32, (self.P.c.n_groups,), self.X.device)
         with _on(self.X.device):
             _check(lib().ec_tc_train_backward(
-                self.P.ref, self.top_k, ctypes.byref(self.drop), _tok_ptr(self.X), _ptr(self.Wg),
-                _ptr(self.W1), _ptr(self.W3), _ptr(self.W2), *_shared_ptrs(self.shared),
-                _tok_ptr(dY), _ptr(dloss), _ptr(self.saved), self.saved.numel(),
-                _tok_ptr(self.dX), _ptr(self.dWg), _ptr(self.dW1), _ptr(self.dW3),
-                _ptr(self.dW2), *_shared_ptrs(self.dshared), _ptr(self.ws_b),
-                self.ws_b.numel(), _stream()))
+                self.P.ref, self.top_k, ctypes.byref(self.drop), *self._inputs(), _addr(dY),
+                _addr(dloss), self.saved.data_ptr(), self.saved.numel(),
+                *[_addr(t) for t in (self.dX, self.dWg, self.dW1, self.dW3, self.dW2,
+                                     *(self.dshared or (None,) * 3))],
+                self.ws_b.data_ptr(), self.ws_b.numel(), _raw_stream(self.X.device)))
         return (self.dX, self.dWg, self.dW1, self.dW3, self.dW2) + tuple(self.dshared or ())
 
 

@@ -1114,8 +1114,11 @@ int ec_tc_train_forward(const ec_problem* p, int32_t top_k, const ec_dropout_des
   EC_TRY(check_ptr(Ws3, "Ws3", P.hs == 0));
   EC_TRY(check_ptr(Ws2, "Ws2", P.hs == 0));
   EC_TRY(check_ptr(Y, "Y", P.N == 0));
-  // the shared experts' output is held in Y before the residual is read
-  if (residual && overlap(residual, Y, (size_t)P.N * P.d * P.esz))
+  // the shared experts' output is held in Y before the residual is read, and the backward
+  // reads X again
+  const size_t tokens = (size_t)P.N * P.d * P.esz;
+  if (overlap(X, Y, tokens)) return fail(EC_ERR_ARG, "X and Y overlap");
+  if (residual && overlap(residual, Y, tokens))
     return fail(EC_ERR_ARG, "the residual and Y overlap");
   EC_TRY(check_ptr(loss, "loss"));
   EC_TRY(check_ptr(counts, "counts"));
@@ -1191,6 +1194,10 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
   EC_TRY(check_ptr(dloss, "dloss", true));
   EC_TRY(check_ptr(saved, "saved"));
   EC_TRY(check_ptr(dX, "dX", P.N == 0));
+  // dX is written while X and dY are still read
+  const size_t tokens = (size_t)P.N * P.d * P.esz;
+  if (overlap(X, dX, tokens) || overlap(dY, dX, tokens))
+    return fail(EC_ERR_ARG, "dX overlaps X or dY");
   EC_TRY(check_ptr(dWg, "dWg"));
   EC_TRY(check_ptr(dW1, "dW1"));
   EC_TRY(check_ptr(dW3, "dW3"));

@@ -532,3 +532,64 @@ def test_operands_that_do_not_fit_are_refused():
         layer.backward(t["dY"], torch.ones(2, device="cuda"))
     with pytest.raises(ec.ECError):
         ec.tc_train_backward(*good.values(), t["dY"], layer.saved[:64], [0, 64], [64], 2)
+
+
+def test_balance_gradient_of_the_step_is_the_standalone_one():
+    """Without an output gradient the step's router gradients are the balance loss's alone:
+    dX = dZ Wg and dWg = dZ^T X with dZ of tc_balance_backward on the layer's scores."""
+    t, _ = draw_layer([90, 0, 41], 128, 12, 64, torch.float32, 81)
+    off, cap, k = [0, 90, 90, 131], [90, 0, 41], 3
+    t["dY"].zero_()
+    dloss = torch.tensor([5.0, 7.0, -3.0], device="cuda")
+    got = step(t, None, off, cap, k, 2.0, 0.0, None, dloss)
+    S = ec.tc_route(t["X"], t["Wg"], off, cap, k, 2.0)[0]
+    loss, counts = ec.tc_balance(S, off, k)
+    assert torch.equal(counts, got["counts"])
+    assert rel_l2(got["loss"], f64(loss)) <= 1e-6
+    dZ = f64(ec.tc_balance_backward(S, counts, dloss, off, k, 2.0))
+    assert rel_l2(got["dX"], dZ @ f64(t["Wg"])) <= 1e-5
+    assert rel_l2(got["dWg"], dZ.T @ f64(t["X"])) <= 1e-5
+    for n in ("dW1", "dW3", "dW2"):
+        assert not got[n].any()
+
+
+def test_two_blocks_trained_together():
+    """As they are used: two token-choice blocks with residuals, dropout and balance losses,
+    then dropout of the result, forward and backward, two steps with the offsets advanced,
+    against the chained float64 oracle.  fp32, tolerance 1e-4: two layers of 1e-5 each, the
+    second's inputs off by the first's error through weights of norm about 2."""
+    lens, d, E, h, k, p = [50, 31], 128, 6, 64, 2, 0.2
+    off, N = offsets(lens), 81
+    cap = ec.tc_capacity(lens, E, k, 1.5)
+    a, _ = draw_layer(lens, d, E, h, torch.float32, 91)
+    b, _ = draw_layer(lens, d, E, h, torch.float32, 92)
+    T = a["dY"]
+    dl = torch.tensor([20.0, 30.0], device="cuda")
+    w = lambda t: (t["Wg"], t["W1"], t["W3"], t["W2"])   # noqa: E731
+    rngs = [rng_pair(11, 3 * i) for i in range(3)]
+    for n in range(2):
+        X = a["X"]
+        H, la, ca, sa = ec.tc_train_forward(X, *w(a), off, cap, k, residual=X, dropout=p, rng=rngs[0])
+        Z, lb, cb, sb = ec.tc_train_forward(H, *w(b), off, cap, k, residual=H, dropout=p, rng=rngs[1])
+        out = ec.dropout(Z, p, rngs[2])
+        dZ = ec.dropout(T, p, rngs[2])
+        gb = ec.tc_train_backward(H, *w(b), dZ, sb, off, cap, k, dropout=p, rng=rngs[1], dloss=dl)
+        dH = gb[0] + dZ
+        ga = ec.tc_train_backward(X, *w(a), dH, sa, off, cap, k, dropout=p, rng=rngs[0], dloss=dl)
+        dX = ga[0] + dH
+        m = [ref.dropout_mask_ref(np.arange(N * d), p, 11, 3 * i + n).reshape(N, d) for i in range(3)]
+        x64, wa, wb = f64(X), [f64(v) for v in w(a)], [f64(v) for v in w(b)]
+        zero = np.zeros((N, d))
+        h64 = ref.tc_train_ref(x64, *wa, zero, off, k, cap, 1.0, None, x64, m[0])["Y"]
+        dz64 = f64(T) * m[2]
+        rb = ref.tc_train_ref(h64, *wb, dz64, off, k, cap, 1.0, None, h64, m[1], f64(dl))
+        dh64 = rb["dX"] + dz64
+        ra = ref.tc_train_ref(x64, *wa, dh64, off, k, cap, 1.0, None, x64, m[0], f64(dl))
+        assert np.array_equal(ca.cpu().numpy(), ra["counts"])
+        assert np.array_equal(cb.cpu().numpy(), rb["counts"])
+        for got, want in ((out, rb["Y"] * m[2]), (dX, ra["dX"] + dh64), (la, ra["loss"]),
+                          (lb, rb["loss"]), *zip(gb[1:], (rb[x] for x in GRADS[1:5])),
+                          *zip(ga[1:], (ra[x] for x in GRADS[1:5]))):
+            assert rel_l2(got, want) <= 1e-4
+        for r in rngs:
+            r[1] += 1

@@ -203,8 +203,9 @@ def test_training_refusals():
                                      a["saved"], sv_, a["ws"], ws_, None)
 
     def bwd(k=2, drop=d, a=None, sv_=sv, ws_=wb, P=P):
-        a = dict({n: FAKE for n in ("X", "Wg", "W1", "W3", "W2", "dY", "dloss", "saved", "dX",
-                                    "dWg", "dW1", "dW3", "dW2", "ws")}, **(a or {}))
+        over, a = a, dict({n: FAKE for n in ("X", "Wg", "W1", "W3", "W2", "dY", "dloss", "saved", "dX",
+                                    "dWg", "dW1", "dW3", "dW2", "ws")}, dX=FAR)
+        a.update(over or {})
         return L.ec_tc_train_backward(P.ref, k, ctypes.byref(drop), a["X"], a["Wg"], a["W1"],
                                       a["W3"], a["W2"], *NONE3, a["dY"], a["dloss"], a["saved"],
                                       sv_, a["dX"], a["dWg"], a["dW1"], a["dW3"], a["dW2"],
@@ -225,6 +226,10 @@ def test_training_refusals():
     assert bwd(a={"dloss": MISALIGNED}) == EC_ERR_ALIGN
     assert fwd(ws_=wf - 1) == EC_ERR_WORKSPACE and bwd(ws_=wb - 1) == EC_ERR_WORKSPACE
     assert fwd(drop=_desc(residual=1 << 30)) == EC_ERR_ARG      # the residual is Y
+    assert fwd(a={"Y": ctypes.c_void_p((1 << 20) + 4096)}) == EC_ERR_ARG    # Y inside X
+    for n in ("X", "dY"):
+        assert bwd(a={"dX": FAKE, ("dY" if n == "X" else "X"): ctypes.c_void_p(1 << 31)}) == EC_ERR_ARG
+    assert bwd(a={"dX": ctypes.c_void_p((1 << 20) + 256 * 128 * 2 - 16)}) == EC_ERR_ARG
     # the backward's [rows, 2 h] buffer is within 2^31 elements; the inference forward's
     # [rows, h] one may be twice as long
     big = binding.Problem(65536, 64, 8, 16384, [0, 65536], [65536], 1.0, torch.bfloat16)
