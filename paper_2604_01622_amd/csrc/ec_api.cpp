@@ -1231,13 +1231,15 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
   EC_HIP(ec::launch_gemm_dA_var(P.dtype, dYm, W2, s.H1, s.H3, b.dH, b.dsp, E, s.rows,
                                 rmax, rmax_e, d, h, s.sel, s.gate, stream));
   EC_HIP(mark(2, stream));
-  EC_HIP(ec::launch_gemm_dW2_var(P.dtype, dYm, s.A, dW2, E, s.rows, s.order, rmax_e, d, h, s.sel,
+  EC_HIP(ec::launch_gemm_dW2_var(P.dtype, dYm, s.A, dW2, E, s.rows, s.order, rmax, rmax_e, d, h,
+                                 s.sel,
                                  stream));
   EC_HIP(mark(3, stream));
   EC_HIP(ec::launch_gemm_dXe_var(P.dtype, b.dH, W1, W3, b.dXe, E, s.rows, rmax, rmax_e,
                                  d, h, stream));
   EC_HIP(mark(4, stream));
-  EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.rows, s.order, rmax_e, d, h,
+  EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.rows, s.order, rmax, rmax_e,
+                                  d, h,
                                   s.sel, stream));
   EC_HIP(mark(5, stream));
   const int chunk = ec::balance_backward_chunk(N);

@@ -186,11 +186,11 @@ hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const 
                                void* dXe, int E, const int32_t* rows, long max_rows,
                                int max_rows_per_expert, int d, int h, hipStream_t st);
 hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
-                               const int32_t* rows, const int32_t* order,
+                               const int32_t* rows, const int32_t* order, long max_rows,
                                int max_rows_per_expert, int d, int h, const int32_t* sel,
                                hipStream_t st);
 hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* dW1, void* dW3,
-                                int E, const int32_t* rows, const int32_t* order,
+                                int E, const int32_t* rows, const int32_t* order, long max_rows,
                                 int max_rows_per_expert, int d, int h, const int32_t* sel,
                                 hipStream_t st);
 

@@ -233,7 +233,8 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
   constexpr int MB = WM / 16, NB = WN / 16, MH = MB / 2, NH = NB / 2;
   constexpr int KK = KSTEP / 32;
   static_assert(KSTEP == 64 && MB % 2 == 0 && NB % 2 == 0, "two 32-wide sub-steps, whole halves");
-  static_assert(STAGES == 2 || (STAGES == 3 && A_KC && B_KC), "ring depth");
+  static_assert(STAGES == 2 || (STAGES == 3 && A_KC && B_KC) || (STAGES == 1 && !A_KC && !B_KC),
+                "ring depth");
   using OA = DmaOperand<BM, A_KC, NT, KSTEP>;
   using OB = DmaOperand<BN, B_KC, NT, KSTEP>;
   constexpr int STAGE_BYTES = OA::BYTES + OB::BYTES;
@@ -613,10 +614,23 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
         kstep(kt, F_{}, T_{}, F_{});
         ++kt;
       }
-    } else {
+    } else if constexpr (STAGES > 1) {
       for (; kt + STAGES < KT; ++kt) kstep(kt, T_{}, F_{}, F_{});
     }
-    for (; kt < KT; ++kt) kstep(kt, F_{}, F_{}, F_{});
+    for (; kt < KT; ++kt) {
+      if constexpr (STAGES == 1) {
+        // the stage's readers met at the barrier inside the last step; what they read of it
+        // after that is read again
+        if (kt > 0) {
+          issue(kt, 0, F_{});
+          wait_younger(0);
+          __builtin_amdgcn_s_barrier();
+          load_a(0, 0, 0);
+          load_b(0, 0, 0);
+        }
+      }
+      kstep(kt, F_{}, F_{}, F_{});
+    }
   }
   if constexpr (LATE_GATE) {
 #pragma unroll
@@ -1081,8 +1095,20 @@ hipError_t run_fwd(const GemmParams& p, hipStream_t st, long max_rows = 0) {
 double var_rounds(const GemmParams& p, long max_rows, int bm, int nt, int at_once) {
   double blocks = (double)max_rows / bm + 0.5 * p.batches;
   if (blocks < p.batches) blocks = p.batches;
+  if (!p.var_rows) blocks = (double)((max_rows + bm - 1) / bm);   // one batch
   const double t = blocks * nt / at_once;
   return t <= 1.0 ? 1.0 : t + 0.5;
+}
+
+// run_dma_var, or for one batch of max_rows rows (VAR false) run_dma.
+template <bool VAR, int BM, int BN, int WGM, int WGN, int STAGES, bool B_KC, int EPI, int TAG,
+          int OPT = 0>
+hipError_t run_rows(const GemmParams& p, long max_rows, hipStream_t st) {
+  if constexpr (VAR)
+    return run_dma_var<BM, BN, WGM, WGN, 64, STAGES, true, B_KC, EPI, false, TAG, OPT>(p, max_rows,
+                                                                                     st);
+  else
+    return run_dma<BM, BN, WGM, WGN, 64, STAGES, true, B_KC, EPI, false, TAG, OPT>(p, st);
 }
 
 // Few rows an expert in enough tiles only stream the weights: 256-row tiles, whose short
@@ -1091,7 +1117,8 @@ bool var_streams(const GemmParams& p, long max_rows, int nt) {
   return max_rows <= 96l * p.batches && (long)p.batches * nt > 128;
 }
 
-// A forward product over packed rows: 256-row tiles, or smaller ones where those leave CUs
+// A forward product over packed rows or (VAR false: the shared experts) all tokens in one
+// batch: 256-row tiles, or smaller ones where those leave CUs
 // idle or end in a poorly filled round, by var_rounds and the time of a tile relative to a
 // 256 x 256 one (192 rows 0.85; 128 rows, three stages, 0.65; 128 x 128 0.4).  Measured
 // with rows spread by a factor of 1.35, us of W1/W3 in tiles of 256, 192, 128 rows and 128 x
@@ -1100,8 +1127,8 @@ bool var_streams(const GemmParams& p, long max_rows, int nt) {
 // 193, 222, 208 and 284; x 512 296, 362, 372 and 503; 64 rows (streaming) 144, 143, 159 and
 // 157.  W2 follows (8 x 128 31, 24, 20, 17; 64 x 128 114, 112, 95, 105; x 512 180, 206, 197,
 // 267).
-template <int EPI, int TAG>
-hipError_t run_fwd_var(const GemmParams& p, long max_rows, hipStream_t st) {
+template <int EPI, int TAG, bool VAR>
+hipError_t run_fwd_rows(const GemmParams& p, long max_rows, hipStream_t st) {
   const int width = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
   const int nt = (width + 255) / 256, nt128 = (width + 127) / 128;
   if (!var_streams(p, max_rows, nt)) {
@@ -1110,31 +1137,28 @@ hipError_t run_fwd_var(const GemmParams& p, long max_rows, hipStream_t st) {
     const double t128 = 0.65 * var_rounds(p, max_rows, 128, nt, 256);
     const double tsq = 0.4 * var_rounds(p, max_rows, 128, nt128, 256);
     if (tsq < t128 && tsq < t192 && tsq < t256)
-      return run_dma_var<128, 128, 2, 2, 64, 3, true, true, EPI, false, TAG, 0>(p, max_rows, st);
+      return run_rows<VAR, 128, 128, 2, 2, 3, true, EPI, TAG>(p, max_rows, st);
     if (t128 < t192 && t128 < t256)
-      return run_dma_var<128, 256, 2, 4, 64, 3, true, true, EPI, false, TAG, 0>(p, max_rows, st);
-    if (t192 < t256)
-      return run_dma_var<192, 256, 2, 2, 64, 2, true, true, EPI, false, TAG, 0>(p, max_rows, st);
+      return run_rows<VAR, 128, 256, 2, 4, 3, true, EPI, TAG>(p, max_rows, st);
+    if (t192 < t256) return run_rows<VAR, 192, 256, 2, 2, 2, true, EPI, TAG>(p, max_rows, st);
   }
-  return run_fwd<256, EPI, TAG, OPT_TAILS, true>(p, st, max_rows);
+  return run_fwd<256, EPI, TAG, VAR ? OPT_TAILS : 0, VAR>(p, st, max_rows);
 }
 
-// A backward product over packed rows (K-major weights): 256 x 256 tiles, or 128 x 128, two
+// A backward product over packed rows or (VAR false) all tokens (K-major weights): 256 x 256 tiles, or 128 x 128, two
 // at a time on a CU, by the same estimate; rel: a CU's time for two of these relative to a
 // 256 x 256 one's (dA 0.6, whose epilogues then overlap the other's MFMAs; dX 0.7).
 // Measured as above, 256 x 256 against 128 x 128: dA of 8 experts x 600 rows, d 2048, h 1024
 // 61 and 44, 64 x 160 143 and 119, x 256 148 and 150, x 512 210 and 234, 24 x 400, d 1024, h
 // 1024 47 and 53; dX 8 x 128 63 and 40, 64 x 128 175 and 165, x 256 191 and 219.
-template <int EPI, int TAG>
-hipError_t run_bwd_var(const GemmParams& p, long max_rows, double rel, hipStream_t st) {
+template <int EPI, int TAG, bool VAR>
+hipError_t run_bwd_rows(const GemmParams& p, long max_rows, double rel, hipStream_t st) {
   constexpr int GM = EPI == EPI_SWIGLU_BWD ? 4 : 2;
   const int nt = (p.N + 255) / 256, nt128 = (p.N + 127) / 128;
   if (!var_streams(p, max_rows, nt) &&
       rel * var_rounds(p, max_rows, 128, nt128, 512) < var_rounds(p, max_rows, 256, nt, 256))
-    return run_dma_var<128, 128, GM, 4 / GM, 64, 2, true, false, EPI, false, TAG, 0>(p, max_rows,
-                                                                                     st);
-  return run_dma_var<256, 256, 4, 2, 64, 2, true, false, EPI, false, TAG, OPT_TAILS>(p, max_rows,
-                                                                                     st);
+    return run_rows<VAR, 128, 128, GM, 4 / GM, 2, false, EPI, TAG>(p, max_rows, st);
+  return run_rows<VAR, 256, 256, 4, 2, 2, false, EPI, TAG, VAR ? OPT_TAILS : 0>(p, max_rows, st);
 }
 
 // Buffers of one 128-row block (three stages): 128 x 128 tiles of four waves while there
@@ -1557,7 +1581,7 @@ hipError_t launch_gemm_w13(int dtype, const void* Xe, const void* W1, const void
   }
   if (shared) {
     if (rows) return hipErrorInvalidValue;   // the shared experts read X as is
-    return run_fwd<256, EPI_SWIGLU, G_SH_W13, 0>(p, st);
+    return run_fwd_rows<EPI_SWIGLU, G_SH_W13, false>(p, M, st);
   }
   switch (fwd_block_rows(M)) {
     case 64: return run_dma<64, 128, 2, 2, 64, 3, true, true, EPI_SWIGLU, false, G_W13>(p, st);
@@ -1576,7 +1600,7 @@ hipError_t launch_gemm_w2(int dtype, const void* A, const void* W2, void* O, int
   p.C = O; p.c_bs = (long)M * d; p.ldc = d;
   if (M == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, true, EPI_STORE>(p, st);
-  if (shared) return run_fwd<256, EPI_STORE, G_SH_W2, 0>(p, st);
+  if (shared) return run_fwd_rows<EPI_STORE, G_SH_W2, false>(p, M, st);
   switch (fwd_block_rows(M)) {
     case 64: return run_dma<64, 128, 2, 2, 64, 3, true, true, EPI_STORE, false, G_W2>(p, st);
     case 128: return run_fwd_128<EPI_STORE, G_W2>(p, st);
@@ -1608,8 +1632,7 @@ hipError_t launch_gemm_dA(int dtype, const void* dO, const void* W2, const void*
   }
   if (shared && rows) return hipErrorInvalidValue;
   // B = W2 K-major: B(n, k) = W2[k, n]
-  if (shared)
-    return run_dma<256, 256, 4, 2, 64, 2, true, false, EPI_SWIGLU_BWD, false, G_SH_DA>(p, st);
+  if (shared) return run_bwd_rows<EPI_SWIGLU_BWD, G_SH_DA, false>(p, M, 0.6, st);
   return run_dma<256, 256, 4, 2, 64, 2, true, false, EPI_SWIGLU_BWD, false, G_DA, OPT_TAILS>(p, st);
 }
 
@@ -1627,8 +1650,7 @@ hipError_t launch_gemm_dXe(int dtype, const void* dH, const void* W1, const void
   // bf16: B K-major, rows k >= h from W3 (h is a multiple of the k-step); the
   // shared experts' input gradient is added to dX
   if (h % 64 != 0) return hipErrorInvalidValue;
-  if (shared)
-    return run_dma<256, 256, 4, 2, 64, 2, true, false, EPI_STORE_ADD, false, G_SH_DXE>(p, st);
+  if (shared) return run_bwd_rows<EPI_STORE_ADD, G_SH_DXE, false>(p, M, 0.7, st);
   return run_dma<256, 256, 4, 2, 64, 2, true, false, EPI_STORE, false, G_DXE, OPT_TAILS>(p, st);
 }
 
@@ -1759,7 +1781,7 @@ hipError_t launch_gemm_w13_var(int dtype, const void* Xe, const void* W1, const 
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, true, EPI_SWIGLU>(p, st, max_rows);
-  return run_fwd_var<EPI_SWIGLU, G_TC_W13>(p, max_rows, st);
+  return run_fwd_rows<EPI_SWIGLU, G_TC_W13, true>(p, max_rows, st);
 }
 
 hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O, int E,
@@ -1773,7 +1795,7 @@ hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O,
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, true, EPI_STORE>(p, st, max_rows);
-  return run_fwd_var<EPI_STORE, G_TC_W2>(p, max_rows, st);
+  return run_fwd_rows<EPI_STORE, G_TC_W2, true>(p, max_rows, st);
 }
 
 hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
@@ -1791,7 +1813,7 @@ hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const v
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, false, EPI_SWIGLU_BWD>(p, st, max_rows);
-  return run_bwd_var<EPI_SWIGLU_BWD, G_TC_DA>(p, max_rows, 0.6, st);
+  return run_bwd_rows<EPI_SWIGLU_BWD, G_TC_DA, true>(p, max_rows, 0.6, st);
 }
 
 hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const void* W3,
@@ -1805,11 +1827,20 @@ hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const 
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, false, EPI_STORE>(p, st, max_rows);
-  return run_bwd_var<EPI_STORE, G_TC_DXE>(p, max_rows, 0.7, st);
+  return run_bwd_rows<EPI_STORE, G_TC_DXE, true>(p, max_rows, 0.7, st);
 }
 
+// The weight gradients over packed rows.  An expert of few rows is an outer product whose
+// time is its output's way to memory: tiles half as wide with one stage (69 KB of LDS, 128
+// registers), two workgroups a CU, so that one's loads run beside the other's stores.
+// Measured, rows spread by a factor of 1.35 to 1.65, us against 256 x 256 tiles of two
+// stages, 64 experts, d 2048, h 1024: dW2 of 16 rows 71 and 60, 64 77 and 68, 128 91 and 84,
+// 384 147 and 143, 512 167 and 170; dW1/dW3 16 rows 117 and 103, 64 131 and 133, 128 168 and
+// 175; and where the wide tiles are few: 16 experts x 300 rows, d 1024, h 512, dW2 (128 wide
+// tiles) 20.5 and 19.8, dW1/dW3 (256) 24.7 and 19.8, 8 x 500, d 2048, h 1024 (256 and 512)
+// 27.7 and 28.3, 48 and 52.
 hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
-                               const int32_t* rows, const int32_t* order,
+                               const int32_t* rows, const int32_t* order, long max_rows,
                                int max_rows_per_expert, int d, int h, const int32_t* sel,
                                hipStream_t st) {
   GemmParams p = base_params();
@@ -1820,18 +1851,15 @@ hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* d
   p.C = dW2; p.c_bs = (long)d * h; p.ldc = h;
   p.var_rows = rows; p.var_order = order;
   if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GA | OPT_KVAR>(p, st);
-  // few tiles: half as wide, so that they fill the chip (128 rows, us: 64 experts, d 512, h
-  // 256, 128 tiles of 256 x 256 17 and 13; 32 experts, d 768, h 512, 192 tiles 24 and 21; 8
-  // experts, d 2048, h 1024, 256 tiles 16 and 18)
-  if ((long)E * ((d + 255) / 256) * ((h + 255) / 256) <= 192)
-    return run_dma<256, 128, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW2,
+  if (max_rows <= 384l * E || (long)E * ((d + 255) / 256) * ((h + 255) / 256) <= 192)
+    return run_dma<256, 128, 4, 2, 64, 1, false, false, EPI_STORE, false, G_TC_DW2,
                    OPT_GA | OPT_KVAR>(p, st);
   return run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW2,
                  OPT_GA | OPT_TAILS | OPT_KVAR>(p, st);
 }
 
 hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* dW1, void* dW3,
-                                int E, const int32_t* rows, const int32_t* order,
+                                int E, const int32_t* rows, const int32_t* order, long max_rows,
                                 int max_rows_per_expert, int d, int h, const int32_t* sel,
                                 hipStream_t st) {
   GemmParams p = base_params();
@@ -1842,6 +1870,9 @@ hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* 
   p.C = dW1; p.C2 = dW3; p.c_split = h; p.c_bs = (long)h * d; p.ldc = d;
   p.var_rows = rows; p.var_order = order;
   if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GB | OPT_KVAR>(p, st);
+  if (max_rows <= 48l * E || (long)E * ((2 * h + 255) / 256) * ((d + 255) / 256) <= 256)
+    return run_dma<128, 256, 2, 4, 64, 1, false, false, EPI_STORE, false, G_TC_DW13,
+                   OPT_GB | OPT_KVAR>(p, st);
   return run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW13,
                  OPT_GB | OPT_TAILS | OPT_KVAR>(p, st);
 }
