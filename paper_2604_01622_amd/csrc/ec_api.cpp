@@ -159,7 +159,7 @@ struct BwdWs {
   int s_splits2, s_splits13;
 };
 
-BwdWs carve_bwd(Carve& c, const Plan& P) {
+BwdWs carve_bwd(Carve& c, const Plan& P, bool one_round = false) {
   BwdWs w;
   w.dXe = c.take((size_t)P.E * P.K * P.d * P.esz);
   w.dsp = (float*)c.take((size_t)P.E * P.K * ec::dsp_parts(P.dtype, P.h) * 4);
@@ -172,8 +172,9 @@ BwdWs carve_bwd(Carve& c, const Plan& P) {
   w.s_splits2 = w.s_splits13 = 0;
   if (P.hs) {
     w.dHs = c.take((size_t)P.N * 2 * P.hs * P.esz);
-    w.s_splits2 = ec::wgrad_splits(P.d, P.hs, P.N);
-    w.s_splits13 = ec::wgrad_splits(2 * P.hs, P.d, P.N);
+    const auto splits = one_round ? ec::wgrad_splits_one_round : ec::wgrad_splits;
+    w.s_splits2 = splits(P.d, P.hs, P.N);
+    w.s_splits13 = splits(2 * P.hs, P.d, P.N);
     const size_t a = (size_t)w.s_splits2 * P.d * P.hs, b = (size_t)w.s_splits13 * 2 * P.hs * P.d;
     if (P.dtype == EC_BF16) w.spart = (float*)c.take((a > b ? a : b) * 4);
   }
@@ -539,8 +540,8 @@ TcTrainBwdWs carve_tc_train_bwd(Carve& c, const Plan& P, long rmax) {
   packed.E = 1;
   packed.K = rmax;
   TcTrainBwdWs w;
-  w.b = carve_bwd(c, packed);
-  w.b.part = (float*)c.take((size_t)w.b.splits * P.E * P.d * 4);
+  w.b = carve_bwd(c, packed, true);
+  w.b.part = (float*)c.take((size_t)w.b.splits * P.E * P.d * 4);   // of all experts
   w.dYm = c.take((size_t)P.N * P.d * P.esz);
   return w;
 }

@@ -2,6 +2,8 @@
 automatic differentiation, differences and published values, and the refusals of the new entry
 points, which happen on the host before anything is enqueued."""
 import ctypes
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -9,7 +11,7 @@ import torch
 
 from oracle import ec_ref as ref
 import paper_2604_01622_amd as ec
-from paper_2604_01622_amd import binding
+from paper_2604_01622_amd import binding, build
 
 EC_OK, EC_ERR_ARG, EC_ERR_SHAPE, EC_ERR_CAPACITY, EC_ERR_DTYPE, EC_ERR_ALIGN, EC_ERR_WORKSPACE = range(7)
 FAKE = ctypes.c_void_p(1 << 20)       # aligned, never dereferenced: validation fails first
@@ -120,6 +122,38 @@ def test_training_gradients_against_autograd_and_differences(top_k, cf, shared, 
     if top_k == 1:   # one choice has the gate 1: only the balance loss reaches the router
         z = ref.tc_train_ref(X, Wg, W1, W3, W2, dY, off, 1, cap, inv_tau, sh, R, mask, None)
         assert not z["dWg"].any()
+
+
+# ---- host arithmetic ------------------------------------------------------------
+
+
+def test_one_round_splits_cover_every_row(tmp_path):
+    """The splits of a shared expert's weight gradient whose tiles are one round: at most 256
+    tiles wherever one split has fewer, whole chunks of 64 rows, every row once."""
+    cc = shutil.which("g++")
+    if cc is None:
+        pytest.skip("needs g++")
+    src, exe = tmp_path / "split.cpp", tmp_path / "split"
+    src.write_text(r"""
+#include <cstdio>
+#include "row_split.h"
+int main() {
+  long bad = 0;
+  for (int n = 1; n <= 9000; ++n)
+    for (int m = 64; m <= 8192; m *= 2) {
+      const int s = ec::wgrad_splits_one_round(m, 640, n);
+      const ec::RowSplit r = ec::split_rows(n, s, 64);
+      const int tiles = ((m + 255) / 256) * 3;
+      bad += s < 1 || r.parts() > s || (long)r.full * r.chunk + r.last != n || r.last >= r.chunk ||
+             (s > 1 && s * tiles > 256);
+    }
+  std::printf("%ld %d\n", bad, ec::wgrad_splits_one_round(1472, 640, 5451));
+}
+""")
+    subprocess.run([cc, "-std=c++17", "-O2", "-Wall", "-Werror", "-I", build.CSRC, str(src), "-o",
+                    str(exe)], check=True, capture_output=True, text=True)
+    out = subprocess.run([str(exe)], check=True, capture_output=True, text=True, timeout=60).stdout
+    assert out.split() == ["0", "14"]
 
 
 # ---- refusals ------------------------------------------------------------------
