@@ -310,6 +310,8 @@ def check_layer(lens, d, E, h, k, cf=0.0, dtype=torch.bfloat16, inv_tau=1.0, p=0
     ([257], 192, 5, 128, 5, 0.0, 0),                  # every expert chosen
     ([129, 64], 64, 65, 64, 4, 0.0, 128),
     ([40, 500], 256, 130, 64, 8, 2.0, 0),
+    ([130, 3], 64, 200, 64, 6, 0.0, 0),
+    ([97], 64, 256, 128, 12, 1.0, 0),
 ])
 def test_training_step(lens, d, E, h, k, cf, hs, dtype):
     check_layer(lens, d, E, h, k, cf, dtype, inv_tau=2.0, hs=hs)
@@ -320,6 +322,71 @@ def test_training_step_wide(dtype):
     # several row blocks per expert, widths that no tile divides, 16 partials a row and more
     check_layer([900, 433], 576, 6, 320, 3, 0.0, dtype, seed=3)
     check_layer([100, 60], 128, 4, 1088, 2, 1.0, dtype, seed=4)
+
+
+@pytest.mark.parametrize("n,d,E,h,k,hs,dtype", [
+    # bf16: which of the tile forms a product takes follows from its rows, experts and widths
+    (700, 768, 4, 640, 2, 256, torch.bfloat16),     # 128 x 128, half-wide weight gradients
+    (700, 64, 32, 512, 4, 0, torch.bfloat16),       # W1/W3 in 128 rows
+    (700, 64, 48, 512, 8, 0, torch.bfloat16),       # ... 192
+    (4000, 64, 48, 512, 2, 0, torch.bfloat16),      # ... 256
+    (700, 1024, 32, 64, 4, 0, torch.bfloat16),      # W2 in 128 rows
+    (700, 1024, 48, 64, 8, 0, torch.bfloat16),      # ... 192, dX in 256
+    (4000, 1024, 48, 64, 2, 640, torch.bfloat16),   # ... 256; shared experts in 192 and 128
+    (2500, 64, 48, 768, 4, 0, torch.bfloat16),      # dA in 256 rows
+    (200, 64, 130, 64, 2, 0, torch.bfloat16),       # few rows an expert: every product streams
+    (900, 256, 130, 256, 8, 0, torch.bfloat16),     # dW1/dW3 in 256 x 256
+    (10000, 64, 200, 64, 8, 0, torch.bfloat16),     # dW2 in 256 x 256
+    (300, 256, 130, 256, 4, 0, torch.float32),      # fp32 weight gradients in 128 x 128
+    (900, 256, 3, 256, 2, 128, torch.float32),      # ... 64 x 128
+])
+def test_training_step_tile_forms(n, d, E, h, k, hs, dtype):
+    check_layer([n], d, E, h, k, 0.0, dtype, seed=n, hs=hs)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_training_step_reads_nothing_it_has_not_written(dtype):
+    """Workspaces, the saved buffer and the outputs full of NaN patterns change no bit."""
+    t, sh = draw_layer([150, 0, 70], 128, 10, 192, dtype, 43, hs=64)
+    dloss = torch.tensor([3.0, 4.0, 5.0], device="cuda")
+    layer = ec.TcLayer(t["X"], t["Wg"], t["W1"], t["W3"], t["W2"], [0, 150, 150, 220], [20, 0, 20],
+                       3, shared=sh, training=True, residual=t["R"], dropout=0.1,
+                       rng=rng_pair(3, 0))
+    runs = []
+    for _ in range(2):
+        for b in (layer.ws_f, layer.ws_b, layer.saved):
+            b.fill_(0xFF)
+        for b in (layer.Y, layer.loss, layer.dX, layer.dWg, layer.dW1, layer.dW3, layer.dW2,
+                  *layer.dshared):
+            b.fill_(float("nan"))
+        layer.counts.fill_(-1)
+        layer.forward()
+        layer.ws_f.fill_(0xFF)
+        out = layer.backward(t["dY"], dloss)
+        runs.append([x.clone() for x in (layer.Y, layer.loss, layer.counts, *out)])
+        for b in (layer.ws_f, layer.ws_b, layer.saved):
+            b.zero_()
+    assert all(torch.isfinite(x.float()).all() for x in runs[0])
+    for b in (layer.ws_f, layer.ws_b, layer.saved):
+        b.zero_()
+    layer.forward()
+    out = layer.backward(t["dY"], dloss)
+    for a, b, c in zip(*runs, (layer.Y, layer.loss, layer.counts, *out)):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_balance_reads_nothing_it_has_not_written():
+    S = scores(700, 40, 8)
+    P = ec.binding._balance_problem(S, [0, 300, 700], 4, 1.0)
+    L = ec.lib()
+    loss = torch.full((2,), float("nan"), device="cuda")
+    counts = torch.full((2, 40), -1, dtype=torch.int32, device="cuda")
+    ws = torch.full((L.ec_tc_workspace_size(P.ref, 4, 2),), 0xFF, dtype=torch.uint8, device="cuda")
+    st = L.ec_tc_balance(P.ref, 4, S.data_ptr(), loss.data_ptr(), counts.data_ptr(), ws.data_ptr(),
+                         ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert st == 0
+    a, b = ec.tc_balance(S, [0, 300, 700], 4)
+    assert torch.equal(a, loss) and torch.equal(b, counts)
 
 
 def test_training_step_many_rows_per_expert():
