@@ -175,10 +175,10 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
   __shared__ uint8_t sflag[TRAIN ? TC_CHOOSE_CHUNK : 1][64 * Q + 4];
   const int g = WHOLE ? blockIdx.x : chunk_group(tab, blockIdx.x);
   const int t0 = WHOLE ? 0 : (blockIdx.x - tab.seg[g]) * tab.chunk;
-  const int t1 = t0 + tab.chunk < tab.len[g] ? t0 + tab.chunk : tab.len[g];
+  const int nt = min(tab.chunk, tab.len[g] - t0);   // tokens of the chunk
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15;
   double sum[Q][4];
-  uint32_t cnt[Q][2];   // two counts a register: a lane's tokens are at most chunk / 4 < 2^16
+  uint32_t cnt[Q][2];   // two counts a register: a lane has at most 2^20 / 48 tokens
 #pragma unroll
   for (int q = 0; q < Q; ++q)
 #pragma unroll
@@ -187,22 +187,22 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
       cnt[q][c / 2] = 0;
     }
   // a wave's four tokens at a time, the next four's scores requested before these are chosen
+  const int first = tab.off[g] + t0;
   float next[Q][4];
   auto request = [&](int tw) {
     const int t = tw + (lane >> 4);
-    load_row<Q>(S + (size_t)(tab.off[g] + (t < t1 ? t : t1 - 1)) * E, E, r, __builtin_nanf(""), next);
+    load_row<Q>(S + (size_t)(first + (t < nt ? t : nt - 1)) * E, E, r, __builtin_nanf(""), next);
   };
-  const int tw0 = t0 + wave * 4;
-  if (tw0 < t1) request(tw0);
-  for (int tw = tw0; tw < t1; tw += 4 * WAVES) {
-    const int t = tw + (lane >> 4), i = tab.off[g] + (t < t1 ? t : t1 - 1);
+  if (wave * 4 < nt) request(wave * 4);
+  for (int tw = wave * 4; tw < nt; tw += 4 * WAVES) {
+    const int t = tw + (lane >> 4), i = first + (t < nt ? t : nt - 1);
     float v[Q][4];
     uint32_t w[Q][4];
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int c = 0; c < 4; ++c) v[q][c] = next[q][c];
-    if (tw + 4 * WAVES < t1) request(tw + 4 * WAVES);
+    if (tw + 4 * WAVES < nt) request(tw + 4 * WAVES);
     take_largest<Q>(w, v, r, k);
     float inv = 1.f;
     if constexpr (TRAIN) {   // the gates' sum, the same in all lanes of the row
@@ -219,17 +219,17 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const bool taken = w[q][c] == 0 && v[q][c] == v[q][c];
-        if (t < t1) {
+        if (t < nt) {
           sum[q][c] += (double)v[q][c];
           cnt[q][c / 2] += taken ? 1u << (c % 2 * 16) : 0u;
         }
         if constexpr (TRAIN) {
-          sflag[t - t0][64 * q + 4 * r + c] = taken;   // t - t0 < TC_CHOOSE_CHUNK
+          sflag[t][64 * q + 4 * r + c] = taken;   // t < TC_CHOOSE_CHUNK
           v[q][c] = taken ? v[q][c] * inv : 0.f;
         }
       }
     if constexpr (TRAIN) {
-      if (t < t1) store_row<Q>(G + (size_t)i * E, E, r, v);
+      if (t < nt) store_row<Q>(G + (size_t)i * E, E, r, v);
     }
   }
   // the four rows of a wave, then the waves in order
@@ -266,10 +266,9 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
     pcnt[(size_t)blockIdx.x * E + j] = n;
   }
   if constexpr (TRAIN) {
-    const int i0 = tab.off[g] + t0, nt = t1 - t0;
     for (int c = threadIdx.x; c < E * TC_CHOOSE_CHUNK; c += BL_THREADS<Q>) {
       const int e = c / TC_CHOOSE_CHUNK, t = c % TC_CHOOSE_CHUNK;
-      if (t < nt) flagT[(size_t)e * N + i0 + t] = sflag[t][e];
+      if (t < nt) flagT[(size_t)e * N + first + t] = sflag[t][e];
     }
   }
 }
@@ -335,7 +334,7 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* S,
                                                                ChunkTable tab, float* dZ) {
   const int g = chunk_group(tab, blockIdx.x);
   const int t0 = (blockIdx.x - tab.seg[g]) * tab.chunk;
-  const int t1 = t0 + tab.chunk < tab.len[g] ? t0 + tab.chunk : tab.len[g];
+  const int nt = min(tab.chunk, tab.len[g] - t0);   // tokens of the chunk
   const int r = threadIdx.x & 15, grp = threadIdx.x >> 4;
   const double L = tab.len[g];
   const double coef = (double)dloss[g] * E / (L * L * k) * inv_tau;
@@ -347,8 +346,8 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* S,
       const int j = 64 * q + 4 * r + c;
       b[q][c] = j < E ? coef * counts[(size_t)g * E + j] : 0.0;
     }
-  for (int t = t0 + grp; t < t1; t += 16) {
-    const size_t at = (size_t)(tab.off[g] + t) * E;
+  for (int t = grp; t < nt; t += 16) {
+    const size_t at = (size_t)(tab.off[g] + t0 + t) * E;
     float v[Q][4];
     load_row<Q>(S + at, E, r, 0.f, v);
     double dot = 0.0;
@@ -386,11 +385,11 @@ __global__ __launch_bounds__(256) void tc_dz_kernel(const float* __restrict__ S,
                                                     ChunkTable tab) {
   const int g = chunk_group(tab, blockIdx.x);
   const int t0 = (blockIdx.x - tab.seg[g]) * tab.chunk;
-  const int t1 = t0 + tab.chunk < tab.len[g] ? t0 + tab.chunk : tab.len[g];
+  const int nt = min(tab.chunk, tab.len[g] - t0);   // tokens of the chunk
   const int r = threadIdx.x & 15, grp = threadIdx.x >> 4;
   const bool gates = k > 1 && max_rows > 0;
-  for (int t = t0 + grp; t < t1; t += 16) {
-    const int i = tab.off[g] + t;
+  for (int t = grp; t < nt; t += 16) {
+    const int i = tab.off[g] + t0 + t;
     float v[Q][4], gt[Q][4], u[Q][4];
     load_row<Q>(G + (size_t)i * E, E, r, 0.f, gt);
     if (dloss) load_row<Q>(S + (size_t)i * E, E, r, 0.f, v);
@@ -494,9 +493,11 @@ void run_tc_dz(int dtype, const float* S, const float* G, const int32_t* slotT, 
 
 }  // namespace
 
-// Sums: 64 tokens a chunk, or so many that a batch has at most 256 chunks and its groups.
+// Sums: 64 tokens a chunk, or so many that a batch has at most 256 chunks and its groups; 2^20
+// at most (a lane's counts are 16 bits).
 int balance_chunk(int N) {
-  return (N + 256 * 64 - 1) / (256 * 64) * 64;
+  const long c = ((long)N + 256 * 64 - 1) / (256 * 64) * 64;
+  return c < 1 << 20 ? (int)c : 1 << 20;
 }
 
 // Gradients: 16 tokens (one each) while the workgroups are at most 1024, else 64.

@@ -276,7 +276,8 @@ int for_chunk_tables(const ec_problem* p, const Plan& P, int chunk, F body) {
       tab.off[tab.n] = p->group_offsets[g];
       tab.len[tab.n] = p->group_offsets[g + 1] - p->group_offsets[g];
       tab.cap[tab.n] = p->capacity[g];
-      tab.seg[tab.n + 1] = tab.seg[tab.n] + (tab.len[tab.n] + tab.chunk - 1) / tab.chunk;
+      tab.seg[tab.n + 1] =
+          tab.seg[tab.n] + (int)(((long)tab.len[tab.n] + tab.chunk - 1) / tab.chunk);
       ++tab.n;
     }
     EC_TRY(body(tab, g0, before));
@@ -293,7 +294,7 @@ struct BalanceWs {
 BalanceWs carve_balance(Carve& c, const ec_problem* p, const Plan& P, int chunk) {
   size_t chunks = 0;
   for (int g = 0; g < P.G; ++g)
-    chunks += (p->group_offsets[g + 1] - p->group_offsets[g] + chunk - 1) / chunk;
+    chunks += ((size_t)(p->group_offsets[g + 1] - p->group_offsets[g]) + chunk - 1) / chunk;
   BalanceWs w;
   w.psum = (double*)c.take(chunks * P.E * 8);
   w.pcnt = (int32_t*)c.take(chunks * P.E * 4);

@@ -1120,11 +1120,10 @@ bool var_streams(const GemmParams& p, long max_rows, int nt) {
 }
 
 // A forward product over packed rows or (VAR false: the shared experts) all tokens in one
-// batch: 256-row tiles, or smaller ones where those leave CUs
-// idle or end in a poorly filled round, by var_rounds and the time of a tile relative to a
-// 256 x 256 one (192 rows 0.85; 128 rows, three stages, 0.65; 128 x 128 0.4).  Measured
-// with rows spread by a factor of 1.35, us of W1/W3 in tiles of 256, 192, 128 rows and 128 x
-// 128: 8 experts x 128 rows, d 2048, h 1024 54, 46, 38 and 31; x 600 65, 52, 65 and 77; 16 x
+// batch: 256-row tiles, or smaller ones where those leave CUs idle or end in a poorly filled
+// round, by var_rounds and the time of a tile relative to a 256 x 256 one (192 rows 0.85; 128
+// rows, three stages, 0.65; 128 x 128 0.4).  Measured with rows spread by a factor of 1.35,
+// us of W1/W3 in tiles of 256, 192, 128 rows and 128 x 128: 8 experts x 128 rows, d 2048, h 1024 54, 46, 38 and 31; x 600 65, 52, 65 and 77; 16 x
 // 300, d 1024, h 512 38, 28, 23 and 32; 64 x 128, d 2048, h 1024 186, 183, 164 and 197; x 256
 // 193, 222, 208 and 284; x 512 296, 362, 372 and 503; 64 rows (streaming) 144, 143, 159 and
 // 157.  W2 follows (8 x 128 31, 24, 20, 17; 64 x 128 114, 112, 95, 105; x 512 180, 206, 197,
@@ -1147,9 +1146,10 @@ hipError_t run_fwd_rows(const GemmParams& p, long max_rows, hipStream_t st) {
   return run_fwd<256, EPI, TAG, VAR ? OPT_TAILS : 0, VAR>(p, st, max_rows);
 }
 
-// A backward product over packed rows or (VAR false) all tokens (K-major weights): 256 x 256 tiles, or 128 x 128, two
-// at a time on a CU, by the same estimate; rel: a CU's time for two of these relative to a
-// 256 x 256 one's (dA 0.6, whose epilogues then overlap the other's MFMAs; dX 0.7).
+// A backward product over packed rows or (VAR false) all tokens, with K-major weights: 256 x
+// 256 tiles, or 128 x 128, two at a time on a CU, by the same estimate; rel: a CU's time for
+// two of these relative to a 256 x 256 one's (dA 0.6, whose epilogues then overlap the other's
+// MFMAs; dX 0.7).
 // Measured as above, 256 x 256 against 128 x 128: dA of 8 experts x 600 rows, d 2048, h 1024
 // 61 and 44, 64 x 160 143 and 119, x 256 148 and 150, x 512 210 and 234, 24 x 400, d 1024, h
 // 1024 47 and 53; dX 8 x 128 63 and 40, 64 x 128 175 and 165, x 256 191 and 219.

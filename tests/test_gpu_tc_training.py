@@ -94,6 +94,31 @@ def test_balance_many_tokens():
     check_balance(scores(70001, 33, 5, sharp=2.0), [69000, 1001], 4)
 
 
+@pytest.mark.parametrize("E,k", [(1, 1), (100, 2)])
+def test_balance_of_the_most_tokens(E, k):
+    """2^24 - 1 tokens (a problem's N 2 d < 2^31 with the smallest d): scores past 2^32 bytes,
+    chunks of more tokens; one more is refused."""
+    N, first = 2 ** 24 - 1, 2 ** 23 + 77
+    S = torch.full((N, E), 0.5 / E, device="cuda")
+    S[:, E - 1] = 0.75
+    off = [0, first, N]
+    loss, counts = ec.tc_balance(S, off, k)
+    want = torch.zeros(2, E, dtype=torch.int32)
+    sums = torch.tensor([float(S[0, 0]), float(S[0, E - 1])], dtype=torch.float64)
+    for g, L in enumerate((first, N - first)):
+        want[g, E - 1] = want[g, 0] = L      # the largest, then the lowest of the equal ones
+        mean = sums[1] + (sums[0] if E > 1 else 0)
+        assert loss[g].item() == pytest.approx(float(E / k * mean), rel=2 * U32)
+    assert torch.equal(counts.cpu(), want)
+    S[-1] = 0.25 / E
+    dZ = ec.tc_balance_backward(S, counts, torch.tensor([1.0, 2.0 ** 20], device="cuda"), off, k)
+    b = 2.0 ** 20 * E / (k * (N - first))
+    last = 0.25 / E
+    assert dZ[-1, E - 1].item() == pytest.approx(last * (b - min(E, 2) * last * b), rel=1e-6)
+    with pytest.raises(ec.ECError, match="32-bit"):
+        ec.tc_balance(S.new_empty((N + 1, 1)), [0, N + 1], 1)
+
+
 def test_balance_collapsed_and_equal_scores():
     S = torch.zeros((500, 48), device="cuda")
     S[:, 7] = 1.0                                # every row the same expert: E / k ties of zero
@@ -322,6 +347,11 @@ def test_training_step_wide(dtype):
     # several row blocks per expert, widths that no tile divides, 16 partials a row and more
     check_layer([900, 433], 576, 6, 320, 3, 0.0, dtype, seed=3)
     check_layer([100, 60], 128, 4, 1088, 2, 1.0, dtype, seed=4)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_training_step_of_many_groups(dtype):
+    check_layer([7, 0, 3] * 100, 64, 8, 64, 2, 1.0, dtype, seed=12)
 
 
 @pytest.mark.parametrize("n,d,E,h,k,hs,dtype", [
