@@ -336,7 +336,8 @@ int ec_tc_train_forward(const ec_problem *p, int32_t top_k, const ec_dropout_des
  *   drop: as in the forward, rng holding the same values (the residual is not
  *   read; its gradient is dY); dloss [G] fp32 (device), NULL: no balance term;
  *   saved: filled by ec_tc_train_forward with the same inputs; outputs as for
- *   ec_moe_backward, dX apart from X and dY.  ws: ec_tc_workspace_size(p, top_k, 4).                   */
+ *   ec_moe_backward, dX apart from X and dY.
+ * ws: ec_tc_workspace_size(p, top_k, 4).                                       */
 int ec_tc_train_backward(const ec_problem *p, int32_t top_k, const ec_dropout_desc *drop,
                          const void *X, const void *Wg, const void *W1, const void *W3,
                          const void *W2, const void *Ws1, const void *Ws3, const void *Ws2,

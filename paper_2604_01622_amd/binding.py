@@ -617,6 +617,7 @@ class TcLayer:
             return
         _layer_operands(X, Wg, W1, W3, W2, shared)
         self.residual, self.rng = residual, rng
+        self._given, self._forward_only, self._ran = saved is not None, not backward, False
         self.drop = _dropout_desc(X, dropout, rng, residual)
         self.P = Problem.of(X, Wg, W1.shape[1], group_offsets, capacity, inv_temperature, shared)
         if len(self.P.off) != len(self.P.cap) + 1:
@@ -649,12 +650,15 @@ class TcLayer:
                                        *_shared_ptrs(self.shared), _ptr(self.Y), _ptr(self.rows),
                                        _ptr(self.ws), self.ws.numel(), _stream()))
             return self.Y
+        if self._given:
+            raise ECError(1, "the layer has another's saved buffer: backward only")
         with _on(self.X.device):
             _check(lib().ec_tc_train_forward(
                 self.P.ref, self.top_k, ctypes.byref(self.drop), *self._inputs(),
                 _addr(self.Y), self.loss.data_ptr(), self.counts.data_ptr(),
                 self.saved.data_ptr(), self.saved.numel(), self.ws_f.data_ptr(),
                 self.ws_f.numel(), _raw_stream(self.X.device)))
+        self._ran = True
         return self.Y
 
     def _inputs(self):
@@ -665,6 +669,10 @@ class TcLayer:
         """dX, dWg, dW1, dW3, dW2 (and dWs1, dWs3, dWs2) of sum(Y * dY) + sum(dloss * loss)."""
         if not self.training:
             raise ECError(1, "backward needs training=True")
+        if self._forward_only:
+            raise ECError(1, "the layer was made with backward=False")
+        if not (self._given or self._ran):   # its rows and tokens would be read from garbage
+            raise ECError(1, "backward before forward")
         _operand("dY", dY, self.X.dtype, self.X.shape, self.X.device)
         if dloss is not None:
             _operand("dloss", dloss, torch.float32, (self.P.c.n_groups,), self.X.device)

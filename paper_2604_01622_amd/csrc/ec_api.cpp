@@ -1019,8 +1019,8 @@ int ec_tc_forward(const ec_problem* p, int32_t top_k, const void* X, const void*
   EC_TRY(enqueue_tc_route(p, P, top_k, X, Wg, w.S, w.G, w.slot, rows, w.sel, rw, stream));
   // the W1/W3 product reads the kept rows of X itself (empty gather stage)
   EC_HIP(mark(3, stream));
-  EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, w.A, nullptr, nullptr, P.E, rows, rmax, rmax_e, P.d,
-                                 P.h, stream, w.sel));
+  EC_HIP(ec::launch_gemm_w13_var(P.dtype, X, W1, W3, w.A, nullptr, nullptr, P.E, rows, rmax,
+                                 rmax_e, P.d, P.h, stream, w.sel));
   EC_HIP(mark(4, stream));
   EC_HIP(ec::launch_gemm_w2_var(P.dtype, w.A, W2, w.O, P.E, rows, rmax, rmax_e, P.d,
                                 P.h, stream));
@@ -1234,15 +1234,13 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
                                 rmax, rmax_e, d, h, s.sel, s.gate, stream));
   EC_HIP(mark(2, stream));
   EC_HIP(ec::launch_gemm_dW2_var(P.dtype, dYm, s.A, dW2, E, s.rows, s.order, rmax, rmax_e, d, h,
-                                 s.sel,
-                                 stream));
+                                 s.sel, stream));
   EC_HIP(mark(3, stream));
   EC_HIP(ec::launch_gemm_dXe_var(P.dtype, b.dH, W1, W3, b.dXe, E, s.rows, rmax, rmax_e,
                                  d, h, stream));
   EC_HIP(mark(4, stream));
   EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.rows, s.order, rmax, rmax_e,
-                                  d, h,
-                                  s.sel, stream));
+                                  d, h, s.sel, stream));
   EC_HIP(mark(5, stream));
   const int chunk = ec::balance_backward_chunk(N);
   EC_TRY(for_chunk_tables(p, P, chunk, [&](const ec::ChunkTable& tab, int g0, long) -> int {

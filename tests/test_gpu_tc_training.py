@@ -631,6 +631,25 @@ def test_operands_that_do_not_fit_are_refused():
         ec.tc_train_backward(*good.values(), t["dY"], layer.saved[:64], [0, 64], [64], 2)
 
 
+def test_calls_of_a_layer_out_of_order_are_refused():
+    t = {"X": (64, 64), "Wg": (8, 64), "W1": (8, 64, 64), "W3": (8, 64, 64), "W2": (8, 64, 64)}
+    t = {n: torch.zeros(s, device="cuda") for n, s in t.items()}
+    off, cap = [0, 64], [64]
+    layer = ec.TcLayer(*t.values(), off, cap, 2, training=True)
+    with pytest.raises(ec.ECError, match="backward before forward"):
+        layer.backward(t["X"])
+    layer.forward()
+    layer.backward(t["X"])
+    later = ec.TcLayer(*t.values(), off, cap, 2, training=True, saved=layer.saved)
+    later.backward(t["X"])
+    with pytest.raises(ec.ECError, match="backward only"):
+        later.forward()
+    first = ec.TcLayer(*t.values(), off, cap, 2, training=True, backward=False)
+    first.forward()
+    with pytest.raises(ec.ECError, match="backward=False"):
+        first.backward(t["X"])
+
+
 def test_balance_gradient_of_the_step_is_the_standalone_one():
     """Without an output gradient the step's router gradients are the balance loss's alone:
     dX = dZ Wg and dWg = dZ^T X with dZ of tc_balance_backward on the layer's scores."""
