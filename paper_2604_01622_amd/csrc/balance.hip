@@ -275,7 +275,7 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
 
 // Counts and loss of a group from its chunks' sums, a workgroup a group: threads share the
 // chunks out, 1024 / (64 Q) at a time, 4 Q loads of each in flight (256 chunks of a group
-// of 65536 tokens and 256 experts: 12.7 us, with a loop of single loads 272; the 32 chunks
+// of 65536 tokens and 256 experts: 12.1 us, with a loop of single loads 272; the 32 chunks
 // of a group of 2048 and 64 experts are four loads).
 template <int Q>
 __global__ __launch_bounds__(1024) void balance_finish_kernel(
