@@ -11,6 +11,11 @@
 // a token: lane r holds experts 4 r + 64 q + {0, 1, 2, 3}, one 16-byte load a quarter row.
 // Chunks' sums are added in a fixed order, no atomics.  Sums of S, the dot product and the
 // difference are in 64 bits (under an even load the difference is far below its terms).
+//
+// Latency bounds all but the largest: 16384 tokens x 64 experts, top 8, 5.9 (sums), 4.3
+// (finish) and 5.4 us (gradient) for 4.2, 0.2 and 8.4 MB.  65536 x 256, top 8: 32.1, 12.1 and 26.5
+// us; the sums are bound by choosing (eight rounds of sixteen compares and selects and a
+// maximum over the row, each waiting for the last), the gradient moves 134 MB at 5.1 TB/s.
 #include <type_traits>
 
 #include "ec_common.h"
@@ -371,7 +376,8 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* S,
 // nothing elsewhere and nothing at all for one choice, whose gate is 1; plus the balance
 // loss's term with dloss.  Latency bounds it: a token's loads depend on each other (gate,
 // slot, partials), so a quarter row's four slots and then all their partials are requested
-// together, whether chosen or not (row 0 stands in for what is not).  NP: partials of a row
+// together, whether chosen or not (row 0 stands in for what is not): 16384 tokens, top 8 of
+// 64, 31.8 -> 10.6 us.  NP: partials of a row
 // read as 16-byte vectors (4, 8, 16; 0: any count, one by one).
 template <int Q, int NP, typename T>
 __global__ __launch_bounds__(256) void tc_dz_kernel(const float* __restrict__ S,

@@ -37,6 +37,15 @@
 // two workgroups a CU, for the weight gradients of few rows are slower (256 rows: dW1/dW3
 // 207 -> 252), as are four row blocks per tile group (one sequence's step 870 -> 887).
 //
+// Token choice packs the rows that each expert keeps one expert after the other; how many
+// is known on the device only (var_rows).  Grids are sized for the most tiles there can be, a
+// wave finds its tile from the offsets by a scan over its lanes (var_tile), and the tile's
+// form is the host's guess of the rounds (var_rounds, run_fwd_rows, run_bwd_rows, the weight
+// gradients' launches).  16384 tokens, top 8 of 64, d 2048, h 1024: W1/W3 1045 us, W2 581, dA
+// 638, dW2 489, dX 1023, dW1/dW3 1001, as expert choice's of as many rows; 512 tokens, top 8
+// (64 rows an expert) 137, 62, 65, 70, 107 and 149, where the weights' bytes bound them (3.6 to 5
+// TB/s).
+//
 // The products that read the selected tokens' rows (of X, or of the output
 // gradient dY) gather them in the operand load: the W1/W3 and dA products per
 // row of their K-contiguous A, the dW2 and dW1/dW3 products per k row of their
