@@ -81,13 +81,51 @@ __device__ __forceinline__ void store_row(float* row, int E, int r, const float 
   }
 }
 
+// v[a] >= v[b] from now on.
+__device__ __forceinline__ void order_pair(uint32_t& a, uint32_t& b) {
+  const uint32_t hi = max(a, b);
+  b = min(a, b);
+  a = hi;
+}
+
+// Eight keys in falling order (19 exchanges, odd-even merging of halves).
+__device__ __forceinline__ void sort8(uint32_t x[8]) {
+  constexpr uint8_t A[19] = {0, 2, 4, 6, 0, 1, 4, 5, 1, 5, 0, 1, 2, 3, 2, 3, 1, 3, 5};
+  constexpr uint8_t B[19] = {1, 3, 5, 7, 2, 3, 6, 7, 2, 6, 4, 5, 6, 7, 4, 5, 2, 4, 6};
+#pragma unroll
+  for (int i = 0; i < 19; ++i) order_pair(x[A[i]], x[B[i]]);
+}
+
+// The eight largest of a lane's 4 Q keys in falling order, zeros behind fewer.
+template <int Q>
+__device__ __forceinline__ void top8(const uint32_t w[Q][4], uint32_t top[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top[i] = i < 4 * Q ? w[i / 4][i % 4] : 0;
+  sort8(top);
+  if constexpr (Q > 2) {   // the larger of the ends of two sorted lists are bitonic
+    uint32_t more[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) more[i] = i + 8 < 4 * Q ? w[i / 4 + 2][i % 4] : 0;
+    sort8(more);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top[i] = max(top[i], more[7 - i]);
+#pragma unroll
+    for (int s = 4; s >= 1; s >>= 1)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if ((i & s) == 0) order_pair(top[i], top[i + s]);
+  }
+}
+
 // Takes the k largest entries out of the four rows that a wave holds (ties: the lower
 // expert; NaN, also in the entries past E, is never taken); a taken entry's key ends as 0.
-// Keys are integers in the scores' order (f32_order_key; 0 for NaN), whose maxima take three
-// operands an instruction and no care for NaN.  A round is a maximum over the row, a compare
-// and a select per entry, and takes every entry equal to the maximum; only where some row so
-// loses more or fewer than k (equal scores among its largest, or not k numbers) does the
-// wave start over, one lowest expert at a time.  Every lane takes part.
+// Keys are integers in the scores' order (f32_order_key; 0 for NaN), whose maxima take no care
+// for NaN.  Every lane sorts its largest eight once; a round is a maximum over the lanes' first
+// ones, and the lanes that held it go on to their next.  The k-th round's maximum is the
+// smallest entry to take (a lane with more than eight entries may run out past eight rounds:
+// then a round is a maximum, a compare and a select per entry).  Only where some row so loses
+// more or fewer than k (equal scores among its largest, or not k numbers) does the wave
+// start over, one lowest expert at a time.  Every lane takes part.
 template <int Q>
 __device__ __forceinline__ void take_largest(uint32_t w[Q][4], const float v[Q][4], int r, int k) {
   auto keys = [&] {
@@ -107,12 +145,31 @@ __device__ __forceinline__ void take_largest(uint32_t w[Q][4], const float v[Q][
     return row16_max_u32(m);
   };
   keys();
-  for (int n = 0; n < k; ++n) {
-    const uint32_t m = row_max();
+  if (Q <= 2 || k <= 8) {
+    constexpr int L = Q == 1 ? 4 : 8;
+    uint32_t top[8], m = 0;
+    top8<Q>(w, top);
+    for (int n = 0; n < k; ++n) {
+      m = row16_max_u32(top[0]);
+      const bool held = top[0] == m;
+#pragma unroll
+      for (int i = 0; i < L; ++i) {   // values, not places: a choice of places is an index
+        const uint32_t stay = top[i], next = i + 1 < L ? top[i + 1] : 0;
+        top[i] = held ? next : stay;
+      }
+    }
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) w[q][c] = w[q][c] == m ? 0 : w[q][c];
+      for (int c = 0; c < 4; ++c) w[q][c] = w[q][c] >= m ? 0 : w[q][c];
+  } else {
+    for (int n = 0; n < k; ++n) {
+      const uint32_t m = row_max();
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[q][c] = w[q][c] == m ? 0 : w[q][c];
+    }
   }
   int took = 0;
 #pragma unroll
