@@ -119,7 +119,7 @@ __device__ __forceinline__ void top8(const uint32_t w[Q][4], uint32_t top[8]) {
 
 // Takes the k largest entries out of the four rows that a wave holds (ties: the lower
 // expert; NaN, also in the entries past E, is never taken); a taken entry's key ends as 0.
-// Keys are integers in the scores' order (f32_order_key; 0 for NaN), whose maxima take no care
+// Keys are integers in the scores' order (f32_order_key's; 0 for NaN), whose maxima take no care
 // for NaN.  Every lane sorts its largest eight once; a round is a maximum over the lanes' first
 // ones, and the lanes that held it go on to their next.  The k-th round's maximum is the
 // smallest entry to take (a lane with more than eight entries may run out past eight rounds:
@@ -132,8 +132,10 @@ __device__ __forceinline__ void take_largest(uint32_t w[Q][4], const float v[Q][
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        w[q][c] = v[q][c] == v[q][c] ? f32_order_key(v[q][c] + 0.f) : 0;   // -0 equals 0
+      for (int c = 0; c < 4; ++c) {
+        const int u = __float_as_int(v[q][c] + 0.f);   // -0 equals 0
+        w[q][c] = v[q][c] == v[q][c] ? (uint32_t)(u ^ (u >> 31 | (int)0x80000000)) : 0;
+      }
   };
   auto row_max = [&]() -> uint32_t {
     uint32_t m = 0;
@@ -158,10 +160,16 @@ __device__ __forceinline__ void take_largest(uint32_t w[Q][4], const float v[Q][
         top[i] = held ? next : stay;
       }
     }
+    int took = m == 0 ? -4 * Q : 0;   // no k numbers: less than any k in all
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) w[q][c] = w[q][c] >= m ? 0 : w[q][c];
+      for (int c = 0; c < 4; ++c) {
+        const bool take = w[q][c] >= m;
+        took += take;
+        w[q][c] = take ? 0 : w[q][c];
+      }
+    if (!__any(row16_sum_i32(took) != k)) return;
   } else {
     for (int n = 0; n < k; ++n) {
       const uint32_t m = row_max();
@@ -170,13 +178,13 @@ __device__ __forceinline__ void take_largest(uint32_t w[Q][4], const float v[Q][
 #pragma unroll
         for (int c = 0; c < 4; ++c) w[q][c] = w[q][c] == m ? 0 : w[q][c];
     }
+    int took = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) took += w[q][c] == 0 && v[q][c] == v[q][c];
+    if (!__any(row16_sum_i32(took) != k)) return;
   }
-  int took = 0;
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) took += w[q][c] == 0 && v[q][c] == v[q][c];
-  if (!__any(row16_sum_i32(took) != k)) return;
   keys();
   for (int n = 0; n < k; ++n) {
     const uint32_t m = row_max();
@@ -199,26 +207,22 @@ __device__ __forceinline__ void take_largest(uint32_t w[Q][4], const float v[Q][
 // experts), whose sums need more registers than a lane of 16 waves has.
 template <int Q> constexpr int BL_THREADS = Q == 4 ? 768 : 1024;
 
+__device__ __forceinline__ float group_loss(double sum, int E, int k, int len) {
+  const double L = len;
+  return len > 0 ? (float)(sum * E / (L * L * k)) : 0.f;
+}
+
 // The group's loss and counts from its sums: thread j < E holds expert j's.
-__device__ __forceinline__ void finish_group(double sum, int count, int E, int k, int len, int cap,
-                                             size_t g, double* red, float* loss, int32_t* counts,
-                                             int32_t* counts2, int32_t* kept) {
+__device__ __forceinline__ void finish_group(double sum, int count, int E, int k, int len, size_t g,
+                                             double* red, float* loss, int32_t* counts) {
   const int j = threadIdx.x;
-  double x = 0.0;
-  if (j < E) {
-    counts[g * E + j] = count;
-    if (counts2) counts2[g * E + j] = count;
-    if (kept) kept[g * E + j] = count < cap ? count : cap;
-    x = sum * (double)count;
-  }
+  if (j < E) counts[g * E + j] = count;
+  double x = j < E ? sum * (double)count : 0.0;
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
   if ((j & 63) == 0 && j < 256) red[j >> 6] = x;   // E <= 256
   __syncthreads();
-  if (j == 0) {
-    const double L = len, all = red[0] + red[1] + red[2] + red[3];
-    loss[g] = len > 0 ? (float)(all * E / (L * L * k)) : 0.f;
-  }
+  if (j == 0) loss[g] = group_loss(red[0] + red[1] + red[2] + red[3], E, k, len);
 }
 
 // Sums of S and choices per expert over one chunk of tokens.  WHOLE: every group is one
@@ -228,8 +232,8 @@ __device__ __forceinline__ void finish_group(double sum, int count, int E, int k
 template <int Q, bool WHOLE, bool TRAIN>
 __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
     const float* __restrict__ S, int E, int k, ChunkTable tab, double* __restrict__ psum,
-    int32_t* __restrict__ pcnt, float* __restrict__ loss, int32_t* __restrict__ counts,
-    float* __restrict__ G, int32_t* __restrict__ flagT, int N) {
+    int32_t* __restrict__ pcnt, int32_t* __restrict__ done, float* __restrict__ loss,
+    int32_t* __restrict__ counts, float* __restrict__ G, int32_t* __restrict__ flagT, int N) {
   constexpr int WAVES = BL_THREADS<Q> / 64;
   __shared__ double ssum[WAVES][64 * Q];
   __shared__ int scnt[WAVES][64 * Q];
@@ -276,20 +280,24 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
           chosen += w[q][c] == 0 && v[q][c] == v[q][c] ? v[q][c] : 0.f;
       inv = 1.0f / row16_sum_even(chosen);
     }
+    auto add = [&](auto all) {   // all: no row of the wave's four lies past the chunk
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
+      for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const bool taken = w[q][c] == 0 && v[q][c] == v[q][c];
-        if (t < nt) {
-          sum[q][c] += (double)v[q][c];
-          cnt[q][c / 2] += taken ? 1u << (c % 2 * 16) : 0u;
+        for (int c = 0; c < 4; ++c) {
+          const bool taken = w[q][c] == 0 && v[q][c] == v[q][c];
+          if (decltype(all)::value || t < nt) {
+            sum[q][c] += (double)v[q][c];
+            cnt[q][c / 2] += taken ? 1u << (c % 2 * 16) : 0u;
+          }
+          if constexpr (TRAIN) {
+            sflag[t][64 * q + 4 * r + c] = taken;   // t < TC_CHOOSE_CHUNK
+            v[q][c] = taken ? v[q][c] * inv : 0.f;
+          }
         }
-        if constexpr (TRAIN) {
-          sflag[t][64 * q + 4 * r + c] = taken;   // t < TC_CHOOSE_CHUNK
-          v[q][c] = taken ? v[q][c] * inv : 0.f;
-        }
-      }
+    };
+    // (training's has no registers for both forms)
+    if (!TRAIN && tw + 4 <= nt) add(std::true_type{}); else add(std::false_type{});
     if constexpr (TRAIN) {
       if (t < nt) store_row<Q>(G + (size_t)i * E, E, r, v);
     }
@@ -322,10 +330,13 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
     }
   }
   if constexpr (WHOLE) {
-    finish_group(s, n, E, k, tab.len[g], 0, g, red, loss, counts, nullptr, nullptr);
-  } else if (j < E) {
-    psum[(size_t)blockIdx.x * E + j] = s;
-    pcnt[(size_t)blockIdx.x * E + j] = n;
+    finish_group(s, n, E, k, tab.len[g], g, red, loss, counts);
+  } else {
+    if (j < E) {
+      psum[(size_t)blockIdx.x * E + j] = s;
+      pcnt[(size_t)blockIdx.x * E + j] = n;
+    }
+    if (j == 0 && t0 == 0) done[g] = 0;
   }
   if constexpr (TRAIN) {
     for (int c = threadIdx.x; c < E * TC_CHOOSE_CHUNK; c += BL_THREADS<Q>) {
@@ -335,56 +346,77 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
   }
 }
 
-// Counts and loss of a group from its chunks' sums, a workgroup a group: threads share the
-// chunks out, 1024 / (64 Q) at a time, 4 Q loads of each in flight (256 chunks of a group
-// of 65536 tokens and 256 experts: 12.1 us, with a loop of single loads 272; the 32 chunks
-// of a group of 2048 and 64 experts are four loads).
+// Counts and loss of a group from its chunks' sums, a workgroup for every 64 experts: its
+// sixteen waves share the chunks out, 4 Q loads of each in flight (256 chunks of a group of 65536
+// tokens and 256 experts: 5.7 us; one workgroup for all 256 experts 12.1, with a loop of single
+// loads 272).  With more than one workgroup a group (Q > 1), the last to arrive adds their
+// parts of the loss, in order: done [n] counts them and is 0 before (the sums' kernel clears it).
 template <int Q>
 __global__ __launch_bounds__(1024) void balance_finish_kernel(
     const double* __restrict__ psum, const int32_t* __restrict__ pcnt, int E, int k,
-    ChunkTable tab, float* __restrict__ loss, int32_t* __restrict__ counts,
-    int32_t* __restrict__ counts2, int32_t* __restrict__ kept) {
-  constexpr int SLICES = 1024 / (64 * Q), B = 4 * Q;
-  __shared__ double ssum[SLICES][64 * Q];
-  __shared__ int scnt[SLICES][64 * Q];
-  __shared__ double red[4];
-  const int g = blockIdx.x, j = threadIdx.x % (64 * Q), sl = threadIdx.x / (64 * Q);
+    ChunkTable tab, double* part, int32_t* done, float* __restrict__ loss,
+    int32_t* __restrict__ counts, int32_t* __restrict__ counts2, int32_t* __restrict__ kept) {
+  constexpr int WAVES = 16, B = 4 * Q;
+  __shared__ double ssum[WAVES][64];
+  __shared__ int scnt[WAVES][64];
+  const int g = blockIdx.x / Q, quarter = blockIdx.x % Q;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = 64 * quarter + lane;
+  const int begin = tab.seg[g], end = tab.seg[g + 1];
   double s = 0.0;
   int n = 0;
-  if (sl < SLICES && j < E) {
-    const int end = tab.seg[g + 1];
-    for (int c0 = tab.seg[g] + sl; c0 < end; c0 += B * SLICES) {
+  if (j < E) {
+    for (int c0 = begin + wave; c0 < end; c0 += B * WAVES) {
       double x[B];
       int y[B];
 #pragma unroll
       for (int u = 0; u < B; ++u) {   // past the end: the last chunk again, not added
-        const int c = c0 + u * SLICES < end ? c0 + u * SLICES : end - 1;
+        const int c = c0 + u * WAVES < end ? c0 + u * WAVES : end - 1;
         x[u] = psum[(size_t)c * E + j];
         y[u] = pcnt[(size_t)c * E + j];
       }
 #pragma unroll
       for (int u = 0; u < B; ++u) {
-        const bool in = c0 + u * SLICES < end;
+        const bool in = c0 + u * WAVES < end;
         s += in ? x[u] : 0.0;
         n += in ? y[u] : 0;
       }
     }
   }
-  if (sl < SLICES) {
-    ssum[sl][j] = s;
-    scnt[sl][j] = n;
-  }
+  ssum[wave][lane] = s;
+  scnt[wave][lane] = n;
   __syncthreads();
-  if (threadIdx.x < 64 * Q) {
-    s = 0.0;
-    n = 0;
+  if (wave != 0) return;
+  s = 0.0;
+  n = 0;
 #pragma unroll
-    for (int w = 0; w < SLICES; ++w) {
-      s += ssum[w][threadIdx.x];
-      n += scnt[w][threadIdx.x];
-    }
+  for (int w = 0; w < WAVES; ++w) {
+    s += ssum[w][lane];
+    n += scnt[w][lane];
   }
-  finish_group(s, n, E, k, tab.len[g], tab.cap[g], g, red, loss, counts, counts2, kept);
+  if (j < E) {
+    const size_t at = (size_t)g * E + j;
+    counts[at] = n;
+    if (counts2) counts2[at] = n;
+    if (kept) kept[at] = n < tab.cap[g] ? n : tab.cap[g];
+  }
+  double x = s * (double)n;   // 0 past the experts
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
+  if (lane != 0) return;
+  if (begin == end) {   // no tokens, so no sums' workgroup that cleared done
+    if (quarter == 0) loss[g] = 0.f;
+    return;
+  }
+  if constexpr (Q > 1) {
+    __hip_atomic_store(part + g * Q + quarter, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__hip_atomic_fetch_add(done + g, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) != Q - 1)
+      return;
+    x = 0.0;
+#pragma unroll
+    for (int i = 0; i < Q; ++i)
+      x += __hip_atomic_load(part + g * Q + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  loss[g] = group_loss(x, E, k, tab.len[g]);
 }
 
 // dZ of the loss alone, fp32 [N, E].
@@ -567,7 +599,7 @@ int balance_chunk(int N) {
 int balance_backward_chunk(int N) { return N <= 16384 ? 16 : 64; }
 
 hipError_t launch_balance_partial(const float* S, int E, int k, const ChunkTable& tab, bool whole,
-                                  double* psum, int32_t* pcnt, float* loss, int32_t* counts,
+                                  const BalanceSums& sums, float* loss, int32_t* counts,
                                   hipStream_t st) {
   const int grid = whole ? tab.n : tab.seg[tab.n];
   if (grid == 0) return hipSuccess;
@@ -575,35 +607,35 @@ hipError_t launch_balance_partial(const float* S, int E, int k, const ChunkTable
     constexpr int Q = decltype(w)::value;
     if (whole)
       balance_partial_kernel<Q, true, false><<<grid, BL_THREADS<Q>, 0, st>>>(
-          S, E, k, tab, psum, pcnt, loss, counts, nullptr, nullptr, 0);
+          S, E, k, tab, nullptr, nullptr, nullptr, loss, counts, nullptr, nullptr, 0);
     else
       balance_partial_kernel<Q, false, false><<<grid, BL_THREADS<Q>, 0, st>>>(
-          S, E, k, tab, psum, pcnt, loss, counts, nullptr, nullptr, 0);
+          S, E, k, tab, sums.psum, sums.pcnt, sums.done, nullptr, nullptr, nullptr, nullptr, 0);
   });
   return hipGetLastError();
 }
 
 hipError_t launch_tc_choose(const float* S, int N, int E, int k, const ChunkTable& tab,
-                            double* psum, int32_t* pcnt, float* G, int32_t* flagT,
-                            hipStream_t st) {
+                            const BalanceSums& sums, float* G, int32_t* flagT, hipStream_t st) {
   const int grid = tab.seg[tab.n];
   if (grid == 0) return hipSuccess;
   if (tab.chunk != TC_CHOOSE_CHUNK) return hipErrorInvalidValue;
   by_width(E, [&](auto w) {
     constexpr int Q = decltype(w)::value;
     balance_partial_kernel<Q, false, true><<<grid, BL_THREADS<Q>, 0, st>>>(
-        S, E, k, tab, psum, pcnt, nullptr, nullptr, G, flagT, N);
+        S, E, k, tab, sums.psum, sums.pcnt, sums.done, nullptr, nullptr, G, flagT, N);
   });
   return hipGetLastError();
 }
 
-hipError_t launch_balance_finish(const double* psum, const int32_t* pcnt, int E, int k,
-                                 const ChunkTable& tab, float* loss, int32_t* counts,
-                                 int32_t* counts2, int32_t* kept, hipStream_t st) {
+hipError_t launch_balance_finish(const BalanceSums& sums, int E, int k, const ChunkTable& tab,
+                                 float* loss, int32_t* counts, int32_t* counts2, int32_t* kept,
+                                 hipStream_t st) {
   if (tab.n == 0) return hipSuccess;
   by_width(E, [&](auto w) {
-    balance_finish_kernel<decltype(w)::value><<<tab.n, 1024, 0, st>>>(
-        psum, pcnt, E, k, tab, loss, counts, counts2, kept);
+    constexpr int Q = decltype(w)::value;
+    balance_finish_kernel<Q><<<tab.n * Q, 1024, 0, st>>>(sums.psum, sums.pcnt, E, k, tab, sums.part,
+                                                         sums.done, loss, counts, counts2, kept);
   });
   return hipGetLastError();
 }

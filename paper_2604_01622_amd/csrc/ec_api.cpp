@@ -286,19 +286,22 @@ int for_chunk_tables(const ec_problem* p, const Plan& P, int chunk, F body) {
   return EC_OK;
 }
 
-struct BalanceWs {
-  double* psum;    // [chunks, E]
-  int32_t* pcnt;
-};
-
-BalanceWs carve_balance(Carve& c, const ec_problem* p, const Plan& P, int chunk) {
+ec::BalanceSums carve_balance(Carve& c, const ec_problem* p, const Plan& P, int chunk) {
   size_t chunks = 0;
   for (int g = 0; g < P.G; ++g)
     chunks += ((size_t)(p->group_offsets[g + 1] - p->group_offsets[g]) + chunk - 1) / chunk;
-  BalanceWs w;
+  ec::BalanceSums w;
   w.psum = (double*)c.take(chunks * P.E * 8);
   w.pcnt = (int32_t*)c.take(chunks * P.E * 4);
+  w.part = (double*)c.take((size_t)P.G * ((P.E + 63) / 64) * 8);
+  w.done = (int32_t*)c.take((size_t)P.G * 4);
   return w;
+}
+
+// Those of a table whose first group is g0, `before` chunks in.
+ec::BalanceSums sums_of(const ec::BalanceSums& w, const Plan& P, int g0, long before) {
+  return {w.psum + before * P.E, w.pcnt + before * P.E, w.part + (size_t)g0 * ((P.E + 63) / 64),
+          w.done + g0};
 }
 
 // Every group is one chunk (BALANCE_WHOLE tokens at most).
@@ -313,17 +316,15 @@ int balance_chunk_of(const ec_problem* p, const Plan& P) {
 }
 
 int enqueue_balance(const ec_problem* p, const Plan& P, int top_k, const float* S, float* loss,
-                    int32_t* counts, int chunk, const BalanceWs& w, hipStream_t st) {
+                    int32_t* counts, int chunk, const ec::BalanceSums& w, hipStream_t st) {
   const bool whole = balance_whole(p, P);
   return for_chunk_tables(p, P, chunk, [&](const ec::ChunkTable& tab, int g0, long before) -> int {
-    double* psum = w.psum + before * P.E;
-    int32_t* pcnt = w.pcnt + before * P.E;
+    const ec::BalanceSums sums = sums_of(w, P, g0, before);
     const size_t at = (size_t)g0 * P.E;
-    EC_HIP(ec::launch_balance_partial(S, P.E, top_k, tab, whole, psum, pcnt, loss + g0,
-                                      counts + at, st));
+    EC_HIP(ec::launch_balance_partial(S, P.E, top_k, tab, whole, sums, loss + g0, counts + at, st));
     if (!whole)
-      EC_HIP(ec::launch_balance_finish(psum, pcnt, P.E, top_k, tab, loss + g0, counts + at,
-                                       nullptr, nullptr, st));
+      EC_HIP(ec::launch_balance_finish(sums, P.E, top_k, tab, loss + g0, counts + at, nullptr,
+                                       nullptr, st));
     return EC_OK;
   });
 }
@@ -389,7 +390,7 @@ TcFwdWs carve_tc_fwd(Carve& c, const Plan& P, long rmax) {
 // What training's routing adds: the loads and the balance loss from the pass that chooses, the
 // packed rows' gates times gate_scale, and the order of the experts in the weight gradients.
 struct TcTrainRoute {
-  BalanceWs sums;
+  ec::BalanceSums sums;
   float* loss;
   int32_t* counts;
   int32_t* saved_counts;
@@ -410,11 +411,10 @@ int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* 
   if (train) {
     EC_TRY(for_chunk_tables(
         p, P, ec::TC_CHOOSE_CHUNK, [&](const ec::ChunkTable& tab, int g0, long before) -> int {
-          double* psum = train->sums.psum + before * P.E;
-          int32_t* pcnt = train->sums.pcnt + before * P.E;
+          const ec::BalanceSums sums = sums_of(train->sums, P, g0, before);
           const size_t at = (size_t)g0 * P.E;
-          EC_HIP(ec::launch_tc_choose(S, P.N, P.E, top_k, tab, psum, pcnt, G, slot, st));
-          EC_HIP(ec::launch_balance_finish(psum, pcnt, P.E, top_k, tab, train->loss + g0,
+          EC_HIP(ec::launch_tc_choose(S, P.N, P.E, top_k, tab, sums, G, slot, st));
+          EC_HIP(ec::launch_balance_finish(sums, P.E, top_k, tab, train->loss + g0,
                                            train->counts + at, train->saved_counts + at,
                                            w.cnt + at, st));
           return EC_OK;
@@ -518,7 +518,7 @@ TcSaved carve_tc_saved(Carve& c, const Plan& P, long rmax) {
 
 struct TcTrainFwdWs {
   TcRouteWs route;
-  BalanceWs balance;
+  ec::BalanceSums balance;
   void* O;           // [R, d]
 };
 

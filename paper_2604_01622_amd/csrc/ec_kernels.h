@@ -213,20 +213,26 @@ int balance_chunk(int N);
 // ... of launch_balance_backward and launch_tc_router_dz, and of launch_tc_choose.
 int balance_backward_chunk(int N);
 constexpr int TC_CHOOSE_CHUNK = 64;
+// What the sums' kernel leaves for launch_balance_finish (chunks and groups of one launch).
+struct BalanceSums {
+  double* psum;      // [chunks, E]
+  int32_t* pcnt;     // [chunks, E]
+  double* part;      // [groups, ceil(E / 64)] parts of the loss
+  int32_t* done;     // [groups]
+};
 // Sums of S and the number of choices among each row's k largest (ties: the lower index),
 // per chunk: psum, pcnt [seg[n], E]; whole: loss [n] and counts [n, E] instead.
 hipError_t launch_balance_partial(const float* S, int E, int k, const ChunkTable& tab, bool whole,
-                                  double* psum, int32_t* pcnt, float* loss, int32_t* counts,
+                                  const BalanceSums& sums, float* loss, int32_t* counts,
                                   hipStream_t st);
 // The same sums in one pass with launch_tc_topk's outputs.
 hipError_t launch_tc_choose(const float* S, int N, int E, int k, const ChunkTable& tab,
-                            double* psum, int32_t* pcnt, float* G, int32_t* flagT,
-                            hipStream_t st);
+                            const BalanceSums& sums, float* G, int32_t* flagT, hipStream_t st);
 // counts [n, E] and loss [n] of the table's groups from their chunks' sums (counts2: a
 // second copy of the counts, kept: the counts capped at tab.cap, unless null).
-hipError_t launch_balance_finish(const double* psum, const int32_t* pcnt, int E, int k,
-                                 const ChunkTable& tab, float* loss, int32_t* counts,
-                                 int32_t* counts2, int32_t* kept, hipStream_t st);
+hipError_t launch_balance_finish(const BalanceSums& sums, int E, int k, const ChunkTable& tab,
+                                 float* loss, int32_t* counts, int32_t* counts2, int32_t* kept,
+                                 hipStream_t st);
 // dZ [N, E] fp32 of the table's groups: the loss's gradient in the logits (counts [n, E] and
 // dloss [n] of these groups).
 hipError_t launch_balance_backward(const float* S, const int32_t* counts, const float* dloss,
