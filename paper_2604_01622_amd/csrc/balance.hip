@@ -440,10 +440,19 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(const float* S,
       const int j = 64 * q + 4 * r + c;
       b[q][c] = j < E ? coef * counts[(size_t)g * E + j] : 0.0;
     }
+  // the next token's scores are requested before this one's are used (S may be dZ: rows of
+  // other tokens)
+  const size_t first = (size_t)(tab.off[g] + t0) * E;
+  float next[Q][4];
+  if (grp < nt) load_row<Q>(S + first + (size_t)grp * E, E, r, 0.f, next);
   for (int t = grp; t < nt; t += 16) {
-    const size_t at = (size_t)(tab.off[g] + t0 + t) * E;
+    const size_t at = first + (size_t)t * E;
     float v[Q][4];
-    load_row<Q>(S + at, E, r, 0.f, v);
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[q][c] = next[q][c];
+    if (t + 16 < nt) load_row<Q>(S + at + (size_t)16 * E, E, r, 0.f, next);
     double dot = 0.0;
 #pragma unroll
     for (int q = 0; q < Q; ++q)
