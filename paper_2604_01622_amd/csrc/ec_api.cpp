@@ -484,7 +484,7 @@ struct TcSaved {
   float* G;          // [N, E] gates of every choice, dropped ones too
   int32_t* slot;     // [E, N] packed row or -1
   int32_t* rows;     // [E + 1]
-  int32_t* order;    // [E] the experts as the weight gradients take them
+  int32_t* order;    // [E, 4] the experts as the weight gradients take them
   int32_t* counts;   // [G, E]
   int32_t* sel;      // [R] token of each packed row
   float* gate;       // [R] its gate
@@ -502,7 +502,7 @@ TcSaved carve_tc_saved(Carve& c, const Plan& P, long rmax) {
   s.G = (float*)c.take((size_t)P.N * P.E * 4);
   s.slot = (int32_t*)c.take((size_t)P.E * P.N * 4);
   s.rows = (int32_t*)c.take((size_t)(P.E + 1) * 4);
-  s.order = (int32_t*)c.take((size_t)P.E * 4);
+  s.order = (int32_t*)c.take((size_t)P.E * 16);
   s.counts = (int32_t*)c.take((size_t)P.G * P.E * 4);
   s.sel = (int32_t*)c.take((size_t)rmax * 4);
   s.gate = (float*)c.take((size_t)rmax * 4);
@@ -1233,14 +1233,14 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
   EC_HIP(ec::launch_gemm_dA_var(P.dtype, dYm, W2, s.H1, s.H3, b.dH, b.dsp, E, s.rows,
                                 rmax, rmax_e, d, h, s.sel, s.gate, stream));
   EC_HIP(mark(2, stream));
-  EC_HIP(ec::launch_gemm_dW2_var(P.dtype, dYm, s.A, dW2, E, s.rows, s.order, rmax, rmax_e, d, h,
-                                 s.sel, stream));
+  EC_HIP(ec::launch_gemm_dW2_var(P.dtype, dYm, s.A, dW2, E, s.order, rmax, rmax_e, d, h, s.sel,
+                                 stream));
   EC_HIP(mark(3, stream));
   EC_HIP(ec::launch_gemm_dXe_var(P.dtype, b.dH, W1, W3, b.dXe, E, s.rows, rmax, rmax_e,
                                  d, h, stream));
   EC_HIP(mark(4, stream));
-  EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.rows, s.order, rmax, rmax_e,
-                                  d, h, s.sel, stream));
+  EC_HIP(ec::launch_gemm_dW13_var(P.dtype, b.dH, X, dW1, dW3, E, s.order, rmax, rmax_e, d, h,
+                                  s.sel, stream));
   EC_HIP(mark(5, stream));
   const int chunk = ec::balance_backward_chunk(N);
   EC_TRY(for_chunk_tables(p, P, chunk, [&](const ec::ChunkTable& tab, int g0, long) -> int {

@@ -151,9 +151,9 @@ hipError_t launch_tc_topk(const float* S, int N, int E, int k, float* G, int32_t
 // cnt[(g0+g) E + j] = min(tokens of group g that chose j, cap_g) for the table's groups.
 hipError_t launch_tc_count(const int32_t* flagT, int N, int E, const GroupTable& tab, int g0,
                            int32_t* cnt, hipStream_t st);
-// Packed row offsets rows [E+1] and per-(group, expert) row offsets seg [G,E]; order [E]
+// Packed row offsets rows [E+1] and per-(group, expert) row offsets seg [G,E]; order [E, 4]
 // (training; may be null): the experts as the products that contract over an expert's rows
-// take them.
+// take them, each with its first row and its number of rows.
 hipError_t launch_tc_offsets(const int32_t* cnt, int G, int E, int32_t* rows, int32_t* seg,
                              int32_t* order, hipStream_t st);
 // slotT: choice flags in, packed rows (-1: not kept) out; sel[row] = token.  Without
@@ -177,8 +177,8 @@ hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O,
 // The backward products over packed rows (conventions of launch_gemm_dA, _dXe, _dW2 and
 // _dW13): sel[r] is the token of packed row r, whose rows of dY (dA, dW2) and X (dW13) the
 // products read themselves.  dH [max_rows, 2h], dsp [max_rows, dsp_parts(dtype, h)].  An
-// expert without rows gets zero weight gradients.  order [E]: the experts as the weight
-// gradients take them (launch_tc_offsets).
+// expert without rows gets zero weight gradients.  order [E, 4]: the experts as the
+// weight gradients take them (launch_tc_offsets).
 hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
                               const void* H3, void* dH, float* dsp, int E, const int32_t* rows, long max_rows, int max_rows_per_expert, int d,
                               int h, const int32_t* sel, const float* gate, hipStream_t st);
@@ -186,11 +186,11 @@ hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const 
                                void* dXe, int E, const int32_t* rows, long max_rows,
                                int max_rows_per_expert, int d, int h, hipStream_t st);
 hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
-                               const int32_t* rows, const int32_t* order, long max_rows,
+                               const int32_t* order, long max_rows,
                                int max_rows_per_expert, int d, int h, const int32_t* sel,
                                hipStream_t st);
 hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* dW1, void* dW3,
-                                int E, const int32_t* rows, const int32_t* order, long max_rows,
+                                int E, const int32_t* order, long max_rows,
                                 int max_rows_per_expert, int d, int h, const int32_t* sel,
                                 hipStream_t st);
 

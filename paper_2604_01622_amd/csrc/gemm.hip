@@ -134,12 +134,13 @@ struct GemmParams {
   // device array of batches + 1 entries (batches <= 256), null for a uniform batch of
   // M rows; the tiles follow from the rows (var_tile).  With OPT_KVAR the
   // rows are the contraction's instead (K-major operands: the weight gradients):
-  // batch e contracts over rows [var_rows[e], var_rows[e+1]) of both, and its
+  // batch e contracts over its rows of both, and its
   // outputs and tiles are those of a uniform batch; the tiles take the batches
-  // in the order var_order [batches] (a device array).  Without var_rows its
+  // in the order of var_order [batches] (a device array of batch, first row and number of
+  // rows, in one load).  Without var_order its
   // batches are a split of k_total rows: K rows each, the last one what is left.
   const int* var_rows;
-  const int* var_order;
+  const int4* var_order;
   int k_total;
 };
 
@@ -905,8 +906,12 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
     const int per_b = p.MT * p.NT;
     tc.e = t / per_b;
     rem = t - tc.e * per_b;
+    int4 own;
     if constexpr (KVAR)
-      if (p.var_rows) tc.e = p.var_order[tc.e];
+      if (p.var_order) {
+        own = p.var_order[tc.e];
+        tc.e = own.x;
+      }
     tc.row0 = 0;
     tc.M = p.M;
     tc.row = (size_t)tc.e * p.M;
@@ -915,9 +920,9 @@ __global__ __launch_bounds__(64 * WGM * WGN, 1) void gemm_dma_kernel(GemmParams 
     tc.c_off = (size_t)tc.e * p.c_bs;
     tc.h_off = (size_t)tc.e * p.h_bs;
     if constexpr (KVAR) {
-      if (p.var_rows) {
-        tc.row0 = p.var_rows[tc.e];
-        tc.K = p.var_rows[tc.e + 1] - tc.row0;
+      if (p.var_order) {
+        tc.row0 = own.y;
+        tc.K = own.z;
       } else {
         tc.row0 = tc.e * p.K;
         tc.K = p.k_total - tc.row0 < p.K ? p.k_total - tc.row0 : p.K;
@@ -989,7 +994,7 @@ bool operands_in_reach(const GemmParams& p) {
 // The rows that OPT_KVAR's batches contract over: their own, or a split of k_total that
 // leaves every batch some.
 bool kvar_given(const GemmParams& p) {
-  if (p.var_rows) return p.var_order != nullptr;
+  if (p.var_order) return p.var_rows == nullptr;
   return p.k_total > 0 && (long)(p.batches - 1) * p.K < p.k_total;
 }
 
@@ -1248,10 +1253,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) 
     e = t / per_b;
     rem = t - e * per_b;
     if constexpr (KVAR) {
-      if (p.var_rows) {
-        e = p.var_order[e];
-        row0 = p.var_rows[e];
-        K = p.var_rows[e + 1] - row0;
+      if (p.var_order) {
+        const int4 own = p.var_order[e];
+        e = own.x;
+        row0 = own.y;
+        K = own.z;
       } else {
         row0 = e * p.K;
         K = p.k_total - row0 < p.K ? p.k_total - row0 : p.K;
@@ -1851,7 +1857,7 @@ hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const 
 // tiles) 20.5 and 19.8, dW1/dW3 (256) 24.7 and 19.8, 8 x 500, d 2048, h 1024 (256 and 512)
 // 27.7 and 28.3, 48 and 52.
 hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
-                               const int32_t* rows, const int32_t* order, long max_rows,
+                               const int32_t* order, long max_rows,
                                int max_rows_per_expert, int d, int h, const int32_t* sel,
                                hipStream_t st) {
   GemmParams p = base_params();
@@ -1860,7 +1866,7 @@ hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* d
   p.B = A; p.ldb = h;
   p.M = d; p.N = h; p.K = K; p.kv_a = K; p.kv_b = K; p.batches = E;
   p.C = dW2; p.c_bs = (long)d * h; p.ldc = h;
-  p.var_rows = rows; p.var_order = order;
+  p.var_order = reinterpret_cast<const int4*>(order);
   if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GA | OPT_KVAR>(p, st);
   if (max_rows <= 384l * E || (long)E * ((d + 255) / 256) * ((h + 255) / 256) <= 192)
     return run_dma<256, 128, 4, 2, 64, 1, false, false, EPI_STORE, false, G_TC_DW2,
@@ -1870,7 +1876,7 @@ hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* d
 }
 
 hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* dW1, void* dW3,
-                                int E, const int32_t* rows, const int32_t* order, long max_rows,
+                                int E, const int32_t* order, long max_rows,
                                 int max_rows_per_expert, int d, int h, const int32_t* sel,
                                 hipStream_t st) {
   GemmParams p = base_params();
@@ -1879,7 +1885,7 @@ hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* 
   p.B = X; p.ldb = d; p.kb_rows = sel;
   p.M = 2 * h; p.N = d; p.K = K; p.kv_a = K; p.kv_b = K; p.batches = E;
   p.C = dW1; p.C2 = dW3; p.c_split = h; p.c_bs = (long)h * d; p.ldc = d;
-  p.var_rows = rows; p.var_order = order;
+  p.var_order = reinterpret_cast<const int4*>(order);
   if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GB | OPT_KVAR>(p, st);
   if (max_rows <= 48l * E || (long)E * ((2 * h + 255) / 256) * ((d + 255) / 256) <= 256)
     return run_dma<128, 256, 2, 4, 64, 1, false, false, EPI_STORE, false, G_TC_DW13,

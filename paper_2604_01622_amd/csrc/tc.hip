@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void tc_count_kernel(const int32_t* __restrict
 
 // Offsets, one workgroup (thread j for expert j, E <= 256): expert j's packed
 // rows start at rows[j] (rows[E] = all kept pairs); group g's tokens in expert
-// j start at seg[g E + j].  order [E] (may be null): a
+// j start at seg[g E + j].  order [E, 4] (may be null; expert, first row, rows, 0): a
 // product that contracts over an expert's rows takes as long for the expert's every tile as
 // it has rows, and each XCD takes an eighth of the list, so the experts are dealt to the
 // eighths by falling row counts, there and back.
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void tc_offsets_kernel(const int32_t* __restri
     // eighths before x: a full round each, and those that the last round reaches
     const int full = E >> 3, rest = E & 7;
     const int before = (full & 1) ? (x > 8 - rest ? x - (8 - rest) : 0) : (x < rest ? x : rest);
-    order[x * full + before + round] = j;
+    reinterpret_cast<int4*>(order)[x * full + before + round] = make_int4(j, first, m, 0);
   }
   for (int g = 0; g < G; ++g) {
     seg[(size_t)g * E + j] = first;
