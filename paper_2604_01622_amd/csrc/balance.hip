@@ -12,10 +12,11 @@
 // Chunks' sums are added in a fixed order, no atomics.  Sums of S, the dot product and the
 // difference are in 64 bits (under an even load the difference is far below its terms).
 //
-// Latency bounds all but the largest: 16384 tokens x 64 experts, top 8, 5.9 (sums), 4.3
-// (finish) and 5.4 us (gradient) for 4.2, 0.2 and 8.4 MB.  65536 x 256, top 8: 32.1, 12.1 and 26.5
-// us; the sums are bound by choosing (eight rounds of sixteen compares and selects and a
-// maximum over the row, each waiting for the last), the gradient moves 134 MB at 5.1 TB/s.
+// Latency bounds all but the largest: 16384 tokens x 64 experts, top 8, 5.6 (sums), 4.2
+// (finish) and 5.6 us (gradient) for 4.2, 0.2 and 8.4 MB.  65536 x 256, top 8: 26.7, 5.6 and 25.6
+// us; the sums are bound by choosing (some 560 instructions a wave for four tokens; a pass
+// over all sixteen registers each round, without the sort, 32.1), the gradient moves 134 MB at
+// 5.2 TB/s.
 #include <type_traits>
 
 #include "ec_common.h"
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
 
 // Counts and loss of a group from its chunks' sums, a workgroup for every 64 experts: its
 // sixteen waves share the chunks out, 4 Q loads of each in flight (256 chunks of a group of 65536
-// tokens and 256 experts: 5.7 us; one workgroup for all 256 experts 12.1, with a loop of single
+// tokens and 256 experts: 5.6 us; one workgroup for all 256 experts 12.1, with a loop of single
 // loads 272).  With more than one workgroup a group (Q > 1), the last to arrive adds their
 // parts of the loss, in order: done [n] counts them and is 0 before (the sums' kernel clears it).
 template <int Q>

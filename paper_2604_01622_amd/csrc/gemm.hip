@@ -41,9 +41,9 @@
 // is known on the device only (var_rows).  Grids are sized for the most tiles there can be, a
 // wave finds its tile from the offsets by a scan over its lanes (var_tile), and the tile's
 // form is the host's guess of the rounds (var_rounds, run_fwd_rows, run_bwd_rows, the weight
-// gradients' launches).  16384 tokens, top 8 of 64, d 2048, h 1024: W1/W3 1045 us, W2 581, dA
-// 638, dW2 489, dX 1023, dW1/dW3 1001, as expert choice's of as many rows; 512 tokens, top 8
-// (64 rows an expert) 137, 62, 65, 70, 107 and 149, where the weights' bytes bound them (3.6 to 5
+// gradients' launches).  16384 tokens, top 8 of 64, d 2048, h 1024: W1/W3 1042 us, W2 571, dA
+// 637, dW2 488, dX 1018, dW1/dW3 988, as expert choice's of as many rows; 512 tokens, top 8
+// (64 rows an expert) 135, 61, 63, 66, 104 and 140, where the weights' bytes bound them (3.6 to 5
 // TB/s).
 //
 // The products that read the selected tokens' rows (of X, or of the output
