@@ -90,6 +90,44 @@ def test_balance_group_lengths(lens):
     check_balance(scores(sum(lens), 24, len(lens)), lens, 3)
 
 
+@pytest.mark.parametrize("E,k", [(100, 3), (129, 8), (193, 9), (256, 8), (256, 200)])
+@pytest.mark.parametrize("lens", [[0, 0, 300] + [3, 0] * 80 + [700], [5000], [257, 0, 49, 289]])
+def test_balance_past_64_experts(E, k, lens):
+    """A group's loss comes in parts of 64 experts: empty groups, more groups than a launch
+    takes, groups of many chunks; k below, at and past the eight entries that a lane sorts."""
+    check_balance(scores(sum(lens), E, k), lens, k, 0.5)
+    check_balance(scores(sum(lens), E, k, ties=True), lens, k)
+
+
+@pytest.mark.parametrize("E,k", [(24, 3), (200, 8)])
+def test_balance_in_a_graph(E, k):
+    S, other, off = scores(1500, E, 1), scores(1500, E, 2), offsets([900, 0, 600])
+    want = [ec.tc_balance(x, off, k) for x in (S, other)]
+    buf, dloss = S.clone(), torch.tensor([1.0, 5.0, -2.0], device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, counts = ec.tc_balance(buf, off, k)
+        dZ = ec.tc_balance_backward(buf, counts, dloss, off, k)
+    for step in range(4):
+        x, (wl, wc) = (S, other)[step % 2], want[step % 2]
+        buf.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, wl) and torch.equal(counts, wc)
+        assert torch.equal(dZ, ec.tc_balance_backward(x, wc, dloss, off, k))
+
+
+def test_balance_ties_between_lanes_and_within_one():
+    """Equal largest scores in one lane (four neighbours of 64), in several, and both."""
+    for E, k in ((64, 3), (128, 8), (256, 8), (256, 12)):
+        S = scores(96, E, E + 1) * 0.25
+        S[:24, 4:8] = 0.5
+        S[24:48, 1::16] = 0.5
+        S[48:72, 4:24] = 0.5
+        S[72:, E - 1] = 0.5
+        check_balance(S, [96], k)
+
+
 def test_balance_many_tokens():
     check_balance(scores(70001, 33, 5, sharp=2.0), [69000, 1001], 4)
 
