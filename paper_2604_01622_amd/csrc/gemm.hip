@@ -57,6 +57,7 @@
 
 #include "ec_common.h"
 #include "ec_kernels.h"
+#include "tile_forms.h"
 
 namespace ec {
 
@@ -1208,17 +1209,6 @@ hipError_t run_fwd_128(const GemmParams& p, hipStream_t st) {
 // busy 78% of the cycles), W2 240 -> 79, dA 268 -> 98, dX 530 -> 155, dW1/dW3 520 -> 158,
 // against a 64 x 64 tile of scalar FMAs; a plain 8192^3 library product reaches 154.
 constexpr int FK = 32;   // k-step
-// 128 x 128 tiles from one per CU on (the same problem in 64 x 64 tiles, whose waves
-// read a third more LDS per MFMA and meet at twice as many barriers: 1037 against 795 us
-// a training step); below that 64 x 64 tiles keep more CUs busy.
-constexpr long F32_BIG_TILES = 256;
-// Packed rows: 64 x 128 tiles of four waves, three workgroups a CU, which end their rounds
-// more evenly (us, 128 x 128 against 64 x 128: W1/W3 of 16 experts x 250 rows, d 1024, h 512
-// 151 and 117, x 2000 655 and 587; dA 94 and 90, 421 and 354; 64 experts x 300 rows 316 and
-// 258; dX 152 and 128, 632 and 630).  The weight gradients take 128 x 128 tiles from two per
-// CU on (16 x 250 rows, dW2 in 512 tiles 53 and 59, dW1/dW3 in 1024 97 and 106; 8 x 1000, dW2
-// in 256 105 and 100; 17 x 900, d 512, h 512, in 272 145 and 111).
-constexpr long F32_BIG_KVAR_TILES = 512;
 
 template <int BM, int BN, int WGM, int WGN, bool A_KC, bool B_KC, int EPI, int OPT>
 __global__ __launch_bounds__(64 * WGM * WGN) void gemm_f32_kernel(GemmParams p) {
@@ -1513,23 +1503,29 @@ hipError_t launch_f32_tile(GemmParams p, long max_rows, hipStream_t st) {
 // OPT, max_rows: as in run_dma and run_dma_var.
 template <bool A_KC, bool B_KC, int EPI, int OPT = 0>
 hipError_t run_f32(const GemmParams& p, hipStream_t st, long max_rows = 0) {
+  constexpr bool KVAR = (OPT & OPT_KVAR) != 0, GATHERED = (OPT & (OPT_GA | OPT_GB)) != 0;
+  // batches of rows of their own are read gathered, a split of k_total as it is
+  constexpr bool PACKED = !KVAR && A_KC, PACKED_K = KVAR && GATHERED;
   if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr) ||
-      ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) ||
-      ((OPT & OPT_KVAR) != 0 && !kvar_given(p)))
+      ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) || (KVAR && !kvar_given(p)) ||
+      (!PACKED && p.var_rows) || PACKED_K != (p.var_order != nullptr))
     return hipErrorInvalidValue;
   const int nw = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
-  const long big = (long)p.batches * ((p.M + 127) / 128) * ((nw + 127) / 128);
-  if constexpr ((OPT & OPT_KVAR) == 0 && A_KC) {
-    if (p.var_rows)
+  const F32Rows rows = p.var_order ? F32Rows::PACKED_K
+                                   : p.var_rows ? F32Rows::PACKED : F32Rows::UNIFORM;
+  const F32Form form = f32_form(rows, p.batches, p.M, nw);
+  if constexpr (PACKED) {
+    if (form == F32Form::WIDE)
       return launch_f32_tile<64, 128, 2, 2, A_KC, B_KC, EPI, OPT | OPT_MVAR>(p, max_rows, st);
   }
-  if constexpr ((OPT & OPT_KVAR) != 0) {
-    if (p.var_rows && big < F32_BIG_KVAR_TILES)
+  if constexpr (PACKED_K) {
+    if (form == F32Form::WIDE)
       return launch_f32_tile<64, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
+  } else {
+    if (form == F32Form::SMALL)
+      return launch_f32_tile<64, 64, 2, 1, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
   }
-  if (big >= F32_BIG_TILES)
-    return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
-  return launch_f32_tile<64, 64, 2, 1, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
+  return launch_f32_tile<128, 128, 2, 2, A_KC, B_KC, EPI, OPT>(p, max_rows, st);
 }
 
 GemmParams base_params() {
