@@ -350,14 +350,12 @@ int tc_validate(const ec_problem* p, int top_k, Plan* P, long* rmax, int* rmax_e
 }
 
 struct TcRouteWs {
-  float* ST;
   int32_t* cnt;
   int32_t* seg;
 };
 
-TcRouteWs carve_tc_route(Carve& c, const Plan& P, bool with_ST = true) {
+TcRouteWs carve_tc_route(Carve& c, const Plan& P) {
   TcRouteWs w;
-  w.ST = with_ST ? (float*)c.take((size_t)P.E * P.N * 4) : nullptr;
   w.cnt = (int32_t*)c.take((size_t)P.G * P.E * 4);
   w.seg = (int32_t*)c.take((size_t)P.G * P.E * 4);
   return w;
@@ -399,14 +397,14 @@ struct TcTrainRoute {
   int32_t* order;
 };
 
-// Router, row top-k, per-(group, expert) counts, offsets and placement; with `train` (null in
-// inference) no transposed scores.
+// Router, row top-k, per-(group, expert) counts, offsets and placement (`train`: null in
+// inference).  No transposed scores: the choice reads rows.
 int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* X, const void* Wg,
                      float* S, float* G, int32_t* slot, int32_t* rows, int32_t* sel,
                      const TcRouteWs& w, hipStream_t st, const TcTrainRoute* train = nullptr) {
   EC_HIP(mark(0, st));
-  EC_HIP(ec::launch_router_softmax(P.dtype, X, Wg, S, train ? nullptr : w.ST, P.N, P.d, P.E,
-                                   p->inv_temperature, st));
+  EC_HIP(ec::launch_router_softmax(P.dtype, X, Wg, S, nullptr, P.N, P.d, P.E, p->inv_temperature,
+                                   st));
   EC_HIP(mark(1, st));
   if (train) {
     EC_TRY(for_chunk_tables(
@@ -524,7 +522,7 @@ struct TcTrainFwdWs {
 
 TcTrainFwdWs carve_tc_train_fwd(Carve& c, const ec_problem* p, const Plan& P, long rmax) {
   TcTrainFwdWs w;
-  w.route = carve_tc_route(c, P, false);
+  w.route = carve_tc_route(c, P);
   w.balance = carve_balance(c, p, P, ec::TC_CHOOSE_CHUNK);
   w.O = c.take((size_t)rmax * P.d * P.esz);
   return w;

@@ -22,8 +22,8 @@ struct GroupTable {
   int seg[TOPK_MAX_GROUPS];         // first row of the group's segment in an expert buffer
 };
 
-// S [N,E] and ST [E,N] fp32 from X [N,d] and Wg [E,d].  ST null (token-choice training): no
-// transposed copy, and experts of equal logits get equal scores to the bit.
+// S [N,E] and ST [E,N] fp32 from X [N,d] and Wg [E,d].  ST null (token choice): no transposed
+// copy, and experts of equal logits get equal scores to the bit.
 hipError_t launch_router_softmax(int dtype, const void* X, const void* Wg, float* S, float* ST,
                                  int N, int d, int E, float inv_tau, hipStream_t st);
 

@@ -1,6 +1,6 @@
 // Router: logits Z = X Wg^T (Wg stored [E, d]) and S = softmax(Z / tau) over the
 // experts of each token (the score matrix S of Section 2.2).  Writes S [N, E]
-// and its transpose ST [E, N]; the column top-k reads ST so that each
+// and, for expert choice, its transpose ST [E, N]; the column top-k reads ST so that each
 // (group, expert) column is contiguous.
 //
 // bf16: one workgroup = 64 tokens, 4 groups of 16 tokens, each group split
