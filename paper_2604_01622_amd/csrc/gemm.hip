@@ -40,8 +40,7 @@
 // Token choice packs the rows that each expert keeps one expert after the other; how many
 // is known on the device only (var_rows).  Grids are sized for the most tiles there can be, a
 // wave finds its tile from the offsets by a scan over its lanes (var_tile), and the tile's
-// form is the host's guess of the rounds (var_rounds, run_fwd_rows, run_bwd_rows, the weight
-// gradients' launches).  16384 tokens, top 8 of 64, d 2048, h 1024: W1/W3 1042 us, W2 571, dA
+// form is the host's guess of the rounds (tile_forms.h).  16384 tokens, top 8 of 64, d 2048, h 1024: W1/W3 1042 us, W2 571, dA
 // 637, dW2 488, dX 1018, dW1/dW3 988, as expert choice's of as many rows; 512 tokens, top 8
 // (64 rows an expert) 135, 61, 63, 66, 104 and 140, where the weights' bytes bound them (3.6 to 5
 // TB/s).
@@ -1105,18 +1104,6 @@ hipError_t run_fwd(const GemmParams& p, hipStream_t st, long max_rows = 0) {
                                                              : run(std::integral_constant<int, 2>{});
 }
 
-// Tiles of batches of variable rows, whose counts the host does not know: it expects half a
-// row block more per batch than max_rows fills, one at least.  What counts is how many tiles
-// a CU takes one after the other (`at_once` run together); past the first, half a tile is
-// the expected wait for the last.
-double var_rounds(const GemmParams& p, long max_rows, int bm, int nt, int at_once) {
-  double blocks = (double)max_rows / bm + 0.5 * p.batches;
-  if (blocks < p.batches) blocks = p.batches;
-  if (!p.var_rows) blocks = (double)((max_rows + bm - 1) / bm);   // one batch
-  const double t = blocks * nt / at_once;
-  return t <= 1.0 ? 1.0 : t + 0.5;
-}
-
 // run_dma_var, or for one batch of max_rows rows (VAR false) run_dma.
 template <bool VAR, int BM, int BN, int WGM, int WGN, int STAGES, bool B_KC, int EPI, int TAG,
           int OPT = 0>
@@ -1128,52 +1115,27 @@ hipError_t run_rows(const GemmParams& p, long max_rows, hipStream_t st) {
     return run_dma<BM, BN, WGM, WGN, 64, STAGES, true, B_KC, EPI, false, TAG, OPT>(p, st);
 }
 
-// Few rows an expert in enough tiles only stream the weights: 256-row tiles, whose short
-// last blocks (OPT_TAILS) are then all there is.
-bool var_streams(const GemmParams& p, long max_rows, int nt) {
-  return max_rows <= 96l * p.batches && (long)p.batches * nt > 128;
-}
-
 // A forward product over packed rows or (VAR false: the shared experts) all tokens in one
-// batch: 256-row tiles, or smaller ones where those leave CUs idle or end in a poorly filled
-// round, by var_rounds and the time of a tile relative to a 256 x 256 one (192 rows 0.85; 128
-// rows, three stages, 0.65; 128 x 128 0.4).  Measured with rows spread by a factor of 1.35,
-// us of W1/W3 in tiles of 256, 192, 128 rows and 128 x 128: 8 experts x 128 rows, d 2048, h 1024 54, 46, 38 and 31; x 600 65, 52, 65 and 77; 16 x
-// 300, d 1024, h 512 38, 28, 23 and 32; 64 x 128, d 2048, h 1024 186, 183, 164 and 197; x 256
-// 193, 222, 208 and 284; x 512 296, 362, 372 and 503; 64 rows (streaming) 144, 143, 159 and
-// 157.  W2 follows (8 x 128 31, 24, 20, 17; 64 x 128 114, 112, 95, 105; x 512 180, 206, 197,
-// 267).
+// batch.
 template <int EPI, int TAG, bool VAR>
 hipError_t run_fwd_rows(const GemmParams& p, long max_rows, hipStream_t st) {
   const int width = EPI == EPI_SWIGLU ? 2 * p.N : p.N;
-  const int nt = (width + 255) / 256, nt128 = (width + 127) / 128;
-  if (!var_streams(p, max_rows, nt)) {
-    const double t256 = var_rounds(p, max_rows, 256, nt, 256);
-    const double t192 = 0.85 * var_rounds(p, max_rows, 192, nt, 256);
-    const double t128 = 0.65 * var_rounds(p, max_rows, 128, nt, 256);
-    const double tsq = 0.4 * var_rounds(p, max_rows, 128, nt128, 256);
-    if (tsq < t128 && tsq < t192 && tsq < t256)
+  switch (fwd_rows_form({VAR, p.batches, max_rows}, width)) {
+    case FwdForm::SQUARE_128:
       return run_rows<VAR, 128, 128, 2, 2, 3, true, EPI, TAG>(p, max_rows, st);
-    if (t128 < t192 && t128 < t256)
+    case FwdForm::ROWS_128:
       return run_rows<VAR, 128, 256, 2, 4, 3, true, EPI, TAG>(p, max_rows, st);
-    if (t192 < t256) return run_rows<VAR, 192, 256, 2, 2, 2, true, EPI, TAG>(p, max_rows, st);
+    case FwdForm::ROWS_192:
+      return run_rows<VAR, 192, 256, 2, 2, 2, true, EPI, TAG>(p, max_rows, st);
+    default: return run_fwd<256, EPI, TAG, VAR ? OPT_TAILS : 0, VAR>(p, st, max_rows);
   }
-  return run_fwd<256, EPI, TAG, VAR ? OPT_TAILS : 0, VAR>(p, st, max_rows);
 }
 
-// A backward product over packed rows or (VAR false) all tokens, with K-major weights: 256 x
-// 256 tiles, or 128 x 128, two at a time on a CU, by the same estimate; rel: a CU's time for
-// two of these relative to a 256 x 256 one's (dA 0.6, whose epilogues then overlap the other's
-// MFMAs; dX 0.7).
-// Measured as above, 256 x 256 against 128 x 128: dA of 8 experts x 600 rows, d 2048, h 1024
-// 61 and 44, 64 x 160 143 and 119, x 256 148 and 150, x 512 210 and 234, 24 x 400, d 1024, h
-// 1024 47 and 53; dX 8 x 128 63 and 40, 64 x 128 175 and 165, x 256 191 and 219.
+// A backward product over packed rows or (VAR false) all tokens, with K-major weights.
 template <int EPI, int TAG, bool VAR>
-hipError_t run_bwd_rows(const GemmParams& p, long max_rows, double rel, hipStream_t st) {
+hipError_t run_bwd_rows(const GemmParams& p, long max_rows, hipStream_t st) {
   constexpr int GM = EPI == EPI_SWIGLU_BWD ? 4 : 2;
-  const int nt = (p.N + 255) / 256, nt128 = (p.N + 127) / 128;
-  if (!var_streams(p, max_rows, nt) &&
-      rel * var_rounds(p, max_rows, 128, nt128, 512) < var_rounds(p, max_rows, 256, nt, 256))
+  if (bwd_rows_half({VAR, p.batches, max_rows}, p.N, EPI == EPI_SWIGLU_BWD))
     return run_rows<VAR, 128, 128, GM, 4 / GM, 2, false, EPI, TAG>(p, max_rows, st);
   return run_rows<VAR, 256, 256, 4, 2, 2, false, EPI, TAG, VAR ? OPT_TAILS : 0>(p, max_rows, st);
 }
@@ -1645,7 +1607,7 @@ hipError_t launch_gemm_dA(int dtype, const void* dO, const void* W2, const void*
   }
   if (shared && rows) return hipErrorInvalidValue;
   // B = W2 K-major: B(n, k) = W2[k, n]
-  if (shared) return run_bwd_rows<EPI_SWIGLU_BWD, G_SH_DA, false>(p, M, 0.6, st);
+  if (shared) return run_bwd_rows<EPI_SWIGLU_BWD, G_SH_DA, false>(p, M, st);
   return run_dma<256, 256, 4, 2, 64, 2, true, false, EPI_SWIGLU_BWD, false, G_DA, OPT_TAILS>(p, st);
 }
 
@@ -1663,7 +1625,7 @@ hipError_t launch_gemm_dXe(int dtype, const void* dH, const void* W1, const void
   // bf16: B K-major, rows k >= h from W3 (h is a multiple of the k-step); the
   // shared experts' input gradient is added to dX
   if (h % 64 != 0) return hipErrorInvalidValue;
-  if (shared) return run_bwd_rows<EPI_STORE_ADD, G_SH_DXE, false>(p, M, 0.7, st);
+  if (shared) return run_bwd_rows<EPI_STORE_ADD, G_SH_DXE, false>(p, M, st);
   return run_dma<256, 256, 4, 2, 64, 2, true, false, EPI_STORE, false, G_DXE, OPT_TAILS>(p, st);
 }
 
@@ -1826,7 +1788,7 @@ hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const v
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, false, EPI_SWIGLU_BWD>(p, st, max_rows);
-  return run_bwd_rows<EPI_SWIGLU_BWD, G_TC_DA, true>(p, max_rows, 0.6, st);
+  return run_bwd_rows<EPI_SWIGLU_BWD, G_TC_DA, true>(p, max_rows, st);
 }
 
 hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const void* W3,
@@ -1840,18 +1802,10 @@ hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const 
   p.var_rows = rows;
   if (max_rows == 0) return hipSuccess;
   if (dtype == DT_F32) return run_f32<true, false, EPI_STORE>(p, st, max_rows);
-  return run_bwd_rows<EPI_STORE, G_TC_DXE, true>(p, max_rows, 0.7, st);
+  return run_bwd_rows<EPI_STORE, G_TC_DXE, true>(p, max_rows, st);
 }
 
-// The weight gradients over packed rows.  An expert of few rows is an outer product whose
-// time is its output's way to memory: tiles half as wide with one stage (69 KB of LDS, 128
-// registers), two workgroups a CU, so that one's loads run beside the other's stores.
-// Measured, rows spread by a factor of 1.35 to 1.65, us against 256 x 256 tiles of two
-// stages, 64 experts, d 2048, h 1024: dW2 of 16 rows 71 and 60, 64 77 and 68, 128 91 and 84,
-// 384 147 and 143, 512 167 and 170; dW1/dW3 16 rows 117 and 103, 64 131 and 133, 128 168 and
-// 175; and where the wide tiles are few: 16 experts x 300 rows, d 1024, h 512, dW2 (128 wide
-// tiles) 20.5 and 19.8, dW1/dW3 (256) 24.7 and 19.8, 8 x 500, d 2048, h 1024 (256 and 512)
-// 27.7 and 28.3, 48 and 52.
+// The weight gradients over packed rows (their forms: dW2_half_wide, dW13_half_wide).
 hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* dW2, int E,
                                const int32_t* order, long max_rows,
                                int max_rows_per_expert, int d, int h, const int32_t* sel,
@@ -1864,7 +1818,7 @@ hipError_t launch_gemm_dW2_var(int dtype, const void* dY, const void* A, void* d
   p.C = dW2; p.c_bs = (long)d * h; p.ldc = h;
   p.var_order = reinterpret_cast<const int4*>(order);
   if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GA | OPT_KVAR>(p, st);
-  if (max_rows <= 384l * E || (long)E * ((d + 255) / 256) * ((h + 255) / 256) <= 192)
+  if (dW2_half_wide(E, max_rows, d, h))
     return run_dma<256, 128, 4, 2, 64, 1, false, false, EPI_STORE, false, G_TC_DW2,
                    OPT_GA | OPT_KVAR>(p, st);
   return run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW2,
@@ -1883,7 +1837,7 @@ hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* 
   p.C = dW1; p.C2 = dW3; p.c_split = h; p.c_bs = (long)h * d; p.ldc = d;
   p.var_order = reinterpret_cast<const int4*>(order);
   if (dtype == DT_F32) return run_f32<false, false, EPI_STORE, OPT_GB | OPT_KVAR>(p, st);
-  if (max_rows <= 48l * E || (long)E * ((2 * h + 255) / 256) * ((d + 255) / 256) <= 256)
+  if (dW13_half_wide(E, max_rows, d, h))
     return run_dma<128, 256, 2, 4, 64, 1, false, false, EPI_STORE, false, G_TC_DW13,
                    OPT_GB | OPT_KVAR>(p, st);
   return run_dma<256, 256, 4, 2, 64, 2, false, false, EPI_STORE, false, G_TC_DW13,
