@@ -282,7 +282,7 @@ int ec_tc_balance(const ec_problem *p, int32_t top_k, const float *S, float *los
  * b_gj = dloss_g E counts_gj / (top_k L^2),
  *   dZ_ij = inv_temperature S_ij (b_gj - sum_m S_im b_gm).
  *   counts [G, E] as ec_tc_balance wrote them; dloss [G] fp32 (device);
- *   dZ [N, E] fp32 out, may be S.  No workspace.                               */
+ *   dZ [N, E] fp32 out, may be S; other overlaps are refused.  No workspace.    */
 int ec_tc_balance_backward(const ec_problem *p, int32_t top_k, const float *S,
                            const int32_t *counts, const float *dloss, float *dZ,
                            hipStream_t stream);

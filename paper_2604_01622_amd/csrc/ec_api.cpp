@@ -1067,6 +1067,9 @@ int ec_tc_balance_backward(const ec_problem* p, int32_t top_k, const float* S,
   EC_TRY(check_ptr(counts, "counts"));
   EC_TRY(check_ptr(dloss, "dloss"));
   EC_TRY(check_ptr(dZ, "dZ", P.N == 0));
+  // in place a row is read by the lanes that write it; at any other offset by others
+  if (dZ != S && overlap(S, dZ, (size_t)P.N * P.E * 4))
+    return fail(EC_ERR_ARG, "S and dZ overlap");
   const int chunk = ec::balance_backward_chunk(P.N);
   return for_chunk_tables(p, P, chunk, [&](const ec::ChunkTable& tab, int g0, long) -> int {
     EC_HIP(ec::launch_balance_backward(S, counts + (size_t)g0 * P.E, dloss + g0, P.E, top_k,
