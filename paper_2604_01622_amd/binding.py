@@ -151,7 +151,7 @@ def _dtype_code(dt: torch.dtype) -> int:
 
 def _i32_array(a: np.ndarray):
     """A contiguous int32 array as a ctypes one over the same memory."""
-    if a.flags.writeable and a.size:
+    if a.size:
         return (ctypes.c_int32 * a.size).from_buffer(a)
     return a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
 
@@ -162,8 +162,10 @@ class Problem:
     def __init__(self, n_tokens: int, d_model: int, n_experts: int, d_ff: int,
                  group_offsets: Sequence[int], capacity: Sequence[int], inv_temperature: float,
                  dtype: torch.dtype, d_shared: int = 0):
-        self.off = np.ascontiguousarray(np.asarray(group_offsets, dtype=np.int32))
-        self.cap = np.ascontiguousarray(np.asarray(capacity, dtype=np.int32))
+        # copies: the library reads them at every call of a planned layer, whose saved buffer
+        # is laid out by them
+        self.off = np.array(np.asarray(group_offsets), dtype=np.int32, order="C", ndmin=1)
+        self.cap = np.array(np.asarray(capacity), dtype=np.int32, order="C", ndmin=1)
         self.dtype = dtype
         self.c = _Problem(int(n_tokens), int(d_model), int(n_experts), int(d_ff),
                           int(len(self.cap)), _i32_array(self.off), _i32_array(self.cap),
