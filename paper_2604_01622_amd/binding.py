@@ -166,6 +166,8 @@ class Problem:
         # is laid out by them
         self.off = np.array(np.asarray(group_offsets), dtype=np.int32, order="C", ndmin=1)
         self.cap = np.array(np.asarray(capacity), dtype=np.int32, order="C", ndmin=1)
+        if self.off.ndim != 1 or self.cap.ndim != 1 or len(self.off) != len(self.cap) + 1:
+            raise ECError(2, "group_offsets must have one entry more than capacity")
         self.dtype = dtype
         self.c = _Problem(int(n_tokens), int(d_model), int(n_experts), int(d_ff),
                           int(len(self.cap)), _i32_array(self.off), _i32_array(self.cap),
@@ -622,8 +624,6 @@ class TcLayer:
         self._given, self._forward_only, self._ran = saved is not None, not backward, False
         self.drop = _dropout_desc(X, dropout, rng, residual)
         self.P = Problem.of(X, Wg, W1.shape[1], group_offsets, capacity, inv_temperature, shared)
-        if len(self.P.off) != len(self.P.cap) + 1:
-            raise ECError(2, "group_offsets must have one entry more than capacity")
         L, k, dev = lib(), self.top_k, X.device
         n_saved = _tc_size(L.ec_tc_saved_size(self.P.ref, k))
         with _on(dev):

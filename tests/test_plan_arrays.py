@@ -1,6 +1,7 @@
 """A problem description keeps group offsets and capacities of its own (CPU only): a caller
 may reuse the arrays it passed while a planned layer is between its forward and backward."""
 import numpy as np
+import pytest
 import torch
 
 import paper_2604_01622_amd as ec
@@ -26,3 +27,11 @@ def test_any_layout_of_the_arrays():
     read_only = np.array([4, 4], dtype=np.int32)
     read_only.flags.writeable = False
     assert binding.Problem(8, 64, 4, 64, [0, 4, 8], read_only, 1.0, torch.float32).K == 8
+
+
+@pytest.mark.parametrize("off,cap", [([0, 8], [4, 4]), ([0, 4, 8], [4]), ([0], [8]), ([8], [8]),
+                                     ([0, 8], [[8]]), ([[0, 8]], [8])])
+def test_one_more_offset_than_capacities(off, cap):
+    """The library takes the group count from the capacities and reads one offset more."""
+    with pytest.raises(ec.ECError, match="group_offsets"):
+        binding.Problem(8, 64, 4, 64, off, cap, 1.0, torch.float32)
