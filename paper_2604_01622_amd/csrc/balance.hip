@@ -245,7 +245,7 @@ __global__ __launch_bounds__(BL_THREADS<Q>) void balance_partial_kernel(
   const int nt = min(tab.chunk, tab.len[g] - t0);   // tokens of the chunk
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15;
   double sum[Q][4];
-  uint32_t cnt[Q][2];   // two counts a register: a lane has at most 2^20 / 48 tokens
+  uint32_t cnt[Q][2];   // two counts a register: a lane has at most 65536 / 48 tokens
 #pragma unroll
   for (int q = 0; q < Q; ++q)
 #pragma unroll
@@ -598,12 +598,9 @@ void run_tc_dz(int dtype, const float* S, const float* G, const int32_t* slotT, 
 
 }  // namespace
 
-// Sums: 64 tokens a chunk, or so many that a batch has at most 256 chunks and its groups; 2^20
-// at most (a lane's counts are 16 bits).
-int balance_chunk(int N) {
-  const long c = ((long)N + 256 * 64 - 1) / (256 * 64) * 64;
-  return c < 1 << 20 ? (int)c : 1 << 20;
-}
+// Sums: 64 tokens a chunk, or so many that a batch has at most 256 chunks and its groups:
+// 65536 for the most tokens, below 2^24.
+int balance_chunk(int N) { return (N + 256 * 64 - 1) / (256 * 64) * 64; }
 
 // Gradients: 16 tokens (one each) while the workgroups are at most 1024, else 64.
 int balance_backward_chunk(int N) { return N <= 16384 ? 16 : 64; }

@@ -197,7 +197,7 @@ hipError_t launch_gemm_dW13_var(int dtype, const void* dH, const void* X, void* 
 // ---- the balance loss of token choice ----
 
 // The tokens of the table's groups go in chunks of `chunk`; tab.seg[g] is the first chunk
-// of group g in the launch and tab.seg[n] their number (balance_table fills it).
+// of group g in the launch and tab.seg[n] their number.
 struct ChunkTable {
   int n;
   int chunk;

@@ -231,7 +231,7 @@ __device__ __forceinline__ int km_swz(int k) { return ((k & 3) << 2) | ((k >> 2)
 // the rows of a K-major A / B through p.ka_rows / p.kb_rows.  OPT_TAILS:
 // the last row block and column block take a smaller tile where one holds them.
 // OPT_TILE_BASE: an ungathered K-contiguous A of any size, addressed tile by tile.
-// OPT_KVAR: the batches contract over rows of their own (GemmParams.var_rows).
+// OPT_KVAR: the batches contract over rows of their own (GemmParams.var_order, k_total).
 // OPT_MVAR: the batches have rows of their own.
 enum { OPT_GA = 1, OPT_GB = 2, OPT_TAILS = 4, OPT_TILE_BASE = 8, OPT_KVAR = 16, OPT_MVAR = 32 };
 template <int BM, int BN, int WGM, int WGN, int KSTEP, int STAGES, bool A_KC, bool B_KC, int EPI,
@@ -1467,7 +1467,8 @@ template <bool A_KC, bool B_KC, int EPI, int OPT = 0>
 hipError_t run_f32(const GemmParams& p, hipStream_t st, long max_rows = 0) {
   constexpr bool KVAR = (OPT & OPT_KVAR) != 0, GATHERED = (OPT & (OPT_GA | OPT_GB)) != 0;
   // batches of rows of their own are read gathered, a split of k_total as it is
-  constexpr bool PACKED = !KVAR && A_KC, PACKED_K = KVAR && GATHERED;
+  // (EPI_STORE_ADD: the shared experts' products alone)
+  constexpr bool PACKED = !KVAR && A_KC && EPI != EPI_STORE_ADD, PACKED_K = KVAR && GATHERED;
   if (((OPT & OPT_GA) != 0) != (p.ka_rows != nullptr) ||
       ((OPT & OPT_GB) != 0) != (p.kb_rows != nullptr) || (KVAR && !kvar_given(p)) ||
       (!PACKED && p.var_rows) || PACKED_K != (p.var_order != nullptr))

@@ -37,7 +37,7 @@ inline int wgrad_splits(int M, int N, int K) {
   return s < most ? s : most > 1 ? most : 1;
 }
 
-// The same where the tiles of all splits are one round: one a CU at most (5451 tokens, d
+// The same where the tiles of all splits are one round: one a CU at most (5450 tokens, d
 // 1472, hs 640: 13 and 8 splits instead of 15 and 9, whose 270 tiles took two rounds).
 inline int wgrad_splits_one_round(int M, int N, int K) {
   const int tiles = ((M + 255) / 256) * ((N + 255) / 256);
