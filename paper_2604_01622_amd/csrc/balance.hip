@@ -14,9 +14,11 @@
 //
 // Latency bounds all but the largest: 16384 tokens x 64 experts, top 8, 5.6 (sums), 4.2
 // (finish) and 5.6 us (gradient) for 4.2, 0.2 and 8.4 MB.  65536 x 256, top 8: 26.7, 5.6 and 25.6
-// us; the sums are bound by choosing (some 560 instructions a wave for four tokens; a pass
-// over all sixteen registers each round, without the sort, 32.1), the gradient moves 134 MB at
-// 5.2 TB/s.
+// us.  Of the sums' 26.7, some 15 are the issue of the instructions that choose (560 a wave for
+// four tokens; a pass over all sixteen registers each round, without the sort, 32.1); a
+// workgroup's twelve waves, one a CU, take its 256 tokens in six passes, the last a third full, and
+// nothing runs beside the reduction over the waves at the end.  The gradient moves 134 MB at 5.2
+// TB/s.
 #include <type_traits>
 
 #include "ec_common.h"
@@ -563,6 +565,7 @@ __global__ __launch_bounds__(256) void tc_dz_kernel(const float* __restrict__ S,
         if (dloss) z[c] = (float)((double)z[c] + (double)v[q][c] * (b[q][c] - dot));
         z[c] *= inv_tau;
       }
+      // (rounded to bf16 as the operand of the router's two products)
       T* out = dZ + (size_t)i * EP + 64 * q + 4 * r;   // EP = 64 Q
       if constexpr (sizeof(T) == 4)
         *reinterpret_cast<float4*>(out) = make_float4(z[0], z[1], z[2], z[3]);

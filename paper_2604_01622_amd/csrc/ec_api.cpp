@@ -494,6 +494,17 @@ struct TcSaved {
   void* As;
 };
 
+// Roundings to bf16 between the products (fp32 storage has none).  A, dH and dZ are operands of
+// the matrix instructions.  H1 and H3, O (the workspace's) and dXe are stored for their bytes:
+// 32 bits would move two more per element both ways, 1.07 GB or 174 us at copy speed for H1 and
+// H3, and as much for O and for dXe, of a step of 16384 tokens, top 8, d 2048, h 1024 (4.7 ms).
+// The shared experts' output lies in Y and the partial sums of dX in dX, [N, d] each, before the
+// combines add the packed rows to them.  One rounding is 1.66e-3 of its tensor in relative
+// 2-norm (2^-8 at most per element), and they are independent of each other: Y is 2.9e-3 off
+// (A, O and Y itself 1.7 each; with shared experts theirs 1.3 and O 1.0), dX 3.5e-3 (H1 and
+// H3 2.0, dH and dXe 1.5 each, dZ 0.7, dX's first write 0.6, its last 1.7; shared experts' 1.4),
+// dW1 and dW3 2.9e-3 (H 1.8, dH 1.7), dW2 2.4e-3 (A 1.7), dWg 3.3e-3 (H 2.8, dZ 1.8): each
+// rounding alone in a 64-bit evaluation of 1024 tokens, top 2 of 8, d 512, h 256.
 TcSaved carve_tc_saved(Carve& c, const Plan& P, long rmax) {
   TcSaved s;
   s.S = (float*)c.take((size_t)P.N * P.E * 4);

@@ -168,9 +168,9 @@ hipError_t launch_tc_place(int32_t* slotT, float* G, int N, int E, const GroupTa
 // gate (may be null): [max_rows] fp32, packed row r is written as A = gate[r] SiLU(H1) H3.
 // H1, H3 (may be null): [max_rows, h], the projections themselves.
 hipError_t launch_gemm_w13_var(int dtype, const void* Xe, const void* W1, const void* W3, void* A,
-                               void* H1, void* H3, int E, const int32_t* rows, long max_rows, int max_rows_per_expert, int d,
-                               int h, hipStream_t st, const int32_t* sel = nullptr,
-                               const float* gate = nullptr);
+                               void* H1, void* H3, int E, const int32_t* rows, long max_rows,
+                               int max_rows_per_expert, int d, int h, hipStream_t st,
+                               const int32_t* sel = nullptr, const float* gate = nullptr);
 hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O, int E,
                               const int32_t* rows, long max_rows,
                               int max_rows_per_expert, int d, int h, hipStream_t st);
@@ -180,8 +180,9 @@ hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O,
 // expert without rows gets zero weight gradients.  order [E, 4]: the experts as the
 // weight gradients take them (launch_tc_offsets).
 hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
-                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows, long max_rows, int max_rows_per_expert, int d,
-                              int h, const int32_t* sel, const float* gate, hipStream_t st);
+                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows,
+                              long max_rows, int max_rows_per_expert, int d, int h,
+                              const int32_t* sel, const float* gate, hipStream_t st);
 hipError_t launch_gemm_dXe_var(int dtype, const void* dH, const void* W1, const void* W3,
                                void* dXe, int E, const int32_t* rows, long max_rows,
                                int max_rows_per_expert, int d, int h, hipStream_t st);

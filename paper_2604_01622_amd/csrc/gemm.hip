@@ -40,10 +40,10 @@
 // Token choice packs the rows that each expert keeps one expert after the other; how many
 // is known on the device only (var_rows).  Grids are sized for the most tiles there can be, a
 // wave finds its tile from the offsets by a scan over its lanes (var_tile), and the tile's
-// form is the host's guess of the rounds (tile_forms.h).  16384 tokens, top 8 of 64, d 2048, h 1024: W1/W3 1042 us, W2 571, dA
-// 637, dW2 488, dX 1018, dW1/dW3 988, as expert choice's of as many rows; 512 tokens, top 8
-// (64 rows an expert) 135, 61, 63, 66, 104 and 140, where the weights' bytes bound them (3.6 to 5
-// TB/s).
+// form is the host's guess of the rounds (tile_forms.h).  16384 tokens, top 8 of 64, d 2048,
+// h 1024: W1/W3 1042 us, W2 571, dA 637, dW2 488, dX 1018, dW1/dW3 988, as expert choice's of
+// as many rows; 512 tokens, top 8 (64 rows an expert) 135, 61, 63, 66, 104 and 140, where the
+// weights' bytes bound them (3.6 to 5 TB/s).
 //
 // The products that read the selected tokens' rows (of X, or of the output
 // gradient dY) gather them in the operand load: the W1/W3 and dA products per
@@ -763,6 +763,7 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
           float a[8];
 #pragma unroll
           for (int u = 0; u < 8; ++u) a[u] = silu_f(v[e][u]) * v3[e][u] * g;
+          // A is the next product's operand; H1 and H3 are bf16 for their bytes (carve_tc_saved)
           Elem<bf16_t>::store8((bf16_t*)p.C + tc.c_off + (size_t)m * p.ldc + n, a);
           if (p.H1) {
             const size_t ho = tc.h_off + (size_t)m * p.ldh + n;
@@ -786,6 +787,7 @@ __device__ __forceinline__ void gemm_dma_tile(const GemmParams& p, const TileCoo
           }
           dots[e] = dot;
           const size_t off = tc.c_off + (size_t)m * p.ldc + n;
+          // operands of the next products
           Elem<bf16_t>::store8((bf16_t*)p.C + off, d1);
           Elem<bf16_t>::store8((bf16_t*)p.C2 + off, d3);
         }
@@ -1743,8 +1745,9 @@ hipError_t launch_shared_dW13(int dtype, const void* dH, const void* X, void* dW
 }
 
 hipError_t launch_gemm_w13_var(int dtype, const void* Xe, const void* W1, const void* W3, void* A,
-                               void* H1, void* H3, int E, const int32_t* rows, long max_rows, int max_rows_per_expert, int d,
-                               int h, hipStream_t st, const int32_t* sel, const float* gate) {
+                               void* H1, void* H3, int E, const int32_t* rows, long max_rows,
+                               int max_rows_per_expert, int d, int h, hipStream_t st,
+                               const int32_t* sel, const float* gate) {
   GemmParams p = base_params();
   p.gate = gate; p.H1 = H1; p.H3 = H3;
   p.A = Xe; p.lda = d;
@@ -1775,8 +1778,9 @@ hipError_t launch_gemm_w2_var(int dtype, const void* A, const void* W2, void* O,
 }
 
 hipError_t launch_gemm_dA_var(int dtype, const void* dY, const void* W2, const void* H1,
-                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows, long max_rows, int max_rows_per_expert, int d,
-                              int h, const int32_t* sel, const float* gate, hipStream_t st) {
+                              const void* H3, void* dH, float* dsp, int E, const int32_t* rows,
+                              long max_rows, int max_rows_per_expert, int d, int h,
+                              const int32_t* sel, const float* gate, hipStream_t st) {
   GemmParams p = base_params();
   p.A = dY; p.lda = d; p.a_rows = sel;
   p.gate = gate;
