@@ -346,6 +346,62 @@ int ec_tc_train_backward(const ec_problem *p, int32_t top_k, const ec_dropout_de
                          void *dW2, void *dWs1, void *dWs3, void *dWs2, void *ws,
                          size_t ws_bytes, hipStream_t stream);
 
+/* ---- Eight bits with scales.  A tensor's e4m3 codes (OCP, largest 448) and, for every 32
+ * consecutive elements of a row, a scale 2^(byte - 127) (E8M0): an element is code * scale.
+ * Written here, a scale is the smallest power of two that brings the block's largest
+ * magnitude to 448 or below, at least 2^-126, so nothing saturates; codes are rounded to
+ * nearest, ties to even.  A block that holds a NaN or an infinity has the byte 255 and NaN
+ * codes.  Rows of codes and of scales are dense.                                 */
+
+/* Q [rows, cols] codes, scale [rows, cols / 32] bytes of X [rows, cols] dtype; cols a
+ * multiple of 32; rows * cols < 2^40.                                           */
+int ec_mx_quantize(int dtype, int64_t rows, int64_t cols, const void *X, uint8_t *Q,
+                   uint8_t *scale, hipStream_t stream);
+
+/* ---- Root-mean-square norm in front of the layer, with the residual's addition:
+ *   H = X + residual, rounded to dtype (H = X without one);
+ *   Y = H (mean of H^2 over the row + eps)^(-1/2) weight, or that in eight bits.
+ * X, residual, H, Y [rows, d] dtype; weight [d] dtype; 1 <= d <= 16384; rows < 2^31;
+ * eps finite and > 0.  H is written where residual is given and may be X or the
+ * residual; other overlaps of outputs are refused.  Either Y or (d a multiple of 32) Q and
+ * scale is given.                                                                */
+int ec_rms_norm(int dtype, int64_t rows, int32_t d, float eps, const void *X,
+                const void *residual, const void *weight, void *H, void *Y, uint8_t *Q,
+                uint8_t *scale, hipStream_t stream);
+
+/* Workspace bytes of ec_rms_norm_backward; 0 on invalid sizes.                    */
+size_t ec_rms_norm_workspace_size(int dtype, int64_t rows, int32_t d);
+
+/* Its backward from H (X without a residual): dX [rows, d] dtype, the gradient in X and in
+ * the residual alike, of sum(Y dY) + sum(H dH) (dH may be NULL); dweight [d] fp32.
+ * dX may be H, dY or dH; other overlaps are refused.  The eight bits have no gradient of
+ * their own.  ws: ec_rms_norm_workspace_size bytes.                               */
+int ec_rms_norm_backward(int dtype, int64_t rows, int32_t d, float eps, const void *H,
+                         const void *weight, const void *dY, const void *dH, void *dX,
+                         float *dweight, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- Token choice for a few tokens (serving: one token a sequence):
+ *   y_i = residual_i + sum over j in C_i of g_ij FFN_j(x_i), plus the shared experts;
+ * C_i the top_k experts by logit (equal logits: the lower index; NaN below every number),
+ * g the softmax of the chosen logits times inv_temperature.  No pair is dropped: p's groups
+ * and capacities are checked but not used.  N <= EC_DECODE_MAX_TOKENS.
+ *   Weights as for ec_tc_forward.  mx (may be NULL): scales of those operands that are given
+ *   as codes: X alone, the six expert weights alone (all that the problem has), or both;
+ *   then dtype is EC_BF16.  Eight bits become bf16 exactly before they are multiplied.
+ *   residual, Y [N, d] dtype (residual may be NULL; Y may be X or the residual);
+ *   experts [N, top_k] int32 out, by falling logit; gates [N, top_k] fp32 out.
+ * ws: ec_tc_decode_workspace_size bytes (0 on an invalid problem), which grow with N.  */
+#define EC_DECODE_MAX_TOKENS 64
+size_t ec_tc_decode_workspace_size(const ec_problem *p, int32_t top_k);
+typedef struct {
+  const uint8_t *X, *W1, *W3, *W2, *Ws1, *Ws3, *Ws2;
+} ec_mx_scales;
+int ec_tc_decode(const ec_problem *p, int32_t top_k, const ec_mx_scales *mx, const void *X,
+                 const void *Wg, const void *W1, const void *W3, const void *W2,
+                 const void *Ws1, const void *Ws3, const void *Ws2, const void *residual,
+                 void *Y, int32_t *experts, float *gates, void *ws, size_t ws_bytes,
+                 hipStream_t stream);
+
 /* Stage timing for profiling.  After this call, every entry point called on
  * the same thread records events[0] on its stream before its first kernel and
  * events[s+1] after stage s, for s < n_events - 1, so that
@@ -363,8 +419,7 @@ int ec_tc_train_backward(const ec_problem *p, int32_t top_k, const ec_dropout_de
  * Stages of ec_route: 0 router+softmax, 1 top-k.
  * ec_tc_train_forward and ec_tc_train_backward have the stages of ec_moe_forward and
  * ec_moe_backward, with the balance loss in the forward's stage 1 and the dropout of
- * dY in the backward's stage 0.  ec_tc_balance, ec_tc_balance_backward and ec_dropout
- * record none.                                                                */
+ * dY in the backward's stage 0.  The other entry points record none.           */
 int ec_set_stage_events(hipEvent_t *events /* HOST array */, int n_events);
 
 #ifdef __cplusplus

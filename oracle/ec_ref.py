@@ -691,3 +691,76 @@ def router_grad_ref(X, Wg, W1, W3, W2, dY, sel_token, inv_tau: float = 1.0) -> n
         dS[rows, j] = np.sum(dYf[rows] * o, axis=1)
     dZ = S * (dS - np.sum(S * dS, axis=1, keepdims=True)) * float(inv_tau)
     return dZ.T @ Xf
+
+
+# ---- eight bits, the norm, a few tokens ------------------------------------------
+
+
+def mx_scale_ref(top):
+    """Scales of blocks whose largest magnitude is `top` (finite): the smallest power of two,
+    at least 2^-126, that brings it to 448 or below."""
+    top = np.asarray(top, dtype=np.float64)
+    m, x = np.frexp(top)                         # top = m 2^x, 1/2 <= m < 1; 448 = 7/8 2^9
+    e = np.where(top > 0, np.where(m <= 0.875, x - 9, x - 8), -126)
+    return np.ldexp(1.0, np.maximum(e, -126).astype(np.int64))
+
+
+def e4m3_ref(v):
+    """v (|v| <= 448) rounded to the nearest e4m3 number, ties to the even one: three bits
+    behind the leading one down to 2^-6, steps of 2^-9 below."""
+    v = np.asarray(v, dtype=np.float64)
+    _, x = np.frexp(np.where(v == 0, 1.0, v))
+    step = np.ldexp(1.0, np.maximum(x - 1, -6) - 3)
+    return np.rint(v / step) * step              # rint: half to even
+
+
+def mx_quantize_ref(X):
+    """Codes (their e4m3 values) [..., c] and scales [..., c / 32] of X."""
+    v = widen(X)
+    blocks = v.reshape(*v.shape[:-1], v.shape[-1] // 32, 32)
+    scale = mx_scale_ref(np.abs(blocks).max(-1))
+    return e4m3_ref(blocks / scale[..., None]).reshape(v.shape), scale
+
+
+def mx_value_ref(codes, scales):
+    """What codes and scales stand for."""
+    blocks = np.asarray(codes, np.float64).reshape(*np.shape(scales), 32)
+    return (blocks * np.asarray(scales, np.float64)[..., None]).reshape(np.shape(codes))
+
+
+def rms_norm_ref(H, weight, eps: float):
+    """H (mean(H^2) + eps)^(-1/2) weight, by rows."""
+    H, w = widen(H), widen(weight)
+    return H / np.sqrt(np.mean(H * H, axis=-1, keepdims=True) + eps) * w
+
+
+def rms_norm_backward_ref(dY, H, weight, eps: float, dH=None):
+    """Gradients of sum(Y dY) + sum(H dH) in H and in the weight (summed over the rows)."""
+    dY, H, w = widen(dY), widen(H), widen(weight)
+    r = 1.0 / np.sqrt(np.mean(H * H, axis=-1, keepdims=True) + eps)
+    g = dY * w
+    dX = r * g - r ** 3 * H * np.mean(g * H, axis=-1, keepdims=True)
+    if dH is not None:
+        dX = dX + widen(dH)
+    return dX, np.sum(dY * H * r, axis=tuple(range(H.ndim - 1)))
+
+
+def tc_decode_ref(X, Wg, W1, W3, W2, top_k: int, inv_tau: float = 1.0, shared=None,
+                  residual=None):
+    """Y, experts and gates of the token-choice layer without groups: every token keeps its
+    top_k experts by logit, lower index first among equals."""
+    Xf, W1f, W3f, W2f = (widen(a) for a in (X, W1, W3, W2))
+    Z = Xf @ widen(Wg).T
+    N, E = Z.shape
+    experts = np.array([sorted(range(E), key=lambda j: (-Z[i, j], j))[:top_k] for i in range(N)],
+                       dtype=np.int64).reshape(N, top_k)
+    z = np.take_along_axis(Z, experts, 1) * float(inv_tau)
+    ex = np.exp(z - z[:, :1])
+    gates = ex / ex.sum(1, keepdims=True)
+    Y = np.zeros_like(Xf) if residual is None else widen(residual).copy()
+    for i in range(N):
+        for j, g in zip(experts[i], gates[i]):
+            Y[i] += g * swiglu_ffn_ref(Xf[i:i + 1], W1f[j], W3f[j], W2f[j])[0]
+    if shared is not None:
+        Y += shared_ffn_ref(Xf, shared)
+    return Y, experts, gates

@@ -24,10 +24,17 @@ from .binding import (  # noqa: F401
     tc_train_forward,
     tc_train_backward,
     dropout,
+    Mx,
+    mx_quantize,
+    rms_norm,
+    rms_norm_backward,
+    tc_decode,
+    TcDecoder,
     Layer,
     TcLayer,
 )
 
 __all__ = ["ECError", "Problem", "Layer", "TcLayer", "route", "route_noalloc", "forward", "backward", "capacity",
            "saved_views", "token_coverage", "tc_capacity", "tc_route", "tc_forward", "tc_balance",
-           "tc_balance_backward", "tc_train_forward", "tc_train_backward", "dropout", "lib"]
+           "tc_balance_backward", "tc_train_forward", "tc_train_backward", "dropout", "Mx", "mx_quantize",
+           "rms_norm", "rms_norm_backward", "tc_decode", "TcDecoder", "lib"]

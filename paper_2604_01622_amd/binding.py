@@ -10,8 +10,9 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import math
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -26,7 +27,9 @@ EXPORTS = ("ec_status_string", "ec_last_error", "ec_total_capacity", "ec_workspa
            "ec_saved_size", "ec_saved_layout_of", "ec_capacity", "ec_route", "ec_route_noalloc", "ec_token_coverage", "ec_moe_forward",
            "ec_moe_backward", "ec_tc_capacity", "ec_tc_workspace_size", "ec_tc_route",
            "ec_tc_forward", "ec_tc_balance", "ec_tc_balance_backward", "ec_dropout",
-           "ec_tc_saved_size", "ec_tc_train_forward", "ec_tc_train_backward",
+           "ec_tc_saved_size", "ec_tc_train_forward", "ec_tc_train_backward", "ec_mx_quantize",
+           "ec_rms_norm", "ec_rms_norm_workspace_size", "ec_rms_norm_backward", "ec_tc_decode_workspace_size",
+           "ec_tc_decode",
            "ec_set_stage_events")
 
 
@@ -42,6 +45,10 @@ class _Problem(ctypes.Structure):
                 ("n_groups", ctypes.c_int32), ("group_offsets", ctypes.POINTER(ctypes.c_int32)),
                 ("capacity", ctypes.POINTER(ctypes.c_int32)), ("inv_temperature", ctypes.c_float),
                 ("dtype", ctypes.c_int), ("d_shared", ctypes.c_int32)]
+
+
+class _MxScales(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("X", "W1", "W3", "W2", "Ws1", "Ws3", "Ws2")]
 
 
 class _SavedLayout(ctypes.Structure):
@@ -115,6 +122,21 @@ def lib() -> ctypes.CDLL:
         L.ec_tc_train_backward.restype = ctypes.c_int
         L.ec_tc_train_backward.argtypes = ([pp, ctypes.c_int32, dp] + [vp] * 11 + [sz] + [vp] * 9
                                            + [sz, vp])
+        i64, f32 = ctypes.c_int64, ctypes.c_float
+        L.ec_mx_quantize.restype = ctypes.c_int
+        L.ec_mx_quantize.argtypes = [ctypes.c_int, i64, i64] + [vp] * 4
+        L.ec_rms_norm.restype = ctypes.c_int
+        L.ec_rms_norm.argtypes = [ctypes.c_int, i64, ctypes.c_int32, f32] + [vp] * 8
+        L.ec_rms_norm_workspace_size.restype = sz
+        L.ec_rms_norm_workspace_size.argtypes = [ctypes.c_int, i64, ctypes.c_int32]
+        L.ec_rms_norm_backward.restype = ctypes.c_int
+        L.ec_rms_norm_backward.argtypes = ([ctypes.c_int, i64, ctypes.c_int32, f32] + [vp] * 7
+                                           + [sz, vp])
+        L.ec_tc_decode_workspace_size.restype = sz
+        L.ec_tc_decode_workspace_size.argtypes = [pp, ctypes.c_int32]
+        L.ec_tc_decode.restype = ctypes.c_int
+        L.ec_tc_decode.argtypes = ([pp, ctypes.c_int32, ctypes.POINTER(_MxScales)] + [vp] * 13
+                                   + [sz, vp])
         L.ec_set_stage_events.restype = ctypes.c_int
         L.ec_set_stage_events.argtypes = [ctypes.POINTER(ctypes.c_void_p), ctypes.c_int]
         _lib = L
@@ -686,6 +708,205 @@ class TcLayer:
                                      *(self.dshared or (None,) * 3))],
                 self.ws_b.data_ptr(), self.ws_b.numel(), _raw_stream(self.X.device)))
         return (self.dX, self.dWg, self.dW1, self.dW3, self.dW2) + tuple(self.dshared or ())
+
+
+class Mx(NamedTuple):
+    """A tensor in eight bits: float8_e4m3fn codes [..., c] and, for every 32 consecutive
+    elements of a row, a power of two, float8_e8m0fnu [..., c / 32] (mx_quantize)."""
+
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _mx_empty(shape, device):
+    return Mx(torch.empty(shape, dtype=torch.float8_e4m3fn, device=device),
+              torch.empty((*shape[:-1], shape[-1] // 32), dtype=torch.float8_e8m0fnu,
+                          device=device))
+
+
+def _mx_operand(name, t, shape, device=None):
+    if not isinstance(t, Mx):
+        raise ECError(1, f"{name} must be in eight bits (Mx)")
+    _operand(f"{name}.codes", t.codes, torch.float8_e4m3fn, shape, device)
+    _operand(f"{name}.scales", t.scales, torch.float8_e8m0fnu,
+             (*t.codes.shape[:-1], t.codes.shape[-1] // 32), t.codes.device)
+
+
+def _rows(name, t):
+    """Rows and width of a tensor [..., d] of a storage type; refuses others."""
+    if not isinstance(t, torch.Tensor) or t.dim() < 1:
+        raise ECError(2, f"{name} must be a tensor of at least one dimension")
+    _dtype_code(t.dtype)
+    _operand(name, t, t.dtype)
+    return math.prod(t.shape[:-1]), t.shape[-1]
+
+
+def mx_quantize(X) -> Mx:
+    """X [..., c] (bf16 or fp32, c a multiple of 32) in eight bits: a scale is the smallest
+    power of two that brings its 32 elements to 448 or below; codes rounded to nearest even.
+    The experts' weights of tc_decode may be held so."""
+    rows, cols = _rows("X", X)
+    if cols % 32:
+        raise ECError(2, f"the last dimension must be a multiple of 32 (got {cols})")
+    with _on(X.device):
+        out = _mx_empty(X.shape, X.device)
+        _check(lib().ec_mx_quantize(_dtype_code(X.dtype), rows, cols, _addr(X), _addr(out.codes),
+                                    _addr(out.scales), _raw_stream(X.device)))
+    return out
+
+
+def rms_norm(X, weight, eps: float = 1e-6, residual=None, mx: bool = False, sum_out=None):
+    """Root-mean-square norm of the rows of X [..., d]: Y = H (mean(H^2) + eps)^-1/2 weight with
+    H = X + residual, rounded.  Returns Y (in eight bits, Mx, with mx), and with a residual
+    (Y, H).  sum_out receives H; it may be X or the residual."""
+    rows, d = _rows("X", X)
+    dev = X.device
+    _operand("weight", weight, X.dtype, (d,), dev)
+    if residual is not None:
+        _operand("residual", residual, X.dtype, X.shape, dev)
+    if sum_out is not None:
+        if residual is None:
+            raise ECError(1, "sum_out needs a residual")
+        _operand("sum_out", sum_out, X.dtype, X.shape, dev)
+    if mx and d % 32:
+        raise ECError(2, f"eight bits need rows of a multiple of 32 (got {d})")
+    with _on(dev):
+        Y = _mx_empty(X.shape, dev) if mx else torch.empty_like(X)
+        H = torch.empty_like(X) if residual is not None and sum_out is None else sum_out
+        _check(lib().ec_rms_norm(_dtype_code(X.dtype), rows, d, float(eps), _addr(X),
+                                 _addr(residual), _addr(weight), _addr(H),
+                                 None if mx else _addr(Y), _addr(Y.codes) if mx else None,
+                                 _addr(Y.scales) if mx else None, _raw_stream(dev)))
+    return Y if residual is None else (Y, H)
+
+
+def rms_norm_backward(dY, H, weight, eps: float = 1e-6, dH=None):
+    """Backward of rms_norm from H (X without a residual): gradients of sum(Y * dY) +
+    sum(H * dH).  Returns dX [..., d], which is the residual's gradient too, and the weight's
+    [d] in fp32."""
+    rows, d = _rows("H", H)
+    dev, code = H.device, _dtype_code(H.dtype)
+    _operand("weight", weight, H.dtype, (d,), dev)
+    _operand("dY", dY, H.dtype, H.shape, dev)
+    if dH is not None:
+        _operand("dH", dH, H.dtype, H.shape, dev)
+    with _on(dev):
+        dX = torch.empty_like(H)
+        dw = torch.empty((d,), dtype=torch.float32, device=dev)
+        ws = _empty(_tc_size(lib().ec_rms_norm_workspace_size(code, rows, d)), dev)
+        _check(lib().ec_rms_norm_backward(code, rows, d, float(eps), _addr(H), _addr(weight),
+                                          _addr(dY), _addr(dH), _addr(dX), dw.data_ptr(),
+                                          ws.data_ptr(), ws.numel(), _raw_stream(dev)))
+    return dX, dw
+
+
+DECODE_MAX_TOKENS = 64
+
+
+def _codes(t):
+    return t.codes if isinstance(t, Mx) else t
+
+
+def _scales(t):
+    return _addr(t.scales) if isinstance(t, Mx) else None
+
+
+class TcDecoder:
+    """The token-choice layer for a few tokens (serving), its weights held: every token takes
+    its top_k experts by logit and none is dropped.  Weights as for tc_forward, W1, W3, W2 and
+    the shared experts' all in the type of Wg or all in eight bits (Mx, with a bf16 Wg).
+    Workspace and outputs are allocated once, for max_tokens (at most 64).  A decoder has one
+    set of buffers: order its calls (and the replays of graphs that captured them)."""
+
+    def __init__(self, Wg, W1, W3, W2, top_k: int, inv_temperature=1.0, shared=None,
+                 max_tokens: int = DECODE_MAX_TOKENS):
+        mx = isinstance(W1, Mx)
+        if not isinstance(Wg, torch.Tensor) or Wg.dim() != 2:
+            raise ECError(2, "Wg must have 2 dimensions")
+        if not isinstance(_codes(W1), torch.Tensor) or _codes(W1).dim() != 3:
+            raise ECError(2, "W1 must have 3 dimensions")
+        _dtype_code(Wg.dtype)
+        dt, dev, (E, d), h = Wg.dtype, Wg.device, Wg.shape, _codes(W1).shape[1]
+        _operand("Wg", Wg, dt)
+        if mx and dt != torch.bfloat16:
+            raise ECError(4, "weights in eight bits need a bf16 Wg")
+        operands = [("W1", W1, (E, h, d)), ("W3", W3, (E, h, d)), ("W2", W2, (E, d, h))]
+        if shared is not None:
+            if len(shared) != 3 or not isinstance(_codes(shared[0]), torch.Tensor):
+                raise ECError(1, "shared must be (Ws1, Ws3, Ws2)")
+            hs = _codes(shared[0]).shape[0]
+            operands += [("Ws1", shared[0], (hs, d)), ("Ws3", shared[1], (hs, d)),
+                         ("Ws2", shared[2], (d, hs))]
+        for name, t, shape in operands:
+            if mx:
+                _mx_operand(name, t, shape, dev)
+            else:
+                _operand(name, t, dt, shape, dev)
+        if not 0 <= int(max_tokens) <= DECODE_MAX_TOKENS:
+            raise ECError(2, f"max_tokens must be in [0, {DECODE_MAX_TOKENS}]")
+        self.Wg, self.W1, self.W3, self.W2, self.shared = Wg, W1, W3, W2, shared
+        self.top_k, self.max_tokens = int(top_k), int(max_tokens)
+        self._device, self._d, self._dtype = dev, d, dt
+        P = Problem(self.max_tokens, d, E, h, [0, self.max_tokens], [0], inv_temperature, dt,
+                    0 if shared is None else _codes(shared[0]).shape[0])
+        n = _tc_size(lib().ec_tc_decode_workspace_size(P.ref, self.top_k))
+        self.P = P
+        six = (W1, W3, W2, *(shared or (None,) * 3))
+        self._weights = [_addr(_codes(t)) for t in (Wg, *six)]
+        self._scales = _MxScales(None, *[_scales(t) for t in six])
+        with _on(dev):
+            self.ws = _empty(n, dev)
+            self.Y = torch.empty((self.max_tokens, d), dtype=dt, device=dev)
+            self.experts = torch.empty((self.max_tokens, self.top_k), dtype=torch.int32,
+                                       device=dev)
+            self.gates = torch.empty((self.max_tokens, self.top_k), dtype=torch.float32,
+                                     device=dev)
+
+    def forward(self, X, residual=None, out=None):
+        """Y = residual + layer(X) of X [N, d] (in the type of Wg, or Mx), the chosen experts
+        [N, top_k] int32 by falling logit (equal logits: the lower index) and their gates
+        [N, top_k] fp32; rows of the decoder's buffers (Y: of out, if given, which may be X or
+        the residual)."""
+        dev, d = self._device, self._d
+        x = _codes(X)
+        if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.shape[1] != d:
+            raise ECError(2, f"X must be [N, {d}]")
+        N = x.shape[0]
+        if N > self.max_tokens:
+            raise ECError(2, f"X has {N} tokens, the decoder takes {self.max_tokens}")
+        if isinstance(X, Mx):
+            if self._dtype != torch.bfloat16:
+                raise ECError(4, "tokens in eight bits need a bf16 Wg")
+            _mx_operand("X", X, (N, d), dev)
+        else:
+            _operand("X", x, self._dtype, (N, d), dev)
+        if residual is not None:
+            _operand("residual", residual, self._dtype, (N, d), dev)
+        if out is not None:
+            _operand("out", out, self._dtype, (N, d), dev)
+        Y = self.Y[:N] if out is None else out
+        experts, gates = self.experts[:N], self.gates[:N]
+        self.P.off[1] = self.P.c.n_tokens = N
+        self._scales.X = _scales(X)
+        with _on(dev):
+            _check(lib().ec_tc_decode(self.P.ref, self.top_k, ctypes.byref(self._scales), _addr(x),
+                                      *self._weights, _addr(residual), _addr(Y), _addr(experts),
+                                      _addr(gates), self.ws.data_ptr(), self.ws.numel(),
+                                      _raw_stream(dev)))
+        return Y, experts, gates
+
+
+def tc_decode(X, Wg, W1, W3, W2, top_k: int, inv_temperature=1.0, shared=None, residual=None,
+              out=None):
+    """Token-choice layer of a few tokens (at most 64), none dropped: see TcDecoder, which keeps
+    the buffers that this allocates.  Returns Y [N,d], experts [N,top_k] and gates [N,top_k]."""
+    x = _codes(X)
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ECError(2, "X must have 2 dimensions")
+    if x.shape[0] > DECODE_MAX_TOKENS:
+        raise ECError(2, f"X has {x.shape[0]} tokens, at most {DECODE_MAX_TOKENS} are taken")
+    layer = TcDecoder(Wg, W1, W3, W2, top_k, inv_temperature, shared, x.shape[0])
+    return layer.forward(X, residual, out)
 
 
 FORWARD_STAGES = ("router", "topk", "gather", "gemm_w13_swiglu", "gemm_w2", "shared_w13_swiglu",

@@ -445,6 +445,48 @@ int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* 
   return EC_OK;
 }
 
+// ---- a few tokens ---------------------------------------------------------------
+
+int decode_validate(const ec_problem* p, int top_k, Plan* P) {
+  long rmax;
+  int rmax_e;
+  EC_TRY(tc_validate(p, top_k, P, &rmax, &rmax_e));
+  if (P->N > EC_DECODE_MAX_TOKENS)
+    return fail(EC_ERR_SHAPE, "n_tokens must be at most %d (got %d)", EC_DECODE_MAX_TOKENS, P->N);
+  return EC_OK;
+}
+
+ec::DecodeCall carve_decode(Carve& c, const Plan& P, int top_k) {
+  ec::DecodeCall w = {};
+  w.dtype = P.dtype;
+  w.N = P.N;
+  w.d = P.d;
+  w.E = P.E;
+  w.h = P.h;
+  w.hs = P.hs;
+  w.k = top_k;
+  const size_t rows = (size_t)P.N * top_k, slots = rows < (size_t)P.E ? rows : P.E;
+  w.Z = (float*)c.take((size_t)P.N * P.E * 4);
+  w.plan.active = (int32_t*)c.take(4);
+  w.plan.list = (uint32_t*)c.take(slots * 4);
+  w.plan.rows = (uint32_t*)c.take(slots * ec::DECODE_TOKENS * 4);
+  w.plan.pick = (uint16_t*)c.take(slots * ec::DECODE_TOKENS * 2);
+  w.Xb = P.dtype == EC_BF16 ? c.take((size_t)P.N * P.d * 2) : nullptr;
+  w.A = c.take(rows * P.h * P.esz);
+  w.As = c.take((size_t)P.N * P.hs * P.esz);
+  w.zero = c.take((size_t)(P.h > P.hs ? P.h : P.hs) * P.esz);
+  return w;
+}
+
+int norm_validate(int dtype, int64_t rows, int32_t d, float eps) {
+  g_last_error[0] = '\0';
+  if (dtype != EC_F32 && dtype != EC_BF16) return fail(EC_ERR_DTYPE, "unknown dtype %d", dtype);
+  if (rows < 0 || rows >= (int64_t)1 << 31) return fail(EC_ERR_SHAPE, "rows must be in [0, 2^31)");
+  if (d < 1 || d > 16384) return fail(EC_ERR_SHAPE, "d must be in [1, 16384] (got %d)", d);
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(EC_ERR_ARG, "eps must be finite and > 0");
+  return EC_OK;
+}
+
 // ---- dropout -------------------------------------------------------------------
 
 // The launch form of a description; without one (or with p below 2^-17) nothing is dropped.
@@ -473,6 +515,13 @@ float take_scale(ec::Dropout* d) {
 bool overlap(const void* a, const void* b, size_t bytes) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return x < y ? y - x < bytes : x - y < bytes;
+}
+
+// Whether two ranges share a byte; a null or empty one meets none.
+bool meet(const void* a, size_t na, const void* b, size_t nb) {
+  if (!a || !b || !na || !nb) return false;
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y ? y - x < na : x - y < nb;
 }
 
 // ---- token-choice training ------------------------------------------------------
@@ -962,6 +1011,14 @@ size_t ec_tc_workspace_size(const ec_problem* p, int32_t top_k, int mode) {
   return c.used;
 }
 
+size_t ec_tc_decode_workspace_size(const ec_problem* p, int32_t top_k) {
+  Plan P;
+  if (decode_validate(p, top_k, &P) != EC_OK) return 0;
+  Carve c(nullptr);
+  carve_decode(c, P, top_k);
+  return c.used;
+}
+
 size_t ec_tc_saved_size(const ec_problem* p, int32_t top_k) {
   Plan P;
   long rmax;
@@ -1289,6 +1346,155 @@ int ec_tc_train_backward(const ec_problem* p, int32_t top_k, const ec_dropout_de
   EC_HIP(mark(12, stream));
   EC_HIP(ec::launch_router_dwg(P.dtype, b.dZ, X, dWg, b.part, b.splits, N, E, P.EP, d, stream));
   EC_HIP(mark(13, stream));
+  return EC_OK;
+}
+
+// ---- eight bits, the norm, a few tokens -------------------------------------------
+
+int ec_mx_quantize(int dtype, int64_t rows, int64_t cols, const void* X, uint8_t* Q,
+                   uint8_t* scale, hipStream_t stream) {
+  g_last_error[0] = '\0';
+  if (dtype != EC_F32 && dtype != EC_BF16) return fail(EC_ERR_DTYPE, "unknown dtype %d", dtype);
+  if (rows < 0 || cols < 0 || cols % 32)
+    return fail(EC_ERR_SHAPE, "rows must be >= 0 and cols a multiple of 32");
+  if (cols && rows >= ((int64_t)1 << 40) / cols)
+    return fail(EC_ERR_SHAPE, "rows * cols must be below 2^40");
+  const int64_t n = rows * cols;
+  EC_TRY(check_ptr(X, "X", n == 0));
+  EC_TRY(check_ptr(Q, "Q", n == 0));
+  EC_TRY(check_ptr(scale, "scale", n == 0));
+  const size_t in = (size_t)n * (dtype == EC_F32 ? 4 : 2);
+  if (meet(X, in, Q, (size_t)n) || meet(X, in, scale, (size_t)n / 32) ||
+      meet(Q, (size_t)n, scale, (size_t)n / 32))
+    return fail(EC_ERR_ARG, "X, Q and scale overlap");
+  EC_HIP(ec::launch_mx_quantize(dtype, X, Q, scale, n, stream));
+  return EC_OK;
+}
+
+int ec_rms_norm(int dtype, int64_t rows, int32_t d, float eps, const void* X, const void* residual,
+                const void* weight, void* H, void* Y, uint8_t* Q, uint8_t* scale,
+                hipStream_t stream) {
+  EC_TRY(norm_validate(dtype, rows, d, eps));
+  const bool none = rows == 0;
+  EC_TRY(check_ptr(X, "X", none));
+  EC_TRY(check_ptr(weight, "weight"));
+  EC_TRY(check_ptr(residual, "residual", true));
+  EC_TRY(check_ptr(H, "H", !residual));
+  if (H && !residual) return fail(EC_ERR_ARG, "H is X without a residual: none is written");
+  if (Y && (Q || scale)) return fail(EC_ERR_ARG, "Y or Q and scale, not both");
+  if (Q || scale) {
+    if (d % 32) return fail(EC_ERR_SHAPE, "eight bits need d a multiple of 32 (got %d)", d);
+    EC_TRY(check_ptr(Q, "Q"));
+    EC_TRY(check_ptr(scale, "scale"));
+  } else {
+    EC_TRY(check_ptr(Y, "Y", none));
+  }
+  const size_t n = (size_t)rows * d, esz = dtype == EC_F32 ? 4 : 2, bytes = n * esz;
+  struct { const void* p; size_t size; } outs[] = {{H, bytes}, {Y, bytes}, {Q, n}, {scale, n / 32}};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (meet(outs[i].p, outs[i].size, outs[j].p, outs[j].size))
+        return fail(EC_ERR_ARG, "outputs overlap");
+    if (meet(outs[i].p, outs[i].size, weight, (size_t)d * esz))
+      return fail(EC_ERR_ARG, "an output overlaps the weight");
+    // H is written by the lane that read the element; anything else may come too early
+    if ((meet(outs[i].p, outs[i].size, X, bytes) && !(i == 0 && H == X)) ||
+        (meet(outs[i].p, outs[i].size, residual, bytes) && !(i == 0 && H == residual)))
+      return fail(EC_ERR_ARG, "an output overlaps X or the residual");
+  }
+  EC_HIP(ec::launch_rms_norm(dtype, X, residual, weight, H, Y, Q, scale, rows, d, eps, stream));
+  return EC_OK;
+}
+
+size_t ec_rms_norm_workspace_size(int dtype, int64_t rows, int32_t d) {
+  if (norm_validate(dtype, rows, d, 1.f) != EC_OK) return 0;
+  return align_up((size_t)ec::rms_norm_backward_blocks(dtype, rows, d) * d * 4);
+}
+
+int ec_rms_norm_backward(int dtype, int64_t rows, int32_t d, float eps, const void* H,
+                         const void* weight, const void* dY, const void* dH, void* dX,
+                         float* dweight, void* ws, size_t ws_bytes, hipStream_t stream) {
+  EC_TRY(norm_validate(dtype, rows, d, eps));
+  const bool none = rows == 0;
+  EC_TRY(check_ptr(H, "H", none));
+  EC_TRY(check_ptr(weight, "weight"));
+  EC_TRY(check_ptr(dY, "dY", none));
+  EC_TRY(check_ptr(dH, "dH", true));
+  EC_TRY(check_ptr(dX, "dX", none));
+  EC_TRY(check_ptr(dweight, "dweight"));
+  EC_TRY(check_ptr(ws, "workspace"));
+  const size_t need = ec_rms_norm_workspace_size(dtype, rows, d);
+  if (ws_bytes < need)
+    return fail(EC_ERR_WORKSPACE, "workspace %zu bytes < %zu required", ws_bytes, need);
+  const size_t esz = dtype == EC_F32 ? 4 : 2, bytes = (size_t)rows * d * esz;
+  const void* ins[] = {H, dY, dH};
+  for (const void* p : ins) {
+    if (dX != p && meet(dX, bytes, p, bytes))
+      return fail(EC_ERR_ARG, "dX overlaps an input at another offset");
+    if (meet(dweight, (size_t)d * 4, p, bytes)) return fail(EC_ERR_ARG, "dweight overlaps an input");
+  }
+  if (meet(dX, bytes, weight, (size_t)d * esz) || meet(dX, bytes, dweight, (size_t)d * 4) ||
+      meet(dweight, (size_t)d * 4, weight, (size_t)d * esz))
+    return fail(EC_ERR_ARG, "dX, dweight and the weight overlap");
+  EC_HIP(ec::launch_rms_norm_backward(dtype, H, weight, dY, dH, dX, dweight, (float*)ws, rows, d,
+                                      eps, stream));
+  return EC_OK;
+}
+
+int ec_tc_decode(const ec_problem* p, int32_t top_k, const ec_mx_scales* mx, const void* X,
+                 const void* Wg, const void* W1, const void* W3, const void* W2, const void* Ws1,
+                 const void* Ws3, const void* Ws2, const void* residual, void* Y, int32_t* experts,
+                 float* gates, void* ws, size_t ws_bytes, hipStream_t stream) {
+  Plan P;
+  EC_TRY(decode_validate(p, top_k, &P));
+  const bool none = P.N == 0;
+  EC_TRY(check_ptr(X, "X", none));
+  EC_TRY(check_ptr(Wg, "Wg"));
+  EC_TRY(check_ptr(W1, "W1"));
+  EC_TRY(check_ptr(W3, "W3"));
+  EC_TRY(check_ptr(W2, "W2"));
+  EC_TRY(check_ptr(Ws1, "Ws1", P.hs == 0));
+  EC_TRY(check_ptr(Ws3, "Ws3", P.hs == 0));
+  EC_TRY(check_ptr(Ws2, "Ws2", P.hs == 0));
+  EC_TRY(check_ptr(residual, "residual", true));
+  EC_TRY(check_ptr(Y, "Y", none));
+  EC_TRY(check_ptr(experts, "experts", none));
+  EC_TRY(check_ptr(gates, "gates", none));
+  const ec_mx_scales no_scales = {};
+  const ec_mx_scales s = mx ? *mx : no_scales;
+  const bool wmx = s.W1 || s.W3 || s.W2 || s.Ws1 || s.Ws3 || s.Ws2;
+  if ((s.X || wmx) && P.dtype != EC_BF16)
+    return fail(EC_ERR_DTYPE, "eight bits need the bf16 storage type");
+  EC_TRY(check_ptr(s.X, "the scales of X", true));
+  if (wmx) {
+    EC_TRY(check_ptr(s.W1, "the scales of W1"));
+    EC_TRY(check_ptr(s.W3, "the scales of W3"));
+    EC_TRY(check_ptr(s.W2, "the scales of W2"));
+    EC_TRY(check_ptr(s.Ws1, "the scales of Ws1", P.hs == 0));
+    EC_TRY(check_ptr(s.Ws3, "the scales of Ws3", P.hs == 0));
+    EC_TRY(check_ptr(s.Ws2, "the scales of Ws2", P.hs == 0));
+  }
+  // Y is written after the last read of X, an element after the residual's
+  const size_t rows = (size_t)P.N * P.d, bytes = rows * P.esz, xbytes = s.X ? rows : bytes;
+  if ((Y != X && meet(Y, bytes, X, xbytes)) ||
+      (Y != residual && meet(Y, bytes, residual, bytes)))
+    return fail(EC_ERR_ARG, "Y overlaps X or the residual at another offset");
+  const size_t need = ec_tc_decode_workspace_size(p, top_k);
+  EC_TRY(check_ptr(ws, "workspace"));
+  if (ws_bytes < need)
+    return fail(EC_ERR_WORKSPACE, "workspace %zu bytes < %zu required", ws_bytes, need);
+  Carve c(ws);
+  ec::DecodeCall call = carve_decode(c, P, top_k);
+  call.inv_tau = p->inv_temperature;
+  call.X = X;
+  call.Xs = s.X;
+  call.Wg = Wg;
+  call.w = {W1, W3, W2, Ws1, Ws3, Ws2, s.W1, s.W3, s.W2, s.Ws1, s.Ws3, s.Ws2};
+  call.R = residual;
+  call.Y = Y;
+  call.experts = experts;
+  call.gates = gates;
+  EC_HIP(ec::launch_decode(call, stream));
   return EC_OK;
 }
 

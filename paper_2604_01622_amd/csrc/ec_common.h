@@ -91,6 +91,57 @@ template <> struct Elem<bf16_t> {
   static __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = (bf16_t)f32_to_bf16(v); }
 };
 
+// VEC consecutive elements as fp32, 16 bytes at most: p is aligned to their size.
+template <typename T, int VEC>
+__device__ __forceinline__ void load_vec(const T* p, float* v) {
+  static_assert(VEC == 1 || VEC * sizeof(T) == 16, "");
+  if constexpr (VEC == 1) {
+    v[0] = Elem<T>::load1(p);
+  } else if constexpr (sizeof(T) == 2) {
+    Elem<T>::load8(p, v);
+  } else {
+    const float4 a = *reinterpret_cast<const float4*>(p);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  }
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ void store_vec(T* p, const float* v) {
+  if constexpr (VEC == 1)
+    Elem<T>::store1(p, v[0]);
+  else if constexpr (VEC == 8)
+    Elem<T>::store8(p, v);
+  else
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+}
+
+// Four consecutive elements.
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, float* v) {
+  if constexpr (sizeof(T) == 2) {
+    const uint2 a = *reinterpret_cast<const uint2*>(p);
+    v[0] = bf16_to_f32(a.x & 0xffffu); v[1] = bf16_to_f32(a.x >> 16);
+    v[2] = bf16_to_f32(a.y & 0xffffu); v[3] = bf16_to_f32(a.y >> 16);
+  } else {
+    load_vec<T, 4>(p, v);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float* v) {
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  else
+    store_vec<T, 4>(p, v);
+}
+
+// A value as the storage type holds it.
+template <typename T>
+__device__ __forceinline__ float round_to(float v) {
+  if constexpr (sizeof(T) == 2) return bf16_to_f32(f32_to_bf16(v));
+  return v;
+}
+
 // Hardware exp2 and reciprocal (about 1 ulp each): the activations feed bf16
 // stores or fp32 sums whose tolerance is far wider.
 __device__ __forceinline__ float sigmoid_f(float z) {

@@ -253,4 +253,59 @@ hipError_t launch_tc_router_dz(int dtype, const float* S, const float* G, const 
 hipError_t launch_zero(void* p, size_t bytes, hipStream_t st);
 
 
+// H = X + R, rounded (H = X where R is null; H may be X or R), and Y = H (mean(H^2) + eps)^-1/2 w
+// a row of d, or its codes Q and scales in eight bits (Y null; d a multiple of 32).
+hipError_t launch_rms_norm(int dtype, const void* X, const void* R, const void* w, void* H, void* Y,
+                           uint8_t* Q, uint8_t* scale, long rows, int d, float eps,
+                           hipStream_t st);
+
+// dX = the norm's gradient + dH (may be null); dw [d] fp32; part: [blocks, d] fp32, used where
+// blocks > 1.  dX may be H, dY or dH.
+int rms_norm_backward_blocks(int dtype, long rows, int d);
+hipError_t launch_rms_norm_backward(int dtype, const void* H, const void* w, const void* dY,
+                                    const void* dH, void* dX, float* dw, float* part, long rows,
+                                    int d, float eps, hipStream_t st);
+
+// Codes and scales of n elements (a multiple of 32).
+hipError_t launch_mx_quantize(int dtype, const void* X, uint8_t* Q, uint8_t* scale, long n,
+                              hipStream_t st);
+
+// The token-choice layer for a few tokens.
+constexpr int DECODE_TOKENS = 64;
+
+// Weights, or their codes beside the scales [rows, columns / 32] (null: storage type).
+struct DecodeWeights {
+  const void *W1, *W3, *W2, *Ws1, *Ws3, *Ws2;
+  const uint8_t *S1, *S3, *S2, *Ss1, *Ss3, *Ss2;
+};
+
+// Who chose what: chosen experts in ascending order ("slots").
+struct DecodePlan {
+  int32_t* active;    // [1] chosen experts
+  uint32_t* list;     // [slots] expert | tokens << 16
+  uint32_t* rows;     // [slots, 64] token << 16 | pick, the tokens that chose it, ascending
+  uint16_t* pick;     // [slots, 64] by token: pick + 1, or 0
+};
+
+struct DecodeCall {
+  int dtype, N, d, E, h, hs, k;
+  float inv_tau;
+  const void* X;          // or the tokens' codes, with their scales Xs (may be null)
+  const uint8_t* Xs;
+  const void* Wg;
+  DecodeWeights w;
+  const void* R;          // residual (may be null)
+  void* Y;
+  int32_t* experts;       // [N, k]
+  float* gates;           // [N, k]
+  // workspace
+  float* Z;               // [N, E]
+  DecodePlan plan;
+  void* Xb;               // [N, d] tokens in eight bits as bf16
+  void* A;                // [N k, h]
+  void* As;               // [N, hs]
+  void* zero;             // [max(h, hs)]
+};
+hipError_t launch_decode(const DecodeCall& c, hipStream_t st);
+
 }  // namespace ec
