@@ -279,12 +279,11 @@ struct DecodeWeights {
   const uint8_t *S1, *S3, *S2, *Ss1, *Ss3, *Ss2;
 };
 
-// Who chose what: chosen experts in ascending order ("slots").
+// Who chose what: the chosen experts in ascending order ("slots").
 struct DecodePlan {
-  int32_t* active;    // [1] chosen experts
+  int32_t* active;    // [1] slots
   uint32_t* list;     // [slots] expert | tokens << 16
   uint32_t* rows;     // [slots, 64] token << 16 | pick, the tokens that chose it, ascending
-  uint16_t* pick;     // [slots, 64] by token: pick + 1, or 0
 };
 
 struct DecodeCall {
@@ -299,13 +298,14 @@ struct DecodeCall {
   int32_t* experts;       // [N, k]
   float* gates;           // [N, k]
   // workspace
-  float* Z;               // [N, E]
+  float* Z;               // [decode_splits(d), N, E] shares of the logits
   DecodePlan plan;
   void* Xb;               // [N, d] tokens in eight bits as bf16
   void* A;                // [N k, h]
   void* As;               // [N, hs]
-  void* zero;             // [max(h, hs)]
+  float* O;               // [N k + N, d] (the last N rows: the shared experts')
 };
+int decode_splits(int d);
 hipError_t launch_decode(const DecodeCall& c, hipStream_t st);
 
 }  // namespace ec
