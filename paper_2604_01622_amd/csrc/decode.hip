@@ -20,9 +20,6 @@ namespace ec {
 
 namespace {
 
-// What a lane holds of a unit, 64 consecutive k of its row (a weight row, or token lane & 15);
-// q = lane >> 4 says which.  The MFMAs take the k in any order that both operands share.
-//
 // Eight codes as bf16, times 2^(byte - 127).
 __device__ __forceinline__ bf16x8 mx_widen8(uint32_t lo, uint32_t hi, float scale) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
@@ -41,81 +38,133 @@ __device__ __forceinline__ f32x4 mma_bf16(u32x4 a, u32x4 b, f32x4 acc) {
                                                  __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
 }
 
-// bf16: 16 bytes at 16 q of both halves, so that an instruction takes 64 consecutive bytes of
-// each of 16 rows.
+// Weights come in chunks, 256 bytes of each of 16 rows: sixteen pieces of 16 bytes a row.  As
+// the MFMAs' A operand a lane needs row lane & 15 and, of each quarter s of the chunk, piece
+// 4 s + q, q = lane >> 4; the k of its column (a token) that they meet are B's.
+//
+// bf16: a chunk is 128 k, a piece 8 of them.
 struct WBf16 {
   typedef bf16_t T;       // tokens and activations
   typedef bf16_t Code;
-  static constexpr int BURST = 4;     // units of one matrix that are requested at once
+  static constexpr int K = 128;       // k of a chunk
   static constexpr bool MX = false;
   struct B {
-    u32x4 r[2];
-    __device__ __forceinline__ void load(const bf16_t* row, int q) {
-      r[0] = *reinterpret_cast<const u32x4*>(row + q * 8);
-      r[1] = *reinterpret_cast<const u32x4*>(row + 32 + q * 8);
+    u32x4 r[4];
+    // row: the token's, at the chunk; `left` k are there (a multiple of 64)
+    __device__ __forceinline__ void load(const bf16_t* row, int q, int left) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) r[s] = *reinterpret_cast<const u32x4*>(row + min(s * 32, left - 32) + q * 8);
     }
   };
-  u32x4 r[2];
-  __device__ __forceinline__ void load(const Code* row, const uint8_t*, int q) {
-    r[0] = *reinterpret_cast<const u32x4*>(row + q * 8);
-    r[1] = *reinterpret_cast<const u32x4*>(row + 32 + q * 8);
-  }
-  __device__ __forceinline__ void mma(f32x4& acc, const B& b) const {
-    acc = mma_bf16(r[0], b.r[0], acc);
-    acc = mma_bf16(r[1], b.r[1], acc);
+  static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const uint2&, const B& b,
+                                             int, int left) {
+    acc = mma_bf16(a[0], b.r[0], acc);
+    acc = mma_bf16(a[1], b.r[1], acc);
+    if (left < K) return;
+    acc = mma_bf16(a[2], b.r[2], acc);
+    acc = mma_bf16(a[3], b.r[3], acc);
   }
 };
 
-// Eight bits: the 16 codes at 16 q, which lie in one block.
+// Eight bits: a chunk is 256 k, a piece 16 of them, which lie in one block; a quarter is two.
 struct WMx {
   typedef bf16_t T;
   typedef uint8_t Code;
-  static constexpr int BURST = 4;
+  static constexpr int K = 256;
   static constexpr bool MX = true;
   struct B {
-    u32x4 r[2];
-    __device__ __forceinline__ void load(const bf16_t* row, int q) {
-      r[0] = *reinterpret_cast<const u32x4*>(row + q * 16);
-      r[1] = *reinterpret_cast<const u32x4*>(row + q * 16 + 8);
+    u32x4 r[8];
+    __device__ __forceinline__ void load(const bf16_t* row, int q, int left) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const bf16_t* p = row + min(s * 64, left - 64) + q * 16;
+        r[2 * s] = *reinterpret_cast<const u32x4*>(p);
+        r[2 * s + 1] = *reinterpret_cast<const u32x4*>(p + 8);
+      }
     }
   };
-  u32x4 r;
-  uint32_t s;
-  __device__ __forceinline__ void load(const Code* row, const uint8_t* scale, int q) {
-    r = *reinterpret_cast<const u32x4*>(row + q * 16);
-    s = scale[q >> 1];
-  }
-  __device__ __forceinline__ void mma(f32x4& acc, const B& b) const {
-    const float f = mx_scale(s);
-    acc = mma_bf16(__builtin_bit_cast(u32x4, mx_widen8(r[0], r[1], f)), b.r[0], acc);
-    acc = mma_bf16(__builtin_bit_cast(u32x4, mx_widen8(r[2], r[3], f)), b.r[1], acc);
+  // scale: the row's eight bytes of the chunk
+  static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const uint2& scale,
+                                             const B& b, int q, int left) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (s * 64 >= left) return;
+      const uint32_t word = s < 2 ? scale.x : scale.y;
+      const float f = mx_scale(__builtin_amdgcn_ubfe(word, (s & 1) * 16 + (q >> 1) * 8, 8));
+      acc = mma_bf16(__builtin_bit_cast(u32x4, mx_widen8(a[s][0], a[s][1], f)), b.r[2 * s], acc);
+      acc = mma_bf16(__builtin_bit_cast(u32x4, mx_widen8(a[s][2], a[s][3], f)), b.r[2 * s + 1], acc);
+    }
   }
 };
 
-// fp32: 16 bytes at 16 q of each quarter.
+// fp32: a chunk is 64 k, a piece four of them.
 struct WF32 {
   typedef float T;
   typedef float Code;
-  static constexpr int BURST = 2;
+  static constexpr int K = 64;
   static constexpr bool MX = false;
   struct B {
     f32x4 r[4];
-    __device__ __forceinline__ void load(const float* row, int q) {
+    __device__ __forceinline__ void load(const float* row, int q, int) {
 #pragma unroll
-      for (int m = 0; m < 4; ++m) r[m] = *reinterpret_cast<const f32x4*>(row + m * 16 + q * 4);
+      for (int s = 0; s < 4; ++s) r[s] = *reinterpret_cast<const f32x4*>(row + s * 16 + q * 4);
     }
   };
-  f32x4 r[4];
-  __device__ __forceinline__ void load(const Code* row, const uint8_t*, int q) {
+  static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const uint2&, const B& b,
+                                             int, int) {
 #pragma unroll
-    for (int m = 0; m < 4; ++m) r[m] = *reinterpret_cast<const f32x4*>(row + m * 16 + q * 4);
-  }
-  __device__ __forceinline__ void mma(f32x4& acc, const B& b) const {
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int s = 0; s < 4; ++s) {
+      const f32x4 v = __builtin_bit_cast(f32x4, a[s]);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(r[m][j], b.r[m][j], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], b.r[s][j], acc, 0, 0, 0);
+    }
+  }
+};
+
+struct __attribute__((packed, aligned(2))) Bytes8 { uint2 v; };
+
+// A chunk on its way: from memory an instruction takes 256 consecutive bytes of four rows (64
+// bytes of each of sixteen, the operand's own order, reach 5.1 to 6.1 TB/s where this reaches
+// 6.6), so lane (q, c) holds piece c of rows 4 m + q.
+template <class F>
+struct Chunk {
+  u32x4 r[4];
+  uint2 scale;
+  // w: row 0 of the tile at the chunk; row: bytes of a row; left: k there
+  __device__ __forceinline__ void load(const typename F::Code* w, size_t row, const uint8_t* s,
+                                       size_t srow, int left) {
+    const int lane = wave_lane(), q = lane >> 4, c = lane & 15;
+    // pieces past the row's end: the last one again, not used
+    const int piece = min(c, left * (int)sizeof(typename F::Code) / 16 - 1);
+    const char* p = reinterpret_cast<const char*>(w) + q * row + piece * 16;
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+      r[m] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + m * 4 * row));
+    if (F::MX) {
+      const uint8_t* b = s + c * srow;
+      if (left >= F::K) {
+        scale = reinterpret_cast<const Bytes8*>(b)->v;
+      } else {
+        uint32_t v[2] = {0, 0};
+        for (int i = 0; i < left / MX_BLOCK; i += 2)
+          v[i >> 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(b + i) << (i & 2) * 8;
+        scale = make_uint2(v[0], v[1]);
+      }
+    }
+  }
+  // through 4 KiB of the wave's own LDS to the operand's order: piece c of row r at place
+  // c ^ r of the row, so that neither side meets in a bank
+  __device__ __forceinline__ void turn(u32x4 (*lds)[16], u32x4 (&a)[4]) const {
+    const int lane = wave_lane(), q = lane >> 4, c = lane & 15;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) lds[4 * m + q][c ^ (4 * m + q)] = r[m];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int s = 0; s < 4; ++s) a[s] = lds[c][(4 * s + q) ^ c];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
   }
 };
 
@@ -185,43 +234,53 @@ __device__ __forceinline__ void load_logits(float (&z)[NQ], const float* __restr
 constexpr int LG_WAVES = 8;
 constexpr int LG_SPLITS = 8;     // splits of k at most
 
-// Z [splits, N, E]: shares of X Wg^T.  A workgroup takes 16 experts and the units of split
-// blockIdx.y, its waves every eighth; they meet in LDS in a fixed order.  XMX: the tokens come
-// in eight bits; their rows go to Xb as bf16 for the expert products.
-template <class F, int TT, bool XMX>
+// Z [splits, N, E]: shares of X Wg^T.  A workgroup takes 16 experts and the 64s of k of split
+// blockIdx.y, its waves every eighth; they meet in LDS in a fixed order.  The few rows of Wg are
+// loaded in the operand's order.  XMX: the tokens come in eight bits; their rows go to Xb as
+// bf16 for the expert products.
+template <typename T, int TT, bool XMX>
 __global__ __launch_bounds__(64 * LG_WAVES) void decode_logits_kernel(
-    const typename F::T* __restrict__ X, const uint8_t* __restrict__ codes,
-    const uint8_t* __restrict__ scales, const typename F::T* __restrict__ Wg,
-    float* __restrict__ Z, bf16_t* __restrict__ Xb, int N, int d, int E) {
+    const T* __restrict__ X, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+    const T* __restrict__ Wg, float* __restrict__ Z, bf16_t* __restrict__ Xb, int N, int d, int E) {
   __shared__ f32x4 red[LG_WAVES][TT][64];
+  constexpr int L = 64 * sizeof(T) / 64;       // 16-byte loads of 64 k: 2 or 4
+  constexpr int P = 16 / sizeof(T);            // k of one
   const int lane = wave_lane(), wave = threadIdx.x >> 6, q = lane >> 4, col = lane & 15;
   const int e0 = blockIdx.x * 16 + col;
-  const typename F::T* wp = Wg + (size_t)(e0 < E ? e0 : E - 1) * d;
+  const T* wp = Wg + (size_t)(e0 < E ? e0 : E - 1) * d + q * P;
   f32x4 acc[TT];
 #pragma unroll
   for (int t = 0; t < TT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int units = d / 64;
   const int u1 = units * (blockIdx.y + 1) / gridDim.y;
   for (int u = units * blockIdx.y / gridDim.y + wave; u < u1; u += LG_WAVES) {
-    F a;
-    a.load(wp + u * 64, nullptr, q);
+    u32x4 a[L];
+#pragma unroll
+    for (int m = 0; m < L; ++m)
+      a[m] = *reinterpret_cast<const u32x4*>(wp + u * 64 + m * 4 * P);
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       const int i = min(t * 16 + col, N - 1);
-      typename F::B b;
-      if constexpr (XMX) {
-        // the lane's k of a bf16 unit: 8 q and 32 + 8 q
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          const size_t at = (size_t)i * d + u * 64 + m * 32 + q * 8;
+      for (int m = 0; m < L; ++m) {
+        const size_t at = (size_t)i * d + u * 64 + m * 4 * P + q * P;
+        u32x4 b;
+        if constexpr (XMX) {
           const uint2 c = *reinterpret_cast<const uint2*>(codes + at);
-          b.r[m] = __builtin_bit_cast(u32x4, mx_widen8(c.x, c.y, mx_scale(scales[at / MX_BLOCK])));
-          if (blockIdx.x == 0) *reinterpret_cast<u32x4*>(Xb + at) = b.r[m];
+          b = __builtin_bit_cast(u32x4, mx_widen8(c.x, c.y, mx_scale(scales[at / MX_BLOCK])));
+          if (blockIdx.x == 0) *reinterpret_cast<u32x4*>(Xb + at) = b;
+        } else {
+          b = *reinterpret_cast<const u32x4*>(X + at);
         }
-      } else {
-        b.load(X + (size_t)i * d + u * 64, q);
+        if constexpr (sizeof(T) == 2) {
+          acc[t] = mma_bf16(a[m], b, acc[t]);
+        } else {
+          const f32x4 fa = __builtin_bit_cast(f32x4, a[m]), fb = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[j], fb[j], acc[t], 0, 0, 0);
+        }
       }
-      a.mma(acc[t], b);
     }
   }
 #pragma unroll
@@ -339,10 +398,11 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
     int k) {
   typedef typename F::T T;
   typedef typename F::Code Code;
-  constexpr int U = TT > 2 ? F::BURST / 2 : F::BURST;    // registers
+  constexpr int TURNS = TT > 2 ? 1 : 2;     // LDS for two workgroups a CU
   constexpr bool OWN = NQ > 0;
   constexpr int OT = OWN ? INLINE_TOKENS : 1;
-  __shared__ f32x4 red[2][W13_WAVES][2 * TT][64];
+  __shared__ f32x4 red[TURNS][W13_WAVES][2 * TT][64];
+  __shared__ u32x4 turned[W13_WAVES][2][16][16];
   __shared__ uint16_t pick[OWN ? 256 : 1][OT];
   __shared__ int count[OWN ? 256 : 1];
   __shared__ uint32_t own_list[OWN ? 256 : 1], own_rows[OWN ? 256 : 1][OT];
@@ -388,8 +448,8 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
   const int t1 = (int)((long)tiles * (blockIdx.x + 1) / gridDim.x);
   int tile = (int)((long)tiles * blockIdx.x / gridDim.x);
   if (tile >= t1) return;
-  const int units = d / 64;
-  const int u0 = units * wave / W13_WAVES, u1 = units * (wave + 1) / W13_WAVES, last = units - 1;
+  const int chunks = (d + F::K - 1) / F::K;
+  const int u0 = chunks * wave / W13_WAVES, u1 = chunks * (wave + 1) / W13_WAVES;
 
   // the weights of tile t, for the requests; columns of the tile in use
   const Code* rows[2];
@@ -398,11 +458,11 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
     const bool shared = t >= routed;
     size_t row;
     if (shared) {
-      row = (size_t)(t - routed) * 16 + col;
+      row = (size_t)(t - routed) * 16;
     } else {
       const int s = t / ht;
       const uint32_t e = OWN ? own_list[s] : plan.list[s];
-      row = (size_t)__builtin_amdgcn_readfirstlane(e & 0xffffu) * h + (t - s * ht) * 16 + col;
+      row = (size_t)__builtin_amdgcn_readfirstlane(e & 0xffffu) * h + (t - s * ht) * 16;
     }
     rows[0] = (const Code*)(shared ? w.Ws1 : w.W1) + row * d;
     rows[1] = (const Code*)(shared ? w.Ws3 : w.W3) + row * d;
@@ -411,14 +471,12 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
       scale[1] = (shared ? w.Ss3 : w.S3) + row * (d / MX_BLOCK);
     }
   };
-  const auto request = [&](F (&to)[2][U], int u) __attribute__((always_inline)) {
+  const auto request = [&](Chunk<F> (&to)[2], int u) __attribute__((always_inline)) {
+    const int k0 = u * F::K;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int at = min(u + i, last);     // past the end: the last unit again, not used
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-        to[m][i].load(rows[m] + at * 64, F::MX ? scale[m] + at * 2 : nullptr, q);
-    }
+    for (int m = 0; m < 2; ++m)
+      to[m].load(rows[m] + k0, d * sizeof(Code), F::MX ? scale[m] + k0 / MX_BLOCK : nullptr,
+                 d / MX_BLOCK, d - k0);
   };
   const T* x[TT];
   int at[TT], n = 0, slot = -1;
@@ -444,41 +502,44 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
     }
   };
 
-  F a[2][2][U];
+  Chunk<F> a[2][2];
   f32x4 acc[2][TT];
   int u = u0, turn = 0;
 #pragma unroll
   for (int t = 0; t < TT; ++t) acc[0][t] = acc[1][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   aim(tile);
-  request(a[0], u0);
+  request(a[0], min(u0, chunks - 1));
   __builtin_amdgcn_sched_barrier(0);
   columns(tile < routed ? tile / ht : active);
-  // one burst of the tile in use; false past the last tile
-  const auto step = [&](F (&now)[2][U], F (&next)[2][U]) __attribute__((always_inline)) {
-    typename F::B b[TT][U];
-#pragma unroll
-    for (int t = 0; t < TT; ++t)
-      if (t == 0 || t * 16 < n)
-#pragma unroll
-        for (int i = 0; i < U; ++i) b[t][i].load(x[t] + min(u + i, last) * 64, q);
-    const bool ends = u + U >= u1;
+  // one chunk of the tile in use; false past the last tile
+  const auto step = [&](Chunk<F> (&now)[2], Chunk<F> (&next)[2]) __attribute__((always_inline)) {
+    const int k0 = min(u, chunks - 1) * F::K;
+    typename F::B b;
+    b.load(x[0] + k0, q, d - k0);     // before the request: memory answers in order
+    const bool ends = u + 1 >= u1;
     if (!ends) {
-      request(next, u + U);
+      request(next, u + 1);
     } else if (tile + 1 < t1) {
       aim(tile + 1);
-      request(next, u0);
+      request(next, min(u0, chunks - 1));
     }
     __builtin_amdgcn_sched_barrier(0);
+    if (u < u1) {                     // else more waves than chunks
+      u32x4 op[2][4];
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-      if (u + i < u1)
+      for (int m = 0; m < 2; ++m) now[m].turn(turned[wave][m], op[m]);
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-          if (t == 0 || t * 16 < n)
+      for (int t = 0; t < TT; ++t) {
+        if (t > 0) {
+          if (t * 16 >= n) break;
+          b.load(x[t] + k0, q, d - k0);
+        }
 #pragma unroll
-            for (int m = 0; m < 2; ++m) now[m][i].mma(acc[m][t], b[t][i]);
+        for (int m = 0; m < 2; ++m) F::mma(acc[m][t], op[m], now[m].scale, b, q, d - k0);
+      }
+    }
     if (!ends) {
-      u += U;
+      ++u;
       return true;
     }
     // the tile's end: the waves' shares meet
@@ -506,7 +567,8 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
         for (int i = 0; i < 4; ++i) v[i] = gate[t] * (f[i] / (1.0f + expf(-f[i]))) * g[i];
         store4<T>((shared ? As : A) + (size_t)at[t] * width + unit, v);
       }
-    turn ^= 1;
+    if (TURNS == 1) __syncthreads();
+    turn ^= TURNS - 1;
     u = u0;
     if (++tile >= t1) return false;
     const int s = tile < routed ? tile / ht : active;
@@ -531,13 +593,15 @@ __global__ __launch_bounds__(64 * W2_WAVES, 2) void decode_w2_kernel(
     DecodePlan plan, float* __restrict__ O, int N, int d, int h, int hs, int k) {
   typedef typename F::T T;
   typedef typename F::Code Code;
-  constexpr int U = TT > 1 ? F::BURST : 2 * F::BURST;
+  constexpr int U = 2;      // chunks of a burst
+  __shared__ u32x4 turned[W2_WAVES][16][16];
   const int lane = wave_lane(), q = lane >> 4, col = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int active = plan.active[0];
   const int dt = d / 16, routed = active * dt, hu = h / 64, su = hs / 64;
-  // shares of equal work, in units
+  // shares of equal work, in 64s of k
   const long waves = (long)gridDim.x * W2_WAVES, total = (long)dt * (active * hu + su);
-  const long g = (long)blockIdx.x * W2_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long g = (long)blockIdx.x * W2_WAVES + wave;
   const auto tile_from = [&](long c) {
     const long r = (long)routed * hu;
     return (int)(c <= r ? (c + hu - 1) / hu : routed + (c - r + su - 1) / su);
@@ -547,23 +611,26 @@ __global__ __launch_bounds__(64 * W2_WAVES, 2) void decode_w2_kernel(
   if (tile >= t1) return;
   const Code* row;
   const uint8_t* scale;
+  int wide;       // k of the tile that is requested
   const auto aim = [&](int t) __attribute__((always_inline)) {
     const bool shared = t >= routed;
     size_t r;
     if (shared) {
-      r = (size_t)(t - routed) * 16 + col;
+      r = (size_t)(t - routed) * 16;
     } else {
       const int s = t / dt;
-      r = (size_t)__builtin_amdgcn_readfirstlane(plan.list[s] & 0xffffu) * d + (t - s * dt) * 16 + col;
+      r = (size_t)__builtin_amdgcn_readfirstlane(plan.list[s] & 0xffffu) * d + (t - s * dt) * 16;
     }
-    row = (const Code*)(shared ? w.Ws2 : w.W2) + r * (shared ? hs : h);
-    if (F::MX) scale = (shared ? w.Ss2 : w.S2) + r * ((shared ? hs : h) / MX_BLOCK);
+    wide = shared ? hs : h;
+    row = (const Code*)(shared ? w.Ws2 : w.W2) + r * wide;
+    if (F::MX) scale = (shared ? w.Ss2 : w.S2) + r * (wide / MX_BLOCK);
   };
-  const auto request = [&](F (&to)[U], int u, int last) __attribute__((always_inline)) {
+  const auto request = [&](Chunk<F> (&to)[U], int u) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int at = min(u + i, last);
-      to[i].load(row + at * 64, F::MX ? scale + at * 2 : nullptr, q);
+      const int k0 = min(u + i, (wide + F::K - 1) / F::K - 1) * F::K;
+      to[i].load(row + k0, wide * sizeof(Code), F::MX ? scale + k0 / MX_BLOCK : nullptr,
+                 wide / MX_BLOCK, wide - k0);
     }
   };
   const T* x[TT];
@@ -585,36 +652,46 @@ __global__ __launch_bounds__(64 * W2_WAVES, 2) void decode_w2_kernel(
       }
     }
   };
-  F a[2][U];
+  Chunk<F> a[2][U];
   f32x4 acc[TT];
 #pragma unroll
   for (int t = 0; t < TT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int u = 0, units = tile < routed ? hu : su;
+  int u = 0, width = tile < routed ? h : hs;
   aim(tile);
-  request(a[0], 0, units - 1);
+  request(a[0], 0);
   __builtin_amdgcn_sched_barrier(0);
   columns(tile < routed ? tile / dt : active);
-  const auto step = [&](F (&now)[U], F (&next)[U]) __attribute__((always_inline)) {
-    typename F::B b[TT][U];
+  const auto step = [&](Chunk<F> (&now)[U], Chunk<F> (&next)[U]) __attribute__((always_inline)) {
+    const int chunks = (width + F::K - 1) / F::K;
+    typename F::B b[U];
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
-      if (t == 0 || t * 16 < n)
-#pragma unroll
-        for (int i = 0; i < U; ++i) b[t][i].load(x[t] + min(u + i, units - 1) * 64, q);
-    const bool ends = u + U >= units;
+    for (int i = 0; i < U; ++i) {
+      const int k0 = min(u + i, chunks - 1) * F::K;
+      b[i].load(x[0] + k0, q, width - k0);
+    }
+    const bool ends = u + U >= chunks;
     if (!ends) {
-      request(next, u + U, units - 1);
+      request(next, u + U);
     } else if (tile + 1 < t1) {
       aim(tile + 1);
-      request(next, 0, (tile + 1 < routed ? hu : su) - 1);
+      request(next, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if (u + i < units)
+      if (u + i < chunks) {
+        const int k0 = (u + i) * F::K;
+        u32x4 op[4];
+        now[i].turn(turned[wave], op);
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-          if (t == 0 || t * 16 < n) now[i].mma(acc[t], b[t][i]);
+        for (int t = 0; t < TT; ++t) {
+          if (t > 0) {
+            if (t * 16 >= n) break;
+            b[0].load(x[t] + k0, q, width - k0);
+          }
+          F::mma(acc[t], op, now[i].scale, t > 0 ? b[0] : b[i], q, width - k0);
+        }
+      }
     if (!ends) {
       u += U;
       return true;
@@ -627,7 +704,7 @@ __global__ __launch_bounds__(64 * W2_WAVES, 2) void decode_w2_kernel(
     }
     u = 0;
     if (++tile >= t1) return false;
-    units = tile < routed ? hu : su;
+    width = tile < routed ? h : hs;
     const int s = tile < routed ? tile / dt : active;
     if (s != slot) columns(s);
     return true;
@@ -661,17 +738,16 @@ __global__ __launch_bounds__(64) void decode_sum_kernel(const float* __restrict_
 template <class F, int TT>
 hipError_t run_decode(const DecodeCall& c, hipStream_t st) {
   typedef typename F::T T;
-  typedef std::conditional_t<sizeof(T) == 4, WF32, WBf16> G;   // the router's weights
   const int splits = decode_splits(c.d);
   const dim3 lg((unsigned)((c.E + 15) / 16), (unsigned)splits);
   if (c.Xs) {
     if constexpr (sizeof(T) == 2)
-      decode_logits_kernel<G, TT, true><<<lg, 64 * LG_WAVES, 0, st>>>(
+      decode_logits_kernel<T, TT, true><<<lg, 64 * LG_WAVES, 0, st>>>(
           nullptr, (const uint8_t*)c.X, c.Xs, (const T*)c.Wg, c.Z, (bf16_t*)c.Xb, c.N, c.d, c.E);
     else
       return hipErrorInvalidValue;
   } else {
-    decode_logits_kernel<G, TT, false><<<lg, 64 * LG_WAVES, 0, st>>>(
+    decode_logits_kernel<T, TT, false><<<lg, 64 * LG_WAVES, 0, st>>>(
         (const T*)c.X, nullptr, nullptr, (const T*)c.Wg, c.Z, nullptr, c.N, c.d, c.E);
   }
   const T* X = (const T*)(c.Xs ? c.Xb : c.X);
