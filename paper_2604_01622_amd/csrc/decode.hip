@@ -20,6 +20,21 @@ namespace ec {
 
 namespace {
 
+// Loads that are known to be of global memory: a generic one waits together with LDS.
+template <typename V>
+__device__ __forceinline__ V load_global(const void* p) {
+  return *(const __attribute__((address_space(1))) V*)p;
+}
+template <typename V>
+__device__ __forceinline__ V stream_global(const void* p) {
+  return __builtin_nontemporal_load((const __attribute__((address_space(1))) V*)p);
+}
+
+// A barrier for LDS alone: __syncthreads() would wait for the requests on their way too.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 // Eight codes as bf16, times 2^(byte - 127).
 __device__ __forceinline__ bf16x8 mx_widen8(uint32_t lo, uint32_t hi, float scale) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
@@ -53,7 +68,7 @@ struct WBf16 {
     // row: the token's, at the chunk; `left` k are there (a multiple of 64)
     __device__ __forceinline__ void load(const bf16_t* row, int q, int left) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s) r[s] = *reinterpret_cast<const u32x4*>(row + min(s * 32, left - 32) + q * 8);
+      for (int s = 0; s < 4; ++s) r[s] = load_global<u32x4>(row + min(s * 32, left - 32) + q * 8);
     }
   };
   static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const uint2&, const B& b,
@@ -78,8 +93,8 @@ struct WMx {
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const bf16_t* p = row + min(s * 64, left - 64) + q * 16;
-        r[2 * s] = *reinterpret_cast<const u32x4*>(p);
-        r[2 * s + 1] = *reinterpret_cast<const u32x4*>(p + 8);
+        r[2 * s] = load_global<u32x4>(p);
+        r[2 * s + 1] = load_global<u32x4>(p + 8);
       }
     }
   };
@@ -107,7 +122,7 @@ struct WF32 {
     f32x4 r[4];
     __device__ __forceinline__ void load(const float* row, int q, int) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s) r[s] = *reinterpret_cast<const f32x4*>(row + s * 16 + q * 4);
+      for (int s = 0; s < 4; ++s) r[s] = load_global<f32x4>(row + s * 16 + q * 4);
     }
   };
   static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const uint2&, const B& b,
@@ -122,47 +137,42 @@ struct WF32 {
   }
 };
 
-struct __attribute__((packed, aligned(2))) Bytes8 { uint2 v; };
-
 // A chunk on its way: from memory an instruction takes 256 consecutive bytes of four rows (64
 // bytes of each of sixteen, the operand's own order, reach 5.1 to 6.1 TB/s where this reaches
-// 6.6), so lane (q, c) holds piece c of rows 4 m + q.
+// 6.6), so lane (q, c) holds piece c of rows 4 m + q, and the scales of quarter q of row c.
 template <class F>
 struct Chunk {
+  struct Lds {
+    u32x4 piece[16][16];
+    uint2 scale[16];
+  };
   u32x4 r[4];
-  uint2 scale;
-  // w: row 0 of the tile at the chunk; row: bytes of a row; left: k there
-  __device__ __forceinline__ void load(const typename F::Code* w, size_t row, const uint8_t* s,
-                                       size_t srow, int left) {
+  uint16_t scale;
+  // w: row 0 of the tile at the chunk; row, srow: bytes of a row; left: k there, 0 for a chunk
+  // that is not used (the same 16 bytes for every lane)
+  __device__ __forceinline__ void load(const typename F::Code* w, uint32_t row, const uint8_t* s,
+                                       uint32_t srow, int left) {
     const int lane = wave_lane(), q = lane >> 4, c = lane & 15;
     // pieces past the row's end: the last one again, not used
-    const int piece = min(c, left * (int)sizeof(typename F::Code) / 16 - 1);
-    const char* p = reinterpret_cast<const char*>(w) + q * row + piece * 16;
+    const int piece = max(min(c, left * (int)sizeof(typename F::Code) / 16 - 1), 0);
+    const uint32_t step = left > 0 ? row : 0;
+    const char* p = reinterpret_cast<const char*>(w) + (q * step + piece * 16);
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
-      r[m] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + m * 4 * row));
-    if (F::MX) {
-      const uint8_t* b = s + c * srow;
-      if (left >= F::K) {
-        scale = reinterpret_cast<const Bytes8*>(b)->v;
-      } else {
-        uint32_t v[2] = {0, 0};
-        for (int i = 0; i < left / MX_BLOCK; i += 2)
-          v[i >> 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(b + i) << (i & 2) * 8;
-        scale = make_uint2(v[0], v[1]);
-      }
-    }
+    for (int m = 0; m < 4; ++m) r[m] = stream_global<u32x4>(p + m * 4 * step);
+    if (F::MX) scale = load_global<uint16_t>(s + (left > 0 ? c * srow : 0) + max(min(q, left / 64 - 1), 0) * 2);
   }
-  // through 4 KiB of the wave's own LDS to the operand's order: piece c of row r at place
-  // c ^ r of the row, so that neither side meets in a bank
-  __device__ __forceinline__ void turn(u32x4 (*lds)[16], u32x4 (&a)[4]) const {
+  // through LDS of the wave's own to the operand's order: piece c of row r at place c ^ r of
+  // the row, so that neither side meets in a bank
+  __device__ __forceinline__ void turn(Lds& lds, u32x4 (&a)[4], uint2& scales) const {
     const int lane = wave_lane(), q = lane >> 4, c = lane & 15;
 #pragma unroll
-    for (int m = 0; m < 4; ++m) lds[4 * m + q][c ^ (4 * m + q)] = r[m];
+    for (int m = 0; m < 4; ++m) lds.piece[4 * m + q][c ^ (4 * m + q)] = r[m];
+    if (F::MX) reinterpret_cast<uint16_t*>(lds.scale)[c * 4 + q] = scale;
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int s = 0; s < 4; ++s) a[s] = lds[c][(4 * s + q) ^ c];
+    for (int s = 0; s < 4; ++s) a[s] = lds.piece[c][(4 * s + q) ^ c];
+    if (F::MX) scales = lds.scale[c];
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
   }
@@ -188,35 +198,33 @@ __device__ __forceinline__ float choose(const float (&z)[NQ], int E, int k, floa
 #pragma unroll
   for (int m = 0; m < NQ; ++m) key[m] = r + 16 * m < E ? logit_key(z[m]) : 0u;
   float z0 = 0.f, sum = 0.f;
-  for (int c = 0; c < k; ++c) {
-    uint32_t bk = 0;
-    int bj = 0;
+  for (int c0 = 0; c0 < k; c0 += 16) {
+    uint32_t mine = 0;
+    int expert = 0;
+    for (int c = c0; c < min(k, c0 + 16); ++c) {
+      uint32_t top = key[0];
 #pragma unroll
-    for (int m = 0; m < NQ; ++m)
-      if (key[m] > bk) {
-        bk = key[m];
-        bj = r + 16 * m;
-      }
-    const auto better = [&](uint32_t ok, uint32_t oj) {
-      if (ok > bk || (ok == bk && (int)oj < bj)) {
-        bk = ok;
-        bj = (int)oj;
-      }
-    };
-    better(dpp_u32<0x128>(bk), dpp_u32<0x128>((uint32_t)bj));
-    better(dpp_u32<0x124>(bk), dpp_u32<0x124>((uint32_t)bj));
-    better(dpp_u32<0x4E>(bk), dpp_u32<0x4E>((uint32_t)bj));
-    better(dpp_u32<0xB1>(bk), dpp_u32<0xB1>((uint32_t)bj));
+      for (int m = 1; m < NQ; ++m) top = max(top, key[m]);
+      top = row16_max_u32(top);
+      int j = 256;
 #pragma unroll
-    for (int m = 0; m < NQ; ++m)
-      if (bj == r + 16 * m) key[m] = 0;
-    const float zc = key_logit(bk);
-    if (c == 0) z0 = zc;
-    const float ex = expf((zc - z0) * inv_tau);
-    sum += ex;
-    if (r == (c & 15)) put(c, bj, ex);
+      for (int m = NQ - 1; m >= 0; --m) j = key[m] == top ? r + 16 * m : j;
+      j = row16_min_i32(j);
+#pragma unroll
+      for (int m = 0; m < NQ; ++m) key[m] = j == r + 16 * m ? 0u : key[m];
+      if (c == 0) z0 = key_logit(top);
+      if (r == c - c0) {
+        mine = top;
+        expert = j;
+      }
+    }
+    if (c0 + r < k) {
+      const float ex = expf((key_logit(mine) - z0) * inv_tau);
+      sum += ex;
+      put(c0 + r, expert, ex);
+    }
   }
-  return sum;
+  return row16_sum_even(sum);
 }
 
 // Logits r, r + 16, ... of a token: the sums of the splits' shares, in order.
@@ -299,81 +307,93 @@ __global__ __launch_bounds__(64 * LG_WAVES) void decode_logits_kernel(
 
 // ---- who chose an expert -------------------------------------------------------------
 
-// The chosen experts in ascending order ("slots"): expert | tokens << 16, and by slot the tokens
-// that chose it, ascending: token << 16 | pick.  TOK: tokens at most, lanes of an expert here.
-// All of the workgroup's NT threads; pick [E, TOK] holds pick + 1 or 0, count [256] is scratch.
-// Returns the number of slots.
-template <int TOK, int NT, typename List, typename Rows>
-__device__ __forceinline__ int list_tokens(const uint16_t (*pick)[TOK], int* count, int E, List list,
-                                           Rows rows) {
-  constexpr int PER = 64 / TOK;         // experts of a wave at a time
-  const int lane = wave_lane(), wave = threadIdx.x >> 6;
-  const int sub = lane / TOK, i = lane % TOK;
-  const unsigned long long mask = TOK == 64 ? ~0ull : (1ull << TOK) - 1;
-  const auto who_of = [&](int e) {
-    const unsigned long long who = __ballot(e < E && pick[min(e, E - 1)][i] != 0);
-    return (who >> (sub * TOK)) & mask;
-  };
-  for (int c = threadIdx.x; c < 256; c += NT) count[c] = 0;
-  __syncthreads();
-  for (int e0 = wave * PER; e0 < E; e0 += NT / 64 * PER) {
-    const unsigned long long who = who_of(e0 + sub);
-    if (i == 0 && e0 + sub < E) count[e0 + sub] = __popcll(who);
+// The choice by expert (DecodePlan): used, bit j: some token chose expert j; pick [E, TOK] by
+// token, pick + 1 or 0.  The chosen experts in ascending order are the "slots".
+template <int TT>
+constexpr int plan_tokens() { return TT == 1 ? 16 : DECODE_TOKENS; }
+
+struct Used {
+  unsigned long long w[4];
+  __device__ __forceinline__ int count() const {
+    return __popcll(w[0]) + __popcll(w[1]) + __popcll(w[2]) + __popcll(w[3]);
   }
-  __syncthreads();
-  unsigned long long used[4];
-  int active = 0;
-#pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    used[m] = __ballot(count[lane + 64 * m] != 0);
-    active += __popcll(used[m]);
-  }
-  for (int e0 = wave * PER; e0 < E; e0 += NT / 64 * PER) {
-    const int e = e0 + sub;
-    const unsigned long long who = who_of(e);
-    if (who == 0) continue;
-    int slot = 0;
+  // the expert of a slot
+  __device__ __forceinline__ int expert(int slot) const {
+    const int lane = wave_lane();
+    int found = 0;
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      if (m * 64 + 64 <= e) slot += __popcll(used[m]);
-      else if (m * 64 <= e) slot += __popcll(used[m] & ((1ull << (e - m * 64)) - 1));
+      const int rank = __popcll(w[m] & ((1ull << lane) - 1));
+      const unsigned long long hit = __ballot(((w[m] >> lane) & 1) && rank == slot);
+      if (hit) found = m * 64 + __builtin_ctzll(hit);
+      slot -= __popcll(w[m]);
     }
-    if (i == 0) list(slot, (uint32_t)e | (uint32_t)__popcll(who) << 16);
-    const uint32_t p = pick[e][i];
-    if (p) rows(slot, __popcll(who & ((1ull << i) - 1)), (uint32_t)i << 16 | (p - 1));
+    return __builtin_amdgcn_readfirstlane(found);
   }
-  return active;
+};
+
+// The columns of an expert's products: with 16 tokens at most each token is its own, else those
+// that chose the expert move together.  p: the lane's token's entry of pick (lane % 16 with
+// 16 tokens).  token, pick: of the columns of this lane, t 16 + lane % 16; mine: bit t, whether the
+// column is a token's (another repeats one, and nothing of it is stored); returns their number.
+template <int TT>
+__device__ __forceinline__ int columns_of(uint32_t p, int (&token)[TT], int (&pick)[TT],
+                                          uint32_t* mine) {
+  const int lane = wave_lane(), col = lane & 15;
+  const unsigned long long who = __ballot(p != 0);
+  *mine = 0;
+  if constexpr (TT == 1) {
+    const int first = __builtin_ctz((uint32_t)who & 0xffffu);
+    const uint32_t q = __builtin_amdgcn_readlane(p, first);
+    token[0] = p ? col : first;
+    pick[0] = (int)(p ? p : q) - 1;
+    *mine = p != 0;
+    return 16;
+  } else {
+    const int n = __popcll(who), before = __popcll(who & ((1ull << lane) - 1));
+    const int to = p ? before : n + lane - before;
+    const int moved = __builtin_amdgcn_ds_permute(to * 4, lane << 16 | (int)(p ? p - 1 : 0));
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      const int c = t * 16 + col;
+      const int v = __shfl(moved, min(c, n - 1));
+      token[t] = v >> 16;
+      pick[t] = v & 0xffff;
+      *mine |= (uint32_t)(c < n) << t;
+    }
+    return n;
+  }
 }
 
 // The choice of more tokens than every workgroup of W1/W3 would make for itself: one workgroup,
 // sixteen lanes a token.
-template <int NQ>
-__global__ __launch_bounds__(1024) void decode_choose_kernel(const float* __restrict__ Z, int N,
-                                                             int E, int k, int splits,
-                                                             float inv_tau,
-                                                             int32_t* __restrict__ experts,
-                                                             float* __restrict__ gates,
-                                                             DecodePlan plan) {
-  __shared__ uint16_t pick[256][DECODE_TOKENS];
-  __shared__ int count[256];
+template <int NQ, int TOK>
+__global__ __launch_bounds__(16 * TOK) void decode_choose_kernel(const float* __restrict__ Z, int N,
+                                                                 int E, int k, int splits,
+                                                                 float inv_tau,
+                                                                 int32_t* __restrict__ experts,
+                                                                 float* __restrict__ gates,
+                                                                 DecodePlan plan) {
+  __shared__ uint32_t pick[256 * TOK / 2];
+  __shared__ unsigned long long used[4];
   const int tid = threadIdx.x, i = tid >> 4, r = tid & 15;
   float z[NQ];
   if (i < N) load_logits<NQ>(z, Z, i, r, N, E, splits);
-  for (int c = tid; c < E * DECODE_TOKENS / 2; c += 1024) reinterpret_cast<uint32_t*>(pick)[c] = 0;
+  for (int c = tid; c < E * TOK / 2; c += 16 * TOK) pick[c] = 0;
+  if (tid < 4) used[tid] = 0;
   __syncthreads();
   if (i < N) {
     const float sum = choose<NQ>(z, E, k, inv_tau, r, [&](int c, int e, float ex) {
       experts[i * k + c] = e;
       gates[i * k + c] = ex;
-      pick[e][i] = (uint16_t)(c + 1);
+      reinterpret_cast<uint16_t*>(pick)[e * TOK + i] = (uint16_t)(c + 1);
+      atomicOr(&used[e >> 6], 1ull << (e & 63));
     });
     for (int c = r; c < k; c += 16) gates[i * k + c] = gates[i * k + c] / sum;
   }
   __syncthreads();
-  const int active = list_tokens<DECODE_TOKENS, 1024>(
-      pick, count, E, [&](int s, uint32_t v) { plan.list[s] = v; },
-      [&](int s, int c, uint32_t v) { plan.rows[s * DECODE_TOKENS + c] = v; });
-  if (tid == 0) plan.active[0] = active;
+  for (int c = tid; c < E * TOK / 2; c += 16 * TOK) reinterpret_cast<uint32_t*>(plan.pick)[c] = pick[c];
+  if (tid < 4) plan.used[tid] = used[tid];
 }
 
 // ---- W1 and W3 -----------------------------------------------------------------------
@@ -385,8 +405,9 @@ constexpr int INLINE_PAIRS = 256;       // many tokens, and pairs of token and e
 
 // Tiles of 16 hidden units: those of the chosen experts, slot after slot, then the shared
 // experts' (for every token).  A workgroup takes a contiguous share of them, its waves a quarter
-// of k each; the expert's tokens are the columns.  A burst's weights are requested before the one
-// before it is used, over the ends of tiles and experts too, so that memory never waits.
+// of k each; the expert's tokens are the columns.  A chunk's weights are requested before the one
+// before it is used, over the ends of tiles and experts too, so that memory never waits; every
+// step requests, at the end what is not used, so that the waits can count.
 //   A [token k + pick, h] = gate silu(W1 x) (W3 x).
 // NQ > 0: the choice is made here, from the logits, by every workgroup (16 NQ experts at most),
 // and the first writes it down.
@@ -400,27 +421,28 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
   typedef typename F::Code Code;
   constexpr int TURNS = TT > 2 ? 1 : 2;     // LDS for two workgroups a CU
   constexpr bool OWN = NQ > 0;
-  constexpr int OT = OWN ? INLINE_TOKENS : 1;
+  constexpr int PT = plan_tokens<TT>();
   __shared__ f32x4 red[TURNS][W13_WAVES][2 * TT][64];
-  __shared__ u32x4 turned[W13_WAVES][2][16][16];
-  __shared__ uint16_t pick[OWN ? 256 : 1][OT];
-  __shared__ int count[OWN ? 256 : 1];
-  __shared__ uint32_t own_list[OWN ? 256 : 1], own_rows[OWN ? 256 : 1][OT];
+  __shared__ typename Chunk<F>::Lds turned[W13_WAVES][2];
+  __shared__ uint32_t own_pick[OWN ? 256 * PT / 2 : 1];
+  __shared__ unsigned long long own_used[4];
   __shared__ float own_gates[OWN ? INLINE_PAIRS : 1];
   const int tid = threadIdx.x, lane = wave_lane(), q = lane >> 4, col = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int active;
+  Used used;
   if constexpr (OWN) {
     const int i = tid >> 4, r = tid & 15;
     float z[NQ];
     if (i < N) load_logits<NQ>(z, Z, i, r, N, E, splits);
-    for (int c = tid; c < E * OT / 2; c += 64 * W13_WAVES) reinterpret_cast<uint32_t*>(pick)[c] = 0;
+    for (int c = tid; c < E * PT / 2; c += 64 * W13_WAVES) own_pick[c] = 0;
+    if (tid < 4) own_used[tid] = 0;
     __syncthreads();
     if (i < N) {
       const float sum = choose<NQ>(z, E, k, inv_tau, r, [&](int c, int e, float ex) {
         if (blockIdx.x == 0) experts[i * k + c] = e;
         own_gates[i * k + c] = ex;
-        pick[e][i] = (uint16_t)(c + 1);
+        reinterpret_cast<uint16_t*>(own_pick)[e * PT + i] = (uint16_t)(c + 1);
+        atomicOr(&own_used[e >> 6], 1ull << (e & 63));
       });
       for (int c = r; c < k; c += 16) {
         const float g = own_gates[i * k + c] / sum;
@@ -429,77 +451,67 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
       }
     }
     __syncthreads();
-    active = list_tokens<OT, 64 * W13_WAVES>(
-        pick, count, E,
-        [&](int s, uint32_t v) {
-          own_list[s] = v;
-          if (blockIdx.x == 0) plan.list[s] = v;
-        },
-        [&](int s, int c, uint32_t v) {
-          own_rows[s][c] = v;
-          if (blockIdx.x == 0) plan.rows[s * DECODE_TOKENS + c] = v;
-        });
-    if (blockIdx.x == 0 && tid == 0) plan.active[0] = active;
-    __syncthreads();
+    if (blockIdx.x == 0) {
+      for (int c = tid; c < E * PT / 2; c += 64 * W13_WAVES)
+        reinterpret_cast<uint32_t*>(plan.pick)[c] = own_pick[c];
+      if (tid < 4) plan.used[tid] = own_used[tid];
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) used.w[m] = own_used[m];
   } else {
-    active = plan.active[0];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) used.w[m] = plan.used[m];
   }
-  const int ht = h / 16, routed = active * ht, tiles = routed + hs / 16;
+  const int active = used.count(), ht = h / 16, tiles = active * ht + hs / 16;
+  const int t0 = (int)((long)tiles * blockIdx.x / gridDim.x);
   const int t1 = (int)((long)tiles * (blockIdx.x + 1) / gridDim.x);
-  int tile = (int)((long)tiles * blockIdx.x / gridDim.x);
-  if (tile >= t1) return;
+  if (t0 >= t1) return;
   const int chunks = (d + F::K - 1) / F::K;
   const int u0 = chunks * wave / W13_WAVES, u1 = chunks * (wave + 1) / W13_WAVES;
 
-  // the weights of tile t, for the requests; columns of the tile in use
-  const Code* rows[2];
-  const uint8_t* scale[2];
-  const auto aim = [&](int t) __attribute__((always_inline)) {
-    const bool shared = t >= routed;
-    size_t row;
-    if (shared) {
-      row = (size_t)(t - routed) * 16;
-    } else {
-      const int s = t / ht;
-      const uint32_t e = OWN ? own_list[s] : plan.list[s];
-      row = (size_t)__builtin_amdgcn_readfirstlane(e & 0xffffu) * h + (t - s * ht) * 16;
-    }
-    rows[0] = (const Code*)(shared ? w.Ws1 : w.W1) + row * d;
-    rows[1] = (const Code*)(shared ? w.Ws3 : w.W3) + row * d;
-    if (F::MX) {
-      scale[0] = (shared ? w.Ss1 : w.S1) + row * (d / MX_BLOCK);
-      scale[1] = (shared ? w.Ss3 : w.S3) + row * (d / MX_BLOCK);
-    }
-  };
-  const auto request = [&](Chunk<F> (&to)[2], int u) __attribute__((always_inline)) {
-    const int k0 = u * F::K;
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-      to[m].load(rows[m] + k0, d * sizeof(Code), F::MX ? scale[m] + k0 / MX_BLOCK : nullptr,
-                 d / MX_BLOCK, d - k0);
+  // the tile in use and, one ahead where it ends, the one that is requested: slot (active: the
+  // shared experts) and tile of it
+  int slot = min(t0 / ht, active), tile = t0 - slot * ht, left = t1 - t0;
+  int rslot = slot, rtile = tile, expert = slot < active ? used.expert(slot) : 0;
+  const auto request = [&](Chunk<F> (&to)[2], int u, bool live) __attribute__((always_inline)) {
+    const bool shared = rslot == active;
+    const size_t row = (size_t)expert * (shared ? 0 : h) + rtile * 16;
+    const int k0 = min(u, chunks - 1) * F::K;
+    const Code* w1 = (const Code*)(shared ? w.Ws1 : w.W1) + (row * d + k0);
+    const Code* w3 = (const Code*)(shared ? w.Ws3 : w.W3) + (row * d + k0);
+    const size_t at = row * (d / MX_BLOCK) + k0 / MX_BLOCK;
+    to[0].load(w1, d * sizeof(Code), F::MX ? (shared ? w.Ss1 : w.S1) + at : nullptr, d / MX_BLOCK,
+               live ? d - k0 : 0);
+    to[1].load(w3, d * sizeof(Code), F::MX ? (shared ? w.Ss3 : w.S3) + at : nullptr, d / MX_BLOCK,
+               live ? d - k0 : 0);
   };
   const T* x[TT];
-  int at[TT], n = 0, slot = -1;
+  int at[TT], n = 0;
+  uint32_t mine = 0;
   float gate[TT];
-  const auto columns = [&](int s) __attribute__((always_inline)) {
-    slot = s;
-    const bool shared = s >= active;
-    n = shared ? N : __builtin_amdgcn_readfirstlane((OWN ? own_list[s] : plan.list[s]) >> 16);
-    // columns past the last token repeat it; nothing of them is stored
+  const auto columns = [&]() __attribute__((always_inline)) {
+    int token[TT], pick[TT];
+    if (slot == active) {
+      n = TT == 1 ? 16 : N;
+      mine = 0;
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      const int c = min(t * 16 + col, n - 1);
-      int token = c;
-      at[t] = c;
-      gate[t] = 1.0f;
-      if (!shared) {
-        const uint32_t p = OWN ? own_rows[s][c] : plan.rows[s * DECODE_TOKENS + c];
-        token = (int)(p >> 16);
-        at[t] = token * k + (int)(p & 0xffffu);
+      for (int t = 0; t < TT; ++t) {
+        at[t] = token[t] = min(t * 16 + col, N - 1);
+        gate[t] = 1.0f;
+        mine |= (uint32_t)(t * 16 + col < N) << t;
+      }
+    } else {
+      const int o = used.expert(slot) * PT + (PT == 16 ? col : lane);
+      n = columns_of<TT>(OWN ? reinterpret_cast<const uint16_t*>(own_pick)[o] : plan.pick[o], token,
+                         pick, &mine);
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        at[t] = token[t] * k + pick[t];
         gate[t] = OWN ? own_gates[at[t]] : gates[at[t]];
       }
-      x[t] = X + (size_t)token * d;
     }
+#pragma unroll
+    for (int t = 0; t < TT; ++t) x[t] = X + (size_t)token[t] * d;
   };
 
   Chunk<F> a[2][2];
@@ -507,27 +519,25 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
   int u = u0, turn = 0;
 #pragma unroll
   for (int t = 0; t < TT; ++t) acc[0][t] = acc[1][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  aim(tile);
-  request(a[0], min(u0, chunks - 1));
-  __builtin_amdgcn_sched_barrier(0);
-  columns(tile < routed ? tile / ht : active);
+  request(a[0], u0, true);
+  columns();
   // one chunk of the tile in use; false past the last tile
   const auto step = [&](Chunk<F> (&now)[2], Chunk<F> (&next)[2]) __attribute__((always_inline)) {
     const int k0 = min(u, chunks - 1) * F::K;
     typename F::B b;
     b.load(x[0] + k0, q, d - k0);     // before the request: memory answers in order
     const bool ends = u + 1 >= u1;
-    if (!ends) {
-      request(next, u + 1);
-    } else if (tile + 1 < t1) {
-      aim(tile + 1);
-      request(next, min(u0, chunks - 1));
+    if (ends && left > 1 && ++rtile == (rslot < active ? ht : hs / 16)) {
+      rtile = 0;
+      expert = ++rslot < active ? used.expert(rslot) : 0;
     }
+    request(next, ends ? u0 : u + 1, !ends || left > 1);
     __builtin_amdgcn_sched_barrier(0);
     if (u < u1) {                     // else more waves than chunks
       u32x4 op[2][4];
+      uint2 scale[2];
 #pragma unroll
-      for (int m = 0; m < 2; ++m) now[m].turn(turned[wave][m], op[m]);
+      for (int m = 0; m < 2; ++m) now[m].turn(turned[wave][m], op[m], scale[m]);
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
         if (t > 0) {
@@ -535,7 +545,7 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
           b.load(x[t] + k0, q, d - k0);
         }
 #pragma unroll
-        for (int m = 0; m < 2; ++m) F::mma(acc[m][t], op[m], now[m].scale, b, q, d - k0);
+        for (int m = 0; m < 2; ++m) F::mma(acc[m][t], op[m], scale[m], b, q, d - k0);
       }
     }
     if (!ends) {
@@ -549,13 +559,11 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
       red[turn][wave][2 * t + 1][lane] = acc[1][t];
       acc[0][t] = acc[1][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    __syncthreads();
+    lds_barrier();
     static_assert(TT <= W13_WAVES, "");
-    const bool shared = tile >= routed;
-    const int width = shared ? hs : h, unit = (shared ? tile - routed : tile % ht) * 16 + q * 4;
 #pragma unroll
     for (int t = 0; t < TT; ++t)
-      if (wave == t && t * 16 + col < n) {
+      if (wave == t && ((mine >> t) & 1)) {
         f32x4 f = red[turn][0][2 * t][lane], g = red[turn][0][2 * t + 1][lane];
 #pragma unroll
         for (int i = 1; i < W13_WAVES; ++i) {
@@ -565,14 +573,18 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = gate[t] * (f[i] / (1.0f + expf(-f[i]))) * g[i];
-        store4<T>((shared ? As : A) + (size_t)at[t] * width + unit, v);
+        T* o = slot < active ? A + (size_t)at[t] * h : As + (size_t)at[t] * hs;
+        store4<T>(o + tile * 16 + q * 4, v);
       }
-    if (TURNS == 1) __syncthreads();
+    if (TURNS == 1) lds_barrier();
     turn ^= TURNS - 1;
     u = u0;
-    if (++tile >= t1) return false;
-    const int s = tile < routed ? tile / ht : active;
-    if (s != slot) columns(s);
+    if (--left == 0) return false;
+    tile = rtile;
+    if (slot != rslot) {
+      slot = rslot;
+      columns();
+    }
     return true;
   };
   while (step(a[0], a[1]) && step(a[1], a[0])) {
@@ -583,85 +595,88 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
 
 constexpr int W2_WAVES = 4;
 
-// Tiles of 16 columns of Y (rows of W2), slot after slot, then the shared experts'.  Each wave
-// streams a contiguous share of them by itself, as in W1/W3; the expert's tokens are the columns
-// of the products, which go to O [token k + pick, d] in fp32 (the shared experts' to the rows
-// from N k).
-template <class F, int TT>
+// Tiles of 16 columns of Y (rows of W2), two side by side (ROWS 2) or one, slot after slot, then the
+// shared experts'.  Each wave streams a contiguous share of them by itself, as in W1/W3, two
+// chunks a step: of the tiles side by side, or two of one tile.  The expert's tokens are the
+// columns of the products, which go to O [token k + pick, d] in fp32 (the shared experts' to the
+// rows from N k).
+template <class F, int TT, int ROWS>
 __global__ __launch_bounds__(64 * W2_WAVES, 2) void decode_w2_kernel(
     const typename F::T* __restrict__ A, const typename F::T* __restrict__ As, DecodeWeights w,
     DecodePlan plan, float* __restrict__ O, int N, int d, int h, int hs, int k) {
   typedef typename F::T T;
   typedef typename F::Code Code;
-  constexpr int U = 2;      // chunks of a burst
-  __shared__ u32x4 turned[W2_WAVES][16][16];
+  constexpr int U = 2 / ROWS;           // chunks of a tile in a step
+  constexpr int PT = plan_tokens<TT>();
+  __shared__ typename Chunk<F>::Lds turned[W2_WAVES][2];
   const int lane = wave_lane(), q = lane >> 4, col = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int active = plan.active[0];
-  const int dt = d / 16, routed = active * dt, hu = h / 64, su = hs / 64;
+  Used used;
+#pragma unroll
+  for (int m = 0; m < 4; ++m) used.w[m] = plan.used[m];
+  const int active = used.count(), dt = d / (16 * ROWS), routed = active * dt;
   // shares of equal work, in 64s of k
+  const int hu = h / 64, su = hs / 64;
   const long waves = (long)gridDim.x * W2_WAVES, total = (long)dt * (active * hu + su);
   const long g = (long)blockIdx.x * W2_WAVES + wave;
   const auto tile_from = [&](long c) {
     const long r = (long)routed * hu;
     return (int)(c <= r ? (c + hu - 1) / hu : routed + (c - r + su - 1) / su);
   };
-  int tile = tile_from(total * g / waves);
-  const int t1 = tile_from(total * (g + 1) / waves);
-  if (tile >= t1) return;
-  const Code* row;
-  const uint8_t* scale;
-  int wide;       // k of the tile that is requested
-  const auto aim = [&](int t) __attribute__((always_inline)) {
-    const bool shared = t >= routed;
-    size_t r;
-    if (shared) {
-      r = (size_t)(t - routed) * 16;
-    } else {
-      const int s = t / dt;
-      r = (size_t)__builtin_amdgcn_readfirstlane(plan.list[s] & 0xffffu) * d + (t - s * dt) * 16;
-    }
-    wide = shared ? hs : h;
-    row = (const Code*)(shared ? w.Ws2 : w.W2) + r * wide;
-    if (F::MX) scale = (shared ? w.Ss2 : w.S2) + r * (wide / MX_BLOCK);
-  };
-  const auto request = [&](Chunk<F> (&to)[U], int u) __attribute__((always_inline)) {
+  const int t0 = tile_from(total * g / waves), t1 = tile_from(total * (g + 1) / waves);
+  if (t0 >= t1) return;
+  int slot = min(t0 / dt, active), tile = t0 - slot * dt, left = t1 - t0;
+  int rslot = slot, rtile = tile, expert = slot < active ? used.expert(slot) : 0;
+  const auto request = [&](Chunk<F> (&to)[2], int u, bool live) __attribute__((always_inline)) {
+    const bool shared = rslot == active;
+    const int wide = shared ? hs : h;
+    const size_t row = (size_t)expert * (shared ? 0 : d) + rtile * (16 * ROWS);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int k0 = min(u + i, (wide + F::K - 1) / F::K - 1) * F::K;
-      to[i].load(row + k0, wide * sizeof(Code), F::MX ? scale + k0 / MX_BLOCK : nullptr,
-                 wide / MX_BLOCK, wide - k0);
+    for (int i = 0; i < 2; ++i) {
+      const size_t r = row + (ROWS == 2 ? i * 16 : 0);
+      const int k0 = (ROWS == 2 ? u : u + i) * F::K;
+      const bool there = live && k0 < wide;
+      const size_t at = r * wide + (there ? k0 : 0);
+      to[i].load((const Code*)(shared ? w.Ws2 : w.W2) + at, wide * sizeof(Code),
+                 F::MX ? (shared ? w.Ss2 : w.S2) + at / MX_BLOCK : nullptr, wide / MX_BLOCK,
+                 there ? wide - k0 : 0);
     }
   };
   const T* x[TT];
-  int at[TT], n = 0, slot = -1;
-  const auto columns = [&](int s) __attribute__((always_inline)) {
-    slot = s;
-    const bool shared = s >= active;
-    n = shared ? N : __builtin_amdgcn_readfirstlane(plan.list[s] >> 16);
+  int at[TT], n = 0;
+  uint32_t mine = 0;
+  const auto columns = [&]() __attribute__((always_inline)) {
+    int token[TT], pick[TT];
+    if (slot == active) {
+      n = TT == 1 ? 16 : N;
+      mine = 0;
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      const int c = min(t * 16 + col, n - 1);
-      if (shared) {
-        x[t] = As + (size_t)c * hs;
-        at[t] = N * k + c;
-      } else {
-        const uint32_t p = plan.rows[s * DECODE_TOKENS + c];
-        at[t] = (int)(p >> 16) * k + (int)(p & 0xffffu);
+      for (int t = 0; t < TT; ++t) {
+        const int c = t * 16 + col;
+        x[t] = As + (size_t)min(c, N - 1) * hs;
+        at[t] = N * k + min(c, N - 1);
+        mine |= (uint32_t)(c < N) << t;
+      }
+    } else {
+      n = columns_of<TT>(plan.pick[used.expert(slot) * PT + (PT == 16 ? col : lane)], token, pick,
+                         &mine);
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        at[t] = token[t] * k + pick[t];
         x[t] = A + (size_t)at[t] * h;
       }
     }
   };
-  Chunk<F> a[2][U];
-  f32x4 acc[TT];
+  Chunk<F> a[2][2];
+  f32x4 acc[ROWS][TT];
+  int u = 0, width = slot < active ? h : hs;
 #pragma unroll
-  for (int t = 0; t < TT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int u = 0, width = tile < routed ? h : hs;
-  aim(tile);
-  request(a[0], 0);
-  __builtin_amdgcn_sched_barrier(0);
-  columns(tile < routed ? tile / dt : active);
-  const auto step = [&](Chunk<F> (&now)[U], Chunk<F> (&next)[U]) __attribute__((always_inline)) {
+  for (int t = 0; t < TT; ++t)
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  request(a[0], 0, true);
+  columns();
+  const auto step = [&](Chunk<F> (&now)[2], Chunk<F> (&next)[2]) __attribute__((always_inline)) {
     const int chunks = (width + F::K - 1) / F::K;
     typename F::B b[U];
 #pragma unroll
@@ -670,43 +685,48 @@ __global__ __launch_bounds__(64 * W2_WAVES, 2) void decode_w2_kernel(
       b[i].load(x[0] + k0, q, width - k0);
     }
     const bool ends = u + U >= chunks;
-    if (!ends) {
-      request(next, u + U);
-    } else if (tile + 1 < t1) {
-      aim(tile + 1);
-      request(next, 0);
+    if (ends && left > 1 && ++rtile == dt) {
+      rtile = 0;
+      expert = ++rslot < active ? used.expert(rslot) : 0;
     }
+    request(next, ends ? 0 : u + U, !ends || left > 1);
     __builtin_amdgcn_sched_barrier(0);
+    u32x4 op[2][4];
+    uint2 scale[2];
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-      if (u + i < chunks) {
-        const int k0 = (u + i) * F::K;
-        u32x4 op[4];
-        now[i].turn(turned[wave], op);
+    for (int i = 0; i < 2; ++i) now[i].turn(turned[wave][i], op[i], scale[i]);
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
-          if (t > 0) {
-            if (t * 16 >= n) break;
-            b[0].load(x[t] + k0, q, width - k0);
-          }
-          F::mma(acc[t], op, now[i].scale, t > 0 ? b[0] : b[i], q, width - k0);
-        }
+    for (int t = 0; t < TT; ++t) {
+      if (t > 0 && t * 16 >= n) break;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (U == 2 && u + i >= chunks) break;
+        const int k0 = (u + i % U) * F::K;
+        typename F::B& bi = b[i % U];
+        if (t > 0 && i < U) bi.load(x[t] + k0, q, width - k0);
+        F::mma(acc[i % ROWS][t], op[i], scale[i], bi, q, width - k0);
       }
+    }
     if (!ends) {
       u += U;
       return true;
     }
-    const int c = (tile < routed ? tile % dt : tile - routed) * 16 + q * 4;
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      if (t * 16 + col < n) *reinterpret_cast<f32x4*>(O + (size_t)at[t] * d + c) = acc[t];
-      acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int m = 0; m < ROWS; ++m) {
+        if ((mine >> t) & 1)
+          *reinterpret_cast<f32x4*>(O + (size_t)at[t] * d + (tile * ROWS + m) * 16 + q * 4) = acc[m][t];
+        acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
     u = 0;
-    if (++tile >= t1) return false;
-    width = tile < routed ? h : hs;
-    const int s = tile < routed ? tile / dt : active;
-    if (s != slot) columns(s);
+    if (--left == 0) return false;
+    tile = rtile;
+    if (slot != rslot) {
+      slot = rslot;
+      width = slot < active ? h : hs;
+      columns();
+    }
     return true;
   };
   while (step(a[0], a[1]) && step(a[1], a[0])) {
@@ -753,7 +773,6 @@ hipError_t run_decode(const DecodeCall& c, hipStream_t st) {
   const T* X = (const T*)(c.Xs ? c.Xb : c.X);
   const int most = c.N * c.k < c.E ? c.N * c.k : c.E;    // chosen experts at most
   const long tiles13 = (long)most * (c.h / 16) + c.hs / 16;
-  const long tiles2 = ((long)most + (c.hs ? 1 : 0)) * (c.d / 16);
   const auto w13 = [&](auto nq) {
     decode_w13_kernel<F, TT, decltype(nq)::value>
         <<<dim3((unsigned)(tiles13 < W13_GRID ? tiles13 : W13_GRID)), 64 * W13_WAVES, 0, st>>>(
@@ -768,17 +787,26 @@ hipError_t run_decode(const DecodeCall& c, hipStream_t st) {
       chosen = true;
     }
   if (!chosen) {
+    constexpr int PT = plan_tokens<TT>();
     if (c.E <= 64)
-      decode_choose_kernel<4><<<1, 1024, 0, st>>>(c.Z, c.N, c.E, c.k, splits, c.inv_tau, c.experts,
-                                                  c.gates, c.plan);
+      decode_choose_kernel<4, PT><<<1, 16 * PT, 0, st>>>(c.Z, c.N, c.E, c.k, splits, c.inv_tau,
+                                                         c.experts, c.gates, c.plan);
     else
-      decode_choose_kernel<16><<<1, 1024, 0, st>>>(c.Z, c.N, c.E, c.k, splits, c.inv_tau, c.experts,
-                                                   c.gates, c.plan);
+      decode_choose_kernel<16, PT><<<1, 16 * PT, 0, st>>>(c.Z, c.N, c.E, c.k, splits, c.inv_tau,
+                                                          c.experts, c.gates, c.plan);
     w13(std::integral_constant<int, 0>{});
   }
-  const long g2 = (tiles2 + W2_WAVES - 1) / W2_WAVES;
-  decode_w2_kernel<F, TT><<<dim3((unsigned)(g2 < W2_GRID ? g2 : W2_GRID)), 64 * W2_WAVES, 0, st>>>(
-      (const T*)c.A, (const T*)c.As, c.w, c.plan, c.O, c.N, c.d, c.h, c.hs, c.k);
+  const long tiles2 = ((long)most + (c.hs ? 1 : 0)) * (c.d / 16);
+  const auto w2 = [&](auto rows) {
+    constexpr int R = decltype(rows)::value;
+    const long grid = (tiles2 / R + W2_WAVES - 1) / W2_WAVES;
+    decode_w2_kernel<F, TT, R>
+        <<<dim3((unsigned)(grid < W2_GRID ? grid : W2_GRID)), 64 * W2_WAVES, 0, st>>>(
+            (const T*)c.A, (const T*)c.As, c.w, c.plan, c.O, c.N, c.d, c.h, c.hs, c.k);
+  };
+  // tiles side by side share a load of the activations, if there is one for every wave
+  if (tiles2 >= 2 * W2_GRID * W2_WAVES) w2(std::integral_constant<int, 2>{});
+  else w2(std::integral_constant<int, 1>{});
   decode_sum_kernel<T><<<dim3((unsigned)((c.d + 255) / 256), (unsigned)c.N), 64, 0, st>>>(
       c.O, (const T*)c.R, (T*)c.Y, c.N, c.d, c.k, c.hs);
   return hipGetLastError();

@@ -467,10 +467,8 @@ ec::DecodeCall carve_decode(Carve& c, const Plan& P, int top_k) {
   w.k = top_k;
   const size_t rows = (size_t)P.N * top_k;
   w.Z = (float*)c.take((size_t)ec::decode_splits(P.d) * P.N * P.E * 4);
-  const size_t slots = rows < (size_t)P.E ? rows : P.E;
-  w.plan.active = (int32_t*)c.take(4);
-  w.plan.list = (uint32_t*)c.take(slots * 4);
-  w.plan.rows = (uint32_t*)c.take(slots * ec::DECODE_TOKENS * 4);
+  w.plan.used = (unsigned long long*)c.take(4 * 8);
+  w.plan.pick = (uint16_t*)c.take((size_t)P.E * ec::DECODE_TOKENS * 2);
   w.Xb = P.dtype == EC_BF16 ? c.take((size_t)P.N * P.d * 2) : nullptr;
   w.A = c.take(rows * P.h * P.esz);
   w.As = c.take((size_t)P.N * P.hs * P.esz);

@@ -279,11 +279,10 @@ struct DecodeWeights {
   const uint8_t *S1, *S3, *S2, *Ss1, *Ss3, *Ss2;
 };
 
-// Who chose what: the chosen experts in ascending order ("slots").
+// Who chose what (decode.hip).
 struct DecodePlan {
-  int32_t* active;    // [1] slots
-  uint32_t* list;     // [slots] expert | tokens << 16
-  uint32_t* rows;     // [slots, 64] token << 16 | pick, the tokens that chose it, ascending
+  unsigned long long* used;   // [4] bit j: expert j was chosen
+  uint16_t* pick;             // [E, 64] or, of 16 tokens at most, [E, 16]
 };
 
 struct DecodeCall {
