@@ -30,11 +30,6 @@ __device__ __forceinline__ V stream_global(const void* p) {
   return __builtin_nontemporal_load((const __attribute__((address_space(1))) V*)p);
 }
 
-// A barrier for LDS alone: __syncthreads() would wait for the requests on their way too.
-__device__ __forceinline__ void lds_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
-
 // Eight codes as bf16, times 2^(byte - 127).
 __device__ __forceinline__ bf16x8 mx_widen8(uint32_t lo, uint32_t hi, float scale) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);

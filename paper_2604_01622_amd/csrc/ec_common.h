@@ -135,6 +135,11 @@ __device__ __forceinline__ void store4(T* p, const float* v) {
     store_vec<T, 4>(p, v);
 }
 
+// A barrier for LDS alone: __syncthreads() would wait for a wave's loads on their way too.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 // A value as the storage type holds it.
 template <typename T>
 __device__ __forceinline__ float round_to(float v) {

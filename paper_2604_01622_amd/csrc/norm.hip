@@ -6,7 +6,8 @@
 //
 // Memory bounds both: every row moves once and is held in registers between its sum and its
 // use.  A row belongs to TPR lanes, each of which takes V pieces of VEC elements (16 bytes, or
-// one element where the row's length leaves its rows unaligned).
+// one element where the row's length leaves its rows unaligned).  Up to eight elements a lane the
+// next row's are requested before this one's are used.
 #include "mx.h"
 #include "ec_kernels.h"
 
@@ -25,19 +26,20 @@ __device__ __forceinline__ float wave_sum(float t) {
 }
 
 // Sums of NS values over a row's lanes: TPR / 64 waves.  `red` holds two sets of NS values a
-// wave, taken in turn, so that one barrier a row is enough.
+// wave of the workgroup, taken in turn, so that one barrier a row is enough.
 template <int TPR, int NS>
 __device__ __forceinline__ void row_sums(float (&s)[NS], float* red, int turn) {
 #pragma unroll
   for (int n = 0; n < NS; ++n) s[n] = wave_sum(s[n]);
   if constexpr (TPR > 64) {
     constexpr int NW = TPR / 64;
-    float* r = red + turn * NW * NS;
     const int w = threadIdx.x >> 6;
+    float* r = red + turn * (int)(blockDim.x >> 6) * NS;
     if (wave_lane() == 0)
 #pragma unroll
       for (int n = 0; n < NS; ++n) r[w * NS + n] = s[n];
-    __syncthreads();
+    lds_barrier();
+    r += w / NW * NW * NS;
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
       s[n] = 0.f;
@@ -47,65 +49,107 @@ __device__ __forceinline__ void row_sums(float (&s)[NS], float* red, int turn) {
   }
 }
 
+// VEC elements as they are stored.
+template <typename T, int VEC>
+struct Piece {
+  std::conditional_t<VEC == 1, T, u32x4> raw;
+  __device__ __forceinline__ void load(const T* p) {
+    raw = *reinterpret_cast<const decltype(raw)*>(p);
+  }
+  __device__ __forceinline__ void get(float* v) const {
+    if constexpr (VEC == 1 && sizeof(T) == 4) {
+      v[0] = raw;
+    } else if constexpr (VEC == 1) {
+      v[0] = bf16_to_f32(raw);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(raw[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = bf16_to_f32(raw[i] & 0xffffu);
+        v[2 * i + 1] = bf16_to_f32(raw[i] >> 16);
+      }
+    }
+  }
+};
+
+// A lane's pieces of a row of p (column c of piece 0, TPR VEC apart; past d none).  live false:
+// one place for all lanes instead, not used: a request in every turn lets the waits count.
+template <typename T, int VEC, int V, int TPR>
+__device__ __forceinline__ void load_row(Piece<T, VEC> (&to)[V], const T* p, long row, int c, int d,
+                                         bool live) {
+  const T* r = p + (live ? row * d : 0);
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int at = c + v * TPR * VEC;
+    to[v].load(r + (live && at < d ? at : 0));
+  }
+}
+
+// Rows that a lane holds at a time, in registers.
+template <int VEC, int V>
+constexpr int row_buffers() { return VEC * V > 8 ? 1 : 2; }
+
 template <int TPR>
 constexpr int norm_threads() { return TPR < 256 ? 256 : TPR; }
 
 // One row a group of TPR lanes and step; MX: eight bits out.
-template <typename T, int VEC, int V, int TPR, bool MX>
+template <typename T, int VEC, int V, int TPR, bool MX, bool RES>
 __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
     const T* X, const T* R, const T* __restrict__ w, T* H, T* __restrict__ Y,
     uint8_t* __restrict__ Q, uint8_t* __restrict__ scale, long rows, int d, float eps) {
   constexpr int RB = norm_threads<TPR>() / TPR;
-  __shared__ float red[2 * (TPR / 64)];
-  const int t = threadIdx.x % TPR;
+  __shared__ float red[2 * norm_threads<TPR>() / 64];
+  const int c0 = threadIdx.x % TPR * VEC;
   const float inv_d = 1.0f / (float)d;
-  int turn = 0;
-  for (long row = (long)blockIdx.x * RB + threadIdx.x / TPR; row < rows;
-       row += (long)gridDim.x * RB, turn ^= 1) {
+  const long stride = (long)gridDim.x * RB;
+  long row = (long)blockIdx.x * RB + threadIdx.x / TPR;
+  if (row >= rows) return;          // a whole wave; with RB = 1 the whole workgroup
+  constexpr int BUF = row_buffers<VEC, V>();
+  Piece<T, VEC> x[BUF][V], r[BUF][RES ? V : 1], pw[V];
+  const auto request = [&](int i, long at, bool live) __attribute__((always_inline)) {
+    load_row<T, VEC, V, TPR>(x[i], X, at, c0, d, live);
+    if constexpr (RES) load_row<T, VEC, V, TPR>(r[i], R, at, c0, d, live);
+  };
+  if (BUF == 2) request(0, row, true);
+  load_row<T, VEC, V, TPR>(pw, w, 0, c0, d, true);
+  const auto step = [&](int turn) __attribute__((always_inline)) {
+    const int i = BUF == 2 ? turn : 0;
+    const bool more = row + stride < rows;
+    if (BUF == 2) request(i ^ 1, row + stride, more);
+    else request(0, row, true);
+    __builtin_amdgcn_sched_barrier(0);
     const long at = row * d;
-    float h[V][VEC];
-    float s[1] = {0.f};
+    float h[V][VEC], s[1] = {0.f};
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + t) * VEC;
-      if (c < d) {
-        load_vec<T, VEC>(X + at + c, h[v]);
-      } else {
+      const int c = c0 + v * TPR * VEC;
+      x[i][v].get(h[v]);
+      if constexpr (RES) {
+        float q[VEC];
+        r[i][v].get(q);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) h[v][i] = 0.f;
+        for (int e = 0; e < VEC; ++e) h[v][e] = round_to<T>(h[v][e] + q[e]);
+        if (c < d) store_vec<T, VEC>(H + at + c, h[v]);
       }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[0] = c < d ? fmaf(h[v][e], h[v][e], s[0]) : s[0];
     }
-    if (R) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int c = (v * TPR + t) * VEC;
-        if (c < d) {
-          float q[VEC];
-          load_vec<T, VEC>(R + at + c, q);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) h[v][i] = round_to<T>(h[v][i] + q[i]);
-        }
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) s[0] = fmaf(h[v][i], h[v][i], s[0]);
     row_sums<TPR, 1>(s, red, turn);
-    const float r = 1.0f / sqrtf(fmaf(s[0], inv_d, eps));
+    const float rs = 1.0f / sqrtf(fmaf(s[0], inv_d, eps));
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + t) * VEC;
+      const int c = c0 + v * TPR * VEC;
       if (c >= d) break;
-      if (R) store_vec<T, VEC>(H + at + c, h[v]);
       float y[VEC], q[VEC];
-      load_vec<T, VEC>(w + c, q);
+      pw[v].get(q);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) y[i] = h[v][i] * r * q[i];
+      for (int e = 0; e < VEC; ++e) y[e] = h[v][e] * rs * q[e];
       if constexpr (MX) {   // d is a multiple of 32: a block's lanes are all here
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) top = max(top, magnitude(y[i]));
+        for (int e = 0; e < VEC; ++e) top = max(top, magnitude(y[e]));
         const uint32_t byte = mx_byte(mx_block_max<VEC>(top));
         const float inverse = mx_inverse(byte);
         if constexpr (VEC == 8)
@@ -118,125 +162,150 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
         store_vec<T, VEC>(Y + at + c, y);
       }
     }
+    row += stride;
+    return more;
+  };
+  while (step(0) && step(1)) {
   }
 }
 
+constexpr int NB_THREADS = 1024;     // of a backward workgroup: 1024 / TPR rows at a time
+
 // A workgroup takes every gridDim.x-th set of rows and keeps its share of dw in registers;
 // part [gridDim.x, d] (dw itself where one workgroup takes all rows).
-template <typename T, int VEC, int V, int TPR>
-__global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_backward_kernel(
+template <typename T, int VEC, int V, int TPR, bool DH>
+__global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
     const T* H, const T* __restrict__ w, const T* dY, const T* dH, T* dX,
     float* __restrict__ part, long rows, int d, float eps) {
-  constexpr int RB = norm_threads<TPR>() / TPR;
-  __shared__ float red[4 * (TPR / 64)];
-  const int t = threadIdx.x % TPR;
+  constexpr int RB = NB_THREADS / TPR;
+  __shared__ float red[4 * NB_THREADS / 64];
+  const int c0 = threadIdx.x % TPR * VEC;
   const float inv_d = 1.0f / (float)d;
+  const long stride = (long)gridDim.x * RB;
+  long first = (long)blockIdx.x * RB;               // of the workgroup's rows
+  const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
   float dw[V][VEC];
+  constexpr int BUF = row_buffers<VEC, V>();
+  Piece<T, VEC> ph[BUF][V], pg[BUF][V], pd[BUF][DH ? V : 1], pw[V];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) dw[v][i] = 0.f;
-  int turn = 0;
-  for (long row = (long)blockIdx.x * RB + threadIdx.x / TPR; row < rows;
-       row += (long)gridDim.x * RB, turn ^= 1) {
-    const long at = row * d;
-    float h[V][VEC], g[V][VEC];
+    for (int e = 0; e < VEC; ++e) dw[v][e] = 0.f;
+  const auto request = [&](int i, long row) __attribute__((always_inline)) {
+    const bool live = row < rows;
+    load_row<T, VEC, V, TPR>(ph[i], H, row, c0, d, live);
+    load_row<T, VEC, V, TPR>(pg[i], dY, row, c0, d, live);
+    if constexpr (DH) load_row<T, VEC, V, TPR>(pd[i], dH, row, c0, d, live);
+  };
+  const auto step = [&](int turn) __attribute__((always_inline)) {
+    const int i = BUF == 2 ? turn : 0;
+    const long row = first + mine;
+    if (BUF == 2) request(i ^ 1, row + stride);
+    else request(0, row);
+    __builtin_amdgcn_sched_barrier(0);
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + t) * VEC;
-      if (c < d) {
-        load_vec<T, VEC>(H + at + c, h[v]);
-        load_vec<T, VEC>(dY + at + c, g[v]);
-      } else {
+      float h[VEC], g[VEC], q[VEC];
+      ph[i][v].get(h);
+      pg[i][v].get(g);
+      pw[v].get(q);
+      const bool in = c0 + v * TPR * VEC < d;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) h[v][i] = g[v][i] = 0.f;
-      }
-    }
-    float wv[V][VEC];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + t) * VEC;
-      if (c < d) load_vec<T, VEC>(w + c, wv[v]);
-      else
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) wv[v][i] = 0.f;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        s[0] = fmaf(h[v][i], h[v][i], s[0]);
-        s[1] = fmaf(g[v][i] * wv[v][i], h[v][i], s[1]);
+      for (int e = 0; e < VEC; ++e) {
+        s[0] = in ? fmaf(h[e], h[e], s[0]) : s[0];
+        s[1] = in ? fmaf(g[e] * q[e], h[e], s[1]) : s[1];
       }
     }
     row_sums<TPR, 2>(s, red, turn);
     const float r = 1.0f / sqrtf(fmaf(s[0], inv_d, eps));
     const float k = r * r * (s[1] * inv_d);
+    if (row < rows) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + t) * VEC;
-      if (c >= d) break;
-      float x[VEC];
+      for (int v = 0; v < V; ++v) {
+        const int c = c0 + v * TPR * VEC;
+        if (c >= d) break;
+        float h[VEC], g[VEC], q[VEC], x[VEC];
+        ph[i][v].get(h);
+        pg[i][v].get(g);
+        pw[v].get(q);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        dw[v][i] = fmaf(g[v][i], h[v][i] * r, dw[v][i]);
-        x[i] = r * (g[v][i] * wv[v][i] - h[v][i] * k);
+        for (int e = 0; e < VEC; ++e) {
+          dw[v][e] = fmaf(g[e], h[e] * r, dw[v][e]);
+          x[e] = r * (g[e] * q[e] - h[e] * k);
+        }
+        if constexpr (DH) {
+          pd[i][v].get(q);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) x[e] += q[e];
+        }
+        store_vec<T, VEC>(dX + row * d + c, x);
       }
-      if (dH) {
-        float q[VEC];
-        load_vec<T, VEC>(dH + at + c, q);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) x[i] += q[i];
-      }
-      store_vec<T, VEC>(dX + at + c, x);
+    }
+    first += stride;
+    return first < rows;
+  };
+  if (rows > 0) {
+    if (BUF == 2) request(0, first + mine);
+    load_row<T, VEC, V, TPR>(pw, w, 0, c0, d, true);
+    while (step(0) && step(1)) {
     }
   }
   float* out = part + (long)blockIdx.x * d;
   if constexpr (RB == 1) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + t) * VEC;
+      const int c = c0 + v * TPR * VEC;
       if (c < d) store_vec<float, VEC>(out + c, dw[v]);
     }
   } else {
-    // the workgroup's row groups add to one another in turn
-    __shared__ float sum[V * TPR * VEC];
-    for (int b = 0; b < RB; ++b) {
-      if ((int)threadIdx.x / TPR == b) {
+    // the workgroup's rows meet, in order
+    constexpr int W = V * TPR * VEC;
+    __shared__ float sum[RB * W];
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            float* p = &sum[(v * TPR + t) * VEC + i];
-            *p = b == 0 ? dw[v][i] : *p + dw[v][i];
-          }
-      }
-      __syncthreads();
+      for (int e = 0; e < VEC; ++e) sum[mine * W + c0 + v * TPR * VEC + e] = dw[v][e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < d; c += NB_THREADS) {
+      float t = sum[c];
+#pragma unroll
+      for (int b = 1; b < RB; ++b) t += sum[b * W + c];
+      out[c] = t;
     }
-    for (int c = threadIdx.x; c < d; c += norm_threads<TPR>()) out[c] = sum[c];
   }
 }
 
-// dw[c] = sum of part[i, c]: 64 columns a workgroup, its 16 waves each every 16th row.
-__global__ __launch_bounds__(1024) void rms_norm_dw_kernel(const float* __restrict__ part,
-                                                           float* __restrict__ dw, int n, int d) {
-  __shared__ float s[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
+// dw[c] = sum of part[i, c]: 16 columns a workgroup, its 16 groups of lanes each every 16th row,
+// eight on their way.
+__global__ __launch_bounds__(256) void rms_norm_dw_kernel(const float* __restrict__ part,
+                                                          float* __restrict__ dw, int n, int d) {
+  __shared__ float s[16][16];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), g = threadIdx.x >> 4;
   float t = 0.f;
   if (c < d)
-    for (int i = g; i < n; i += 16) t += part[(long)i * d + c];
-  s[g][threadIdx.x & 63] = t;
+    for (int i0 = g; i0 < n; i0 += 16 * 8) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = part[(long)min(i0 + j * 16, n - 1) * d + c];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t += i0 + j * 16 < n ? v[j] : 0.f;
+    }
+  s[g][threadIdx.x & 15] = t;
   __syncthreads();
   if (g == 0 && c < d) {
-    t = 0.f;
+    t = s[0][threadIdx.x];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += s[i][threadIdx.x];
+    for (int i = 1; i < 16; ++i) t += s[i][threadIdx.x];
     dw[c] = t;
   }
 }
 
-constexpr int kNormGrid = 1 << 20;   // workgroups of a forward launch at most
+constexpr int NORM_GRID = 2048;      // workgroups at most: each loops over rows
+constexpr int NB_GRID = 512;
 
-// Calls body(VEC, V, TPR) as types with the smallest group of lanes that holds a row in at most
-// four pieces each.
+// Calls body(VEC, V, TPR) as types with the smallest group of lanes that holds a row in one piece
+// of 16 bytes each, or four of one element (past 1024 lanes more).
 template <typename T, typename F>
 hipError_t with_shape(int d, F body) {
   constexpr int W = 16 / sizeof(T);
@@ -245,12 +314,12 @@ hipError_t with_shape(int d, F body) {
   if (d % W == 0) {
     const int u = d / W;
     if (u <= 64) return ints(EC_I(W), EC_I(1), EC_I(64));
-    if (u <= 128) return ints(EC_I(W), EC_I(2), EC_I(64));
-    if (u <= 256) return ints(EC_I(W), EC_I(4), EC_I(64));
-    if (u <= 512) return ints(EC_I(W), EC_I(2), EC_I(256));
-    if (u <= 1024) return ints(EC_I(W), EC_I(4), EC_I(256));
+    if (u <= 128) return ints(EC_I(W), EC_I(1), EC_I(128));
+    if (u <= 256) return ints(EC_I(W), EC_I(1), EC_I(256));
+    if (u <= 512) return ints(EC_I(W), EC_I(1), EC_I(512));
+    if (u <= 1024) return ints(EC_I(W), EC_I(1), EC_I(1024));
     if (u <= 2048) return ints(EC_I(W), EC_I(2), EC_I(1024));
-    return ints(EC_I(W), EC_I(4), EC_I(1024));
+    if constexpr (W == 4) return ints(EC_I(W), EC_I(4), EC_I(1024));
   }
   if (d <= 256) return ints(EC_I(1), EC_I(4), EC_I(64));
   if (d <= 1024) return ints(EC_I(1), EC_I(4), EC_I(256));
@@ -266,16 +335,22 @@ hipError_t run_norm(const void* X, const void* R, const void* w, void* H, void* 
     constexpr int VEC = decltype(vec)::value, V = decltype(v)::value, TPR = decltype(tpr)::value;
     constexpr int RB = norm_threads<TPR>() / TPR;
     const long blocks = (rows + RB - 1) / RB;
-    const dim3 grid((unsigned)(blocks < kNormGrid ? blocks : kNormGrid));
+    const dim3 grid((unsigned)(blocks < NORM_GRID ? blocks : NORM_GRID));
+    const auto go = [&](auto mx, auto res) {
+      rms_norm_kernel<T, VEC, V, TPR, decltype(mx)::value, decltype(res)::value>
+          <<<grid, norm_threads<TPR>(), 0, st>>>((const T*)X, (const T*)R, (const T*)w, (T*)H,
+                                                 (T*)Y, Q, scale, rows, d, eps);
+    };
     if (Q) {
-      if constexpr (VEC > 1)
-        rms_norm_kernel<T, VEC, V, TPR, true><<<grid, norm_threads<TPR>(), 0, st>>>(
-            (const T*)X, (const T*)R, (const T*)w, (T*)H, nullptr, Q, scale, rows, d, eps);
-      else
+      if constexpr (VEC > 1) {
+        if (R) go(std::true_type{}, std::true_type{});
+        else go(std::true_type{}, std::false_type{});
+      } else {
         return hipErrorInvalidValue;
+      }
     } else {
-      rms_norm_kernel<T, VEC, V, TPR, false><<<grid, norm_threads<TPR>(), 0, st>>>(
-          (const T*)X, (const T*)R, (const T*)w, (T*)H, (T*)Y, nullptr, nullptr, rows, d, eps);
+      if (R) go(std::false_type{}, std::true_type{});
+      else go(std::false_type{}, std::false_type{});
     }
     return hipGetLastError();
   });
@@ -287,14 +362,18 @@ hipError_t run_norm_backward(const void* H, const void* w, const void* dY, const
                              hipStream_t st) {
   hipError_t e = with_shape<T>(d, [&](auto vec, auto v, auto tpr) {
     constexpr int VEC = decltype(vec)::value, V = decltype(v)::value, TPR = decltype(tpr)::value;
-    rms_norm_backward_kernel<T, VEC, V, TPR>
-        <<<dim3((unsigned)blocks), norm_threads<TPR>(), 0, st>>>(
-            (const T*)H, (const T*)w, (const T*)dY, (const T*)dH, (T*)dX,
-            blocks > 1 ? part : dw, rows, d, eps);
+    const auto go = [&](auto dh) {
+      rms_norm_backward_kernel<T, VEC, V, TPR, decltype(dh)::value>
+          <<<dim3((unsigned)blocks), NB_THREADS, 0, st>>>(
+              (const T*)H, (const T*)w, (const T*)dY, (const T*)dH, (T*)dX,
+              blocks > 1 ? part : dw, rows, d, eps);
+    };
+    if (dH) go(std::true_type{});
+    else go(std::false_type{});
     return hipGetLastError();
   });
   if (e != hipSuccess || blocks <= 1) return e;
-  rms_norm_dw_kernel<<<dim3((unsigned)((d + 63) / 64)), 1024, 0, st>>>(part, dw, blocks, d);
+  rms_norm_dw_kernel<<<dim3((unsigned)((d + 15) / 16)), 256, 0, st>>>(part, dw, blocks, d);
   return hipGetLastError();
 }
 
@@ -303,14 +382,13 @@ hipError_t run_norm_backward(const void* H, const void* w, const void* dY, const
 int rms_norm_backward_blocks(int dtype, long rows, int d) {
   long per = 1;   // rows of a workgroup's step
   const auto rows_of = [&](auto, auto, auto tpr) {
-    constexpr int TPR = decltype(tpr)::value;
-    per = norm_threads<TPR>() / TPR;
+    per = NB_THREADS / decltype(tpr)::value;
     return hipSuccess;
   };
   const hipError_t e =
       dtype == DT_F32 ? with_shape<float>(d, rows_of) : with_shape<bf16_t>(d, rows_of);
   const long steps = e == hipSuccess ? (rows + per - 1) / per : 1;
-  return (int)(steps < 1 ? 1 : steps < 512 ? steps : 512);
+  return (int)(steps < 1 ? 1 : steps < NB_GRID ? steps : NB_GRID);
 }
 
 hipError_t launch_rms_norm(int dtype, const void* X, const void* R, const void* w, void* H, void* Y,
