@@ -115,6 +115,32 @@ __device__ __forceinline__ void store_vec(T* p, const float* v) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
 }
 
+// VEC elements as they are stored, read once (a streaming load: norm of 16384 x 2048 bf16 45.6 ->
+// 44.2 us).
+template <typename T, int VEC>
+struct Piece {
+  std::conditional_t<VEC == 1, T, u32x4> raw;
+  __device__ __forceinline__ void load(const T* p) {
+    raw = __builtin_nontemporal_load(reinterpret_cast<const decltype(raw)*>(p));
+  }
+  __device__ __forceinline__ void get(float* v) const {
+    if constexpr (VEC == 1 && sizeof(T) == 4) {
+      v[0] = raw;
+    } else if constexpr (VEC == 1) {
+      v[0] = bf16_to_f32(raw);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(raw[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = bf16_to_f32(raw[i] & 0xffffu);
+        v[2 * i + 1] = bf16_to_f32(raw[i] >> 16);
+      }
+    }
+  }
+};
+
 // Four consecutive elements.
 template <typename T>
 __device__ __forceinline__ void load4(const T* p, float* v) {

@@ -45,4 +45,13 @@ __device__ __forceinline__ uint32_t mx_block_max(uint32_t t) {
   return t;
 }
 
+// The codes of VEC elements.
+template <int VEC>
+__device__ __forceinline__ void mx_store(uint8_t* q, const float* v, float inverse) {
+  if constexpr (VEC == 8)
+    *reinterpret_cast<uint2*>(q) = make_uint2(mx_codes4(v, inverse), mx_codes4(v + 4, inverse));
+  else
+    *reinterpret_cast<uint32_t*>(q) = mx_codes4(v, inverse);
+}
+
 }  // namespace ec

@@ -49,31 +49,6 @@ __device__ __forceinline__ void row_sums(float (&s)[NS], float* red, int turn) {
   }
 }
 
-// VEC elements as they are stored.
-template <typename T, int VEC>
-struct Piece {
-  std::conditional_t<VEC == 1, T, u32x4> raw;
-  __device__ __forceinline__ void load(const T* p) {
-    raw = *reinterpret_cast<const decltype(raw)*>(p);
-  }
-  __device__ __forceinline__ void get(float* v) const {
-    if constexpr (VEC == 1 && sizeof(T) == 4) {
-      v[0] = raw;
-    } else if constexpr (VEC == 1) {
-      v[0] = bf16_to_f32(raw);
-    } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(raw[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = bf16_to_f32(raw[i] & 0xffffu);
-        v[2 * i + 1] = bf16_to_f32(raw[i] >> 16);
-      }
-    }
-  }
-};
-
 // A lane's pieces of a row of p (column c of piece 0, TPR VEC apart; past d none).  live false:
 // one place for all lanes instead, not used: a request in every turn lets the waits count.
 template <typename T, int VEC, int V, int TPR>
@@ -106,29 +81,21 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
   const long stride = (long)gridDim.x * RB;
   long row = (long)blockIdx.x * RB + threadIdx.x / TPR;
   if (row >= rows) return;          // a whole wave; with RB = 1 the whole workgroup
-  constexpr int BUF = row_buffers<VEC, V>();
-  Piece<T, VEC> x[BUF][V], r[BUF][RES ? V : 1], pw[V];
-  const auto request = [&](int i, long at, bool live) __attribute__((always_inline)) {
-    load_row<T, VEC, V, TPR>(x[i], X, at, c0, d, live);
-    if constexpr (RES) load_row<T, VEC, V, TPR>(r[i], R, at, c0, d, live);
-  };
-  if (BUF == 2) request(0, row, true);
-  load_row<T, VEC, V, TPR>(pw, w, 0, c0, d, true);
-  const auto step = [&](int turn) __attribute__((always_inline)) {
-    const int i = BUF == 2 ? turn : 0;
-    const bool more = row + stride < rows;
-    if (BUF == 2) request(i ^ 1, row + stride, more);
-    else request(0, row, true);
-    __builtin_amdgcn_sched_barrier(0);
+  int turn = 0;
+  do {
+    Piece<T, VEC> x[V], r[RES ? V : 1], pw[V];
+    load_row<T, VEC, V, TPR>(x, X, row, c0, d, true);
+    if constexpr (RES) load_row<T, VEC, V, TPR>(r, R, row, c0, d, true);
+    load_row<T, VEC, V, TPR>(pw, w, 0, c0, d, true);
     const long at = row * d;
     float h[V][VEC], s[1] = {0.f};
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int c = c0 + v * TPR * VEC;
-      x[i][v].get(h[v]);
+      x[v].get(h[v]);
       if constexpr (RES) {
         float q[VEC];
-        r[i][v].get(q);
+        r[v].get(q);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) h[v][e] = round_to<T>(h[v][e] + q[e]);
         if (c < d) store_vec<T, VEC>(H + at + c, h[v]);
@@ -151,22 +118,15 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
 #pragma unroll
         for (int e = 0; e < VEC; ++e) top = max(top, magnitude(y[e]));
         const uint32_t byte = mx_byte(mx_block_max<VEC>(top));
-        const float inverse = mx_inverse(byte);
-        if constexpr (VEC == 8)
-          *reinterpret_cast<uint2*>(Q + at + c) =
-              make_uint2(mx_codes4(y, inverse), mx_codes4(y + 4, inverse));
-        else
-          *reinterpret_cast<uint32_t*>(Q + at + c) = mx_codes4(y, inverse);
+        mx_store<VEC>(Q + at + c, y, mx_inverse(byte));
         if (c % MX_BLOCK == 0) scale[(at + c) / MX_BLOCK] = (uint8_t)byte;
       } else {
         store_vec<T, VEC>(Y + at + c, y);
       }
     }
     row += stride;
-    return more;
-  };
-  while (step(0) && step(1)) {
-  }
+    turn ^= 1;
+  } while (row < rows);
 }
 
 constexpr int NB_THREADS = 1024;     // of a backward workgroup: 1024 / TPR rows at a time
@@ -301,8 +261,8 @@ __global__ __launch_bounds__(256) void rms_norm_dw_kernel(const float* __restric
   }
 }
 
-constexpr int NORM_GRID = 2048;      // workgroups at most: each loops over rows
-constexpr int NB_GRID = 512;
+constexpr int NORM_GRID = 1 << 20;   // workgroups at most
+constexpr int NB_GRID = 256;         // of a backward launch: one a CU
 
 // Calls body(VEC, V, TPR) as types with the smallest group of lanes that holds a row in one piece
 // of 16 bytes each, or four of one element (past 1024 lanes more).
