@@ -222,20 +222,31 @@ __device__ __forceinline__ float choose(const float (&z)[NQ], int E, int k, floa
   return row16_sum_even(sum);
 }
 
-// Logits r, r + 16, ... of a token: the sums of the splits' shares, in order.
+constexpr int LG_SPLITS = 8;     // splits of the logits' k at most
+
+// Logits r, r + 16, ... of a token: the sums of the splits' shares, in order, requested together.
 template <int NQ>
 __device__ __forceinline__ void load_logits(float (&z)[NQ], const float* __restrict__ Z, int i, int r,
                                             int N, int E, int splits) {
+  constexpr int S = NQ > 4 ? 2 : LG_SPLITS;     // registers
 #pragma unroll
   for (int m = 0; m < NQ; ++m) z[m] = 0.f;
-  for (int s = 0; s < splits; ++s)
+  for (int s0 = 0; s0 < splits; s0 += S) {
+    float v[S][NQ];
 #pragma unroll
-    for (int m = 0; m < NQ; ++m)
-      if (r + 16 * m < E) z[m] += Z[((size_t)s * N + i) * E + r + 16 * m];
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int m = 0; m < NQ; ++m)
+        v[s][m] = Z[((size_t)min(s0 + s, splits - 1) * N + i) * E + min(r + 16 * m, E - 1)];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (s0 + s < splits)
+#pragma unroll
+        for (int m = 0; m < NQ; ++m) z[m] += v[s][m];
+  }
 }
 
 constexpr int LG_WAVES = 8;
-constexpr int LG_SPLITS = 8;     // splits of k at most
 
 // Z [splits, N, E]: shares of X Wg^T.  A workgroup takes 16 experts and the 64s of k of split
 // blockIdx.y, its waves every eighth; they meet in LDS in a fixed order.  The few rows of Wg are
@@ -394,7 +405,9 @@ __global__ __launch_bounds__(16 * TOK) void decode_choose_kernel(const float* __
 // ---- W1 and W3 -----------------------------------------------------------------------
 
 constexpr int W13_WAVES = 4;
-constexpr int W13_GRID = 512, W2_GRID = 512;    // workgroups at most: two a CU
+// Workgroups at most, two or four a CU (64 tokens: 512 of W2 51.5 us, 1024 45.5, 2048 50.5; of W1/W3
+// 87.6, 85.0, 84.7; where each of these chooses, 512 are best).
+constexpr int W13_GRID = 1024, W13_OWN_GRID = 512, W2_GRID = 1024;
 constexpr int INLINE_TOKENS = 16;       // every workgroup of W1/W3 chooses for itself up to so
 constexpr int INLINE_PAIRS = 256;       // many tokens, and pairs of token and expert
 
@@ -769,8 +782,9 @@ hipError_t run_decode(const DecodeCall& c, hipStream_t st) {
   const int most = c.N * c.k < c.E ? c.N * c.k : c.E;    // chosen experts at most
   const long tiles13 = (long)most * (c.h / 16) + c.hs / 16;
   const auto w13 = [&](auto nq) {
+    constexpr long most_wgs = decltype(nq)::value ? W13_OWN_GRID : W13_GRID;
     decode_w13_kernel<F, TT, decltype(nq)::value>
-        <<<dim3((unsigned)(tiles13 < W13_GRID ? tiles13 : W13_GRID)), 64 * W13_WAVES, 0, st>>>(
+        <<<dim3((unsigned)(tiles13 < most_wgs ? tiles13 : most_wgs)), 64 * W13_WAVES, 0, st>>>(
             X, c.w, c.Z, splits, c.inv_tau, c.E, c.experts, c.gates, c.plan, (T*)c.A, (T*)c.As, c.N,
             c.d, c.h, c.hs, c.k);
   };
