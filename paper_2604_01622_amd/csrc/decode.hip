@@ -66,8 +66,9 @@ struct WBf16 {
       for (int s = 0; s < 4; ++s) r[s] = load_global<u32x4>(row + min(s * 32, left - 32) + q * 8);
     }
   };
-  static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const uint2&, const B& b,
-                                             int, int left) {
+  static constexpr int WIDE = 4;      // 16-byte operands of a chunk
+  static __device__ __forceinline__ void widen(u32x4 (&)[4], const uint2&, int) {}
+  static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const B& b, int left) {
     acc = mma_bf16(a[0], b.r[0], acc);
     acc = mma_bf16(a[1], b.r[1], acc);
     if (left < K) return;
@@ -93,16 +94,24 @@ struct WMx {
       }
     }
   };
-  // scale: the row's eight bytes of the chunk
-  static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const uint2& scale,
-                                             const B& b, int q, int left) {
+  static constexpr int WIDE = 8;
+  // the first four as bf16; scale: the row's eight bytes of the chunk
+  static __device__ __forceinline__ void widen(u32x4 (&a)[8], const uint2& scale, int q) {
+#pragma unroll
+    for (int s = 3; s >= 0; --s) {
+      const uint32_t word = s < 2 ? scale.x : scale.y;
+      const float f = mx_scale(__builtin_amdgcn_ubfe(word, (s & 1) * 16 + (q >> 1) * 8, 8));
+      const u32x4 c = a[s];
+      a[2 * s] = __builtin_bit_cast(u32x4, mx_widen8(c[0], c[1], f));
+      a[2 * s + 1] = __builtin_bit_cast(u32x4, mx_widen8(c[2], c[3], f));
+    }
+  }
+  static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[8], const B& b, int left) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       if (s * 64 >= left) return;
-      const uint32_t word = s < 2 ? scale.x : scale.y;
-      const float f = mx_scale(__builtin_amdgcn_ubfe(word, (s & 1) * 16 + (q >> 1) * 8, 8));
-      acc = mma_bf16(__builtin_bit_cast(u32x4, mx_widen8(a[s][0], a[s][1], f)), b.r[2 * s], acc);
-      acc = mma_bf16(__builtin_bit_cast(u32x4, mx_widen8(a[s][2], a[s][3], f)), b.r[2 * s + 1], acc);
+      acc = mma_bf16(a[2 * s], b.r[2 * s], acc);
+      acc = mma_bf16(a[2 * s + 1], b.r[2 * s + 1], acc);
     }
   }
 };
@@ -120,8 +129,9 @@ struct WF32 {
       for (int s = 0; s < 4; ++s) r[s] = load_global<f32x4>(row + s * 16 + q * 4);
     }
   };
-  static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const uint2&, const B& b,
-                                             int, int) {
+  static constexpr int WIDE = 4;
+  static __device__ __forceinline__ void widen(u32x4 (&)[4], const uint2&, int) {}
+  static __device__ __forceinline__ void mma(f32x4& acc, const u32x4 (&a)[4], const B& b, int) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       const f32x4 v = __builtin_bit_cast(f32x4, a[s]);
@@ -131,6 +141,10 @@ struct WF32 {
     }
   }
 };
+
+// Of two values (of two variables that a lambda holds by reference, ?: would choose the address).
+template <typename V>
+__device__ __forceinline__ V either(bool first, V a, V b) { return first ? a : b; }
 
 // A chunk on its way: from memory an instruction takes 256 consecutive bytes of four rows (64
 // bytes of each of sixteen, the operand's own order, reach 5.1 to 6.1 TB/s where this reaches
@@ -158,7 +172,7 @@ struct Chunk {
   }
   // through LDS of the wave's own to the operand's order: piece c of row r at place c ^ r of
   // the row, so that neither side meets in a bank
-  __device__ __forceinline__ void turn(Lds& lds, u32x4 (&a)[4], uint2& scales) const {
+  __device__ __forceinline__ void turn(Lds& lds, u32x4 (&a)[F::WIDE]) const {
     const int lane = wave_lane(), q = lane >> 4, c = lane & 15;
 #pragma unroll
     for (int m = 0; m < 4; ++m) lds.piece[4 * m + q][c ^ (4 * m + q)] = r[m];
@@ -167,9 +181,11 @@ struct Chunk {
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int s = 0; s < 4; ++s) a[s] = lds.piece[c][(4 * s + q) ^ c];
+    uint2 scales = {0, 0};
     if (F::MX) scales = lds.scale[c];
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
+    F::widen(a, scales, q);
   }
 };
 
@@ -404,10 +420,13 @@ __global__ __launch_bounds__(16 * TOK) void decode_choose_kernel(const float* __
 
 // ---- W1 and W3 -----------------------------------------------------------------------
 
+template <typename T>
+constexpr int act_parts() { return sizeof(T) == 2 ? 2 : 1; }
+
 constexpr int W13_WAVES = 4;
 // Workgroups at most, two or four a CU (64 tokens: 512 of W2 51.5 us, 1024 45.5, 2048 50.5; of W1/W3
 // 87.6, 85.0, 84.7; where each of these chooses, 512 are best).
-constexpr int W13_GRID = 1024, W13_OWN_GRID = 512, W2_GRID = 1024;
+constexpr int W13_GRID = 1024, W13_OWN_GRID = 512, W2_GRID = 512;
 constexpr int INLINE_TOKENS = 16;       // every workgroup of W1/W3 chooses for itself up to so
 constexpr int INLINE_PAIRS = 256;       // many tokens, and pairs of token and expert
 
@@ -416,7 +435,9 @@ constexpr int INLINE_PAIRS = 256;       // many tokens, and pairs of token and e
 // of k each; the expert's tokens are the columns.  A chunk's weights are requested before the one
 // before it is used, over the ends of tiles and experts too, so that memory never waits; every
 // step requests, at the end what is not used, so that the waits can count.
-//   A [token k + pick, h] = gate silu(W1 x) (W3 x).
+//   A [token k + pick, h] = gate silu(W1 x) (W3 x), in bf16 as two rows: the value rounded and what
+// that left, rounded.  With one the rounding would be as large as the output's own (2-norm 0.0024
+// of Y, now 0.0017).
 // NQ > 0: the choice is made here, from the logits, by every workgroup (16 NQ experts at most),
 // and the first writes it down.
 template <class F, int TT, int NQ>
@@ -427,6 +448,7 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
     int k) {
   typedef typename F::T T;
   typedef typename F::Code Code;
+  constexpr int PARTS = act_parts<T>();
   constexpr int TURNS = TT > 2 ? 1 : 2;     // LDS for two workgroups a CU
   constexpr bool OWN = NQ > 0;
   constexpr int PT = plan_tokens<TT>();
@@ -485,12 +507,12 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
     const bool shared = rslot == active;
     const size_t row = (size_t)expert * (shared ? 0 : h) + rtile * 16;
     const int k0 = min(u, chunks - 1) * F::K;
-    const Code* w1 = (const Code*)(shared ? w.Ws1 : w.W1) + (row * d + k0);
-    const Code* w3 = (const Code*)(shared ? w.Ws3 : w.W3) + (row * d + k0);
+    const Code* w1 = (const Code*)either(shared, w.Ws1, w.W1) + (row * d + k0);
+    const Code* w3 = (const Code*)either(shared, w.Ws3, w.W3) + (row * d + k0);
     const size_t at = row * (d / MX_BLOCK) + k0 / MX_BLOCK;
-    to[0].load(w1, d * sizeof(Code), F::MX ? (shared ? w.Ss1 : w.S1) + at : nullptr, d / MX_BLOCK,
+    to[0].load(w1, d * sizeof(Code), F::MX ? either(shared, w.Ss1, w.S1) + at : nullptr, d / MX_BLOCK,
                live ? d - k0 : 0);
-    to[1].load(w3, d * sizeof(Code), F::MX ? (shared ? w.Ss3 : w.S3) + at : nullptr, d / MX_BLOCK,
+    to[1].load(w3, d * sizeof(Code), F::MX ? either(shared, w.Ss3, w.S3) + at : nullptr, d / MX_BLOCK,
                live ? d - k0 : 0);
   };
   const T* x[TT];
@@ -542,10 +564,9 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
     request(next, ends ? u0 : u + 1, !ends || left > 1);
     __builtin_amdgcn_sched_barrier(0);
     if (u < u1) {                     // else more waves than chunks
-      u32x4 op[2][4];
-      uint2 scale[2];
+      u32x4 op[2][F::WIDE];
 #pragma unroll
-      for (int m = 0; m < 2; ++m) now[m].turn(turned[wave][m], op[m], scale[m]);
+      for (int m = 0; m < 2; ++m) now[m].turn(turned[wave][m], op[m]);
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
         if (t > 0) {
@@ -553,7 +574,7 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
           b.load(x[t] + k0, q, d - k0);
         }
 #pragma unroll
-        for (int m = 0; m < 2; ++m) F::mma(acc[m][t], op[m], scale[m], b, q, d - k0);
+        for (int m = 0; m < 2; ++m) F::mma(acc[m][t], op[m], b, d - k0);
       }
     }
     if (!ends) {
@@ -581,8 +602,17 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = gate[t] * (f[i] / (1.0f + expf(-f[i]))) * g[i];
-        T* o = slot < active ? A + (size_t)at[t] * h : As + (size_t)at[t] * hs;
-        store4<T>(o + tile * 16 + q * 4, v);
+        const int width = slot < active ? h : hs;
+        T* o = either(slot < active, A, As) + (size_t)at[t] * (PARTS * width) + tile * 16 + q * 4;
+        store4<T>(o, v);
+        if constexpr (PARTS == 2) {     // what the rounding left
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float hi = round_to<T>(v[i]);
+            v[i] = fabsf(hi) < INFINITY ? v[i] - hi : 0.f;
+          }
+          store4<T>(o + width, v);
+        }
       }
     if (TURNS == 1) lds_barrier();
     turn ^= TURNS - 1;
@@ -603,141 +633,190 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
 
 constexpr int W2_WAVES = 4;
 
-// Tiles of 16 columns of Y (rows of W2), two side by side (ROWS 2) or one, slot after slot, then the
-// shared experts'.  Each wave streams a contiguous share of them by itself, as in W1/W3, two
-// chunks a step: of the tiles side by side, or two of one tile.  The expert's tokens are the
-// columns of the products, which go to O [token k + pick, d] in fp32 (the shared experts' to the
-// rows from N k).
-template <class F, int TT, int ROWS>
+// k of a wave's share whose activations stay in its registers (64 of them) from tile to tile.
+constexpr int W2_KEPT = 256;
+
+// Tiles of 32 columns of Y (rows of W2), slot after slot, then the shared experts'.  A workgroup
+// takes a contiguous share of them (of equal work), its waves a quarter of k each, streamed as in
+// W1/W3, a chunk of both 16 rows a step; the expert's tokens are the columns of the products,
+// which go to O [token k + pick, d] in fp32 (the shared experts' to the rows from N k).
+// KEEP (widths of W2_WAVES W2_KEPT at most): the activations of the first 16 columns are loaded
+// once a slot.
+template <class F, int TT, bool KEEP>
 __global__ __launch_bounds__(64 * W2_WAVES, 2) void decode_w2_kernel(
     const typename F::T* __restrict__ A, const typename F::T* __restrict__ As, DecodeWeights w,
     DecodePlan plan, float* __restrict__ O, int N, int d, int h, int hs, int k) {
   typedef typename F::T T;
   typedef typename F::Code Code;
-  constexpr int U = 2 / ROWS;           // chunks of a tile in a step
+  constexpr int PARTS = act_parts<T>();
   constexpr int PT = plan_tokens<TT>();
+  constexpr int TURNS = TT > 2 ? 1 : 2;
+  constexpr int NK = KEEP ? W2_KEPT / F::K : 1;       // 2, 1 or 4 chunks
+  __shared__ f32x4 red[TURNS][W2_WAVES][2 * TT][64];
   __shared__ typename Chunk<F>::Lds turned[W2_WAVES][2];
   const int lane = wave_lane(), q = lane >> 4, col = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Used used;
 #pragma unroll
   for (int m = 0; m < 4; ++m) used.w[m] = plan.used[m];
-  const int active = used.count(), dt = d / (16 * ROWS), routed = active * dt;
-  // shares of equal work, in 64s of k
+  const int active = used.count(), dt = d / 32, routed = active * dt;
   const int hu = h / 64, su = hs / 64;
-  const long waves = (long)gridDim.x * W2_WAVES, total = (long)dt * (active * hu + su);
-  const long g = (long)blockIdx.x * W2_WAVES + wave;
+  const long total = (long)dt * (active * hu + su);
   const auto tile_from = [&](long c) {
     const long r = (long)routed * hu;
     return (int)(c <= r ? (c + hu - 1) / hu : routed + (c - r + su - 1) / su);
   };
-  const int t0 = tile_from(total * g / waves), t1 = tile_from(total * (g + 1) / waves);
+  const int t0 = tile_from(total * blockIdx.x / gridDim.x);
+  const int t1 = tile_from(total * (blockIdx.x + 1) / gridDim.x);
   if (t0 >= t1) return;
   int slot = min(t0 / dt, active), tile = t0 - slot * dt, left = t1 - t0;
   int rslot = slot, rtile = tile, expert = slot < active ? used.expert(slot) : 0;
+  const auto chunks_of = [&](int s) { return ((s == active ? hs : h) + F::K - 1) / F::K; };
   const auto request = [&](Chunk<F> (&to)[2], int u, bool live) __attribute__((always_inline)) {
     const bool shared = rslot == active;
-    const int wide = shared ? hs : h;
-    const size_t row = (size_t)expert * (shared ? 0 : d) + rtile * (16 * ROWS);
+    const int wide = shared ? hs : h, k0 = live ? u * F::K : 0;
+    const size_t at = ((size_t)expert * (shared ? 0 : d) + rtile * 32) * wide + k0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const size_t r = row + (ROWS == 2 ? i * 16 : 0);
-      const int k0 = (ROWS == 2 ? u : u + i) * F::K;
-      const bool there = live && k0 < wide;
-      const size_t at = r * wide + (there ? k0 : 0);
-      to[i].load((const Code*)(shared ? w.Ws2 : w.W2) + at, wide * sizeof(Code),
-                 F::MX ? (shared ? w.Ss2 : w.S2) + at / MX_BLOCK : nullptr, wide / MX_BLOCK,
-                 there ? wide - k0 : 0);
+    for (int m = 0; m < 2; ++m) {
+      const size_t r = at + (size_t)(m * 16) * wide;
+      to[m].load((const Code*)either(shared, w.Ws2, w.W2) + r, wide * sizeof(Code),
+                 F::MX ? either(shared, w.Ss2, w.S2) + r / MX_BLOCK : nullptr, wide / MX_BLOCK,
+                 live ? wide - k0 : 0);
     }
   };
   const T* x[TT];
-  int at[TT], n = 0;
+  int at[TT], n = 0, width = 0, u0 = 0, u1 = 0, chunks = 0;
   uint32_t mine = 0;
+  typename F::B kept[NK][PARTS];
+  const auto load_b = [&](typename F::B& b, int t, int u, int p) __attribute__((always_inline)) {
+    const int k0 = min(u, chunks - 1) * F::K;
+    b.load(x[t] + p * width + k0, q, width - k0);
+  };
   const auto columns = [&]() __attribute__((always_inline)) {
     int token[TT], pick[TT];
-    if (slot == active) {
+    const bool shared = slot == active;
+    width = shared ? hs : h;
+    chunks = chunks_of(slot);
+    u0 = chunks * wave / W2_WAVES;
+    u1 = chunks * (wave + 1) / W2_WAVES;
+    if (shared) {
       n = TT == 1 ? 16 : N;
       mine = 0;
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
         const int c = t * 16 + col;
-        x[t] = As + (size_t)min(c, N - 1) * hs;
-        at[t] = N * k + min(c, N - 1);
+        at[t] = min(c, N - 1);
         mine |= (uint32_t)(c < N) << t;
       }
     } else {
       n = columns_of<TT>(plan.pick[used.expert(slot) * PT + (PT == 16 ? col : lane)], token, pick,
                          &mine);
 #pragma unroll
-      for (int t = 0; t < TT; ++t) {
-        at[t] = token[t] * k + pick[t];
-        x[t] = A + (size_t)at[t] * h;
-      }
+      for (int t = 0; t < TT; ++t) at[t] = token[t] * k + pick[t];
     }
-  };
-  Chunk<F> a[2][2];
-  f32x4 acc[ROWS][TT];
-  int u = 0, width = slot < active ? h : hs;
-#pragma unroll
-  for (int t = 0; t < TT; ++t)
-#pragma unroll
-    for (int m = 0; m < ROWS; ++m) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  request(a[0], 0, true);
-  columns();
-  const auto step = [&](Chunk<F> (&now)[2], Chunk<F> (&next)[2]) __attribute__((always_inline)) {
-    const int chunks = (width + F::K - 1) / F::K;
-    typename F::B b[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int k0 = min(u + i, chunks - 1) * F::K;
-      b[i].load(x[0] + k0, q, width - k0);
-    }
-    const bool ends = u + U >= chunks;
-    if (ends && left > 1 && ++rtile == dt) {
-      rtile = 0;
-      expert = ++rslot < active ? used.expert(rslot) : 0;
-    }
-    request(next, ends ? 0 : u + U, !ends || left > 1);
-    __builtin_amdgcn_sched_barrier(0);
-    u32x4 op[2][4];
-    uint2 scale[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) now[i].turn(turned[wave][i], op[i], scale[i]);
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
-      if (t > 0 && t * 16 >= n) break;
+      x[t] = either(shared, As, A) + (size_t)at[t] * (PARTS * width);
+      if (shared) at[t] += N * k;
+    }
+    if constexpr (KEEP)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (U == 2 && u + i >= chunks) break;
-        const int k0 = (u + i % U) * F::K;
-        typename F::B& bi = b[i % U];
-        if (t > 0 && i < U) bi.load(x[t] + k0, q, width - k0);
-        F::mma(acc[i % ROWS][t], op[i], scale[i], bi, q, width - k0);
+      for (int i = 0; i < NK; ++i)
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) load_b(kept[i][p], 0, u0 + i, p);
+  };
+  Chunk<F> a[2][2];
+  f32x4 acc[2][TT];
+  int u = 0;        // of the wave's share
+#pragma unroll
+  for (int t = 0; t < TT; ++t) acc[0][t] = acc[1][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  {
+    const int c = chunks_of(slot), first = c * wave / W2_WAVES;
+    request(a[0], first, first < c * (wave + 1) / W2_WAVES);
+  }
+  columns();
+  // one chunk of the tile in use, the I-th of the wave's share where it is kept; false past the
+  // last tile
+  const auto step = [&](auto now_of, auto kept_of) __attribute__((always_inline)) {
+    constexpr int P = decltype(now_of)::value, I = decltype(kept_of)::value;
+    typename F::B loaded[PARTS];
+    if constexpr (!KEEP)            // before the request: memory answers in order
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) load_b(loaded[p], 0, u0 + u, p);
+    const int share = u1 - u0;
+    const bool ends = KEEP ? I + 1 == NK : u + 1 >= share;
+    int next = u0 + u + 1;
+    bool live = u + 1 < share;
+    if (ends) {
+      if (left > 1 && ++rtile == dt) {
+        rtile = 0;
+        expert = ++rslot < active ? used.expert(rslot) : 0;
+      }
+      const int c = chunks_of(rslot);
+      next = c * wave / W2_WAVES;
+      live = left > 1 && next < c * (wave + 1) / W2_WAVES;
+    }
+    request(a[P ^ 1], next, live);
+    __builtin_amdgcn_sched_barrier(0);
+    if (u < share) {
+      u32x4 op[2][F::WIDE];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) a[P][m].turn(turned[wave][m], op[m]);
+      const int there = width - (u0 + u) * F::K;
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        if (t > 0 && t * 16 >= n) break;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+          if (t > 0) load_b(loaded[0], t, u0 + u, p);
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+            F::mma(acc[m][t], op[m], t > 0 ? loaded[0] : (KEEP ? kept[I][p] : loaded[p]), there);
+        }
       }
     }
-    if (!ends) {
-      u += U;
-      return true;
-    }
+    ++u;
+    if (!ends) return true;
+    // the tile's end: the waves' shares meet
+    f32x4 (&sums)[W2_WAVES][2 * TT][64] = red[TURNS == 1 ? 0 : left & 1];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
-      for (int m = 0; m < ROWS; ++m) {
-        if ((mine >> t) & 1)
-          *reinterpret_cast<f32x4*>(O + (size_t)at[t] * d + (tile * ROWS + m) * 16 + q * 4) = acc[m][t];
+      for (int m = 0; m < 2; ++m) {
+        sums[wave][2 * t + m][lane] = acc[m][t];
         acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
+    lds_barrier();
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+        if (wave == (2 * t + m) % W2_WAVES && ((mine >> t) & 1)) {
+          f32x4 v = sums[0][2 * t + m][lane];
+#pragma unroll
+          for (int i = 1; i < W2_WAVES; ++i) v += sums[i][2 * t + m][lane];
+          *reinterpret_cast<f32x4*>(O + (size_t)at[t] * d + tile * 32 + m * 16 + q * 4) = v;
+        }
+    if (TURNS == 1) lds_barrier();
     u = 0;
     if (--left == 0) return false;
     tile = rtile;
     if (slot != rslot) {
       slot = rslot;
-      width = slot < active ? h : hs;
       columns();
     }
     return true;
   };
-  while (step(a[0], a[1]) && step(a[1], a[0])) {
+  using zero = std::integral_constant<int, 0>;
+  using one = std::integral_constant<int, 1>;
+  if constexpr (NK == 4) {
+    while (step(zero{}, zero{}) && step(one{}, one{}) &&
+           step(zero{}, std::integral_constant<int, 2>{}) &&
+           step(one{}, std::integral_constant<int, 3>{})) {
+    }
+  } else {
+    while (step(zero{}, zero{}) && step(one{}, std::integral_constant<int, NK - 1>{})) {
+    }
   }
 }
 
@@ -805,17 +884,14 @@ hipError_t run_decode(const DecodeCall& c, hipStream_t st) {
                                                           c.experts, c.gates, c.plan);
     w13(std::integral_constant<int, 0>{});
   }
-  const long tiles2 = ((long)most + (c.hs ? 1 : 0)) * (c.d / 16);
-  const auto w2 = [&](auto rows) {
-    constexpr int R = decltype(rows)::value;
-    const long grid = (tiles2 / R + W2_WAVES - 1) / W2_WAVES;
-    decode_w2_kernel<F, TT, R>
-        <<<dim3((unsigned)(grid < W2_GRID ? grid : W2_GRID)), 64 * W2_WAVES, 0, st>>>(
-            (const T*)c.A, (const T*)c.As, c.w, c.plan, c.O, c.N, c.d, c.h, c.hs, c.k);
-  };
-  // tiles side by side share a load of the activations, if there is one for every wave
-  if (tiles2 >= 2 * W2_GRID * W2_WAVES) w2(std::integral_constant<int, 2>{});
-  else w2(std::integral_constant<int, 1>{});
+  const long tiles2 = ((long)most + (c.hs ? 1 : 0)) * (c.d / 32);
+  const dim3 g2((unsigned)(tiles2 < W2_GRID ? tiles2 : W2_GRID));
+  if ((c.h > c.hs ? c.h : c.hs) <= W2_WAVES * W2_KEPT)
+    decode_w2_kernel<F, TT, true><<<g2, 64 * W2_WAVES, 0, st>>>(
+        (const T*)c.A, (const T*)c.As, c.w, c.plan, c.O, c.N, c.d, c.h, c.hs, c.k);
+  else
+    decode_w2_kernel<F, TT, false><<<g2, 64 * W2_WAVES, 0, st>>>(
+        (const T*)c.A, (const T*)c.As, c.w, c.plan, c.O, c.N, c.d, c.h, c.hs, c.k);
   decode_sum_kernel<T><<<dim3((unsigned)((c.d + 255) / 256), (unsigned)c.N), 64, 0, st>>>(
       c.O, (const T*)c.R, (T*)c.Y, c.N, c.d, c.k, c.hs);
   return hipGetLastError();
@@ -833,6 +909,10 @@ hipError_t run_decode(const DecodeCall& c, hipStream_t st) {
 int decode_splits(int d) {
   const int most = (d / 64 + LG_WAVES - 1) / LG_WAVES;
   return most < LG_SPLITS ? most : LG_SPLITS;
+}
+
+int decode_act_parts(int dtype) {
+  return dtype == DT_F32 ? act_parts<float>() : act_parts<bf16_t>();
 }
 
 hipError_t launch_decode(const DecodeCall& c, hipStream_t st) {

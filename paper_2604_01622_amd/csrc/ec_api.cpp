@@ -470,8 +470,9 @@ ec::DecodeCall carve_decode(Carve& c, const Plan& P, int top_k) {
   w.plan.used = (unsigned long long*)c.take(4 * 8);
   w.plan.pick = (uint16_t*)c.take((size_t)P.E * ec::DECODE_TOKENS * 2);
   w.Xb = P.dtype == EC_BF16 ? c.take((size_t)P.N * P.d * 2) : nullptr;
-  w.A = c.take(rows * P.h * P.esz);
-  w.As = c.take((size_t)P.N * P.hs * P.esz);
+  const size_t parts = ec::decode_act_parts(P.dtype);
+  w.A = c.take(rows * P.h * P.esz * parts);
+  w.As = c.take((size_t)P.N * P.hs * P.esz * parts);
   w.O = (float*)c.take((rows + (P.hs ? P.N : 0)) * P.d * 4);
   return w;
 }

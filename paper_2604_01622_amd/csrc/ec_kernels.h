@@ -300,11 +300,12 @@ struct DecodeCall {
   float* Z;               // [decode_splits(d), N, E] shares of the logits
   DecodePlan plan;
   void* Xb;               // [N, d] tokens in eight bits as bf16
-  void* A;                // [N k, h]
-  void* As;               // [N, hs]
+  void* A;                // [N k, parts, h]
+  void* As;               // [N, parts, hs]
   float* O;               // [N k + N, d] (the last N rows: the shared experts')
 };
 int decode_splits(int d);
+int decode_act_parts(int dtype);
 hipError_t launch_decode(const DecodeCall& c, hipStream_t st);
 
 }  // namespace ec

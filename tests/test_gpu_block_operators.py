@@ -15,8 +15,8 @@ Tolerances, from the arithmetic (u = 2^-24, a rounding's half step in fp32; b = 
   * few tokens: X and Wg lie on grids coarse enough that a logit is the same number whatever
     the order of its sum, so choices are equal; gates: the exponent's argument is off by u of
     itself, exp by 2 u, the sum of k by k u, division u: (2 |arg| + k + 8) u.  Y, relative
-    2-norm: the stored tensors on the way, A and Y, b each: sqrt(2) b; fp32: products of at
-    most 2048 terms, (sqrt(2048) + a few) u each and three in a chain: 1e-5.
+    2-norm: fp32: products of at most 2048 terms, (sqrt(2048) + a few) u each and three in a
+    chain: 1e-5; bf16: Y's rounding b beside that and the activations' two parts, b^2: 1.01 b.
 """
 import numpy as np
 import pytest
@@ -335,7 +335,7 @@ def check_decode(got, X, Wg, W1, W3, W2, k, inv_tau=1.0, shared=None, residual=N
     arg = (np.take_along_axis(z, e, 1) - z.max(1, keepdims=True)) * inv_tau
     # a gate below fp32's normal numbers is off by its last bit
     assert np.all(np.abs(f64(gates) - g) <= (2 * np.abs(arg) + k + 8) * U * g + 2.0 ** -149)
-    assert rel_l2(Y, want) <= (1e-5 if Y.dtype == torch.float32 else 2 ** 0.5 * B)
+    assert rel_l2(Y, want) <= (1e-5 if Y.dtype == torch.float32 else 1.01 * B)
 
 
 FORMS = [(torch.bfloat16, False, False), (torch.bfloat16, True, False), (torch.bfloat16, True, True),
@@ -397,8 +397,8 @@ def test_decode_agrees_with_token_choice():
     want, rows = ec.tc_forward(X, Wg, W1, W3, W2, [0, 64], [64], 4, shared=sh)
     assert torch.equal(torch.bincount(experts.view(-1).long(), minlength=32).cumsum(0),
                        rows[1:].long())
-    # each is off the definition by its roundings: A and Y here, O and the shared Y there too
-    assert rel_l2(Y, f64(want)) <= (2 ** 0.5 + 2) * B
+    # each is off the definition by its roundings: Y here, A, O and the shared Y there too
+    assert rel_l2(Y, f64(want)) <= (1.01 + 2) * B
 
 
 def test_decode_reads_the_chosen_experts_alone():
@@ -609,4 +609,4 @@ def test_serving_step_of_a_block(mx):
     for i in range(33):
         for j, s in zip(e[i], g[i]):
             want[i] += s * ref.swiglu_ffn_ref(value(y)[i:i + 1], *(t[j] for t in W))[0]
-    assert rel_l2(Y, want) <= 2 ** 0.5 * B
+    assert rel_l2(Y, want) <= 1.01 * B
