@@ -10,7 +10,6 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
-import math
 import os
 from typing import NamedTuple, Optional, Sequence
 
@@ -732,26 +731,42 @@ def _mx_operand(name, t, shape, device=None):
              (*t.codes.shape[:-1], t.codes.shape[-1] // 32), t.codes.device)
 
 
+_TYPE_CODES = {torch.bfloat16: EC_BF16, torch.float32: EC_F32}
+
+
 def _rows(name, t):
-    """Rows and width of a tensor [..., d] of a storage type; refuses others."""
+    """Type code and width of a tensor [..., d] of a storage type; refuses others."""
     if not isinstance(t, torch.Tensor) or t.dim() < 1:
         raise ECError(2, f"{name} must be a tensor of at least one dimension")
-    _dtype_code(t.dtype)
-    _operand(name, t, t.dtype)
-    return math.prod(t.shape[:-1]), t.shape[-1]
+    code = _TYPE_CODES.get(t.dtype)
+    if code is None:
+        _dtype_code(t.dtype)
+    if not (t.is_cuda and t.is_contiguous()):
+        _operand(name, t, t.dtype)
+    return code, t.shape[-1]
+
+
+def _beside(name, t, X, shape):
+    """Refuses t unless it is laid out like X, in the shape given: _operand in one look."""
+    if not (isinstance(t, torch.Tensor) and t.dtype == X.dtype and t.shape == shape
+            and t.device == X.device and t.is_contiguous()):
+        _operand(name, t, X.dtype, shape, X.device)
 
 
 def mx_quantize(X) -> Mx:
     """X [..., c] (bf16 or fp32, c a multiple of 32) in eight bits: a scale is the smallest
     power of two that brings its 32 elements to 448 or below; codes rounded to nearest even.
     The experts' weights of tc_decode may be held so."""
-    rows, cols = _rows("X", X)
+    code, cols = _rows("X", X)
     if cols % 32:
         raise ECError(2, f"the last dimension must be a multiple of 32 (got {cols})")
-    with _on(X.device):
-        out = _mx_empty(X.shape, X.device)
-        _check(lib().ec_mx_quantize(_dtype_code(X.dtype), rows, cols, _addr(X), _addr(out.codes),
-                                    _addr(out.scales), _raw_stream(X.device)))
+    dev = X.device
+    with _on(dev):
+        out = _mx_empty(X.shape, dev)
+        status = lib().ec_mx_quantize(code, X.numel() // cols if cols else 0, cols, _addr(X),
+                                      _addr(out.codes), _addr(out.scales), _raw_stream(dev))
+    if status:
+        _check(status)
     return out
 
 
@@ -759,44 +774,57 @@ def rms_norm(X, weight, eps: float = 1e-6, residual=None, mx: bool = False, sum_
     """Root-mean-square norm of the rows of X [..., d]: Y = H (mean(H^2) + eps)^-1/2 weight with
     H = X + residual, rounded.  Returns Y (in eight bits, Mx, with mx), and with a residual
     (Y, H).  sum_out receives H; it may be X or the residual."""
-    rows, d = _rows("X", X)
+    code, d = _rows("X", X)
     dev = X.device
-    _operand("weight", weight, X.dtype, (d,), dev)
+    _beside("weight", weight, X, (d,))
     if residual is not None:
-        _operand("residual", residual, X.dtype, X.shape, dev)
+        _beside("residual", residual, X, X.shape)
     if sum_out is not None:
         if residual is None:
             raise ECError(1, "sum_out needs a residual")
-        _operand("sum_out", sum_out, X.dtype, X.shape, dev)
+        _beside("sum_out", sum_out, X, X.shape)
     if mx and d % 32:
         raise ECError(2, f"eight bits need rows of a multiple of 32 (got {d})")
     with _on(dev):
-        Y = _mx_empty(X.shape, dev) if mx else torch.empty_like(X)
         H = torch.empty_like(X) if residual is not None and sum_out is None else sum_out
-        _check(lib().ec_rms_norm(_dtype_code(X.dtype), rows, d, float(eps), _addr(X),
-                                 _addr(residual), _addr(weight), _addr(H),
-                                 None if mx else _addr(Y), _addr(Y.codes) if mx else None,
-                                 _addr(Y.scales) if mx else None, _raw_stream(dev)))
+        if mx:
+            Y = _mx_empty(X.shape, dev)
+            out = (None, _addr(Y.codes), _addr(Y.scales))
+        else:
+            Y = torch.empty_like(X)
+            out = (_addr(Y), None, None)
+        status = lib().ec_rms_norm(code, X.numel() // d if d else 0, d, eps, _addr(X),
+                                   _addr(residual), _addr(weight), _addr(H), *out,
+                                   _raw_stream(dev))
+    if status:
+        _check(status)
     return Y if residual is None else (Y, H)
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_workspace(code, rows, d):
+    return _tc_size(lib().ec_rms_norm_workspace_size(code, rows, d))
 
 
 def rms_norm_backward(dY, H, weight, eps: float = 1e-6, dH=None):
     """Backward of rms_norm from H (X without a residual): gradients of sum(Y * dY) +
     sum(H * dH).  Returns dX [..., d], which is the residual's gradient too, and the weight's
     [d] in fp32."""
-    rows, d = _rows("H", H)
-    dev, code = H.device, _dtype_code(H.dtype)
-    _operand("weight", weight, H.dtype, (d,), dev)
-    _operand("dY", dY, H.dtype, H.shape, dev)
+    code, d = _rows("H", H)
+    dev, rows = H.device, H.numel() // d if d else 0
+    _beside("weight", weight, H, (d,))
+    _beside("dY", dY, H, H.shape)
     if dH is not None:
-        _operand("dH", dH, H.dtype, H.shape, dev)
+        _beside("dH", dH, H, H.shape)
     with _on(dev):
         dX = torch.empty_like(H)
         dw = torch.empty((d,), dtype=torch.float32, device=dev)
-        ws = _empty(_tc_size(lib().ec_rms_norm_workspace_size(code, rows, d)), dev)
-        _check(lib().ec_rms_norm_backward(code, rows, d, float(eps), _addr(H), _addr(weight),
-                                          _addr(dY), _addr(dH), _addr(dX), dw.data_ptr(),
-                                          ws.data_ptr(), ws.numel(), _raw_stream(dev)))
+        ws = _empty(_norm_workspace(code, rows, d), dev)
+        status = lib().ec_rms_norm_backward(code, rows, d, eps, _addr(H), _addr(weight), _addr(dY),
+                                            _addr(dH), _addr(dX), dw.data_ptr(), ws.data_ptr(),
+                                            ws.numel(), _raw_stream(dev))
+    if status:
+        _check(status)
     return dX, dw
 
 
@@ -811,6 +839,13 @@ def _scales(t):
     return _addr(t.scales) if isinstance(t, Mx) else None
 
 
+@functools.lru_cache(maxsize=256)
+def _decode_plan(N, d, E, h, hs, top_k, inv_temperature, dtype):
+    """Problem description and workspace bytes of a few tokens, by the sizes alone."""
+    P = Problem(N, d, E, h, [0, N], [0], inv_temperature, dtype, hs)
+    return P, _tc_size(lib().ec_tc_decode_workspace_size(P.ref, top_k))
+
+
 class TcDecoder:
     """The token-choice layer for a few tokens (serving), its weights held: every token takes
     its top_k experts by logit and none is dropped.  Weights as for tc_forward, W1, W3, W2 and
@@ -820,14 +855,13 @@ class TcDecoder:
 
     def __init__(self, Wg, W1, W3, W2, top_k: int, inv_temperature=1.0, shared=None,
                  max_tokens: int = DECODE_MAX_TOKENS):
-        mx = isinstance(W1, Mx)
+        mx, w1 = isinstance(W1, Mx), _codes(W1)
         if not isinstance(Wg, torch.Tensor) or Wg.dim() != 2:
             raise ECError(2, "Wg must have 2 dimensions")
-        if not isinstance(_codes(W1), torch.Tensor) or _codes(W1).dim() != 3:
+        if not isinstance(w1, torch.Tensor) or w1.dim() != 3:
             raise ECError(2, "W1 must have 3 dimensions")
-        _dtype_code(Wg.dtype)
-        dt, dev, (E, d), h = Wg.dtype, Wg.device, Wg.shape, _codes(W1).shape[1]
-        _operand("Wg", Wg, dt)
+        _rows("Wg", Wg)
+        dt, dev, (E, d), h, hs = Wg.dtype, Wg.device, Wg.shape, w1.shape[1], 0
         if mx and dt != torch.bfloat16:
             raise ECError(4, "weights in eight bits need a bf16 Wg")
         operands = [("W1", W1, (E, h, d)), ("W3", W3, (E, h, d)), ("W2", W2, (E, d, h))]
@@ -841,19 +875,17 @@ class TcDecoder:
             if mx:
                 _mx_operand(name, t, shape, dev)
             else:
-                _operand(name, t, dt, shape, dev)
+                _beside(name, t, Wg, shape)
         if not 0 <= int(max_tokens) <= DECODE_MAX_TOKENS:
             raise ECError(2, f"max_tokens must be in [0, {DECODE_MAX_TOKENS}]")
         self.Wg, self.W1, self.W3, self.W2, self.shared = Wg, W1, W3, W2, shared
         self.top_k, self.max_tokens = int(top_k), int(max_tokens)
-        self._device, self._d, self._dtype = dev, d, dt
-        P = Problem(self.max_tokens, d, E, h, [0, self.max_tokens], [0], inv_temperature, dt,
-                    0 if shared is None else _codes(shared[0]).shape[0])
-        n = _tc_size(lib().ec_tc_decode_workspace_size(P.ref, self.top_k))
-        self.P = P
+        self._device, self._d = dev, d
+        self._sizes = (d, E, h, hs, self.top_k, float(inv_temperature), dt)
+        n = _decode_plan(self.max_tokens, *self._sizes)[1]
         six = (W1, W3, W2, *(shared or (None,) * 3))
         self._weights = [_addr(_codes(t)) for t in (Wg, *six)]
-        self._scales = _MxScales(None, *[_scales(t) for t in six])
+        self._scales = [_scales(t) for t in six]
         with _on(dev):
             self.ws = _empty(n, dev)
             self.Y = torch.empty((self.max_tokens, d), dtype=dt, device=dev)
@@ -867,32 +899,35 @@ class TcDecoder:
         [N, top_k] int32 by falling logit (equal logits: the lower index) and their gates
         [N, top_k] fp32; rows of the decoder's buffers (Y: of out, if given, which may be X or
         the residual)."""
-        dev, d = self._device, self._d
-        x = _codes(X)
+        dev, d, x = self._device, self._d, _codes(X)
         if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.shape[1] != d:
             raise ECError(2, f"X must be [N, {d}]")
         N = x.shape[0]
         if N > self.max_tokens:
             raise ECError(2, f"X has {N} tokens, the decoder takes {self.max_tokens}")
         if isinstance(X, Mx):
-            if self._dtype != torch.bfloat16:
+            if self.Wg.dtype != torch.bfloat16:
                 raise ECError(4, "tokens in eight bits need a bf16 Wg")
             _mx_operand("X", X, (N, d), dev)
         else:
-            _operand("X", x, self._dtype, (N, d), dev)
+            _beside("X", x, self.Wg, (N, d))
         if residual is not None:
-            _operand("residual", residual, self._dtype, (N, d), dev)
+            _beside("residual", residual, self.Wg, (N, d))
         if out is not None:
-            _operand("out", out, self._dtype, (N, d), dev)
-        Y = self.Y[:N] if out is None else out
-        experts, gates = self.experts[:N], self.gates[:N]
-        self.P.off[1] = self.P.c.n_tokens = N
-        self._scales.X = _scales(X)
+            _beside("out", out, self.Wg, (N, d))
+        whole = N == self.max_tokens
+        Y = out if out is not None else self.Y if whole else self.Y[:N]
+        experts = self.experts if whole else self.experts[:N]
+        gates = self.gates if whole else self.gates[:N]
+        P = _decode_plan(N, *self._sizes)[0]
+        scales = _MxScales(_scales(X), *self._scales)
         with _on(dev):
-            _check(lib().ec_tc_decode(self.P.ref, self.top_k, ctypes.byref(self._scales), _addr(x),
-                                      *self._weights, _addr(residual), _addr(Y), _addr(experts),
-                                      _addr(gates), self.ws.data_ptr(), self.ws.numel(),
-                                      _raw_stream(dev)))
+            status = lib().ec_tc_decode(P.ref, self.top_k, ctypes.byref(scales), _addr(x),
+                                        *self._weights, _addr(residual), _addr(Y), _addr(experts),
+                                        _addr(gates), self.ws.data_ptr(), self.ws.numel(),
+                                        _raw_stream(dev))
+        if status:
+            _check(status)
         return Y, experts, gates
 
 
