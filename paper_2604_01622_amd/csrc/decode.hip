@@ -5,8 +5,12 @@
 //
 // The weights of the chosen experts bound it: each is read once, for at most 64 tokens, far
 // below the operations that the matrix cores need to be the limit.  So weight rows are the
-// MFMAs' A operand, streamed from memory straight into registers, and the tokens that chose
-// the expert are its 16 columns.  Launches: logits, (many tokens) choice, W1/W3, W2, sum.
+// MFMAs' A operand, streamed from memory into registers, and the tokens that chose the expert
+// are its 16 columns.  Launches: logits, (past 16 tokens) choice, W1/W3, W2, sum.
+//
+// Measured, d 2048, 64 experts of 1024, top 8, bf16: 64 tokens 5.0 + 6.1 + 86 + 48 + 4.8 us for
+// 806 MB (W1/W3 6.2 TB/s, W2 5.6), one token 3.0 + 16.5 + 8.8 + 3.9 for 101 MB.  In eight bits 16
+// tokens 4.7 + 49 + 26 + 4.7 for 363 MB.  A kernel's first 2 to 4 us are its launch.
 //
 // Weights come in the storage type or in eight bits with scales (mx.h), which turn into bf16
 // exactly (four leading bits) on their way to the matrix cores; the tokens and activations
@@ -424,11 +428,14 @@ template <typename T>
 constexpr int act_parts() { return sizeof(T) == 2 ? 2 : 1; }
 
 constexpr int W13_WAVES = 4;
-// Workgroups at most, two or four a CU (64 tokens: 512 of W2 51.5 us, 1024 45.5, 2048 50.5; of W1/W3
-// 87.6, 85.0, 84.7; where each of these chooses, 512 are best).
+// Workgroups at most, two or four a CU (64 tokens: W1/W3 512 87.6 us, 1024 85.0, 2048 84.7, and 512
+// are best where each of them chooses; W2 512 47.9, 1024 48.9, 2048 53.6).
 constexpr int W13_GRID = 1024, W13_OWN_GRID = 512, W2_GRID = 512;
-constexpr int INLINE_TOKENS = 16;       // every workgroup of W1/W3 chooses for itself up to so
-constexpr int INLINE_PAIRS = 256;       // many tokens, and pairs of token and expert
+// Up to so many tokens, and pairs of token and expert, every workgroup of W1/W3 chooses for
+// itself (3.3 us at its start; the choice in a launch of its own takes 6.1).
+constexpr int INLINE_TOKENS = 16;
+constexpr int INLINE_PAIRS = 256;
+static_assert(INLINE_TOKENS == plan_tokens<1>(), "one tile of columns");
 
 // Tiles of 16 hidden units: those of the chosen experts, slot after slot, then the shared
 // experts' (for every token).  A workgroup takes a contiguous share of them, its waves a quarter
@@ -641,7 +648,7 @@ constexpr int W2_KEPT = 256;
 // W1/W3, a chunk of both 16 rows a step; the expert's tokens are the columns of the products,
 // which go to O [token k + pick, d] in fp32 (the shared experts' to the rows from N k).
 // KEEP (widths of W2_WAVES W2_KEPT at most): the activations of the first 16 columns are loaded
-// once a slot.
+// once a slot (64 tokens 58.0 -> 48.9 us, 16 in eight bits 32.6 -> 27.9).
 template <class F, int TT, bool KEEP>
 __global__ __launch_bounds__(64 * W2_WAVES, 2) void decode_w2_kernel(
     const typename F::T* __restrict__ A, const typename F::T* __restrict__ As, DecodeWeights w,

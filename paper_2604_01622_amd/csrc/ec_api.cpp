@@ -447,6 +447,8 @@ int enqueue_tc_route(const ec_problem* p, const Plan& P, int top_k, const void* 
 
 // ---- a few tokens ---------------------------------------------------------------
 
+static_assert(EC_DECODE_MAX_TOKENS == ec::DECODE_TOKENS, "");
+
 int decode_validate(const ec_problem* p, int top_k, Plan* P) {
   long rmax;
   int rmax_e;

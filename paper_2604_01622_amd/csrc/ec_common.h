@@ -91,20 +91,7 @@ template <> struct Elem<bf16_t> {
   static __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = (bf16_t)f32_to_bf16(v); }
 };
 
-// VEC consecutive elements as fp32, 16 bytes at most: p is aligned to their size.
-template <typename T, int VEC>
-__device__ __forceinline__ void load_vec(const T* p, float* v) {
-  static_assert(VEC == 1 || VEC * sizeof(T) == 16, "");
-  if constexpr (VEC == 1) {
-    v[0] = Elem<T>::load1(p);
-  } else if constexpr (sizeof(T) == 2) {
-    Elem<T>::load8(p, v);
-  } else {
-    const float4 a = *reinterpret_cast<const float4*>(p);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  }
-}
-
+// VEC consecutive elements from fp32: p is aligned to their size.
 template <typename T, int VEC>
 __device__ __forceinline__ void store_vec(T* p, const float* v) {
   if constexpr (VEC == 1)
@@ -149,7 +136,8 @@ __device__ __forceinline__ void load4(const T* p, float* v) {
     v[0] = bf16_to_f32(a.x & 0xffffu); v[1] = bf16_to_f32(a.x >> 16);
     v[2] = bf16_to_f32(a.y & 0xffffu); v[3] = bf16_to_f32(a.y >> 16);
   } else {
-    load_vec<T, 4>(p, v);
+    const float4 a = *reinterpret_cast<const float4*>(p);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
   }
 }
 

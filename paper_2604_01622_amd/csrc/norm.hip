@@ -6,8 +6,12 @@
 //
 // Memory bounds both: every row moves once and is held in registers between its sum and its
 // use.  A row belongs to TPR lanes, each of which takes V pieces of VEC elements (16 bytes, or
-// one element where the row's length leaves its rows unaligned).  Up to eight elements a lane the
-// next row's are requested before this one's are used.
+// one element where the row's length leaves its rows unaligned).  Forward, a group of lanes
+// takes one row and leaves: many short workgroups keep more on its way than loops over rows
+// with the next one requested ahead (16384 x 2048 bf16 with a residual: 44.2 us, 6.1 TB/s,
+// against 51.2; eight bits out 41, 5.7 TB/s).  Backward, where a workgroup keeps its share of dw,
+// the loop it needs requests ahead (45 us and 4.7 for the sum of the shares, 5.4 TB/s; a row in
+// one wave, without: 64 and 11).  One row takes 1.9 us, the launch.
 #include "mx.h"
 #include "ec_kernels.h"
 
@@ -66,8 +70,9 @@ __device__ __forceinline__ void load_row(Piece<T, VEC> (&to)[V], const T* p, lon
 template <int VEC, int V>
 constexpr int row_buffers() { return VEC * V > 8 ? 1 : 2; }
 
+// Of a forward workgroup: four rows of a wave each, or one row, whose waves meet in barriers.
 template <int TPR>
-constexpr int norm_threads() { return TPR < 256 ? 256 : TPR; }
+constexpr int norm_threads() { return TPR == 64 ? 256 : TPR; }
 
 // One row a group of TPR lanes and step; MX: eight bits out.
 template <typename T, int VEC, int V, int TPR, bool MX, bool RES>
@@ -80,7 +85,7 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
   const float inv_d = 1.0f / (float)d;
   const long stride = (long)gridDim.x * RB;
   long row = (long)blockIdx.x * RB + threadIdx.x / TPR;
-  if (row >= rows) return;          // a whole wave; with RB = 1 the whole workgroup
+  if (row >= rows) return;          // a wave without barriers, or the whole workgroup
   int turn = 0;
   do {
     Piece<T, VEC> x[V], r[RES ? V : 1], pw[V];
@@ -262,7 +267,7 @@ __global__ __launch_bounds__(256) void rms_norm_dw_kernel(const float* __restric
 }
 
 constexpr int NORM_GRID = 1 << 20;   // workgroups at most
-constexpr int NB_GRID = 256;         // of a backward launch: one a CU
+constexpr int NB_GRID = 256;         // of a backward launch: one a CU (512: 45.7 us instead of 44.2)
 
 // Calls body(VEC, V, TPR) as types with the smallest group of lanes that holds a row in one piece
 // of 16 bytes each, or four of one element (past 1024 lanes more).
