@@ -456,6 +456,7 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
   typedef typename F::T T;
   typedef typename F::Code Code;
   constexpr int PARTS = act_parts<T>();
+  constexpr int AHEAD = F::MX && TT > 2 ? 2 : TT;   // tiles of columns requested ahead: registers
   constexpr int TURNS = TT > 2 ? 1 : 2;     // LDS for two workgroups a CU
   constexpr bool OWN = NQ > 0;
   constexpr int PT = plan_tokens<TT>();
@@ -561,8 +562,10 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
   // one chunk of the tile in use; false past the last tile
   const auto step = [&](Chunk<F> (&now)[2], Chunk<F> (&next)[2]) __attribute__((always_inline)) {
     const int k0 = min(u, chunks - 1) * F::K;
-    typename F::B b;
-    b.load(x[0] + k0, q, d - k0);     // before the request: memory answers in order
+    typename F::B b[AHEAD];
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t)     // before the request: memory answers in order
+      if (t == 0 || t * 16 < n) b[t].load(x[t] + k0, q, d - k0);
     const bool ends = u + 1 >= u1;
     if (ends && left > 1 && ++rtile == (rslot < active ? ht : hs / 16)) {
       rtile = 0;
@@ -576,12 +579,11 @@ __global__ __launch_bounds__(64 * W13_WAVES, 2) void decode_w13_kernel(
       for (int m = 0; m < 2; ++m) now[m].turn(turned[wave][m], op[m]);
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
-        if (t > 0) {
-          if (t * 16 >= n) break;
-          b.load(x[t] + k0, q, d - k0);
-        }
+        if (t > 0 && t * 16 >= n) break;
+        typename F::B& bt = b[t % AHEAD];
+        if (t >= AHEAD) bt.load(x[t] + k0, q, d - k0);
 #pragma unroll
-        for (int m = 0; m < 2; ++m) F::mma(acc[m][t], op[m], b, d - k0);
+        for (int m = 0; m < 2; ++m) F::mma(acc[m][t], op[m], bt, d - k0);
       }
     }
     if (!ends) {

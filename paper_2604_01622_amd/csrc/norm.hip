@@ -5,8 +5,10 @@
 // Sums in fp32; y is rounded once, to the storage type or to eight bits (mx.h).
 //
 // Memory bounds both: every row moves once and is held in registers between its sum and its
-// use.  A row belongs to TPR lanes, each of which takes V pieces of VEC elements (16 bytes, or
-// one element where the row's length leaves its rows unaligned).  Forward, a group of lanes
+// use.  A row belongs to TPR lanes, each of which takes V pieces of 16 bytes.  Where d leaves rows
+// unaligned (ODD) the pieces are too, and a row's last one ends with the row: what it shares
+// with the piece before it is that one's (5000 x 4097 bf16: 39 us, backward 55; an element a lane 116
+// and 316).  Forward, a group of lanes
 // takes one row and leaves: many short workgroups keep more on its way than loops over rows
 // with the next one requested ahead (16384 x 2048 bf16 with a residual: 44.2 us, 6.1 TB/s,
 // against 51.2; eight bits out 41, 5.7 TB/s).  Backward, where a workgroup keeps its share of dw,
@@ -53,16 +55,37 @@ __device__ __forceinline__ void row_sums(float (&s)[NS], float* red, int turn) {
   }
 }
 
-// A lane's pieces of a row of p (column c of piece 0, TPR VEC apart; past d none).  live false:
-// one place for all lanes instead, not used: a request in every turn lets the waits count.
-template <typename T, int VEC, int V, int TPR>
-__device__ __forceinline__ void load_row(Piece<T, VEC> (&to)[V], const T* p, long row, int c, int d,
-                                         bool live) {
+// Where a lane's piece of a row stands, and how many of its first elements are not its own.
+struct Place {
+  int at, skip;
+};
+template <int VEC, bool ODD>
+__device__ __forceinline__ Place place(int c, int d) {
+  if (c >= d) return {0, VEC};
+  if (!ODD) return {c, 0};
+  const int at = min(c, d - VEC);
+  return {at, c - at};
+}
+
+// A lane's pieces of a row of p.  live false: one place for all lanes instead, not used: a
+// request in every turn lets the waits count.
+template <typename T, int VEC, int V, bool ODD>
+__device__ __forceinline__ void load_row(Piece<T, VEC, ODD> (&to)[V], const T* p, long row,
+                                         const Place (&my)[V], int d, bool live) {
   const T* r = p + (live ? row * d : 0);
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int at = c + v * TPR * VEC;
-    to[v].load(r + (live && at < d ? at : 0));
+  for (int v = 0; v < V; ++v) to[v].load(r + (live ? my[v].at : 0));
+}
+
+// A piece's own elements into row r.
+template <typename T, int VEC, bool ODD>
+__device__ __forceinline__ void store_own(T* r, const Place& my, const float* v) {
+  if (my.skip == 0) {
+    store_vec<T, VEC, ODD>(r + my.at, v);
+  } else if (ODD) {
+#pragma unroll
+    for (int e = 1; e < VEC; ++e)
+      if (e >= my.skip) Elem<T>::store1(r + my.at + e, v[e]);
   }
 }
 
@@ -75,50 +98,53 @@ template <int TPR>
 constexpr int norm_threads() { return TPR == 64 ? 256 : TPR; }
 
 // One row a group of TPR lanes and step; MX: eight bits out.
-template <typename T, int VEC, int V, int TPR, bool MX, bool RES>
+template <typename T, int VEC, int V, int TPR, bool ODD, bool MX, bool RES>
 __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
     const T* X, const T* R, const T* __restrict__ w, T* H, T* __restrict__ Y,
     uint8_t* __restrict__ Q, uint8_t* __restrict__ scale, long rows, int d, float eps) {
   constexpr int RB = norm_threads<TPR>() / TPR;
   __shared__ float red[2 * norm_threads<TPR>() / 64];
-  const int c0 = threadIdx.x % TPR * VEC;
+  Place my[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    my[v] = place<VEC, ODD>((v * TPR + (int)threadIdx.x % TPR) * VEC, d);
   const float inv_d = 1.0f / (float)d;
   const long stride = (long)gridDim.x * RB;
   long row = (long)blockIdx.x * RB + threadIdx.x / TPR;
   if (row >= rows) return;          // a wave without barriers, or the whole workgroup
   int turn = 0;
   do {
-    Piece<T, VEC> x[V], r[RES ? V : 1], pw[V];
-    load_row<T, VEC, V, TPR>(x, X, row, c0, d, true);
-    if constexpr (RES) load_row<T, VEC, V, TPR>(r, R, row, c0, d, true);
-    load_row<T, VEC, V, TPR>(pw, w, 0, c0, d, true);
+    Piece<T, VEC, ODD> x[V], r[RES ? V : 1], pw[V];
+    load_row<T, VEC, V>(x, X, row, my, d, true);
+    if constexpr (RES) load_row<T, VEC, V>(r, R, row, my, d, true);
+    load_row<T, VEC, V>(pw, w, 0, my, d, true);
+    __builtin_amdgcn_sched_barrier(0);      // all on their way before the first is used
     const long at = row * d;
     float h[V][VEC], s[1] = {0.f};
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = c0 + v * TPR * VEC;
       x[v].get(h[v]);
       if constexpr (RES) {
         float q[VEC];
         r[v].get(q);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) h[v][e] = round_to<T>(h[v][e] + q[e]);
-        if (c < d) store_vec<T, VEC>(H + at + c, h[v]);
+        store_own<T, VEC, ODD>(H + at, my[v], h[v]);
       }
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s[0] = c < d ? fmaf(h[v][e], h[v][e], s[0]) : s[0];
+      for (int e = 0; e < VEC; ++e) s[0] = e >= my[v].skip ? fmaf(h[v][e], h[v][e], s[0]) : s[0];
     }
     row_sums<TPR, 1>(s, red, turn);
     const float rs = 1.0f / sqrtf(fmaf(s[0], inv_d, eps));
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = c0 + v * TPR * VEC;
-      if (c >= d) break;
+      if (my[v].skip == VEC) break;
       float y[VEC], q[VEC];
       pw[v].get(q);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) y[e] = h[v][e] * rs * q[e];
       if constexpr (MX) {   // d is a multiple of 32: a block's lanes are all here
+        const int c = my[v].at;
         uint32_t top = 0;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) top = max(top, magnitude(y[e]));
@@ -126,7 +152,7 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
         mx_store<VEC>(Q + at + c, y, mx_inverse(byte));
         if (c % MX_BLOCK == 0) scale[(at + c) / MX_BLOCK] = (uint8_t)byte;
       } else {
-        store_vec<T, VEC>(Y + at + c, y);
+        store_own<T, VEC, ODD>(Y + at, my[v], y);
       }
     }
     row += stride;
@@ -138,29 +164,32 @@ constexpr int NB_THREADS = 1024;     // of a backward workgroup: 1024 / TPR rows
 
 // A workgroup takes every gridDim.x-th set of rows and keeps its share of dw in registers;
 // part [gridDim.x, d] (dw itself where one workgroup takes all rows).
-template <typename T, int VEC, int V, int TPR, bool DH>
+template <typename T, int VEC, int V, int TPR, bool ODD, bool DH>
 __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
     const T* H, const T* __restrict__ w, const T* dY, const T* dH, T* dX,
     float* __restrict__ part, long rows, int d, float eps) {
   constexpr int RB = NB_THREADS / TPR;
   __shared__ float red[4 * NB_THREADS / 64];
-  const int c0 = threadIdx.x % TPR * VEC;
+  Place my[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    my[v] = place<VEC, ODD>((v * TPR + (int)threadIdx.x % TPR) * VEC, d);
   const float inv_d = 1.0f / (float)d;
   const long stride = (long)gridDim.x * RB;
   long first = (long)blockIdx.x * RB;               // of the workgroup's rows
   const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
   float dw[V][VEC];
   constexpr int BUF = row_buffers<VEC, V>();
-  Piece<T, VEC> ph[BUF][V], pg[BUF][V], pd[BUF][DH ? V : 1], pw[V];
+  Piece<T, VEC, ODD> ph[BUF][V], pg[BUF][V], pd[BUF][DH ? V : 1], pw[V];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) dw[v][e] = 0.f;
   const auto request = [&](int i, long row) __attribute__((always_inline)) {
     const bool live = row < rows;
-    load_row<T, VEC, V, TPR>(ph[i], H, row, c0, d, live);
-    load_row<T, VEC, V, TPR>(pg[i], dY, row, c0, d, live);
-    if constexpr (DH) load_row<T, VEC, V, TPR>(pd[i], dH, row, c0, d, live);
+    load_row<T, VEC, V>(ph[i], H, row, my, d, live);
+    load_row<T, VEC, V>(pg[i], dY, row, my, d, live);
+    if constexpr (DH) load_row<T, VEC, V>(pd[i], dH, row, my, d, live);
   };
   const auto step = [&](int turn) __attribute__((always_inline)) {
     const int i = BUF == 2 ? turn : 0;
@@ -175,9 +204,9 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
       ph[i][v].get(h);
       pg[i][v].get(g);
       pw[v].get(q);
-      const bool in = c0 + v * TPR * VEC < d;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
+        const bool in = e >= my[v].skip;
         s[0] = in ? fmaf(h[e], h[e], s[0]) : s[0];
         s[1] = in ? fmaf(g[e] * q[e], h[e], s[1]) : s[1];
       }
@@ -188,8 +217,7 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
     if (row < rows) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int c = c0 + v * TPR * VEC;
-        if (c >= d) break;
+        if (my[v].skip == VEC) break;
         float h[VEC], g[VEC], q[VEC], x[VEC];
         ph[i][v].get(h);
         pg[i][v].get(g);
@@ -204,7 +232,7 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
 #pragma unroll
           for (int e = 0; e < VEC; ++e) x[e] += q[e];
         }
-        store_vec<T, VEC>(dX + row * d + c, x);
+        store_own<T, VEC, ODD>(dX + row * d, my[v], x);
       }
     }
     first += stride;
@@ -212,17 +240,14 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
   };
   if (rows > 0) {
     if (BUF == 2) request(0, first + mine);
-    load_row<T, VEC, V, TPR>(pw, w, 0, c0, d, true);
+    load_row<T, VEC, V>(pw, w, 0, my, d, true);
     while (step(0) && step(1)) {
     }
   }
   float* out = part + (long)blockIdx.x * d;
   if constexpr (RB == 1) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = c0 + v * TPR * VEC;
-      if (c < d) store_vec<float, VEC>(out + c, dw[v]);
-    }
+    for (int v = 0; v < V; ++v) store_own<float, VEC, ODD>(out, my[v], dw[v]);
   } else {
     // the workgroup's rows meet, in order
     constexpr int W = V * TPR * VEC;
@@ -230,7 +255,8 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) sum[mine * W + c0 + v * TPR * VEC + e] = dw[v][e];
+      for (int e = 0; e < VEC; ++e)
+        if (e >= my[v].skip) sum[mine * W + my[v].at + e] = dw[v][e];
     __syncthreads();
     for (int c = threadIdx.x; c < d; c += NB_THREADS) {
       float t = sum[c];
@@ -269,45 +295,44 @@ __global__ __launch_bounds__(256) void rms_norm_dw_kernel(const float* __restric
 constexpr int NORM_GRID = 1 << 20;   // workgroups at most
 constexpr int NB_GRID = 256;         // of a backward launch: one a CU (512: 45.7 us instead of 44.2)
 
-// Calls body(VEC, V, TPR) as types with the smallest group of lanes that holds a row in one piece
-// of 16 bytes each, or four of one element (past 1024 lanes more).
+// Calls body(VEC, V, TPR, ODD) as types with the smallest group of lanes that holds a row in one
+// piece of 16 bytes each (past 1024 lanes more); rows shorter than a piece by elements.
 template <typename T, typename F>
 hipError_t with_shape(int d, F body) {
   constexpr int W = 16 / sizeof(T);
-  const auto ints = [&](auto vec, auto v, auto tpr) { return body(vec, v, tpr); };
 #define EC_I(n) std::integral_constant<int, n>{}
-  if (d % W == 0) {
-    const int u = d / W;
-    if (u <= 64) return ints(EC_I(W), EC_I(1), EC_I(64));
-    if (u <= 128) return ints(EC_I(W), EC_I(1), EC_I(128));
-    if (u <= 256) return ints(EC_I(W), EC_I(1), EC_I(256));
-    if (u <= 512) return ints(EC_I(W), EC_I(1), EC_I(512));
-    if (u <= 1024) return ints(EC_I(W), EC_I(1), EC_I(1024));
-    if (u <= 2048) return ints(EC_I(W), EC_I(2), EC_I(1024));
-    if constexpr (W == 4) return ints(EC_I(W), EC_I(4), EC_I(1024));
-  }
-  if (d <= 256) return ints(EC_I(1), EC_I(4), EC_I(64));
-  if (d <= 1024) return ints(EC_I(1), EC_I(4), EC_I(256));
-  if (d <= 4096) return ints(EC_I(1), EC_I(4), EC_I(1024));
-  return ints(EC_I(1), EC_I(16), EC_I(1024));
+  if (d < W) return body(EC_I(1), EC_I(1), EC_I(64), std::false_type{});
+  const int u = (d + W - 1) / W;
+  const auto with = [&](auto odd) {
+    if (u <= 64) return body(EC_I(W), EC_I(1), EC_I(64), odd);
+    if (u <= 128) return body(EC_I(W), EC_I(1), EC_I(128), odd);
+    if (u <= 256) return body(EC_I(W), EC_I(1), EC_I(256), odd);
+    if (u <= 512) return body(EC_I(W), EC_I(1), EC_I(512), odd);
+    if (u <= 1024) return body(EC_I(W), EC_I(1), EC_I(1024), odd);
+    if constexpr (W == 4)
+      if (u > 2048) return body(EC_I(W), EC_I(4), EC_I(1024), odd);
+    return body(EC_I(W), EC_I(2), EC_I(1024), odd);
+  };
 #undef EC_I
+  return d % W == 0 ? with(std::false_type{}) : with(std::true_type{});
 }
 
 template <typename T>
 hipError_t run_norm(const void* X, const void* R, const void* w, void* H, void* Y, uint8_t* Q,
                     uint8_t* scale, long rows, int d, float eps, hipStream_t st) {
-  return with_shape<T>(d, [&](auto vec, auto v, auto tpr) {
+  return with_shape<T>(d, [&](auto vec, auto v, auto tpr, auto odd) {
+    constexpr bool ODD = decltype(odd)::value;
     constexpr int VEC = decltype(vec)::value, V = decltype(v)::value, TPR = decltype(tpr)::value;
     constexpr int RB = norm_threads<TPR>() / TPR;
     const long blocks = (rows + RB - 1) / RB;
     const dim3 grid((unsigned)(blocks < NORM_GRID ? blocks : NORM_GRID));
     const auto go = [&](auto mx, auto res) {
-      rms_norm_kernel<T, VEC, V, TPR, decltype(mx)::value, decltype(res)::value>
+      rms_norm_kernel<T, VEC, V, TPR, ODD, decltype(mx)::value, decltype(res)::value>
           <<<grid, norm_threads<TPR>(), 0, st>>>((const T*)X, (const T*)R, (const T*)w, (T*)H,
                                                  (T*)Y, Q, scale, rows, d, eps);
     };
     if (Q) {
-      if constexpr (VEC > 1) {
+      if constexpr (VEC > 1 && !ODD) {
         if (R) go(std::true_type{}, std::true_type{});
         else go(std::true_type{}, std::false_type{});
       } else {
@@ -325,10 +350,11 @@ template <typename T>
 hipError_t run_norm_backward(const void* H, const void* w, const void* dY, const void* dH, void* dX,
                              float* dw, float* part, int blocks, long rows, int d, float eps,
                              hipStream_t st) {
-  hipError_t e = with_shape<T>(d, [&](auto vec, auto v, auto tpr) {
+  hipError_t e = with_shape<T>(d, [&](auto vec, auto v, auto tpr, auto odd) {
+    constexpr bool ODD = decltype(odd)::value;
     constexpr int VEC = decltype(vec)::value, V = decltype(v)::value, TPR = decltype(tpr)::value;
     const auto go = [&](auto dh) {
-      rms_norm_backward_kernel<T, VEC, V, TPR, decltype(dh)::value>
+      rms_norm_backward_kernel<T, VEC, V, TPR, ODD, decltype(dh)::value>
           <<<dim3((unsigned)blocks), NB_THREADS, 0, st>>>(
               (const T*)H, (const T*)w, (const T*)dY, (const T*)dH, (T*)dX,
               blocks > 1 ? part : dw, rows, d, eps);
@@ -346,7 +372,7 @@ hipError_t run_norm_backward(const void* H, const void* w, const void* dY, const
 
 int rms_norm_backward_blocks(int dtype, long rows, int d) {
   long per = 1;   // rows of a workgroup's step
-  const auto rows_of = [&](auto, auto, auto tpr) {
+  const auto rows_of = [&](auto, auto, auto tpr, auto) {
     per = NB_THREADS / decltype(tpr)::value;
     return hipSuccess;
   };

@@ -147,7 +147,7 @@ def check_norm_mx(Y, H, w, eps):
     assert np.all(np.abs(got - want) <= step * (1 + 50 * U) + 50 * U * np.abs(want))
 
 
-WIDTHS = [1, 7, 32, 63, 64, 96, 131, 512, 1000, 1001, 1024, 2048, 2056, 4092, 4096, 4097, 8192,
+WIDTHS = [1, 3, 4, 7, 8, 9, 15, 32, 63, 64, 96, 131, 512, 1000, 1001, 1024, 2048, 2056, 4092, 4096, 4097, 8192,
           12001, 16383, 16384]
 
 
@@ -193,6 +193,32 @@ def test_norm_shapes_in_place_and_refusals(dtype):
                 lambda: ec.rms_norm_backward(x, x, w, dH=r[:, :64])):
         with pytest.raises(ec.ECError):
             bad()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [9, 131, 1003, 2048, 4099, 12002])
+def test_norm_and_backward_in_place(d, dtype):
+    """H over X and over the residual; dX over H, dY and dH (the library's interface): rows whose
+    last piece shares elements with the one before it among them."""
+    x, r, w = norm_inputs(37, d, dtype, d)
+    Y, H = ec.rms_norm(x, w, residual=r)
+    for place in ("x", "r"):
+        a, b = x.clone(), r.clone()
+        Y2, H2 = ec.rms_norm(a, w, residual=b, sum_out=a if place == "x" else b)
+        assert torch.equal(Y2, Y) and torch.equal(H2, H)
+    dX, dw = ec.rms_norm_backward(Y, H, w, dH=r)
+    L, code = ec.lib(), {torch.float32: 0, torch.bfloat16: 1}[dtype]
+    n = L.ec_rms_norm_workspace_size(code, 37, d)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    for place in range(3):
+        t = [H.clone(), Y.clone(), r.clone()]
+        got = torch.empty_like(dw)
+        assert L.ec_rms_norm_backward(code, 37, d, 1e-6, t[0].data_ptr(), w.data_ptr(),
+                                      t[1].data_ptr(), t[2].data_ptr(), t[place].data_ptr(),
+                                      got.data_ptr(), ws.data_ptr(), n, stream) == 0
+        torch.cuda.synchronize()
+        assert torch.equal(t[place], dX) and torch.equal(got, dw)
 
 
 def test_norm_of_no_numbers_stays_in_its_row():
