@@ -895,8 +895,10 @@ hipError_t run_decode(const DecodeCall& c, hipStream_t st) {
   }
   const long tiles2 = ((long)most + (c.hs ? 1 : 0)) * (c.d / 32);
   const dim3 g2((unsigned)(tiles2 < W2_GRID ? tiles2 : W2_GRID));
-  if ((c.h > c.hs ? c.h : c.hs) <= W2_WAVES * W2_KEPT)
-    decode_w2_kernel<F, TT, true><<<g2, 64 * W2_WAVES, 0, st>>>(
+  // (in eight bits and four tiles of columns the registers hold no more)
+  constexpr bool CAN_KEEP = !(F::MX && TT > 2);
+  if (CAN_KEEP && (c.h > c.hs ? c.h : c.hs) <= W2_WAVES * W2_KEPT)
+    decode_w2_kernel<F, TT, CAN_KEEP><<<g2, 64 * W2_WAVES, 0, st>>>(
         (const T*)c.A, (const T*)c.As, c.w, c.plan, c.O, c.N, c.d, c.h, c.hs, c.k);
   else
     decode_w2_kernel<F, TT, false><<<g2, 64 * W2_WAVES, 0, st>>>(

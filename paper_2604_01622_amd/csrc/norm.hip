@@ -162,13 +162,15 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
 
 constexpr int NB_THREADS = 1024;     // of a backward workgroup: 1024 / TPR rows at a time
 
-// A workgroup takes every gridDim.x-th set of rows and keeps its share of dw in registers;
+// A workgroup takes every gridDim.x-th set of rows and keeps its share of dw in registers, of rows
+// of more than 1024 pieces in LDS, with the weight and dH loaded again for a piece at a time: the
+// registers would spill (2048 x 16384 fp32 113 us, 4.8 TB/s, instead of 161; bf16 68 and 76).
 // part [gridDim.x, d] (dw itself where one workgroup takes all rows).
 template <typename T, int VEC, int V, int TPR, bool ODD, bool DH>
 __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
     const T* H, const T* __restrict__ w, const T* dY, const T* dH, T* dX,
     float* __restrict__ part, long rows, int d, float eps) {
-  constexpr int RB = NB_THREADS / TPR;
+  constexpr int RB = NB_THREADS / TPR, BUF = row_buffers<VEC, V>();
   __shared__ float red[4 * NB_THREADS / 64];
   Place my[V];
 #pragma unroll
@@ -178,18 +180,22 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
   const long stride = (long)gridDim.x * RB;
   long first = (long)blockIdx.x * RB;               // of the workgroup's rows
   const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+  // long rows: in LDS, a lane's own
+  __shared__ float long_dw[BUF == 1 ? V * TPR * VEC : 1];
   float dw[V][VEC];
-  constexpr int BUF = row_buffers<VEC, V>();
   Piece<T, VEC, ODD> ph[BUF][V], pg[BUF][V], pd[BUF][DH ? V : 1], pw[V];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) dw[v][e] = 0.f;
+    for (int e = 0; e < VEC; ++e) {
+      if (BUF == 1) long_dw[(v * TPR + threadIdx.x) * VEC + e] = 0.f;
+      else dw[v][e] = 0.f;
+    }
   const auto request = [&](int i, long row) __attribute__((always_inline)) {
     const bool live = row < rows;
     load_row<T, VEC, V>(ph[i], H, row, my, d, live);
     load_row<T, VEC, V>(pg[i], dY, row, my, d, live);
-    if constexpr (DH) load_row<T, VEC, V>(pd[i], dH, row, my, d, live);
+    if constexpr (DH && BUF == 2) load_row<T, VEC, V>(pd[i], dH, row, my, d, live);
   };
   const auto step = [&](int turn) __attribute__((always_inline)) {
     const int i = BUF == 2 ? turn : 0;
@@ -200,6 +206,10 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int v = 0; v < V; ++v) {
+      if constexpr (BUF == 1) {
+        __builtin_amdgcn_sched_barrier(0);
+        pw[v].load(w + my[v].at);
+      }
       float h[VEC], g[VEC], q[VEC];
       ph[i][v].get(h);
       pg[i][v].get(g);
@@ -218,13 +228,19 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         if (my[v].skip == VEC) break;
+        if constexpr (BUF == 1) {
+          __builtin_amdgcn_sched_barrier(0);
+          pw[v].load(w + my[v].at);
+          if constexpr (DH) pd[0][v].load(dH + row * d + my[v].at);
+        }
         float h[VEC], g[VEC], q[VEC], x[VEC];
         ph[i][v].get(h);
         pg[i][v].get(g);
         pw[v].get(q);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          dw[v][e] = fmaf(g[e], h[e] * r, dw[v][e]);
+          float& t = BUF == 1 ? long_dw[(v * TPR + threadIdx.x) * VEC + e] : dw[v][e];
+          t = fmaf(g[e], h[e] * r, t);
           x[e] = r * (g[e] * q[e] - h[e] * k);
         }
         if constexpr (DH) {
@@ -240,14 +256,24 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
   };
   if (rows > 0) {
     if (BUF == 2) request(0, first + mine);
-    load_row<T, VEC, V>(pw, w, 0, my, d, true);
-    while (step(0) && step(1)) {
+    if (BUF == 2) load_row<T, VEC, V>(pw, w, 0, my, d, true);
+    if constexpr (BUF == 2) {
+      while (step(0) && step(1)) {
+      }
+    } else {
+      for (int turn = 0; step(turn); turn ^= 1) {
+      }
     }
   }
   float* out = part + (long)blockIdx.x * d;
   if constexpr (RB == 1) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) store_own<float, VEC, ODD>(out, my[v], dw[v]);
+    for (int v = 0; v < V; ++v) {
+      if (BUF == 1)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) dw[v][e] = long_dw[(v * TPR + threadIdx.x) * VEC + e];
+      store_own<float, VEC, ODD>(out, my[v], dw[v]);
+    }
   } else {
     // the workgroup's rows meet, in order
     constexpr int W = V * TPR * VEC;
