@@ -362,7 +362,8 @@ int ec_mx_quantize(int dtype, int64_t rows, int64_t cols, const void *X, uint8_t
  *   H = X + residual, rounded to dtype (H = X without one);
  *   Y = H (mean of H^2 over the row + eps)^(-1/2) weight, or that in eight bits.
  * X, residual, H, Y [rows, d] dtype; weight [d] dtype; 1 <= d <= 16384; rows < 2^31;
- * eps finite and > 0.  H is written where residual is given and may be X or the
+ * eps finite and > 0.  The squares are summed in fp32: a row whose sum passes its range
+ * (elements of 10^19) has Y = 0.  H is written where residual is given and may be X or the
  * residual; other overlaps of outputs are refused.  Either Y or (d a multiple of 32) Q and
  * scale is given.                                                                */
 int ec_rms_norm(int dtype, int64_t rows, int32_t d, float eps, const void *X,

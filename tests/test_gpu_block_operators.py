@@ -238,6 +238,17 @@ def test_norm_of_no_numbers_stays_in_its_row():
     assert bool(torch.isfinite(dX[[0, 2, 4, 5]]).all()) and bool(torch.isnan(dX[1]).all())
 
 
+def test_norm_of_squares_past_fp32():
+    x, r, w = norm_inputs(3, 640, torch.float32)
+    want, (dX, _) = ec.rms_norm(x, w), ec.rms_norm_backward(r, x, w)
+    big = x.clone()
+    big[1] = 1e25
+    Y, (dX2, dw2) = ec.rms_norm(big, w), ec.rms_norm_backward(r, big, w)
+    for i in (0, 2):
+        assert torch.equal(Y[i], want[i]) and torch.equal(dX2[i], dX[i])
+    assert bool((Y[1] == 0).all()) and bool(torch.isfinite(dw2).all())
+
+
 def test_norm_past_32_bits():
     rows, d = 2 ** 20 + 3, 4096
     x = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda")
