@@ -108,6 +108,11 @@ struct Piece {
     else
       raw = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
   }
+  // what other workgroups read too: kept in the caches
+  __device__ __forceinline__ void load_shared(const T* p) {
+    if constexpr (VEC == 1) raw = *p;
+    else raw = *reinterpret_cast<const std::conditional_t<ODD, u32x4_odd, u32x4>*>(p);
+  }
   __device__ __forceinline__ void get(float* v) const {
     if constexpr (VEC == 1 && sizeof(T) == 4) {
       v[0] = raw;

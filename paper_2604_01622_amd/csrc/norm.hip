@@ -7,9 +7,8 @@
 // Memory bounds both: every row moves once and is held in registers between its sum and its
 // use.  A row belongs to TPR lanes, each of which takes V pieces of 16 bytes.  Where d leaves rows
 // unaligned (ODD) the pieces are too, and a row's last one ends with the row: what it shares
-// with the piece before it is that one's (5000 x 4097 bf16: 39 us, backward 55; an element a lane 116
-// and 316).  Forward, a group of lanes
-// takes one row and leaves: many short workgroups keep more on its way than loops over rows
+// with the piece before it is that one's (5000 x 4097 bf16: 37 us, backward 57; an element a lane 116
+// and 316).  Forward, a group of lanes takes one row and leaves: many short workgroups keep more on its way than loops over rows
 // with the next one requested ahead (16384 x 2048 bf16 with a residual: 44.2 us, 6.1 TB/s,
 // against 51.2; eight bits out 41, 5.7 TB/s).  Backward, where a workgroup keeps its share of dw,
 // the loop it needs requests ahead (45 us and 4.7 for the sum of the shares, 5.4 TB/s; a row in
@@ -117,7 +116,8 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
     Piece<T, VEC, ODD> x[V], r[RES ? V : 1], pw[V];
     load_row<T, VEC, V>(x, X, row, my, d, true);
     if constexpr (RES) load_row<T, VEC, V>(r, R, row, my, d, true);
-    load_row<T, VEC, V>(pw, w, 0, my, d, true);
+#pragma unroll          // the one operand of all workgroups (8192 x 8192 bf16 90 -> 85 us)
+    for (int v = 0; v < V; ++v) pw[v].load_shared(w + my[v].at);
     __builtin_amdgcn_sched_barrier(0);      // all on their way before the first is used
     const long at = row * d;
     float h[V][VEC], s[1] = {0.f};
@@ -164,7 +164,7 @@ constexpr int NB_THREADS = 1024;     // of a backward workgroup: 1024 / TPR rows
 
 // A workgroup takes every gridDim.x-th set of rows and keeps its share of dw in registers, of rows
 // of more than 1024 pieces in LDS, with the weight and dH loaded again for a piece at a time: the
-// registers would spill (2048 x 16384 fp32 113 us, 4.8 TB/s, instead of 161; bf16 68 and 76).
+// registers would spill (2048 x 16384 fp32 107 us, 5.0 TB/s, instead of 161; bf16 63 and 76).
 // part [gridDim.x, d] (dw itself where one workgroup takes all rows).
 template <typename T, int VEC, int V, int TPR, bool ODD, bool DH>
 __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
     for (int v = 0; v < V; ++v) {
       if constexpr (BUF == 1) {
         __builtin_amdgcn_sched_barrier(0);
-        pw[v].load(w + my[v].at);
+        pw[v].load_shared(w + my[v].at);
       }
       float h[VEC], g[VEC], q[VEC];
       ph[i][v].get(h);
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
         if (my[v].skip == VEC) break;
         if constexpr (BUF == 1) {
           __builtin_amdgcn_sched_barrier(0);
-          pw[v].load(w + my[v].at);
+          pw[v].load_shared(w + my[v].at);
           if constexpr (DH) pd[0][v].load(dH + row * d + my[v].at);
         }
         float h[VEC], g[VEC], q[VEC], x[VEC];
@@ -256,8 +256,8 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
   };
   if (rows > 0) {
     if (BUF == 2) request(0, first + mine);
-    if (BUF == 2) load_row<T, VEC, V>(pw, w, 0, my, d, true);
     if constexpr (BUF == 2) {
+      load_row<T, VEC, V>(pw, w, 0, my, d, true);
       while (step(0) && step(1)) {
       }
     } else {
@@ -322,8 +322,11 @@ constexpr int NORM_GRID = 1 << 20;   // workgroups at most
 constexpr int NB_GRID = 256;         // of a backward launch: one a CU (512: 45.7 us instead of 44.2)
 
 // Calls body(VEC, V, TPR, ODD) as types with the smallest group of lanes that holds a row in one
-// piece of 16 bytes each (past 1024 lanes more); rows shorter than a piece by elements.
-template <typename T, typename F>
+// piece of 16 bytes each (past 1024 lanes more); rows shorter than a piece by elements.  Forward,
+// of 513 to 1024 pieces, two a lane: two rows a CU wait for one another less than one would (8192 x
+// 8192 bf16 90 us instead of 107, 16384 x 4096 fp32 201 and 218); of more in bf16 four
+// (4096 x 8198 56 and 66, 4096 x 12000 64.6 and 64.7; in fp32 113 and 103).
+template <typename T, bool BACK, typename F>
 hipError_t with_shape(int d, F body) {
   constexpr int W = 16 / sizeof(T);
 #define EC_I(n) std::integral_constant<int, n>{}
@@ -334,7 +337,9 @@ hipError_t with_shape(int d, F body) {
     if (u <= 128) return body(EC_I(W), EC_I(1), EC_I(128), odd);
     if (u <= 256) return body(EC_I(W), EC_I(1), EC_I(256), odd);
     if (u <= 512) return body(EC_I(W), EC_I(1), EC_I(512), odd);
-    if (u <= 1024) return body(EC_I(W), EC_I(1), EC_I(1024), odd);
+    if (u <= 1024 && BACK) return body(EC_I(W), EC_I(1), EC_I(1024), odd);
+    if (u <= 1024) return body(EC_I(W), EC_I(2), EC_I(512), odd);
+    if constexpr (W == 8 && !BACK) return body(EC_I(W), EC_I(4), EC_I(512), odd);
     if constexpr (W == 4)
       if (u > 2048) return body(EC_I(W), EC_I(4), EC_I(1024), odd);
     return body(EC_I(W), EC_I(2), EC_I(1024), odd);
@@ -346,7 +351,7 @@ hipError_t with_shape(int d, F body) {
 template <typename T>
 hipError_t run_norm(const void* X, const void* R, const void* w, void* H, void* Y, uint8_t* Q,
                     uint8_t* scale, long rows, int d, float eps, hipStream_t st) {
-  return with_shape<T>(d, [&](auto vec, auto v, auto tpr, auto odd) {
+  return with_shape<T, false>(d, [&](auto vec, auto v, auto tpr, auto odd) {
     constexpr bool ODD = decltype(odd)::value;
     constexpr int VEC = decltype(vec)::value, V = decltype(v)::value, TPR = decltype(tpr)::value;
     constexpr int RB = norm_threads<TPR>() / TPR;
@@ -376,7 +381,7 @@ template <typename T>
 hipError_t run_norm_backward(const void* H, const void* w, const void* dY, const void* dH, void* dX,
                              float* dw, float* part, int blocks, long rows, int d, float eps,
                              hipStream_t st) {
-  hipError_t e = with_shape<T>(d, [&](auto vec, auto v, auto tpr, auto odd) {
+  hipError_t e = with_shape<T, true>(d, [&](auto vec, auto v, auto tpr, auto odd) {
     constexpr bool ODD = decltype(odd)::value;
     constexpr int VEC = decltype(vec)::value, V = decltype(v)::value, TPR = decltype(tpr)::value;
     const auto go = [&](auto dh) {
@@ -403,7 +408,7 @@ int rms_norm_backward_blocks(int dtype, long rows, int d) {
     return hipSuccess;
   };
   const hipError_t e =
-      dtype == DT_F32 ? with_shape<float>(d, rows_of) : with_shape<bf16_t>(d, rows_of);
+      dtype == DT_F32 ? with_shape<float, true>(d, rows_of) : with_shape<bf16_t, true>(d, rows_of);
   const long steps = e == hipSuccess ? (rows + per - 1) / per : 1;
   return (int)(steps < 1 ? 1 : steps < NB_GRID ? steps : NB_GRID);
 }
