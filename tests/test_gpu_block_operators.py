@@ -316,6 +316,37 @@ def test_norm_backward_of_no_rows():
     assert dX.shape == (0, 64) and bool((dw == 0).all())
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,d", [(700, 512), (40, 131), (300, 12000)])
+def test_norm_backward_in_a_graph(rows, d, dtype):
+    """Captured with the eight bits of its result and replayed on other rows, with eager calls
+    between the replays."""
+    sets = [norm_inputs(rows, d, dtype, 10 * i) for i in range(3)]
+    w = sets[0][2]
+
+    def step(H, dY):
+        dX, dw = ec.rms_norm_backward(dY, H, w, dH=H)
+        return (dX, dw, *(ec.mx_quantize(dX) if d % 32 == 0 else ()))
+
+    def equal(got, want):
+        return all(equal_bits(a, b) if a.element_size() == 1 else torch.equal(a, b)
+                   for a, b in zip(got, want))
+
+    want = [step(H, dY) for H, dY, _ in sets]
+    H, dY = sets[0][0].clone(), sets[0][1].clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = step(H, dY)
+    for n in (0, 1, 2, 1, 0):
+        H.copy_(sets[n][0]), dY.copy_(sets[n][1])
+        graph.replay()
+        again = step(*sets[n][:2])
+        torch.cuda.synchronize()
+        assert equal(out, want[n]) and equal(again, want[n])
+
+
 def test_norm_backward_against_differences():
     """The forward kernel's own outputs, a step either way along a direction."""
     x, r, w = norm_inputs(9, 200, torch.float32, 5)
