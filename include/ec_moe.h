@@ -362,10 +362,11 @@ int ec_mx_quantize(int dtype, int64_t rows, int64_t cols, const void *X, uint8_t
  *   H = X + residual, rounded to dtype (H = X without one);
  *   Y = H (mean of H^2 over the row + eps)^(-1/2) weight, or that in eight bits.
  * X, residual, H, Y [rows, d] dtype; weight [d] dtype; 1 <= d <= 16384; rows < 2^31;
- * eps finite and > 0.  The squares are summed in fp32: a row whose sum passes its range
- * (elements of 10^19) has Y = 0.  H is written where residual is given and may be X or the
- * residual; other overlaps of outputs are refused.  Either Y or (d a multiple of 32) Q and
- * scale is given.                                                                */
+ * eps finite and > 0.  The squares are summed in fp32: a row whose sum of squares passes its
+ * range, 2^128 (a root mean square above 2^64 / sqrt(d): 1.8e19 for d = 1, 1.4e17 for d = 16384),
+ * is divided by infinity: Y = 0 (NaN where H itself is infinite).  H is written where residual
+ * is given and may be X or the residual; other overlaps of outputs are refused.  Either Y or
+ * (d a multiple of 32) Q and scale is given.                                      */
 int ec_rms_norm(int dtype, int64_t rows, int32_t d, float eps, const void *X,
                 const void *residual, const void *weight, void *H, void *Y, uint8_t *Q,
                 uint8_t *scale, hipStream_t stream);
@@ -376,7 +377,9 @@ size_t ec_rms_norm_workspace_size(int dtype, int64_t rows, int32_t d);
 /* Its backward from H (X without a residual): dX [rows, d] dtype, the gradient in X and in
  * the residual alike, of sum(Y dY) + sum(H dH) (dH may be NULL); dweight [d] fp32.
  * dX may be H, dY or dH; other overlaps are refused.  The eight bits have no gradient of
- * their own.  ws: ec_rms_norm_workspace_size bytes.                               */
+ * their own.  A row whose Y is 0 because its squares pass fp32's range has dX = dH (0 without;
+ * NaN where H is infinite) and adds nothing to dweight; of other rows the sum of weight dY H
+ * has to stay in that range.  ws: ec_rms_norm_workspace_size bytes.               */
 int ec_rms_norm_backward(int dtype, int64_t rows, int32_t d, float eps, const void *H,
                          const void *weight, const void *dY, const void *dH, void *dX,
                          float *dweight, void *ws, size_t ws_bytes, hipStream_t stream);

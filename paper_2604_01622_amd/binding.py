@@ -773,7 +773,8 @@ def mx_quantize(X) -> Mx:
 def rms_norm(X, weight, eps: float = 1e-6, residual=None, mx: bool = False, sum_out=None):
     """Root-mean-square norm of the rows of X [..., d]: Y = H (mean(H^2) + eps)^-1/2 weight with
     H = X + residual, rounded.  Returns Y (in eight bits, Mx, with mx), and with a residual
-    (Y, H).  sum_out receives H; it may be X or the residual."""
+    (Y, H).  sum_out receives H; it may be X or the residual.  A row whose squares sum past fp32's
+    range (2^128) has Y = 0."""
     code, d = _rows("X", X)
     dev = X.device
     _beside("weight", weight, X, (d,))
@@ -809,7 +810,8 @@ def _norm_workspace(code, rows, d):
 def rms_norm_backward(dY, H, weight, eps: float = 1e-6, dH=None):
     """Backward of rms_norm from H (X without a residual): gradients of sum(Y * dY) +
     sum(H * dH).  Returns dX [..., d], which is the residual's gradient too, and the weight's
-    [d] in fp32."""
+    [d] in fp32.  A row whose squares sum past fp32's range (2^128) has dX = dH and adds nothing
+    to the weight's."""
     code, d = _rows("H", H)
     dev, rows = H.device, H.numel() // d if d else 0
     _beside("weight", weight, H, (d,))

@@ -223,7 +223,9 @@ __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
     }
     row_sums<TPR, 2>(s, red, turn);
     const float r = 1.0f / sqrtf(fmaf(s[0], inv_d, eps));
-    const float k = r * (r * (s[1] * inv_d));    // r * r passes fp32's range for a subnormal eps
+    // r * r passes fp32's range for a subnormal eps; r 0: the squares passed it, k 0 as Y is, though
+    // the other sum may have passed it too
+    const float k = r == 0.f ? 0.f : r * (r * (s[1] * inv_d));
     if (row < rows) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
