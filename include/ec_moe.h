@@ -379,7 +379,7 @@ size_t ec_rms_norm_workspace_size(int dtype, int64_t rows, int32_t d);
  * dX may be H, dY or dH; other overlaps are refused.  The eight bits have no gradient of
  * their own.  A row whose Y is 0 because its squares pass fp32's range has dX = dH (0 without;
  * NaN where H is infinite) and adds nothing to dweight; of other rows the sum of weight dY H
- * has to stay in that range.  ws: ec_rms_norm_workspace_size bytes.               */
+ * has to stay in that range.  ws: ec_rms_norm_workspace_size bytes, apart from the rest. */
 int ec_rms_norm_backward(int dtype, int64_t rows, int32_t d, float eps, const void *H,
                          const void *weight, const void *dY, const void *dH, void *dX,
                          float *dweight, void *ws, size_t ws_bytes, hipStream_t stream);

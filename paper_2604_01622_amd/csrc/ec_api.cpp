@@ -1437,6 +1437,11 @@ int ec_rms_norm_backward(int dtype, int64_t rows, int32_t d, float eps, const vo
   if (meet(dX, bytes, weight, (size_t)d * esz) || meet(dX, bytes, dweight, (size_t)d * 4) ||
       meet(dweight, (size_t)d * 4, weight, (size_t)d * esz))
     return fail(EC_ERR_ARG, "dX, dweight and the weight overlap");
+  // the workgroups' shares of dweight are written while rows are still read
+  if (meet(ws, need, H, bytes) || meet(ws, need, dY, bytes) || meet(ws, need, dH, bytes) ||
+      meet(ws, need, dX, bytes) || meet(ws, need, weight, (size_t)d * esz) ||
+      meet(ws, need, dweight, (size_t)d * 4))
+    return fail(EC_ERR_ARG, "the workspace overlaps an operand");
   EC_HIP(ec::launch_rms_norm_backward(dtype, H, weight, dY, dH, dX, dweight, (float*)ws, rows, d,
                                       eps, stream));
   return EC_OK;
