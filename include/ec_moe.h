@@ -394,7 +394,8 @@ int ec_rms_norm_backward(int dtype, int64_t rows, int32_t d, float eps, const vo
  *   then dtype is EC_BF16.  Eight bits become bf16 exactly before they are multiplied.
  *   residual, Y [N, d] dtype (residual may be NULL; Y may be X or the residual);
  *   experts [N, top_k] int32 out, by falling logit; gates [N, top_k] fp32 out.
- * ws: ec_tc_decode_workspace_size bytes (0 on an invalid problem), which grow with N.  */
+ * ws: ec_tc_decode_workspace_size bytes (0 on an invalid problem), which grow with N.
+ * Other overlaps of Y, experts, gates and ws with one another or an input are refused.  */
 #define EC_DECODE_MAX_TOKENS 64
 size_t ec_tc_decode_workspace_size(const ec_problem *p, int32_t top_k);
 typedef struct {

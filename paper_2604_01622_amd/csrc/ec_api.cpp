@@ -1480,15 +1480,33 @@ int ec_tc_decode(const ec_problem* p, int32_t top_k, const ec_mx_scales* mx, con
     EC_TRY(check_ptr(s.Ws3, "the scales of Ws3", P.hs == 0));
     EC_TRY(check_ptr(s.Ws2, "the scales of Ws2", P.hs == 0));
   }
-  // Y is written after the last read of X, an element after the residual's
-  const size_t rows = (size_t)P.N * P.d, bytes = rows * P.esz, xbytes = s.X ? rows : bytes;
-  if ((Y != X && meet(Y, bytes, X, xbytes)) ||
-      (Y != residual && meet(Y, bytes, residual, bytes)))
-    return fail(EC_ERR_ARG, "Y overlaps X or the residual at another offset");
   const size_t need = ec_tc_decode_workspace_size(p, top_k);
   EC_TRY(check_ptr(ws, "workspace"));
   if (ws_bytes < need)
     return fail(EC_ERR_WORKSPACE, "workspace %zu bytes < %zu required", ws_bytes, need);
+  if (!none) {
+    // the choice, the gates and the workspace are written while other workgroups still read; Y
+    // after the last read of X, and an element after the residual's
+    const size_t rows = (size_t)P.N * P.d, bytes = rows * P.esz, xbytes = s.X ? rows : bytes;
+    const size_t wsz = wmx ? 1 : P.esz, w = (size_t)P.E * P.h * P.d, sw = (size_t)P.hs * P.d;
+    const size_t pairs = (size_t)P.N * top_k * 4;
+    const struct { const void* p; size_t size; } outs[] = {
+        {Y, bytes}, {experts, pairs}, {gates, pairs}, {ws, need}},
+      ins[] = {{X, xbytes}, {residual, bytes}, {Wg, (size_t)P.E * P.d * P.esz}, {W1, w * wsz},
+               {W3, w * wsz}, {W2, w * wsz}, {Ws1, sw * wsz}, {Ws3, sw * wsz}, {Ws2, sw * wsz},
+               {s.X, rows / 32}, {s.W1, w / 32}, {s.W3, w / 32}, {s.W2, w / 32}, {s.Ws1, sw / 32},
+               {s.Ws3, sw / 32}, {s.Ws2, sw / 32}};
+    for (int i = 0; i < 4; ++i) {
+      for (int j = 0; j < i; ++j)
+        if (meet(outs[i].p, outs[i].size, outs[j].p, outs[j].size))
+          return fail(EC_ERR_ARG, "Y, experts, gates and the workspace overlap");
+      for (const auto& in : ins) {
+        const bool in_place = i == 0 && &in < ins + 2 && in.p == Y;    // of X or the residual
+        if (!in_place && meet(outs[i].p, outs[i].size, in.p, in.size))
+          return fail(EC_ERR_ARG, "Y, experts, gates or the workspace overlaps an input");
+      }
+    }
+  }
   Carve c(ws);
   ec::DecodeCall call = carve_decode(c, P, top_k);
   call.inv_tau = p->inv_temperature;

@@ -45,3 +45,56 @@ def norm_backward(sizes=NORM, **over):
 def test_norm_backward_workspace(other):
     sizes = dict(NORM, ws=ec.lib().ec_rms_norm_workspace_size(1, ROWS, D))
     shares(norm_backward, sizes, "ws", other)
+
+
+# ---- a few tokens --------------------------------------------------------------
+
+N, d, E, h, hs, K = 16, 128, 8, 64, 192, 2
+
+
+def problem(n=N):
+    return binding.Problem(n, d, E, h, [0, n], [0], 1.0, torch.bfloat16, hs)
+
+
+def decode_sizes(mx):
+    w = 1 if mx else 2
+    sizes = {"X": N * d * w, "Wg": E * d * 2, "W1": E * h * d * w, "W3": E * h * d * w,
+             "W2": E * h * d * w, "Ws1": hs * d * w, "Ws3": hs * d * w, "Ws2": hs * d * w,
+             "R": N * d * 2, "Y": N * d * 2, "experts": N * K * 4, "gates": N * K * 4,
+             "ws": ec.lib().ec_tc_decode_workspace_size(problem().ref, K)}
+    if mx:
+        sizes.update({"scales of " + n: sizes[n] // 32
+                      for n in ("X", "W1", "W3", "W2", "Ws1", "Ws3", "Ws2")})
+    return sizes
+
+
+def decode(mx, n=N, **over):
+    sizes = decode_sizes(mx)
+    a = {**places(sizes), **over}
+    p = {k: ctypes.c_void_p(v) for k, v in a.items()}
+    s = binding._MxScales(**{k[10:]: v for k, v in a.items() if k.startswith("scales of ")})
+    return ec.lib().ec_tc_decode(problem(n).ref, K, ctypes.byref(s), p["X"], p["Wg"], p["W1"],
+                                 p["W3"], p["W2"], p["Ws1"], p["Ws3"], p["Ws2"], p["R"], p["Y"],
+                                 p["experts"], p["gates"], p["ws"], sizes["ws"], None)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("out", ["Y", "experts", "gates", "ws"])
+def test_decode_outputs_and_workspace(out, mx):
+    """Y is the last that is written, but the workspace, the choice and the gates are while the
+    tokens and weights are still read."""
+    sizes = decode_sizes(mx)
+    at = places(sizes)
+    for other in sizes:
+        if other == out:
+            continue
+        if out == "Y" and other in ("X", "R"):       # whole, they may share a place
+            for where in (at[other] + 16, at[other] + (sizes[other] - 1) // 16 * 16,
+                          at[other] - (sizes[out] - 1) // 16 * 16):
+                assert decode(mx, **{out: where}) == EC_ERR_ARG
+            continue
+        shares(lambda **over: decode(mx, **over), sizes, out, other)
+
+
+def test_decode_of_no_tokens_writes_nothing():
+    assert decode(False, n=0, Y=GAP, experts=GAP, gates=GAP, ws=GAP) == EC_OK
