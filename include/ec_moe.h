@@ -391,7 +391,10 @@ int ec_rms_norm_backward(int dtype, int64_t rows, int32_t d, float eps, const vo
  * and capacities are checked but not used.  N <= EC_DECODE_MAX_TOKENS.
  *   Weights as for ec_tc_forward.  mx (may be NULL): scales of those operands that are given
  *   as codes: X alone, the six expert weights alone (all that the problem has), or both;
- *   then dtype is EC_BF16.  Eight bits become bf16 exactly before they are multiplied.
+ *   then dtype is EC_BF16.  Eight bits become bf16 before they are multiplied: exactly for
+ *   scale bytes 3 to 246 (ec_mx_quantize's of blocks whose largest magnitude is in [2^-116,
+ *   1.75 2^127]); under smaller bytes rounded to a multiple of 2^-133, under larger ones
+ *   infinite from 2^128 on; NaN under 255.
  *   residual, Y [N, d] dtype (residual may be NULL; Y may be X or the residual);
  *   experts [N, top_k] int32 out, by falling logit; gates [N, top_k] fp32 out.
  * ws: ec_tc_decode_workspace_size bytes (0 on an invalid problem), which grow with N.

@@ -13,8 +13,9 @@
 // tokens 4.7 + 49 + 26 + 4.7 for 363 MB.  A kernel's first 2 to 4 us are its launch.
 //
 // Weights come in the storage type or in eight bits with scales (mx.h), which turn into bf16
-// exactly (four leading bits) on their way to the matrix cores; the tokens and activations
-// that they meet are bf16, so eight bits cost no accuracy beyond the weights' own.
+// on their way to the matrix cores, exactly (four leading bits) for scale bytes 3 to 246: below,
+// the last bit may lie under bf16's 2^-133, above, the value past its range.  The tokens and
+// activations that they meet are bf16, so eight bits cost no accuracy beyond the weights' own.
 #include <hip/hip_runtime.h>
 
 #include "ec_kernels.h"
@@ -43,6 +44,7 @@ __device__ __forceinline__ bf16x8 mx_widen8(uint32_t lo, uint32_t hi, float scal
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// The scale as widening takes it, by its exponent field alone: 0 there is 2^-127 too.
 __device__ __forceinline__ float mx_scale(uint32_t byte) {
   return __uint_as_float(byte == MX_NAN ? 0x7fc00000u : byte << 23);
 }
