@@ -851,43 +851,37 @@ def _decode_plan(N, d, E, h, hs, top_k, inv_temperature, dtype):
 class TcDecoder:
     """The token-choice layer for a few tokens (serving), its weights held: every token takes
     its top_k experts by logit and none is dropped.  Weights as for tc_forward, W1, W3, W2 and
-    the shared experts' all in the type of Wg or all in eight bits (Mx, with a bf16 Wg).
+    the shared experts' all in the type of Wg or all in eight bits (Mx, with a bf16 Wg); others
+    of the same shapes and type may take their place between calls.
     Workspace and outputs are allocated once, for max_tokens (at most 64).  A decoder has one
     set of buffers: order its calls (and the replays of graphs that captured them)."""
 
     def __init__(self, Wg, W1, W3, W2, top_k: int, inv_temperature=1.0, shared=None,
                  max_tokens: int = DECODE_MAX_TOKENS):
-        mx, w1 = isinstance(W1, Mx), _codes(W1)
+        self._mx, w1 = isinstance(W1, Mx), _codes(W1)
         if not isinstance(Wg, torch.Tensor) or Wg.dim() != 2:
             raise ECError(2, "Wg must have 2 dimensions")
         if not isinstance(w1, torch.Tensor) or w1.dim() != 3:
             raise ECError(2, "W1 must have 3 dimensions")
         _rows("Wg", Wg)
         dt, dev, (E, d), h, hs = Wg.dtype, Wg.device, Wg.shape, w1.shape[1], 0
-        if mx and dt != torch.bfloat16:
+        if self._mx and dt != torch.bfloat16:
             raise ECError(4, "weights in eight bits need a bf16 Wg")
-        operands = [("W1", W1, (E, h, d)), ("W3", W3, (E, h, d)), ("W2", W2, (E, d, h))]
         if shared is not None:
             if len(shared) != 3 or not isinstance(_codes(shared[0]), torch.Tensor):
                 raise ECError(1, "shared must be (Ws1, Ws3, Ws2)")
             hs = _codes(shared[0]).shape[0]
-            operands += [("Ws1", shared[0], (hs, d)), ("Ws3", shared[1], (hs, d)),
-                         ("Ws2", shared[2], (d, hs))]
-        for name, t, shape in operands:
-            if mx:
-                _mx_operand(name, t, shape, dev)
-            else:
-                _beside(name, t, Wg, shape)
+        self.Wg, self.W1, self.W3, self.W2, self.shared = Wg, W1, W3, W2, shared
+        self._device, self._d, self._dtype, self._bound = dev, d, dt, None
+        self._shapes = (("W1", (E, h, d)), ("W3", (E, h, d)), ("W2", (E, d, h)),
+                        ("Ws1", (hs, d)), ("Ws3", (hs, d)), ("Ws2", (d, hs)))
+        self._n_weights = 3 if shared is None else 6
+        self._bind()
         if not 0 <= int(max_tokens) <= DECODE_MAX_TOKENS:
             raise ECError(2, f"max_tokens must be in [0, {DECODE_MAX_TOKENS}]")
-        self.Wg, self.W1, self.W3, self.W2, self.shared = Wg, W1, W3, W2, shared
         self.top_k, self.max_tokens = int(top_k), int(max_tokens)
-        self._device, self._d = dev, d
         self._sizes = (d, E, h, hs, self.top_k, float(inv_temperature), dt)
         n = _decode_plan(self.max_tokens, *self._sizes)[1]
-        six = (W1, W3, W2, *(shared or (None,) * 3))
-        self._weights = [_addr(_codes(t)) for t in (Wg, *six)]
-        self._scales = [_scales(t) for t in six]
         with _on(dev):
             self.ws = _empty(n, dev)
             self.Y = torch.empty((self.max_tokens, d), dtype=dt, device=dev)
@@ -896,11 +890,39 @@ class TcDecoder:
             self.gates = torch.empty((self.max_tokens, self.top_k), dtype=torch.float32,
                                      device=dev)
 
+    def _bind(self):
+        """The addresses of the weights as they are now; they are checked where a tensor, its
+        memory or its shape is another than at the call before."""
+        held = Wg, W1, W3, W2, shared = self.Wg, self.W1, self.W3, self.W2, self.shared
+        if self._bound is not None:
+            a, b, c, e, f = self._bound
+            if (Wg is a and W1 is b and W3 is c and W2 is e and shared is f
+                    and self._seen == [(t.data_ptr(), t.shape) for t in self._tensors]):
+                return
+        _operand("Wg", Wg, self._dtype, (self._shapes[0][1][0], self._d), self._device)
+        six = (W1, W3, W2, *(shared or ()))
+        if len(six) != self._n_weights:
+            raise ECError(1, "shared must be (Ws1, Ws3, Ws2), or None as the decoder was made")
+        for (name, shape), t in zip(self._shapes, six):
+            if self._mx:
+                _mx_operand(name, t, shape, self._device)
+            else:
+                _beside(name, t, Wg, shape)
+        tensors = [Wg, *(part for t in six for part in (t if self._mx else (t,)))]
+        none = (None,) * (6 - len(six))
+        self._weights = [_addr(Wg), *(_addr(_codes(t)) for t in six), *none]
+        self._scales = [*map(_scales, six), *none]
+        # a tuple: a list could be given other tensors unseen
+        self.shared = shared if shared is None else tuple(shared)
+        self._tensors, self._seen = tensors, [(t.data_ptr(), t.shape) for t in tensors]
+        self._bound = (*held[:4], self.shared)
+
     def forward(self, X, residual=None, out=None):
         """Y = residual + layer(X) of X [N, d] (in the type of Wg, or Mx), the chosen experts
         [N, top_k] int32 by falling logit (equal logits: the lower index) and their gates
         [N, top_k] fp32; rows of the decoder's buffers (Y: of out, if given, which may be X or
         the residual)."""
+        self._bind()
         dev, d, x = self._device, self._d, _codes(X)
         if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.shape[1] != d:
             raise ECError(2, f"X must be [N, {d}]")
