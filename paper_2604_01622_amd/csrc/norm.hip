@@ -162,9 +162,10 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void rms_norm_kernel(
 
 constexpr int NB_THREADS = 1024;     // of a backward workgroup: 1024 / TPR rows at a time
 
-// A workgroup takes every gridDim.x-th set of rows and keeps its share of dw in registers, of rows
-// of more than 1024 pieces in LDS, with the weight and dH loaded again for a piece at a time: the
-// registers would spill (2048 x 16384 fp32 107 us, 5.0 TB/s, instead of 161; bf16 63 and 76).
+// A workgroup takes every gridDim.x-th set of rows and keeps its share of dw in registers; of more
+// than eight elements a lane (d above 8192) in LDS, with the weight and dH loaded again for a piece
+// at a time: the registers would spill (2048 x 16384 fp32 107 us, 5.0 TB/s, instead of 161; bf16
+// 63 and 76).
 // part [gridDim.x, d] (dw itself where one workgroup takes all rows).
 template <typename T, int VEC, int V, int TPR, bool ODD, bool DH>
 __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
