@@ -8,9 +8,13 @@
 // MFMAs' A operand, streamed from memory into registers, and the tokens that chose the expert
 // are its 16 columns.  Launches: logits, (past 16 tokens) choice, W1/W3, W2, sum.
 //
-// Measured, d 2048, 64 experts of 1024, top 8, bf16: 64 tokens 5.0 + 6.1 + 86 + 48 + 4.8 us for
-// 806 MB (W1/W3 6.2 TB/s, W2 5.6), one token 3.0 + 16.5 + 8.8 + 3.9 for 101 MB.  In eight bits 16
-// tokens 4.7 + 49 + 26 + 4.7 for 363 MB.  A kernel's first 2 to 4 us are its launch.
+// Measured, d 2048, 64 experts of 1024, top 8, bf16: 64 tokens 5.2 + 6.5 + 87 + 48 + 5.1 us for
+// 806 MB (W1/W3 6.2 TB/s, W2 5.5), one token 3.0 + 16.6 + 8.8 + 3.8 for 101 MB.  In eight bits 16
+// tokens 4.6 + 49 + 25 + 4.6 for 367 MB.  A kernel's first 2 to 4 us are its launch.  Slower by the
+// byte: more than 16 tokens an expert, whose activations every tile reads (64 tokens, 16 such
+// experts, W1/W3 34 and W2 26 us: 4.0 and 2.6 TB/s), shared experts beside 64 tokens (of 1024, W1/W3
+// 124 and W2 88 us), and shares of whole tiles that do not come out even (one token, experts of
+// 1088: W1/W3 21.4 us).
 //
 // Weights come in the storage type or in eight bits with scales (mx.h), which turn into bf16
 // on their way to the matrix cores, exactly (four leading bits) for scale bytes 3 to 246: below,
@@ -651,8 +655,9 @@ constexpr int W2_KEPT = 256;
 // takes a contiguous share of them (of equal work), its waves a quarter of k each, streamed as in
 // W1/W3, a chunk of both 16 rows a step; the expert's tokens are the columns of the products,
 // which go to O [token k + pick, d] in fp32 (the shared experts' to the rows from N k).
-// KEEP (widths of W2_WAVES W2_KEPT at most): the activations of the first 16 columns are loaded
-// once a slot (64 tokens 58.0 -> 48.9 us, 16 in eight bits 32.6 -> 27.9).
+// KEEP (both widths W2_WAVES W2_KEPT at most): the activations of the first 16 columns are loaded
+// once a slot (64 tokens 58.0 -> 48.9 us, 16 in eight bits 32.6 -> 27.9).  Wider ones do not fit the
+// registers (experts of 1088 beside 1024: 66 and 48 us, in eight bits 39 and 25).
 template <class F, int TT, bool KEEP>
 __global__ __launch_bounds__(64 * W2_WAVES, 2) void decode_w2_kernel(
     const typename F::T* __restrict__ A, const typename F::T* __restrict__ As, DecodeWeights w,

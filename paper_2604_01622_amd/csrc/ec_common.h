@@ -94,9 +94,11 @@ template <> struct Elem<bf16_t> {
 // 16 bytes at any element's address: the hardware takes them in one access all the same.
 typedef u32x4 u32x4_odd __attribute__((aligned(2)));
 
-// VEC elements as they are stored, read once (a streaming load: norm of 16384 x 2048 bf16 45.6 ->
-// 44.2 us).  ODD: at any element's address, where neighbouring loads share lines that a streaming
-// one would give up (5000 x 4097 bf16: 53 us with, 39 without), else aligned to their size.
+// VEC elements as they are stored, read once by a streaming load (16384 x 2048 bf16, with and
+// without: the norm's backward pass 48.0 and 49.1 us, forward with a residual 44.3 and 43.8, without
+// one 26.3 and 22.4).  ODD: at any element's address, where neighbouring loads share lines that a
+// streaming one would give up (norm of 5000 x 4097 bf16 with a residual: 50.5 us with, 37.2
+// without), else aligned to their size.
 template <typename T, int VEC, bool ODD = false>
 struct Piece {
   std::conditional_t<VEC == 1, T, u32x4> raw;
@@ -132,8 +134,8 @@ struct Piece {
 };
 
 // VEC elements from fp32, 16 or (fp32, eight) 32 bytes.  bf16 at any element's address in streaming
-// stores (norm of 5000 x 4097: 50.6 us without, 39.0), else in plain ones (16384 x 2048: 47.9 and
-// 45.0).
+// stores (norm of 5000 x 4097 with a residual: 50.2 us without, 37.2), else in plain ones (16384 x
+// 2048: 46.0 and 44.3).
 template <typename T, int VEC, bool ODD>
 __device__ __forceinline__ void store_vec(T* p, const float* v) {
   typedef std::conditional_t<ODD, u32x4_odd, u32x4> V;

@@ -1,7 +1,7 @@
 // A tensor in eight bits with scales (mx.h): the layout in which the experts' weights are
 // held for serving.
 //
-// Memory bounds it: 65536 x 2048 bf16 in 60.9 us, 6.7 TB/s (one piece of 16 bytes a lane on its
+// Memory bounds it: 65536 x 2048 bf16 in 61.0 us, 6.7 TB/s (one piece of 16 bytes a lane on its
 // way instead of four: 69.6; streaming loads save 2 of that).  640 x 1472 fp32, 4.7 MB: 2.7 us,
 // the launch.
 #include "mx.h"

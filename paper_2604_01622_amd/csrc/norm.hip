@@ -7,12 +7,14 @@
 // Memory bounds both: every row moves once and is held in registers between its sum and its
 // use.  A row belongs to TPR lanes, each of which takes V pieces of 16 bytes.  Where d leaves rows
 // unaligned (ODD) the pieces are too, and a row's last one ends with the row: what it shares
-// with the piece before it is that one's (5000 x 4097 bf16: 37 us, backward 57; an element a lane 116
-// and 316).  Forward, a group of lanes takes one row and leaves: many short workgroups keep more on its way than loops over rows
-// with the next one requested ahead (16384 x 2048 bf16 with a residual: 44.2 us, 6.1 TB/s,
-// against 51.2; eight bits out 41, 5.7 TB/s).  Backward, where a workgroup keeps its share of dw,
-// the loop it needs requests ahead (45 us and 4.7 for the sum of the shares, 5.4 TB/s; a row in
-// one wave, without: 64 and 11).  One row takes 1.9 us, the launch.
+// with the piece before it is that one's (5000 x 4097 bf16: 37 us, backward 55; an element a lane 116
+// and 316).  Forward, a group of lanes takes one row and leaves: many short workgroups keep more on
+// its way than loops over rows with the next one requested ahead (16384 x 2048 bf16 with a residual: 44.3 us, 6.1 TB/s,
+// against 51.2; eight bits out 40, 5.9 TB/s).  Backward, where a workgroup keeps its share of dw,
+// the loop it needs requests ahead (43 us and 5 for the sum of the shares, 5.6 TB/s; a row in
+// one wave, without: 64 and 11).  One row takes 2.0 us, the launch.  Of narrow rows most lanes of a
+// wave have nothing to do (40000 x 64 bf16 13.7 us, 1.5 TB/s; x 256 19.0, 4.3; backward 15.4 + 3.9
+// and 18.6 + 4.0).
 #include "mx.h"
 #include "ec_kernels.h"
 
@@ -164,8 +166,8 @@ constexpr int NB_THREADS = 1024;     // of a backward workgroup: 1024 / TPR rows
 
 // A workgroup takes every gridDim.x-th set of rows and keeps its share of dw in registers; of more
 // than eight elements a lane (d above 8192) in LDS, with the weight and dH loaded again for a piece
-// at a time: the registers would spill (2048 x 16384 fp32 107 us, 5.0 TB/s, instead of 161; bf16
-// 63 and 76).
+// at a time: the registers would spill (2048 x 16384 fp32 105 us, 5.1 TB/s, instead of 161; bf16
+// 62 and 76).
 // part [gridDim.x, d] (dw itself where one workgroup takes all rows).
 template <typename T, int VEC, int V, int TPR, bool ODD, bool DH>
 __global__ __launch_bounds__(NB_THREADS) void rms_norm_backward_kernel(
