@@ -9,12 +9,12 @@
 // unaligned (ODD) the pieces are too, and a row's last one ends with the row: what it shares
 // with the piece before it is that one's (5000 x 4097 bf16: 37 us, backward 55; an element a lane 116
 // and 316).  Forward, a group of lanes takes one row and leaves: many short workgroups keep more on
-// its way than loops over rows with the next one requested ahead (16384 x 2048 bf16 with a residual: 44.3 us, 6.1 TB/s,
-// against 51.2; eight bits out 40, 5.9 TB/s).  Backward, where a workgroup keeps its share of dw,
-// the loop it needs requests ahead (43 us and 5 for the sum of the shares, 5.6 TB/s; a row in
-// one wave, without: 64 and 11).  One row takes 2.0 us, the launch.  Of narrow rows most lanes of a
-// wave have nothing to do (40000 x 64 bf16 13.7 us, 1.5 TB/s; x 256 19.0, 4.3; backward 15.4 + 3.9
-// and 18.6 + 4.0).
+// its way than loops over rows with the next one requested ahead (16384 x 2048 bf16 with a
+// residual: 44.3 us, 6.1 TB/s, against 51.2; eight bits out 40, 5.9 TB/s).  Backward, where a
+// workgroup keeps its share of dw, the loop it needs requests ahead (43 us and 5 for the sum of the
+// shares, 5.6 TB/s; a row in one wave, without: 64 and 11).  One row takes 2.0 us, the launch.  Of
+// narrow rows most lanes of a wave have nothing to do (40000 x 64 bf16 13.7 us, 1.5 TB/s; x 256
+// 19.0, 4.3; backward 15.4 + 3.9 and 18.6 + 4.0).
 #include "mx.h"
 #include "ec_kernels.h"
 
