@@ -879,8 +879,8 @@ class TcDecoder:
         self._bind()
         if not 0 <= int(max_tokens) <= DECODE_MAX_TOKENS:
             raise ECError(2, f"max_tokens must be in [0, {DECODE_MAX_TOKENS}]")
-        self.top_k, self.max_tokens = int(top_k), int(max_tokens)
-        self._sizes = (d, E, h, hs, self.top_k, float(inv_temperature), dt)
+        self.max_tokens = int(max_tokens)
+        self._sizes = (d, E, h, hs, int(top_k), float(inv_temperature), dt)
         n = _decode_plan(self.max_tokens, *self._sizes)[1]
         with _on(dev):
             self.ws = _empty(n, dev)
@@ -889,6 +889,11 @@ class TcDecoder:
                                        device=dev)
             self.gates = torch.empty((self.max_tokens, self.top_k), dtype=torch.float32,
                                      device=dev)
+
+    @property
+    def top_k(self):
+        """Experts a token; the buffers are planned for it."""
+        return self._sizes[4]
 
     def _bind(self):
         """The addresses of the weights as they are now; they are checked where a tensor, its

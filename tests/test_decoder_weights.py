@@ -114,3 +114,19 @@ def test_weights_that_do_not_fit_are_refused(calls, make):
         dec.W1.data = dec.W1.data[:1]           # the same address
         with pytest.raises(ec.ECError):
             dec.forward(weight(3, D))
+
+
+def test_the_number_of_choices_is_fixed(calls):
+    """The places of the choice and the gates are planned for it: with 64 tokens and one choice of
+    256 narrow experts, the workspace would do for 16 tokens and ten choices, whose 160 pairs do
+    not fit the 64 places."""
+    size = ec.lib().ec_tc_decode_workspace_size
+
+    def problem(n):
+        return binding.Problem(n, 64, 256, 64, [0, n], [0], 1.0, torch.bfloat16).ref
+
+    assert size(problem(16), 10) <= size(problem(64), 1)
+    dec = decoder(weight)
+    with pytest.raises(AttributeError):
+        dec.top_k = 3
+    assert dec.top_k == 2 and dec.experts.shape == (8, 2)
